@@ -30,8 +30,9 @@
  *                   pass/fail verdict of each candidate.
  * Around them: the separate position pass (kb_screen_locate), multi-output
  * candidates (kb_screen_multi), the rung benchmarker's statistics and
- * promotion decision (kb_rung_stats, kb_rung_promote, kb_rung_survival), and
- * kb_screen_noalloc for callers that cannot allocate.
+ * promotion decision (kb_rung_stats, kb_rung_promote, kb_rung_survival),
+ * kb_screen_noalloc for callers that cannot allocate, and operators whose
+ * outputs serve as references (kb_norm_forward, kb_norm_backward).
  *
  * Conventions
  *   - Every function is extern "C" and returns an int status: KB_OK (0) or a
@@ -51,7 +52,8 @@
  *     KB_INLINE_CANDS candidates is given a launch-table buffer of the
  *     caller's pinned host memory (kb_screen_ex, kb_screen_multi).
  *   - Device buffers must be 16-byte aligned (hipMalloc and torch
- *     allocations are); element counts may be anything, including 0.
+ *     allocations are), the tensors of the reference operators to their
+ *     element only; element counts may be anything, including 0.
  *   - A "data pointer" of a tensor points at element 0; strides are in
  *     elements.
  */
@@ -641,6 +643,54 @@ enum {
  * Errors: KB_ERR_INVALID_ARG, KB_ERR_DTYPE, KB_ERR_ALIGNMENT, KB_ERR_HIP. */
 int kb_gen_scatter(void* dst, const void* ref, int dtype, uint64_t n, const uint64_t* idx, uint32_t m,
                    int mode, hipStream_t stream);
+
+/* --------------------------------------------------- reference operators --
+ * A screen needs the reference output that candidates are compared with
+ * (Section 3.4: the Verifier checks a candidate's output against the
+ * reference on seeded inputs).  These calls compute the references of one
+ * attention sublayer's kernels, forward and backward, from seeded inputs on
+ * the device: layer norm over rows and softmax attention.  Each result is a
+ * fixed function of its inputs on a given device: no atomics, sums in a fixed
+ * order, the same bits on every call.  Sums, row statistics and softmax terms
+ * are held in binary32; an output is rounded once, to nearest even, except
+ * where a call's text says what else is rounded.
+ *
+ * All calls: tensors are device views whose last dimension is contiguous
+ * (stride 1 where it has more than one element); the other strides are in
+ * elements, at least 0, and for an output such that no two elements share
+ * memory.  A data pointer is aligned to its element only, so rows and slices
+ * of a larger tensor are valid views; an empty tensor's may be NULL.  `data`
+ * of an output view is written.  An output must not overlap an input or
+ * another output (kb_norm_forward's y may be x).  Asynchronous and
+ * stream-ordered; on error nothing is launched. */
+
+/* Layer norm of the rows of x [rows][cols]:
+ *   mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),
+ *   y = (x - mean) rstd w + b.
+ * x, y: one dtype, F32, F16 or BF16.  w, b: [cols], each NULL (1 and 0) or of
+ * x's dtype or F32, both the same.  mean, rstd: device float[rows], each may
+ * be NULL; kb_norm_backward takes them.  The deviations are taken from the
+ * rounded mean (two passes over the row).  eps finite and >= 0.
+ * Errors: KB_ERR_INVALID_ARG (null descriptors or data, a shape, stride or eps
+ * out of range, cols = 0 with rows > 0), KB_ERR_DTYPE, KB_ERR_ALIGNMENT (a
+ * pointer not aligned to its element), KB_ERR_HIP. */
+int kb_norm_forward(const kb_tensor* x, const kb_tensor* w, const kb_tensor* b, float eps,
+                    const kb_tensor* y, float* mean, float* rstd, hipStream_t stream);
+
+/* Gradients of kb_norm_forward: with z = (x - mean) rstd and g = dy w,
+ *   dx = rstd (g - sum_c g / cols - z sum_c (g z) / cols),
+ *   dw = sum_rows dy z,  db = sum_rows dy.
+ * dy, x, dx: [rows][cols] of one dtype; w: NULL (1) or [cols]; mean, rstd: the
+ * forward call's.  dw, db: [cols], each may be NULL (not computed); of x's
+ * dtype or F32, w, dw and db all the same.  dx may be NULL likewise.  dw and
+ * db of zero rows are 0.  workspace: 16-byte aligned, not less than
+ * kb_norm_backward_workspace_bytes; it needs no initialisation and may be NULL
+ * when neither dw nor db is wanted.
+ * Errors as kb_norm_forward, and KB_ERR_WORKSPACE. */
+size_t kb_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w, const float* mean,
+                     const float* rstd, const kb_tensor* dx, const kb_tensor* dw, const kb_tensor* db,
+                     void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ----------------------------------------------------------------- misc -- */
 

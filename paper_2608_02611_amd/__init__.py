@@ -5,7 +5,8 @@ library's HIP kernels; torch provides device memory, tensor metadata and the
 current stream.  The names mirror the C interface in include/kb.h:
 
     kb_policy_check, kb_screen_workspace_bytes, kb_screen_launch, kb_screen,
-    kb_screen_stats, kb_gen_inputs, kb_last_error, kb_version
+    kb_screen_stats, kb_gen_inputs, kb_norm_forward, kb_norm_backward,
+    kb_last_error, kb_version
 
 plus `screen(...)`, which chains the gate, the kernel and the readback for the
 common case.  The pass/fail verdict of each record comes from the library
@@ -13,8 +14,10 @@ common case.  The pass/fail verdict of each record comes from the library
 dicts.  Loading fails loudly (KbError) when libkb.so has not been built;
 there is no fallback implementation.
 """
+import contextlib
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libkb.so")
@@ -133,6 +136,7 @@ EXPORTS = ("kb_policy_check", "kb_screen_workspace_bytes", "kb_screen_positions_
            "kb_screen_stats", "kb_summarize", "kb_gen_inputs",
            "kb_screen_locate", "kb_rung_stats", "kb_rung_promote", "kb_rung_survival", "kb_screen_multi",
            "kb_screen_multi_workspace_bytes", "kb_screen_multi_host_table_bytes", "kb_summarize_multi",
+           "kb_norm_forward", "kb_norm_backward", "kb_norm_backward_workspace_bytes",
            "kb_screen_noalloc", "kb_gen_softmax_rows", "kb_gen_indices", "kb_gen_perturb", "kb_gen_scatter",
            "kb_last_error", "kb_version")
 
@@ -207,6 +211,14 @@ def lib():
         L.kb_gen_perturb.restype = i32
         L.kb_gen_scatter.argtypes = [vp, vp, i32, u64, vp, u32, i32, vp]
         L.kb_gen_scatter.restype = i32
+        i64, size = ctypes.c_int64, ctypes.c_size_t
+        # descriptors of these calls are passed as packed bytes (pack_view)
+        L.kb_norm_forward.argtypes = [vp, vp, vp, f32, vp, vp, vp, vp]
+        L.kb_norm_forward.restype = i32
+        L.kb_norm_backward_workspace_bytes.argtypes = [i64, i64]
+        L.kb_norm_backward_workspace_bytes.restype = size
+        L.kb_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.kb_norm_backward.restype = i32
         L.kb_last_error.argtypes = []
         L.kb_last_error.restype = ctypes.c_char_p
         L.kb_version.argtypes = []
@@ -745,6 +757,109 @@ def kb_gen_scatter(dst, ref, idx, mode, stream=None):
                                 dst.numel(), idx.data_ptr(), idx.numel(), int(mode),
                                 _stream_handle(stream)))
     return dst
+
+
+# ---------------------------------------------------- reference operators ---
+
+_VIEW = struct.Struct("Pii16q")
+_ZEROS = tuple((0,) * n for n in range(KB_MAX_DIMS + 1))
+assert _VIEW.size == ctypes.sizeof(KbTensor)
+
+
+def pack_view(t):
+    """The kb_tensor descriptor of a device tensor as bytes (None: a NULL
+    pointer).  The same bytes as describe()'s, without a ctypes object: 1 us
+    of host time instead of 3, for calls of up to nine tensors."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("a tensor of the device is needed")
+    shape = t.shape
+    n = len(shape)
+    if n > KB_MAX_DIMS:
+        raise ValueError("more than %d dimensions" % KB_MAX_DIMS)
+    pad = _ZEROS[KB_MAX_DIMS - n]
+    return _VIEW.pack(t.data_ptr(), dtype_code(t), n, *shape, *pad, *t.stride(), *pad)
+
+
+def _floats(t, shape, name):
+    """Address of a dense float32 device tensor of a shape (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != _torch().float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be a contiguous float32 device tensor of shape %s" % (name, tuple(shape)))
+    return t.data_ptr()
+
+
+def _on(stream):
+    """Tensors made inside belong to `stream` (None: the current one)."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
+def _scratch(workspace, nbytes, device):
+    """The caller's workspace, or a new one of nbytes (None for 0)."""
+    if workspace is None and nbytes:
+        workspace = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    return workspace
+
+
+def _extent(t):
+    """(address, bytes) of a workspace tensor."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError("the workspace must be a contiguous device tensor")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _rows(t):
+    """A tensor as [rows][cols] over its last axis (a view, never a copy)."""
+    return t if t is None or t.dim() == 2 else t.view(-1, t.shape[-1])
+
+
+def kb_norm_forward(x, w, b, eps=1e-5, y=None, mean=None, rstd=None, stream=None):
+    """Layer norm over the last axis of x; w and b may be None.  Returns
+    (y, mean, rstd), made here where not given; mean and rstd are float32 of
+    x's other axes."""
+    torch = _torch()
+    with _on(stream):
+        if y is None:
+            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if mean is None:
+            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        if rstd is None:
+            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    _check(lib().kb_norm_forward(pack_view(_rows(x)), pack_view(w), pack_view(b), float(eps), pack_view(_rows(y)),
+                                 _floats(mean, x.shape[:-1], "mean"), _floats(rstd, x.shape[:-1], "rstd"),
+                                 _stream_handle(stream)))
+    return y, mean, rstd
+
+
+def kb_norm_backward_workspace_bytes(rows, cols):
+    return lib().kb_norm_backward_workspace_bytes(rows, cols)
+
+
+def kb_norm_backward(dy, x, w, mean, rstd, dx=None, dw=None, db=None, workspace=None, stream=None):
+    """Gradients of kb_norm_forward: (dx, dw, db), made here where not given;
+    dw and db of w's dtype (x's without a weight)."""
+    torch = _torch()
+    cols = x.shape[-1]
+    L = lib()
+    with _on(stream):
+        if dx is None:
+            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if dw is None:
+            dw = torch.empty(cols, dtype=x.dtype if w is None else w.dtype, device=x.device)
+        if db is None:
+            db = torch.empty(cols, dtype=dw.dtype, device=x.device)
+        if workspace is None:
+            rows = x.numel() // cols if cols else 0
+            workspace = _scratch(None, L.kb_norm_backward_workspace_bytes(rows, cols), x.device)
+    ws, nbytes = _extent(workspace)
+    _check(L.kb_norm_backward(pack_view(_rows(dy)), pack_view(_rows(x)), pack_view(w),
+                              _floats(mean, x.shape[:-1], "mean"), _floats(rstd, x.shape[:-1], "rstd"),
+                              pack_view(_rows(dx)), pack_view(dw), pack_view(db), ws, nbytes, _stream_handle(stream)))
+    return dx, dw, db
 
 
 def kb_summarize(records):

@@ -28,6 +28,8 @@ namespace {
 // nothing).
 thread_local char g_error[512];
 
+}  // namespace
+
 void clear_error() { g_error[0] = '\0'; }
 
 int fail(int code, const char* fmt, ...) {
@@ -43,6 +45,8 @@ int fail(int code, const char* fmt, ...) {
 int fail_hip(hipError_t e, const char* what) {
     return fail(KB_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
 
 bool is_float_dtype(int dt) { return dt == DT_F32 || dt == DT_F16 || dt == DT_BF16; }
 size_t elem_size(int dt) { return dt == DT_F32 || dt == DT_U32 ? 4 : 2; }

@@ -1,0 +1,123 @@
+// kb_ops.hpp -- the reference operators (layer norm, attention): parameters
+// that the host fills in, launchers, and the device helpers they share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "kb_device.hpp"
+
+namespace kb {
+
+// ------------------------------------------------------------- layer norm --
+
+// A [rows][cols] view with contiguous rows; stride in elements.
+struct RowView {
+    const void* p;
+    int64_t stride;
+};
+
+struct NormForwardParams {
+    RowView x, y;
+    const void* w;  // NULL: 1
+    const void* b;  // NULL: 0
+    float* mean;    // each may be NULL
+    float* rstd;
+    int64_t rows;
+    int cols;
+    float eps;
+};
+
+struct NormBackwardParams {
+    RowView dy, x, dx;  // dx.p may be NULL
+    const void* w;      // NULL: 1
+    const float* mean;
+    const float* rstd;
+    void* dw;  // each may be NULL
+    void* db;
+    float* part;  // partial column sums: [parts][2][cols] (dw, db)
+    int64_t rows;
+    int cols;
+};
+
+// Row stripes whose column sums are kept apart (NormBackwardParams::part).
+constexpr int kNormMaxParts = 512;
+inline size_t norm_part_bytes(int64_t rows, int64_t cols) {
+    const int64_t parts = rows < kNormMaxParts ? rows : (int64_t)kNormMaxParts;
+    return ((size_t)parts * 2 * (size_t)cols * sizeof(float) + 15) & ~(size_t)15;
+}
+
+// dtype: x's and y's; wdtype: w's, b's, dw's and db's (dtype or DT_F32).
+hipError_t launch_norm_forward(int dtype, int wdtype, const NormForwardParams& p, hipStream_t stream);
+hipError_t launch_norm_backward(int dtype, int wdtype, const NormBackwardParams& p, hipStream_t stream);
+
+// ------------------------------------------------------- storage <-> float --
+
+template <int DT>
+struct Storage;
+template <>
+struct Storage<DT_F32> {
+    using type = float;
+};
+template <>
+struct Storage<DT_F16> {
+    using type = _Float16;
+};
+template <>
+struct Storage<DT_BF16> {
+    using type = __bf16;
+};
+template <int DT>
+using storage_t = typename Storage<DT>::type;
+
+// 16 bytes of elements, readable at any element's alignment (gfx950 loads
+// and stores dwords at any byte address).
+template <typename T>
+struct Vec16 {
+    static constexpr int N = 16 / (int)sizeof(T);
+    typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
+};
+
+// Elements [0, n) of p as floats, 0 past them (n >= N: all).
+template <typename T>
+__device__ __forceinline__ void load_vec(const T* p, int n, float (&out)[Vec16<T>::N]) {
+    constexpr int N = Vec16<T>::N;
+    if (n >= N) {
+        const typename Vec16<T>::type v = *(const typename Vec16<T>::type*)p;
+#pragma unroll
+        for (int e = 0; e < N; ++e) out[e] = (float)v[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) out[e] = e < n ? (float)p[e] : 0.f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(T* p, int n, const float (&in)[Vec16<T>::N]) {
+    constexpr int N = Vec16<T>::N;
+    if (n >= N) {
+        typename Vec16<T>::type v;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v[e] = (T)in[e];
+        *(typename Vec16<T>::type*)p = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < n) p[e] = (T)in[e];
+    }
+}
+
+// Sum over the 64 lanes, the same bits in every lane.
+__device__ __forceinline__ float wave_sum_f32(float v) {
+    const auto step = [](float a, uint32_t b) { return a + __uint_as_float(b); };
+    v = step(v, dpp_u32<DPP_QUAD_XOR1>(__float_as_uint(v)));
+    v = step(v, dpp_u32<DPP_QUAD_XOR2>(__float_as_uint(v)));
+    v = step(v, dpp_u32<DPP_ROW_HALF_MIRROR>(__float_as_uint(v)));
+    v = step(v, dpp_u32<DPP_ROW_MIRROR>(__float_as_uint(v)));
+    const uint32_t u = __float_as_uint(v);
+    return (__uint_as_float(readlane_u32(u, 0)) + __uint_as_float(readlane_u32(u, 16))) +
+           (__uint_as_float(readlane_u32(u, 32)) + __uint_as_float(readlane_u32(u, 48)));
+}
+
+}  // namespace kb

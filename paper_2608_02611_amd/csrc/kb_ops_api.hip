@@ -1,0 +1,258 @@
+// kb_ops_api.hip -- host side of the reference operators (include/kb.h):
+// argument checks, then the launchers.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "kb_internal.hpp"
+#include "kb_ops.hpp"
+
+namespace kb {
+namespace {
+
+bool float_dtype(int dt) { return dt == DT_F32 || dt == DT_F16 || dt == DT_BF16; }
+int element_bytes(int dt) { return dt == DT_F32 ? 4 : 2; }
+
+bool is_empty(const kb_tensor& t) {
+    for (int i = 0; i < t.ndim; ++i)
+        if (t.shape[i] == 0) return true;
+    return false;
+}
+
+// A view of ndim dimensions of a float dtype, its last dimension contiguous,
+// every offset below 2^62 elements.  An output's elements must be distinct:
+// with its dimensions in order of their strides, each stride is at least the
+// extent of the dimensions below it.
+int check_view(const char* call, const char* name, const kb_tensor* t, int ndim, bool output) {
+    if (t == nullptr) return fail(KB_ERR_INVALID_ARG, "%s: null %s", call, name);
+    if (!float_dtype(t->dtype)) return fail(KB_ERR_DTYPE, "%s: %s has dtype %d", call, name, t->dtype);
+    if (t->ndim != ndim) return fail(KB_ERR_INVALID_ARG, "%s: %s has %d dimensions, not %d", call, name, t->ndim, ndim);
+    for (int i = 0; i < ndim; ++i)
+        if (t->shape[i] < 0 || t->shape[i] > INT32_MAX)
+            return fail(KB_ERR_INVALID_ARG, "%s: dimension %d of %s is %lld", call, i, name, (long long)t->shape[i]);
+    if (is_empty(*t)) return KB_OK;
+    if (t->data == nullptr) return fail(KB_ERR_INVALID_ARG, "%s: null data of %s", call, name);
+    if ((uintptr_t)t->data % element_bytes(t->dtype))
+        return fail(KB_ERR_ALIGNMENT, "%s: %s is not aligned to its element", call, name);
+    if (t->shape[ndim - 1] > 1 && t->strides[ndim - 1] != 1)
+        return fail(KB_ERR_INVALID_ARG, "%s: the last dimension of %s is not contiguous", call, name);
+    for (int i = 0; i < ndim; ++i)
+        if (t->shape[i] > 1 && (t->strides[i] < 0 || t->strides[i] > ((int64_t)1 << 60) / t->shape[i]))
+            return fail(KB_ERR_INVALID_ARG, "%s: stride %d of %s is %lld", call, i, name, (long long)t->strides[i]);
+    if (!output) return KB_OK;
+    int order[KB_MAX_DIMS], n = 0;
+    for (int i = 0; i < ndim; ++i) {
+        if (t->shape[i] <= 1) continue;
+        int at = n++;
+        for (; at > 0 && t->strides[order[at - 1]] > t->strides[i]; --at) order[at] = order[at - 1];
+        order[at] = i;
+    }
+    int64_t extent = 1;  // elements from the first to the last of the dimensions so far
+    for (int k = 0; k < n; ++k) {
+        const int i = order[k];
+        if (t->strides[i] < extent)
+            return fail(KB_ERR_INVALID_ARG, "%s: elements of %s share memory (stride %lld)", call, name,
+                        (long long)t->strides[i]);
+        extent += t->strides[i] * (t->shape[i] - 1);
+    }
+    return KB_OK;
+}
+
+int check_shape(const char* call, const char* name, const kb_tensor& t, const char* like, const kb_tensor& ref) {
+    if (t.dtype != ref.dtype)
+        return fail(KB_ERR_DTYPE, "%s: %s has dtype %d, %s has %d", call, name, t.dtype, like, ref.dtype);
+    for (int i = 0; i < ref.ndim; ++i)
+        if (t.shape[i] != ref.shape[i])
+            return fail(KB_ERR_INVALID_ARG, "%s: dimension %d of %s is %lld, of %s %lld", call, i, name,
+                        (long long)t.shape[i], like, (long long)ref.shape[i]);
+    return KB_OK;
+}
+
+// A weight-like vector [cols]: of x's dtype or F32, and of the others'.
+int check_vector(const char* call, const char* name, const kb_tensor* t, const kb_tensor& x, int* wdtype, bool output) {
+    if (t == nullptr) return KB_OK;
+    if (const int rc = check_view(call, name, t, 1, output)) return rc;
+    if (t->shape[0] != x.shape[1])
+        return fail(KB_ERR_INVALID_ARG, "%s: %s has %lld elements, not %lld", call, name, (long long)t->shape[0],
+                    (long long)x.shape[1]);
+    if (t->dtype != x.dtype && t->dtype != DT_F32)
+        return fail(KB_ERR_DTYPE, "%s: %s has dtype %d, neither x's nor F32", call, name, t->dtype);
+    if (*wdtype >= 0 && *wdtype != t->dtype)
+        return fail(KB_ERR_DTYPE, "%s: %s has dtype %d, another vector %d", call, name, t->dtype, *wdtype);
+    *wdtype = t->dtype;
+    return KB_OK;
+}
+
+// [first, last] bytes of a view that is not empty.
+void byte_range(const kb_tensor& t, uintptr_t* first, uintptr_t* last) {
+    int64_t extent = 1;
+    for (int i = 0; i < t.ndim; ++i)
+        if (t.shape[i] > 1) extent += t.strides[i] * (t.shape[i] - 1);
+    *first = (uintptr_t)t.data;
+    *last = *first + (uintptr_t)extent * element_bytes(t.dtype) - 1;
+}
+
+// Whether two views can share memory: overlapping ranges, unless both walk the
+// memory with the same strides, at places that never meet (the q, k and v
+// columns of one projection).
+bool may_overlap(const kb_tensor& a, const kb_tensor& b) {
+    if (is_empty(a) || is_empty(b)) return false;
+    uintptr_t a0, a1, b0, b1;
+    byte_range(a, &a0, &a1);
+    byte_range(b, &b0, &b1);
+    if (a1 < b0 || b1 < a0) return false;
+    if (a.ndim != b.ndim || a.dtype != b.dtype) return true;
+    // the offset between them in strides, largest first, must place b's block
+    // beside a's along one dimension within one period of the next larger
+    int64_t off = (int64_t)((a0 < b0 ? b0 - a0 : a0 - b0));
+    if (off % element_bytes(a.dtype)) return true;
+    off /= element_bytes(a.dtype);
+    const kb_tensor& lo = a0 < b0 ? a : b;
+    const kb_tensor& hi = a0 < b0 ? b : a;
+    // the common outer dimensions: those whose stride (equal in both) exceeds
+    // the offset plus the extent of everything inside
+    for (int64_t bound = INT64_MAX;;) {
+        // the largest stride below bound among the dimensions with more than one element
+        int64_t s = -1;
+        for (int i = 0; i < a.ndim; ++i) {
+            if (lo.shape[i] > 1 && lo.strides[i] < bound && lo.strides[i] > s) s = lo.strides[i];
+            if (hi.shape[i] > 1 && hi.strides[i] < bound && hi.strides[i] > s) s = hi.strides[i];
+        }
+        if (s <= 0) return true;
+        int64_t ext_lo = 1, ext_hi = 1;  // of the dimensions with smaller strides
+        for (int i = 0; i < a.ndim; ++i) {
+            if (lo.shape[i] > 1 && lo.strides[i] < s) ext_lo += lo.strides[i] * (lo.shape[i] - 1);
+            if (hi.shape[i] > 1 && hi.strides[i] < s) ext_hi += hi.strides[i] * (hi.shape[i] - 1);
+        }
+        // modulo s the two blocks are [0, ext_lo) and [off mod s, off mod s + ext_hi)
+        const int64_t at = off % s;
+        if (ext_lo <= s && ext_hi <= s && at >= ext_lo && at + ext_hi <= s) {
+            // apart modulo s: apart altogether if every larger stride is a multiple of s
+            bool multiple = true;
+            for (int i = 0; i < a.ndim; ++i) {
+                if (lo.shape[i] > 1 && lo.strides[i] > s && lo.strides[i] % s) multiple = false;
+                if (hi.shape[i] > 1 && hi.strides[i] > s && hi.strides[i] % s) multiple = false;
+            }
+            if (multiple) return false;
+        }
+        bound = s;
+    }
+}
+
+struct Named {
+    const char* name;
+    const kb_tensor* t;
+};
+
+// Every output apart from the inputs and from the other outputs.
+int check_apart(const char* call, const Named* outs, int n_outs, const Named* ins, int n_ins) {
+    for (int o = 0; o < n_outs; ++o) {
+        if (outs[o].t == nullptr) continue;
+        for (int k = 0; k < o + n_ins; ++k) {
+            const Named& other = k < o ? outs[k] : ins[k - o];
+            if (other.t != nullptr && may_overlap(*outs[o].t, *other.t))
+                return fail(KB_ERR_INVALID_ARG, "%s: %s overlaps %s", call, outs[o].name, other.name);
+        }
+    }
+    return KB_OK;
+}
+
+// A dense float array as a view, for check_apart.
+kb_tensor float_array(const float* p, int64_t n) {
+    kb_tensor t{};
+    t.data = p;
+    t.dtype = DT_F32;
+    t.ndim = 1;
+    t.shape[0] = p ? n : 0;
+    t.strides[0] = 1;
+    return t;
+}
+
+int check_workspace(const char* call, const void* ws, size_t bytes, size_t need) {
+    if (need == 0) return KB_OK;
+    if (ws == nullptr || bytes < need)
+        return fail(KB_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", call, ws ? bytes : (size_t)0, need);
+    if ((uintptr_t)ws & 15u) return fail(KB_ERR_ALIGNMENT, "%s: workspace not 16-byte aligned", call);
+    return KB_OK;
+}
+
+RowView row_view(const kb_tensor* t) {
+    return t ? RowView{t->data, t->shape[0] > 1 ? t->strides[0] : 0} : RowView{nullptr, 0};
+}
+
+const void* data_of(const kb_tensor* t) { return t ? t->data : nullptr; }
+
+int check_rows(const char* call, const kb_tensor& x) {
+    if (x.shape[1] == 0 && x.shape[0] > 0) return fail(KB_ERR_INVALID_ARG, "%s: rows of no element", call);
+    return KB_OK;
+}
+
+}  // namespace
+}  // namespace kb
+
+using namespace kb;
+
+extern "C" {
+
+int kb_norm_forward(const kb_tensor* x, const kb_tensor* w, const kb_tensor* b, float eps, const kb_tensor* y,
+                    float* mean, float* rstd, hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_norm_forward";
+    int rc, wdtype = -1;
+    if ((rc = check_view(call, "x", x, 2, false)) || (rc = check_rows(call, *x)) ||
+        (rc = check_view(call, "y", y, 2, true)) || (rc = check_shape(call, "y", *y, "x", *x)) ||
+        (rc = check_vector(call, "w", w, *x, &wdtype, false)) || (rc = check_vector(call, "b", b, *x, &wdtype, false)))
+        return rc;
+    if (!std::isfinite(eps) || eps < 0.f) return fail(KB_ERR_INVALID_ARG, "%s: eps not finite and >= 0", call);
+    if (((uintptr_t)mean | (uintptr_t)rstd) & 3u)
+        return fail(KB_ERR_ALIGNMENT, "%s: mean or rstd not aligned to its element", call);
+    if (is_empty(*x)) return KB_OK;
+    const bool in_place = y->data == x->data && (x->shape[0] == 1 || y->strides[0] == x->strides[0]);
+    const kb_tensor tm = float_array(mean, x->shape[0]), tr = float_array(rstd, x->shape[0]);
+    const Named outs[] = {{"y", y}, {"mean", &tm}, {"rstd", &tr}};
+    const Named ins[] = {{"w", w}, {"b", b}, {"x", x}};
+    if ((rc = check_apart(call, outs, 1, ins, in_place ? 2 : 3)) || (rc = check_apart(call, outs, 3, ins, 2)) ||
+        (rc = check_apart(call, outs + 1, 2, ins, 3)))
+        return rc;
+    const NormForwardParams p{row_view(x), row_view(y), data_of(w), data_of(b), mean, rstd, x->shape[0],
+                              (int)x->shape[1], eps};
+    const hipError_t e = launch_norm_forward(x->dtype, wdtype < 0 ? x->dtype : wdtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_norm_forward: launch");
+}
+
+size_t kb_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || rows > INT32_MAX || cols > INT32_MAX) return 0;
+    return norm_part_bytes(rows, cols);
+}
+
+int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w, const float* mean, const float* rstd,
+                     const kb_tensor* dx, const kb_tensor* dw, const kb_tensor* db, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_norm_backward";
+    int rc, wdtype = -1;
+    if ((rc = check_view(call, "dy", dy, 2, false)) || (rc = check_view(call, "x", x, 2, false)) ||
+        (rc = check_rows(call, *x)) || (rc = check_shape(call, "dy", *dy, "x", *x)) ||
+        (dx && ((rc = check_view(call, "dx", dx, 2, true)) || (rc = check_shape(call, "dx", *dx, "x", *x)))) ||
+        (rc = check_vector(call, "w", w, *x, &wdtype, false)) || (rc = check_vector(call, "dw", dw, *x, &wdtype, true)) ||
+        (rc = check_vector(call, "db", db, *x, &wdtype, true)))
+        return rc;
+    if (!is_empty(*x) && (mean == nullptr || rstd == nullptr))
+        return fail(KB_ERR_INVALID_ARG, "%s: null mean or rstd", call);
+    if (((uintptr_t)mean | (uintptr_t)rstd) & 3u)
+        return fail(KB_ERR_ALIGNMENT, "%s: mean or rstd not aligned to its element", call);
+    const size_t need = dw || db ? norm_part_bytes(x->shape[0], x->shape[1]) : 0;
+    if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
+    const kb_tensor tm = float_array(mean, x->shape[0]), tr = float_array(rstd, x->shape[0]);
+    const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
+    const Named outs[] = {{"dx", dx}, {"dw", dw}, {"db", db}, {"the workspace", &tw}};
+    const Named ins[] = {{"dy", dy}, {"x", x}, {"w", w}, {"mean", &tm}, {"rstd", &tr}};
+    if ((rc = check_apart(call, outs, 4, ins, 5))) return rc;
+    if (x->shape[1] == 0 || (x->shape[0] == 0 && !dw && !db)) return KB_OK;
+    const NormBackwardParams p{row_view(dy), row_view(x), row_view(dx), data_of(w), mean, rstd, (void*)data_of(dw),
+                               (void*)data_of(db), (float*)workspace, x->shape[0], (int)x->shape[1]};
+    const hipError_t e = launch_norm_backward(x->dtype, wdtype < 0 ? x->dtype : wdtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_norm_backward: launch");
+}
+
+}  // extern "C"

@@ -32,7 +32,8 @@
  * candidates (kb_screen_multi), the rung benchmarker's statistics and
  * promotion decision (kb_rung_stats, kb_rung_promote, kb_rung_survival),
  * kb_screen_noalloc for callers that cannot allocate, and operators whose
- * outputs serve as references (kb_norm_forward, kb_norm_backward).
+ * outputs serve as references (kb_norm_forward, kb_norm_backward,
+ * kb_attn_forward, kb_attn_backward).
  *
  * Conventions
  *   - Every function is extern "C" and returns an int status: KB_OK (0) or a
@@ -691,6 +692,64 @@ size_t kb_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
 int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w, const float* mean,
                      const float* rstd, const kb_tensor* dx, const kb_tensor* dw, const kb_tensor* db,
                      void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Largest head dimension of the attention calls. */
+#define KB_ATTN_MAX_DIM 128
+
+/* kb_attn_opts.flags */
+enum {
+    KB_ATTN_CAUSAL = 1u << 0 /* query i of a sequence with Q queries and K keys sees keys j <= i + K - Q */
+};
+
+/* What the two attention calls share.  q_lens, k_lens: device int32[batch],
+ * or NULL: sequence b has queries 0 .. q_lens[b) and keys 0 .. k_lens[b) (a
+ * value outside [0, len] counts as the nearer end); rows past them are
+ * padding, never read as a query or key, whatever they hold. */
+typedef struct kb_attn_opts {
+    float scale; /* of the scores; finite and > 0 */
+    uint32_t flags;
+    const int32_t* q_lens;
+    const int32_t* k_lens;
+} kb_attn_opts;
+
+/* Softmax attention.  q, o: [batch][heads][len_q][dim]; k, v:
+ * [batch][kv_heads][len_k][dim]; query head h reads key head
+ * h / (heads / kv_heads).  For query i, over the keys j that it sees:
+ *   s_j = scale q_i . k_j,  lse_i = log sum_j exp(s_j),
+ *   o_i = sum_j exp(s_j - lse_i) v_j.
+ * A query that sees no key (or only scores of -infinity), and a query of the
+ * padding, has o = 0 and lse = -infinity.  A NaN or infinity reaches just the
+ * queries that see it.  q, k, v, o: one dtype, F32, F16 or BF16.  lse: device
+ * float[batch][heads][len_q], never NULL.  With a 16-bit dtype the softmax
+ * terms are rounded to it before their product with v (as they are at most 1
+ * before the division by their sum, by at most 2^-11 or 2^-8 of the largest).
+ * workspace: 16-byte aligned, not less than kb_attn_forward_workspace_bytes
+ * (which may be 0: then NULL will do); it needs no initialisation.
+ * Errors: KB_ERR_INVALID_ARG (null descriptors or data, shapes that do not
+ * fit, dim not in [1, KB_ATTN_MAX_DIM], strides, scale or flags out of
+ * range), KB_ERR_DTYPE, KB_ERR_ALIGNMENT, KB_ERR_WORKSPACE, KB_ERR_HIP. */
+size_t kb_attn_forward_workspace_bytes(const kb_tensor* q, const kb_tensor* k);
+int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
+                    const kb_attn_opts* opts, const kb_tensor* o, float* lse, void* workspace,
+                    size_t workspace_bytes, hipStream_t stream);
+
+/* Gradients of kb_attn_forward, the probabilities computed again from q, k
+ * and lse: with p_ij = exp(s_ij - lse_i), D_i = dout_i . o_i and
+ * t_ij = p_ij (dout_i . v_j - D_i),
+ *   dq_i = scale sum_j t_ij k_j,  dk_j = scale sum_i t_ij q_i,
+ *   dv_j = sum_i p_ij dout_i,
+ * dk and dv summed over the query heads that share the key head.  Padding has
+ * gradient 0.  dout, o, dq: q's shape; dk, dv: k's; lse: the forward call's.
+ * One dtype throughout.  With a 16-bit dtype p and t are rounded to it before
+ * their products (F16: scaled by powers of two so that small ones keep their
+ * bits).  workspace: 16-byte aligned, not less than
+ * kb_attn_backward_workspace_bytes; it needs no initialisation.
+ * Errors as kb_attn_forward. */
+size_t kb_attn_backward_workspace_bytes(const kb_tensor* q, const kb_tensor* k);
+int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
+                     const kb_tensor* o, const float* lse, const kb_attn_opts* opts,
+                     const kb_tensor* dq, const kb_tensor* dk, const kb_tensor* dv, void* workspace,
+                     size_t workspace_bytes, hipStream_t stream);
 
 /* ----------------------------------------------------------------- misc -- */
 

@@ -6,7 +6,7 @@ current stream.  The names mirror the C interface in include/kb.h:
 
     kb_policy_check, kb_screen_workspace_bytes, kb_screen_launch, kb_screen,
     kb_screen_stats, kb_gen_inputs, kb_norm_forward, kb_norm_backward,
-    kb_last_error, kb_version
+    kb_attn_forward, kb_attn_backward, kb_last_error, kb_version
 
 plus `screen(...)`, which chains the gate, the kernel and the readback for the
 common case.  The pass/fail verdict of each record comes from the library
@@ -35,6 +35,8 @@ KB_STATUS_OK, KB_REJECT_NULL, KB_REJECT_DTYPE, KB_REJECT_SHAPE, KB_REJECT_LAYOUT
 KB_EQUAL_NAN = 1
 KB_FAIL_FAST = 2
 KB_MAX_DIMS = 8
+KB_ATTN_CAUSAL = 1
+KB_ATTN_MAX_DIM = 128
 
 ERROR_NAMES = {KB_ERR_INVALID_ARG: "KB_ERR_INVALID_ARG", KB_ERR_DTYPE: "KB_ERR_DTYPE",
                KB_ERR_WORKSPACE: "KB_ERR_WORKSPACE", KB_ERR_ALIGNMENT: "KB_ERR_ALIGNMENT",
@@ -137,6 +139,8 @@ EXPORTS = ("kb_policy_check", "kb_screen_workspace_bytes", "kb_screen_positions_
            "kb_screen_locate", "kb_rung_stats", "kb_rung_promote", "kb_rung_survival", "kb_screen_multi",
            "kb_screen_multi_workspace_bytes", "kb_screen_multi_host_table_bytes", "kb_summarize_multi",
            "kb_norm_forward", "kb_norm_backward", "kb_norm_backward_workspace_bytes",
+           "kb_attn_forward", "kb_attn_forward_workspace_bytes",
+           "kb_attn_backward", "kb_attn_backward_workspace_bytes",
            "kb_screen_noalloc", "kb_gen_softmax_rows", "kb_gen_indices", "kb_gen_perturb", "kb_gen_scatter",
            "kb_last_error", "kb_version")
 
@@ -219,6 +223,13 @@ def lib():
         L.kb_norm_backward_workspace_bytes.restype = size
         L.kb_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
         L.kb_norm_backward.restype = i32
+        for name in ("kb_attn_forward_workspace_bytes", "kb_attn_backward_workspace_bytes"):
+            getattr(L, name).argtypes = [vp, vp]
+            getattr(L, name).restype = size
+        L.kb_attn_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.kb_attn_forward.restype = i32
+        L.kb_attn_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.kb_attn_backward.restype = i32
         L.kb_last_error.argtypes = []
         L.kb_last_error.restype = ctypes.c_char_p
         L.kb_version.argtypes = []
@@ -762,8 +773,9 @@ def kb_gen_scatter(dst, ref, idx, mode, stream=None):
 # ---------------------------------------------------- reference operators ---
 
 _VIEW = struct.Struct("Pii16q")
+_OPTS = struct.Struct("fIPP")
 _ZEROS = tuple((0,) * n for n in range(KB_MAX_DIMS + 1))
-assert _VIEW.size == ctypes.sizeof(KbTensor)
+assert _VIEW.size == ctypes.sizeof(KbTensor) and _OPTS.size == 24
 
 
 def pack_view(t):
@@ -860,6 +872,77 @@ def kb_norm_backward(dy, x, w, mean, rstd, dx=None, dw=None, db=None, workspace=
                               _floats(mean, x.shape[:-1], "mean"), _floats(rstd, x.shape[:-1], "rstd"),
                               pack_view(_rows(dx)), pack_view(dw), pack_view(db), ws, nbytes, _stream_handle(stream)))
     return dx, dw, db
+
+
+def _lens(t, batch, name):
+    """Address of an int32 device tensor of one length per sequence (None: NULL as 0)."""
+    if t is None:
+        return 0
+    if t.dtype != _torch().int32 or tuple(t.shape) != (batch,) or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be a contiguous int32 device tensor of %d lengths" % (name, batch))
+    return t.data_ptr()
+
+
+def _attn_opts(q, scale, causal, q_lens, k_lens):
+    batch, dim = q.shape[0], q.shape[-1]
+    if scale is None:
+        scale = max(dim, 1) ** -0.5
+    return _OPTS.pack(scale, KB_ATTN_CAUSAL if causal else 0, _lens(q_lens, batch, "q_lens"),
+                      _lens(k_lens, batch, "k_lens"))
+
+
+def kb_attn_forward_workspace_bytes(q, k):
+    return lib().kb_attn_forward_workspace_bytes(pack_view(q), pack_view(k))
+
+
+def kb_attn_forward(q, k, v, scale=None, causal=False, q_lens=None, k_lens=None, o=None, lse=None, workspace=None,
+                    stream=None):
+    """Softmax attention of q [batch][heads][len_q][dim] on k and v
+    [batch][kv_heads][len_k][dim], views of any strides with a contiguous last
+    dimension; scale: dim^-1/2 if None; q_lens, k_lens: int32 [batch] device
+    tensors of lengths.  Returns (o, lse), made here where not given."""
+    torch = _torch()
+    L = lib()
+    opts = _attn_opts(q, scale, causal, q_lens, k_lens)
+    pq, pk = pack_view(q), pack_view(k)
+    with _on(stream):
+        if o is None:
+            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+        if workspace is None:
+            workspace = _scratch(None, L.kb_attn_forward_workspace_bytes(pq, pk), q.device)
+    ws, nbytes = _extent(workspace)
+    _check(L.kb_attn_forward(pq, pk, pack_view(v), opts, pack_view(o), _floats(lse, q.shape[:-1], "lse"), ws, nbytes,
+                             _stream_handle(stream)))
+    return o, lse
+
+
+def kb_attn_backward_workspace_bytes(q, k):
+    return lib().kb_attn_backward_workspace_bytes(pack_view(q), pack_view(k))
+
+
+def kb_attn_backward(dout, q, k, v, o, lse, scale=None, causal=False, q_lens=None, k_lens=None, dq=None, dk=None,
+                     dv=None, workspace=None, stream=None):
+    """Gradients of kb_attn_forward: (dq, dk, dv), made here where not given
+    (dense, of q's and k's shapes)."""
+    torch = _torch()
+    L = lib()
+    opts = _attn_opts(q, scale, causal, q_lens, k_lens)
+    pq, pk = pack_view(q), pack_view(k)
+    with _on(stream):
+        if dq is None:
+            dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if dk is None:
+            dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        if dv is None:
+            dv = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        if workspace is None:
+            workspace = _scratch(None, L.kb_attn_backward_workspace_bytes(pq, pk), q.device)
+    ws, nbytes = _extent(workspace)
+    _check(L.kb_attn_backward(pack_view(dout), pq, pk, pack_view(v), pack_view(o), _floats(lse, q.shape[:-1], "lse"),
+                              opts, pack_view(dq), pack_view(dk), pack_view(dv), ws, nbytes, _stream_handle(stream)))
+    return dq, dk, dv
 
 
 def kb_summarize(records):

@@ -1,0 +1,279 @@
+// kb_attn.hpp -- device helpers of the attention kernels: tiles of rows in
+// LDS, the fragments that the matrix instructions take from them, masks.
+//
+// Matrix products are 32x32 tiles, 16 along the contraction at a time.  Lane l
+// (c = l % 32, g = l / 32) holds for the left operand A[m = c][k = 8g .. 8g+7],
+// for the right one B[k = 8g .. 8g+7][n = c], and of the result
+// C[m = 8(r/4) + 4g + r%4][n = c], r = 0..15.  A result is the right operand of
+// the next product without moving: its rows r = 8j .. 8j+7 are a right operand
+// whose contraction index runs 16j + {4g .. 4g+3, 8+4g .. 8+4g+3}, and the left
+// operand is read from LDS in that order (col_frag).  So scores are computed
+// transposed where the next product runs over keys, and straight where it runs
+// over queries.
+#pragma once
+
+#include "kb_ops.hpp"
+
+namespace kb {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32v4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Eight elements along the contraction.
+template <int DT>
+struct Frag {
+    typedef storage_t<DT> type __attribute__((ext_vector_type(8)));
+};
+template <int DT>
+using frag_t = typename Frag<DT>::type;
+
+__device__ __forceinline__ f32x16 mma(frag_t<DT_F16> a, frag_t<DT_F16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mma(frag_t<DT_BF16> a, frag_t<DT_BF16> b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+// binary32: element e of the eight is one product of contraction length 2.
+__device__ __forceinline__ f32x16 mma(frag_t<DT_F32> a, frag_t<DT_F32> b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+
+// A tile of rows in LDS: DP elements a row (the head dimension rounded up,
+// zeros past it) at a pitch of 64 or 128 elements, in 16-byte chunks.  Chunk
+// c of row r lies at c ^ turn(r), so that neither the 16 rows that a row read
+// touches at one chunk nor the 4 rows x 64 bytes of a transposed read fall on
+// the same banks.
+template <int DT, int DP>
+struct Tile {
+    using T = storage_t<DT>;
+    static constexpr int VEC = 16 / (int)sizeof(T);
+    static constexpr int PITCH = DP <= 64 ? 64 : 128;
+    static constexpr int CHUNKS = DP / VEC;
+    static constexpr int PITCH_BYTES = PITCH * (int)sizeof(T);
+
+    __device__ static __forceinline__ int turn(int row) {
+        if (PITCH_BYTES == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+        return ((row & 3) << 2) | ((row >> 2) & 3);
+    }
+    __device__ static __forceinline__ int at(int row, int d) {
+        return row * PITCH + (((d / VEC) ^ turn(row)) * VEC) + d % VEC;
+    }
+};
+
+// 16 bytes of a row from element d on, zeros past dim (unaligned rows are fine).
+template <typename T>
+__device__ __forceinline__ u32v4 load_chunk(const T* row, int d, int dim) {
+    constexpr int N = Vec16<T>::N;
+    typename Vec16<T>::type v;
+    if (d + N <= dim) return __builtin_bit_cast(u32v4, *(const typename Vec16<T>::type*)(row + d));
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = d + e < dim ? row[d + e] : (T)0.f;
+    return __builtin_bit_cast(u32v4, v);
+}
+
+// Rows [r0, r0 + ROWS) of a view into a tile by NT threads; rows from n on are
+// zeros and not read.
+template <int DT, int DP, int ROWS, int NT>
+__device__ __forceinline__ void stage(storage_t<DT>* tile, const storage_t<DT>* base, int64_t stride, int r0, int n,
+                                      int dim) {
+    using L = Tile<DT, DP>;
+#pragma unroll
+    for (int k = 0; k < (ROWS * L::CHUNKS + NT - 1) / NT; ++k) {
+        const int idx = k * NT + (int)threadIdx.x;
+        if (ROWS * L::CHUNKS % NT != 0 && idx >= ROWS * L::CHUNKS) break;
+        const int row = idx / L::CHUNKS, d = idx % L::CHUNKS * L::VEC;
+        u32v4 v = {0, 0, 0, 0};
+        if (r0 + row < n) v = load_chunk(base + (int64_t)(r0 + row) * stride, d, dim);
+        *(u32v4*)(tile + L::at(row, d)) = v;
+    }
+}
+
+// Elements d = 16c + 8g .. +7 of a row of the tile.
+template <int DT, int DP>
+__device__ __forceinline__ frag_t<DT> row_frag(const storage_t<DT>* tile, int row, int c, int g) {
+    using L = Tile<DT, DP>;
+    if constexpr (DT == DT_F32) {
+        const f32x4 a = *(const f32x4*)(tile + L::at(row, 16 * c + 8 * g));
+        const f32x4 b = *(const f32x4*)(tile + L::at(row, 16 * c + 8 * g + 4));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+        return *(const frag_t<DT>*)(tile + L::at(row, 16 * c + 8 * g));
+    }
+}
+
+// Column d = 32 db + c of rows row0 + {4g .. 4g+3, 8+4g .. 8+4g+3}.  In 16 bits
+// each four come from one transposed read: of 16 lanes, lane i gives the
+// address of 4 elements of row i/4, columns 4(i%4) .., and receives column i of
+// the four rows.
+template <int DT, int DP>
+__device__ __forceinline__ frag_t<DT> col_frag(const storage_t<DT>* tile, int row0, int db, int lane) {
+    using L = Tile<DT, DP>;
+    const int g = lane >> 5;
+    if constexpr (DT == DT_F32) {
+        frag_t<DT> f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = tile[L::at(row0 + 8 * (e >> 2) + 4 * g + (e & 3), 32 * db + (lane & 31))];
+        return f;
+    } else {
+        const int row = row0 + 4 * g + ((lane & 15) >> 2), d = 32 * db + (lane & 16) + 4 * (lane & 3);
+        using lds_ptr = __attribute__((address_space(3))) s16x4*;
+        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)(tile + L::at(row, d)));
+        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)(tile + L::at(row + 8, d)));
+        return __builtin_bit_cast(frag_t<DT>, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+}
+
+// Eight elements of a row in memory, d = 16c + 8g .., zeros past dim or if !in.
+template <int DT>
+__device__ __forceinline__ frag_t<DT> load_frag(const storage_t<DT>* row, int c, int g, int dim, bool in) {
+    using T = storage_t<DT>;
+    constexpr int N = Vec16<T>::N;
+    frag_t<DT> f;
+#pragma unroll
+    for (int k = 0; k < 8 / N; ++k) {
+        u32v4 v = {0, 0, 0, 0};
+        if (in) v = load_chunk(row, 16 * c + 8 * g + k * N, dim);
+        const typename Vec16<T>::type t = __builtin_bit_cast(typename Vec16<T>::type, v);
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[k * N + e] = t[e];
+    }
+    return f;
+}
+
+// Rows 8j .. 8j+7 of a result as a right operand in the storage type.
+template <int DT>
+__device__ __forceinline__ frag_t<DT> narrow(const f32x16& s, int j) {
+    frag_t<DT> f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = (storage_t<DT>)s[8 * j + e];
+    return f;
+}
+
+template <int DT>
+__device__ __forceinline__ bool any_non_finite(frag_t<DT> f) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (DT == DT_F32)
+            bad |= (__float_as_uint(f[e]) & 0x7F800000u) == 0x7F800000u;
+        else if constexpr (DT == DT_F16)
+            bad |= (__builtin_bit_cast(uint16_t, (_Float16)f[e]) & 0x7C00u) == 0x7C00u;
+        else
+            bad |= (__builtin_bit_cast(uint16_t, (__bf16)f[e]) & 0x7F80u) == 0x7F80u;
+    }
+    return bad;
+}
+
+// acc += A B over 16 rows of a tile where column n of B sees rows [lo, hi) of
+// it only (lo, hi: the lane's column's).  B is 0 elsewhere, and A's values
+// there drop out of the product as they are finite; where they are not, this
+// form is taken: a product for each column with A's other rows cleared.
+template <int DT>
+__device__ void mma_seen(f32x16& acc, frag_t<DT> a, frag_t<DT> b, int row0, int lo, int hi, int lane) {
+    const int g = lane >> 5;
+    for (int n = 0; n < 32; ++n) {
+        const int from = __builtin_amdgcn_readlane(lo, n), to = __builtin_amdgcn_readlane(hi, n);
+        frag_t<DT> cut = a;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int row = row0 + 8 * (e >> 2) + 4 * g + (e & 3);
+            if (row < from || row >= to) cut[e] = (storage_t<DT>)0.f;
+        }
+        f32x16 t = {};
+        t = mma(cut, b, t);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = (lane & 31) == n ? acc[r] + t[r] : acc[r];
+    }
+}
+
+// acc[db] += (rows [row0, row0 + 32) of the tile)^T b, b in two halves; with
+// `part` some (row, column) pairs are not seen, and the rows are looked through
+// for values that must not reach the columns that do not see them.
+template <int DT, int DP>
+__device__ __forceinline__ void mma_rows(f32x16 (&acc)[DP / 32], const storage_t<DT>* tile, int row0,
+                                         const frag_t<DT> (&b)[2], bool part, int lo, int hi, int lane) {
+    if (part) {
+        bool bad = false;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) bad |= any_non_finite<DT>(col_frag<DT, DP>(tile, row0 + 16 * j, db, lane));
+        if (__any(bad)) {
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+                for (int j = 0; j < 2; ++j)
+                    mma_seen<DT>(acc[db], col_frag<DT, DP>(tile, row0 + 16 * j, db, lane), j ? b[1] : b[0],
+                                 row0 + 16 * j, lo, hi, lane);
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+            acc[db] = mma(col_frag<DT, DP>(tile, row0 + 16 * j, db, lane), b[j], acc[db]);
+}
+
+// Elements d = 32 db + 8 q4 + 4 g .. +3 of a row of results.
+template <int DT>
+__device__ __forceinline__ void store_quad(storage_t<DT>* row, int d, int dim, float a, float b, float c, float e) {
+    using T = storage_t<DT>;
+    typedef T quad __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    const float v[4] = {a, b, c, e};
+    if (d + 4 <= dim) {
+        quad t;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = (T)v[k];
+        *(quad*)(row + d) = t;
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (d + k < dim) row[d + k] = (T)v[k];
+    }
+}
+
+// A column of transposed results (the lane's) as a row in memory, times f;
+// zeros if !live (whatever the accumulators hold).
+template <int DT, int DP>
+__device__ __forceinline__ void store_column(storage_t<DT>* row, const f32x16 (&acc)[DP / 32], float f, bool live,
+                                             int dim, int g) {
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            store_quad<DT>(row, 32 * db + 2 * r + 4 * g, dim, live ? acc[db][r] * f : 0.f,
+                           live ? acc[db][r + 1] * f : 0.f, live ? acc[db][r + 2] * f : 0.f,
+                           live ? acc[db][r + 3] * f : 0.f);
+}
+
+// Lengths of sequence b.
+__device__ __forceinline__ int seq_len(const int32_t* lens, int b, int full) {
+    return lens ? min(max(lens[b], 0), full) : full;
+}
+
+// Query i sees keys [0, key_limit).
+__device__ __forceinline__ int key_limit(int i, int qlen, int klen, int causal) {
+    return causal ? min(klen, max(0, i + 1 + klen - qlen)) : klen;
+}
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// Work-groups are numbered so that those of one key head follow each other at
+// a distance of all (batch, head) pairs: with a multiple of 8 pairs (the usual
+// case) a head's work-groups land on one XCD, whose L2 then holds its keys.
+struct HeadBlock {
+    int b, h, block;
+};
+__device__ __forceinline__ HeadBlock head_block(int kv_heads, int pairs) {
+    const int pair = (int)blockIdx.x % pairs;
+    return {pair / kv_heads, pair % kv_heads, (int)blockIdx.x / pairs};
+}
+
+}  // namespace kb

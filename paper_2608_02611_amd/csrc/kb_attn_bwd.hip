@@ -1,0 +1,295 @@
+// kb_attn_bwd.hip -- softmax attention, backward.  With p_ij = exp(s_ij - lse_i),
+// D_i = dout_i . o_i and t_ij = p_ij (dout_i . v_j - D_i):
+//   dq_i = scale S_j t_ij k_j,  dk_j = scale S_i t_ij q_i,  dv_j = S_i p_ij dout_i.
+//
+// The probabilities are computed again, once where the keys stay and the
+// queries pass (dk, dv: 4 products) and once where the queries stay and the
+// keys pass (dq: 3 products).  The 2 products more than the 5 that are needed
+// buy sums in registers: no atomics, no partial gradients in memory, the same
+// bits on every call.
+//
+// F16 holds p and t of a long row badly (its least normal number is 6e-5), so
+// they are scaled by powers of two before they are rounded: p, at most 1, by
+// 2^10; t, at most 2 |dout| |v|, so that this bound comes to at most 2^15.
+#include "kb_attn.hpp"
+
+namespace kb {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kProbScale = 1024.f;
+
+// Workspace: D, then the blocks' largest squared norms of dout and of v.
+__host__ __device__ __forceinline__ int64_t dout_norms_at(const AttnParams& p) {
+    return (int64_t)p.batch * p.heads * p.len_q;
+}
+__host__ __device__ __forceinline__ int64_t v_norms_at(const AttnParams& p) {
+    return dout_norms_at(p) + (int64_t)p.batch * p.heads * ((p.len_q + kNormBlock - 1) / kNormBlock);
+}
+
+// Before the products: D_i for 64 query rows a work-group, 16 lanes a row.  F16:
+// also the largest finite squared norm of the block's rows of dout, and, in
+// the work-groups after those, of 64 rows of v.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p) {
+    using T = storage_t<DT>;
+    constexpr int N = Vec16<T>::N;
+    __shared__ float largest[kThreads / 16];
+    const int q_blocks = (p.len_q + kNormBlock - 1) / kNormBlock, k_blocks = (p.len_k + kNormBlock - 1) / kNormBlock;
+    const int64_t q_total = (int64_t)p.batch * p.heads * q_blocks;
+    const bool of_v = (int64_t)blockIdx.x >= q_total;
+    const int64_t id = of_v ? (int64_t)blockIdx.x - q_total : (int64_t)blockIdx.x;
+    const int blocks = of_v ? k_blocks : q_blocks, heads = of_v ? p.kv_heads : p.heads;
+    const int block = (int)(id % blocks), h = (int)(id / blocks % heads), b = (int)(id / blocks / heads);
+    const int n = of_v ? seq_len(p.k_lens, b, p.len_k) : seq_len(p.q_lens, b, p.len_q);
+    const int sub = threadIdx.x & 15;
+    float top = 0.f;
+    for (int k = 0; k < kNormBlock / 16; ++k) {
+        const int i = block * kNormBlock + k * 16 + (threadIdx.x >> 4);
+        float dot = 0.f, sq = 0.f;
+        if (i < n) {
+            const HeadView& a = of_v ? p.v : p.dout;
+            const T* x = (const T*)a.p + b * a.sb + h * a.sh + i * a.sl;
+            const T* y = (const T*)p.o.p + b * p.o.sb + h * p.o.sh + i * p.o.sl;
+            for (int d = sub * N; d < p.dim; d += 16 * N) {
+                float u[N], w[N];
+                load_vec(x + d, p.dim - d, u);
+                if (!of_v) load_vec(y + d, p.dim - d, w);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (!of_v) dot = fmaf(u[e], w[e], dot);
+                    sq = fmaf(u[e], u[e], sq);
+                }
+            }
+        }
+#pragma unroll
+        for (int s = 1; s < 16; s <<= 1) {
+            dot += __shfl_xor(dot, s);
+            sq += __shfl_xor(sq, s);
+        }
+        if (!of_v && sub == 0 && i < p.len_q) p.ws[((int64_t)b * p.heads + h) * p.len_q + i] = dot;
+        if (sq < INFINITY) top = fmaxf(top, sq);
+    }
+    if (DT != DT_F16) return;
+    if (sub == 0) largest[threadIdx.x >> 4] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < kThreads / 16; ++k) top = fmaxf(top, largest[k]);
+        p.ws[(of_v ? v_norms_at(p) : dout_norms_at(p)) + id] = top;
+    }
+}
+
+// e with |x| < 2^e from the largest x^2 (0 for x = 0).
+__device__ __forceinline__ int bound_exponent(float sq) {
+    if (!(sq > 0.f)) return 0;
+    const int ex = (int)(__float_as_uint(sq) >> 23) - 127;  // sq < 2^(ex + 1)
+    return ((ex + 1) >> 1) + ((ex + 1) & 1);
+}
+
+// F16: 2^(14 - e), |t| < 2^(1 + e) over the heads that share key head h of
+// sequence b; 1 for the other types.  Called by every thread of a work-group.
+template <int DT>
+__device__ __forceinline__ float score_scale(const AttnParams& p, int b, int h, float* shared) {
+    if (DT != DT_F16) return 1.f;
+    const int q_blocks = (p.len_q + kNormBlock - 1) / kNormBlock, k_blocks = (p.len_k + kNormBlock - 1) / kNormBlock;
+    const float* dn = p.ws + dout_norms_at(p) + ((int64_t)b * p.heads + h * p.group) * q_blocks;
+    const float* vn = p.ws + v_norms_at(p) + ((int64_t)b * p.kv_heads + h) * k_blocks;
+    float d = 0.f, v = 0.f;
+    for (int64_t k = threadIdx.x; k < (int64_t)q_blocks * p.group; k += kThreads) d = fmaxf(d, dn[k]);
+    for (int k = threadIdx.x; k < k_blocks; k += kThreads) v = fmaxf(v, vn[k]);
+    const uint32_t wd = wave_max_u32(__float_as_uint(d)), wv = wave_max_u32(__float_as_uint(v));
+    if ((threadIdx.x & 63) == 0) {
+        shared[threadIdx.x >> 6] = __uint_as_float(wd);
+        shared[4 + (threadIdx.x >> 6)] = __uint_as_float(wv);
+    }
+    __syncthreads();
+    d = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
+    v = fmaxf(fmaxf(shared[4], shared[5]), fmaxf(shared[6], shared[7]));
+    return __uint_as_float((uint32_t)(127 + 14 - bound_exponent(d) - bound_exponent(v)) << 23);
+}
+
+// dk and dv of 128 keys, 32 a wave, kept with their key and value rows in
+// registers while the query rows of every head of the group pass in tiles of 32.
+constexpr int kKeyRows = 128;
+constexpr int kQueries = 32;
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams p) {
+    using T = storage_t<DT>;
+    using L = Tile<DT, DP>;
+    __shared__ __align__(16) T qt[kQueries * L::PITCH];
+    __shared__ __align__(16) T dt[kQueries * L::PITCH];
+    __shared__ __align__(16) float norm[kQueries], dots[kQueries], scratch[8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+    const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
+    const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
+    const int first = at.block * kKeyRows, j = first + wave * 32 + (lane & 31);
+    const bool live = j < klen;
+    const float t_scale = score_scale<DT>(p, at.b, at.h, scratch);
+    const float p_scale = DT == DT_F16 ? kProbScale : 1.f;
+
+    const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh + (int64_t)j * p.k.sl;
+    const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh + (int64_t)j * p.v.sl;
+    frag_t<DT> kf[DP / 16], vf[DP / 16];
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        kf[c] = load_frag<DT>(k, c, g, p.dim, live);
+        vf[c] = load_frag<DT>(v, c, g, p.dim, live);
+    }
+    // the queries that see a key: [sees(j), qlen)
+    const auto sees = [&](int key) { return p.causal ? min(qlen, max(0, key - (klen - qlen))) : 0; };
+    const int lo = live ? sees(j) : qlen;
+    const int wave_key = first + wave * 32;
+    const int start = first < klen ? sees(first) / kQueries * kQueries : qlen;
+    const int wave_lo = wave_key < klen ? sees(wave_key) : qlen;
+    const int wave_hi = sees(min(wave_key + 31, klen - 1));  // from here on every key of the wave is seen
+
+    const float to_log2 = p.scale * kLog2e;
+    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    for (int h = 0; h < p.group; ++h) {
+        const int hq = at.h * p.group + h;
+        const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh;
+        const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh;
+        const int64_t rows = ((int64_t)at.b * p.heads + hq) * p.len_q;
+        for (int i0 = start; i0 < qlen; i0 += kQueries) {
+            __syncthreads();
+            stage<DT, DP, kQueries, kThreads>(qt, q, p.q.sl, i0, qlen, p.dim);
+            stage<DT, DP, kQueries, kThreads>(dt, dout, p.dout.sl, i0, qlen, p.dim);
+            if (threadIdx.x < kQueries) {
+                const int i = i0 + (int)threadIdx.x;
+                const float lse = i < qlen ? p.lse[rows + i] : 0.f;
+                norm[threadIdx.x] = lse == -INFINITY ? 0.f : lse * kLog2e;
+                dots[threadIdx.x] = i < qlen ? p.ws[rows + i] : 0.f;
+            }
+            __syncthreads();
+            if (i0 + kQueries <= wave_lo) continue;
+            f32x16 s = {}, t = {};
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                s = mma(row_frag<DT, DP>(qt, lane & 31, c, g), kf[c], s);
+                t = mma(row_frag<DT, DP>(dt, lane & 31, c, g), vf[c], t);
+            }
+            const bool part = i0 < wave_hi || i0 + kQueries > qlen || wave_key + 32 > klen;
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                const f32x4 lse = *(const f32x4*)(norm + 8 * r4 + 4 * g), dot = *(const f32x4*)(dots + 8 * r4 + 4 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = 4 * r4 + e, i = i0 + 8 * r4 + 4 * g + e;
+                    const bool seen = !part || (i >= lo && i < qlen);
+                    const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse[e]));
+                    t[r] = seen ? prob * (t[r] - dot[e]) * t_scale : 0.f;
+                    s[r] = seen ? prob * p_scale : 0.f;
+                }
+            }
+            const frag_t<DT> pf[2] = {narrow<DT>(s, 0), narrow<DT>(s, 1)}, tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
+            mma_rows<DT, DP>(dv, dt, 0, pf, part, lo - i0, qlen - i0, lane);
+            mma_rows<DT, DP>(dk, qt, 0, tf, part, lo - i0, qlen - i0, lane);
+        }
+    }
+    if (j >= p.len_k) return;
+    store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, p.scale / t_scale, live, p.dim, g);
+    store_column<DT, DP>((T*)p.dv.p + at.b * p.dv.sb + at.h * p.dv.sh + j * p.dv.sl, dv, 1.f / p_scale, live, p.dim, g);
+}
+
+// dq of 128 query rows (row = query * group + head, as in the forward pass),
+// 32 a wave, while the keys pass in tiles of 32.
+constexpr int kRows = 128;
+constexpr int kKeys = 32;
+
+template <int DT, int DP>
+__global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnParams p) {
+    using T = storage_t<DT>;
+    using L = Tile<DT, DP>;
+    __shared__ __align__(16) T kt[kKeys * L::PITCH];
+    __shared__ __align__(16) T vt[kKeys * L::PITCH];
+    __shared__ float scratch[8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+    const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
+    const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
+    const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;
+    const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
+    const float t_scale = score_scale<DT>(p, at.b, at.h, scratch);
+
+    const int64_t row = first + wave * 32 + (lane & 31);
+    const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
+    const bool exists = i < p.len_q, live = i < qlen;
+    const int wave_first = (int)((first + wave * 32) / p.group), wave_last = (int)((first + wave * 32 + 31) / p.group);
+    const int block_last = (int)((first + kRows - 1) / p.group);
+    const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
+    const int wave_all = key_limit(min(wave_first, qlen - 1), qlen, klen, p.causal);
+    const int wave_any = wave_first < qlen ? key_limit(min(wave_last, qlen - 1), qlen, klen, p.causal) : 0;
+    const int end = (int)(first / p.group) < qlen ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
+
+    const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh + i * p.q.sl;
+    const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh + i * p.dout.sl;
+    const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh;
+    const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh;
+    frag_t<DT> qf[DP / 16], df[DP / 16];
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        qf[c] = load_frag<DT>(q, c, g, p.dim, live);
+        df[c] = load_frag<DT>(dout, c, g, p.dim, live);
+    }
+    const int64_t at_row = ((int64_t)at.b * p.heads + hq) * p.len_q + i;
+    float lse = live ? p.lse[at_row] : 0.f;
+    lse = lse == -INFINITY ? 0.f : lse * kLog2e;
+    const float dot = live ? p.ws[at_row] : 0.f;
+
+    const float to_log2 = p.scale * kLog2e;
+    f32x16 dq[DP / 32] = {};
+    for (int j0 = 0; j0 < end; j0 += kKeys) {
+        __syncthreads();
+        stage<DT, DP, kKeys, kThreads>(kt, k, p.k.sl, j0, klen, p.dim);
+        stage<DT, DP, kKeys, kThreads>(vt, v, p.v.sl, j0, klen, p.dim);
+        __syncthreads();
+        if (j0 >= wave_any) continue;
+        f32x16 s = {}, t = {};
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) {
+            s = mma(row_frag<DT, DP>(kt, lane & 31, c, g), qf[c], s);
+            t = mma(row_frag<DT, DP>(vt, lane & 31, c, g), df[c], t);
+        }
+        const bool part = j0 + kKeys > wave_all;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const bool seen = !part || j0 + 8 * (r >> 2) + 4 * g + (r & 3) < lim;
+            const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse));
+            t[r] = seen ? prob * (t[r] - dot) * t_scale : 0.f;
+        }
+        const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
+        mma_rows<DT, DP>(dq, kt, 0, tf, part, 0, lim - j0, lane);
+    }
+    if (!exists) return;
+    store_column<DT, DP>((T*)p.dq.p + at.b * p.dq.sb + hq * p.dq.sh + i * p.dq.sl, dq, p.scale / t_scale, live, p.dim, g);
+}
+
+template <int DT, int DP>
+hipError_t backward(const AttnParams& p, hipStream_t stream) {
+    const int64_t pairs = (int64_t)p.batch * p.kv_heads;
+    const int64_t key_blocks = ((int64_t)p.len_k + kKeyRows - 1) / kKeyRows * pairs;
+    const int64_t row_blocks = ((int64_t)p.len_q * p.group + kRows - 1) / kRows * pairs;
+    const int64_t rows = (int64_t)p.batch * p.heads * norm_blocks(p.len_q) +
+                         (DT == DT_F16 ? pairs * norm_blocks(p.len_k) : 0);
+    if (rows > 0) attn_rows_kernel<DT><<<dim3((unsigned)rows), kThreads, 0, stream>>>(p);
+    if (key_blocks > 0) attn_backward_keys_kernel<DT, DP><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
+    if (row_blocks > 0) attn_backward_queries_kernel<DT, DP><<<dim3((unsigned)row_blocks), kThreads, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t backward(const AttnParams& p, hipStream_t stream) {
+    if (p.dim <= 64) return backward<DT, 64>(p, stream);
+    if (p.dim <= 96) return backward<DT, 96>(p, stream);
+    return backward<DT, 128>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_attn_backward(int dtype, const AttnParams& p, hipStream_t stream) {
+    if (dtype == DT_F32) return backward<DT_F32>(p, stream);
+    if (dtype == DT_F16) return backward<DT_F16>(p, stream);
+    return backward<DT_BF16>(p, stream);
+}
+
+}  // namespace kb

@@ -52,6 +52,36 @@ inline size_t norm_part_bytes(int64_t rows, int64_t cols) {
 hipError_t launch_norm_forward(int dtype, int wdtype, const NormForwardParams& p, hipStream_t stream);
 hipError_t launch_norm_backward(int dtype, int wdtype, const NormBackwardParams& p, hipStream_t stream);
 
+// -------------------------------------------------------------- attention --
+
+// A [batch][heads][len][dim] view; strides in elements, dim contiguous.
+struct HeadView {
+    const void* p;
+    int64_t sb, sh, sl;
+};
+
+struct AttnParams {
+    HeadView q, k, v, o;
+    HeadView dout, dq, dk, dv;  // backward
+    float* lse;                 // [batch][heads][len_q]
+    const int32_t* q_lens;      // each may be NULL
+    const int32_t* k_lens;
+    int batch, heads, kv_heads, group;  // group = heads / kv_heads
+    int len_q, len_k, dim;
+    float scale;
+    int causal;
+    float* ws;
+};
+
+// Workspace of the backward pass, in floats: D_i for every query row, then
+// (F16) the largest squared norm of each block of kNormBlock rows of dout and
+// of v.
+constexpr int kNormBlock = 64;
+inline int64_t norm_blocks(int64_t len) { return (len + kNormBlock - 1) / kNormBlock; }
+
+hipError_t launch_attn_forward(int dtype, const AttnParams& p, hipStream_t stream);
+hipError_t launch_attn_backward(int dtype, const AttnParams& p, hipStream_t stream);
+
 // ------------------------------------------------------- storage <-> float --
 
 template <int DT>

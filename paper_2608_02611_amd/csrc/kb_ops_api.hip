@@ -187,6 +187,76 @@ int check_rows(const char* call, const kb_tensor& x) {
     return KB_OK;
 }
 
+HeadView head_view(const kb_tensor* t) { return HeadView{t->data, t->strides[0], t->strides[1], t->strides[2]}; }
+
+constexpr int64_t kMaxLen = (int64_t)1 << 30;
+
+// Sizes of an attention call; false if q and k do not fit together.
+bool attn_sizes(const kb_tensor& q, const kb_tensor& k, AttnParams* p) {
+    if (q.ndim != 4 || k.ndim != 4 || !float_dtype(q.dtype) || k.dtype != q.dtype) return false;
+    for (int i = 0; i < 4; ++i)
+        if (q.shape[i] < 0 || k.shape[i] < 0 || q.shape[i] > kMaxLen || k.shape[i] > kMaxLen) return false;
+    if (k.shape[0] != q.shape[0] || k.shape[3] != q.shape[3] || q.shape[3] < 1 || q.shape[3] > KB_ATTN_MAX_DIM) return false;
+    // key heads divide the query heads (none of either is an empty call)
+    if (k.shape[1] == 0 ? q.shape[1] != 0 : q.shape[1] % k.shape[1] != 0) return false;
+    // work-groups and rows are numbered with 31 bits at most
+    const int64_t heads = q.shape[1] > k.shape[1] ? q.shape[1] : k.shape[1];
+    const int64_t len = q.shape[2] > k.shape[2] ? q.shape[2] : k.shape[2];
+    if (q.shape[0] * heads > kMaxLen || (len > 0 && q.shape[0] * heads > ((int64_t)1 << 36) / len)) return false;
+    p->batch = (int)q.shape[0];
+    p->heads = (int)q.shape[1];
+    p->kv_heads = (int)k.shape[1];
+    p->group = k.shape[1] ? (int)(q.shape[1] / k.shape[1]) : 0;
+    p->len_q = (int)q.shape[2];
+    p->len_k = (int)k.shape[2];
+    p->dim = (int)q.shape[3];
+    return true;
+}
+
+size_t attn_backward_bytes(const AttnParams& p) {
+    const int64_t rows = (int64_t)p.batch * p.heads, pairs = (int64_t)p.batch * p.kv_heads;
+    const int64_t floats = rows * p.len_q + rows * norm_blocks(p.len_q) + pairs * norm_blocks(p.len_k);
+    return ((size_t)floats * sizeof(float) + 15) & ~(size_t)15;
+}
+
+// q, k, v and what hangs on their sizes; fills p.
+int check_attn(const char* call, const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, const kb_attn_opts* opts,
+               AttnParams* p) {
+    int rc;
+    if ((rc = check_view(call, "q", q, 4, false)) || (rc = check_view(call, "k", k, 4, false)) ||
+        (rc = check_view(call, "v", v, 4, false)))
+        return rc;
+    if (k->dtype != q->dtype) return fail(KB_ERR_DTYPE, "%s: k has dtype %d, q has %d", call, k->dtype, q->dtype);
+    if (q->shape[3] < 1 || q->shape[3] > KB_ATTN_MAX_DIM)
+        return fail(KB_ERR_INVALID_ARG, "%s: head dimension %lld not in [1, %d]", call, (long long)q->shape[3],
+                    KB_ATTN_MAX_DIM);
+    if (!attn_sizes(*q, *k, p))
+        return fail(KB_ERR_INVALID_ARG, "%s: q and k do not fit together, or are too large", call);
+    if ((rc = check_shape(call, "v", *v, "k", *k))) return rc;
+    if (opts == nullptr) return fail(KB_ERR_INVALID_ARG, "%s: null opts", call);
+    if (!std::isfinite(opts->scale) || !(opts->scale > 0.f))
+        return fail(KB_ERR_INVALID_ARG, "%s: scale not finite and > 0", call);
+    if (opts->flags & ~(uint32_t)KB_ATTN_CAUSAL)
+        return fail(KB_ERR_INVALID_ARG, "%s: unknown flags 0x%x", call, opts->flags);
+    if (((uintptr_t)opts->q_lens | (uintptr_t)opts->k_lens) & 3u)
+        return fail(KB_ERR_ALIGNMENT, "%s: q_lens or k_lens not aligned to its element", call);
+    p->q = head_view(q);
+    p->k = head_view(k);
+    p->v = head_view(v);
+    p->scale = opts->scale;
+    p->causal = (opts->flags & KB_ATTN_CAUSAL) != 0;
+    p->q_lens = opts->q_lens;
+    p->k_lens = opts->k_lens;
+    return KB_OK;
+}
+
+int check_lse(const char* call, const float* lse, const kb_tensor& q) {
+    if (lse == nullptr && q.shape[0] * q.shape[1] * q.shape[2] > 0)
+        return fail(KB_ERR_INVALID_ARG, "%s: null lse", call);
+    if ((uintptr_t)lse & 3u) return fail(KB_ERR_ALIGNMENT, "%s: lse not aligned to its element", call);
+    return KB_OK;
+}
+
 }  // namespace
 }  // namespace kb
 
@@ -253,6 +323,76 @@ int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w
                                (void*)data_of(db), (float*)workspace, x->shape[0], (int)x->shape[1]};
     const hipError_t e = launch_norm_backward(x->dtype, wdtype < 0 ? x->dtype : wdtype, p, stream);
     return e == hipSuccess ? KB_OK : fail_hip(e, "kb_norm_backward: launch");
+}
+
+size_t kb_attn_forward_workspace_bytes(const kb_tensor* q, const kb_tensor* k) {
+    AttnParams p{};
+    if (q == nullptr || k == nullptr || !attn_sizes(*q, *k, &p)) return 0;
+    return 0;
+}
+
+int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, const kb_attn_opts* opts,
+                    const kb_tensor* o, float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_attn_forward";
+    AttnParams p{};
+    int rc;
+    if ((rc = check_attn(call, q, k, v, opts, &p)) || (rc = check_view(call, "o", o, 4, true)) ||
+        (rc = check_shape(call, "o", *o, "q", *q)) || (rc = check_lse(call, lse, *q)))
+        return rc;
+    const size_t need = kb_attn_forward_workspace_bytes(q, k);
+    if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
+    const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
+    const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
+    const Named outs[] = {{"o", o}, {"lse", &tl}, {"the workspace", &tw}};
+    const Named ins[] = {{"q", q}, {"k", k}, {"v", v}};
+    if ((rc = check_apart(call, outs, 3, ins, 3))) return rc;
+    if (is_empty(*q)) return KB_OK;
+    p.o = head_view(o);
+    p.lse = lse;
+    p.ws = (float*)workspace;
+    const hipError_t e = launch_attn_forward(q->dtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_attn_forward: launch");
+}
+
+size_t kb_attn_backward_workspace_bytes(const kb_tensor* q, const kb_tensor* k) {
+    AttnParams p{};
+    if (q == nullptr || k == nullptr || !attn_sizes(*q, *k, &p)) return 0;
+    return attn_backward_bytes(p);
+}
+
+int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
+                     const kb_tensor* o, const float* lse, const kb_attn_opts* opts, const kb_tensor* dq,
+                     const kb_tensor* dk, const kb_tensor* dv, void* workspace, size_t workspace_bytes,
+                     hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_attn_backward";
+    AttnParams p{};
+    int rc;
+    if ((rc = check_attn(call, q, k, v, opts, &p)) || (rc = check_view(call, "dout", dout, 4, false)) ||
+        (rc = check_shape(call, "dout", *dout, "q", *q)) || (rc = check_view(call, "o", o, 4, false)) ||
+        (rc = check_shape(call, "o", *o, "q", *q)) || (rc = check_lse(call, lse, *q)) ||
+        (rc = check_view(call, "dq", dq, 4, true)) || (rc = check_shape(call, "dq", *dq, "q", *q)) ||
+        (rc = check_view(call, "dk", dk, 4, true)) || (rc = check_shape(call, "dk", *dk, "k", *k)) ||
+        (rc = check_view(call, "dv", dv, 4, true)) || (rc = check_shape(call, "dv", *dv, "k", *k)))
+        return rc;
+    const size_t need = attn_backward_bytes(p);
+    if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
+    const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
+    const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
+    const Named outs[] = {{"dq", dq}, {"dk", dk}, {"dv", dv}, {"the workspace", &tw}};
+    const Named ins[] = {{"dout", dout}, {"q", q}, {"k", k}, {"v", v}, {"o", o}, {"lse", &tl}};
+    if ((rc = check_apart(call, outs, 4, ins, 6))) return rc;
+    if (p.batch == 0 || p.kv_heads == 0 || p.heads == 0) return KB_OK;
+    p.dout = head_view(dout);
+    p.o = head_view(o);
+    p.dq = head_view(dq);
+    p.dk = head_view(dk);
+    p.dv = head_view(dv);
+    p.lse = (float*)lse;
+    p.ws = (float*)workspace;
+    const hipError_t e = launch_attn_backward(q->dtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_attn_backward: launch");
 }
 
 }  // extern "C"

@@ -47,9 +47,10 @@ __device__ __forceinline__ f32x16 mma(frag_t<DT_F32> a, frag_t<DT_F32> b, f32x16
 
 // A tile of rows in LDS: DP elements a row (the head dimension rounded up,
 // zeros past it) at a pitch of 64 or 128 elements, in 16-byte chunks.  Chunk
-// c of row r lies at c ^ turn(r), so that neither the 16 rows that a row read
-// touches at one chunk nor the 4 rows x 64 bytes of a transposed read fall on
-// the same banks.
+// c of row r lies at place c ^ turn(r) of its row, and 16 bytes are left free
+// after every KB, so that neither the 16 rows that a row read touches at one
+// chunk nor the 4 rows x 64 bytes of a transposed read fall on the same banks,
+// while few bits of c are turned: the others are constants in the reads.
 template <int DT, int DP>
 struct Tile {
     using T = storage_t<DT>;
@@ -57,14 +58,18 @@ struct Tile {
     static constexpr int PITCH = DP <= 64 ? 64 : 128;
     static constexpr int CHUNKS = DP / VEC;
     static constexpr int PITCH_BYTES = PITCH * (int)sizeof(T);
+    static constexpr int KB_ROWS = 1024 / PITCH_BYTES;          // rows of a KB
+    static constexpr int KB = (1024 + 16) / (int)sizeof(T);     // elements from one KB to the next
 
     __device__ static __forceinline__ int turn(int row) {
-        if (PITCH_BYTES == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
-        return ((row & 3) << 2) | ((row >> 2) & 3);
+        if (PITCH_BYTES == 128) return (((row >> 1) & 1) << 2) | (((row >> 2) & 1) << 1);
+        if (PITCH_BYTES == 256) return (row & 3) << 2;
+        return (row & 1) << 3;
     }
     __device__ static __forceinline__ int at(int row, int d) {
-        return row * PITCH + (((d / VEC) ^ turn(row)) * VEC) + d % VEC;
+        return row / KB_ROWS * KB + row % KB_ROWS * PITCH + (((d / VEC) ^ turn(row)) * VEC) + d % VEC;
     }
+    static constexpr int size(int rows) { return rows / KB_ROWS * KB; }
 };
 
 // 16 bytes of a row from element d on, zeros past dim (unaligned rows are fine).
@@ -95,51 +100,159 @@ __device__ __forceinline__ void stage(storage_t<DT>* tile, const storage_t<DT>* 
     }
 }
 
-// Elements d = 16c + 8g .. +7 of a row of the tile.
-template <int DT, int DP>
-__device__ __forceinline__ frag_t<DT> row_frag(const storage_t<DT>* tile, int row, int c, int g) {
+// A tile filled in the background: each thread's 16-byte chunks go from memory
+// straight to LDS, with no register in between, and have arrived once the
+// thread has waited (tile_wait) and the work-group has met.  LDS takes a wave's
+// chunks in the order of its lanes, so the tile's order (Tile::at) is made by
+// what each lane reads.  For rows of whole chunks only (AttnParams::whole);
+// stage() serves the others.
+template <int DT, int DP, int ROWS, int NT>
+struct Filler {
+    using T = storage_t<DT>;
     using L = Tile<DT, DP>;
-    if constexpr (DT == DT_F32) {
-        const f32x4 a = *(const f32x4*)(tile + L::at(row, 16 * c + 8 * g));
-        const f32x4 b = *(const f32x4*)(tile + L::at(row, 16 * c + 8 * g + 4));
-        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-    } else {
-        return *(const frag_t<DT>*)(tile + L::at(row, 16 * c + 8 * g));
-    }
-}
+    static constexpr int SLOTS = L::PITCH / L::VEC;  // chunk places of a row
+    static constexpr int STEP = NT / SLOTS;          // rows that the work-group fills at once
+    static constexpr int STEPS = ROWS / STEP;
+    static_assert(NT % SLOTS == 0 && ROWS % STEP == 0, "a tile is filled in whole steps");
+    static_assert(STEP % 8 == 0, "turn() is the same in every step");
+    int row0;
+    uint32_t offset;  // bytes from the step's first row to the lane's chunk
+    bool in;          // the chunk lies within dim
 
-// Column d = 32 db + c of rows row0 + {4g .. 4g+3, 8+4g .. 8+4g+3}.  In 16 bits
-// each four come from one transposed read: of 16 lanes, lane i gives the
-// address of 4 elements of row i/4, columns 4(i%4) .., and receives column i of
-// the four rows.
-template <int DT, int DP>
-__device__ __forceinline__ frag_t<DT> col_frag(const storage_t<DT>* tile, int row0, int db, int lane) {
-    using L = Tile<DT, DP>;
-    const int g = lane >> 5;
-    if constexpr (DT == DT_F32) {
-        frag_t<DT> f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = tile[L::at(row0 + 8 * (e >> 2) + 4 * g + (e & 3), 32 * db + (lane & 31))];
-        return f;
-    } else {
-        const int row = row0 + 4 * g + ((lane & 15) >> 2), d = 32 * db + (lane & 16) + 4 * (lane & 3);
-        using lds_ptr = __attribute__((address_space(3))) s16x4*;
-        const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)(tile + L::at(row, d)));
-        const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)(tile + L::at(row + 8, d)));
-        return __builtin_bit_cast(frag_t<DT>, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    __device__ __forceinline__ Filler(int64_t stride, int dim) {
+        row0 = (int)threadIdx.x / SLOTS;
+        const int d = ((int)threadIdx.x % SLOTS ^ L::turn(row0)) * L::VEC;
+        in = d < dim;
+        offset = ((uint32_t)row0 * (uint32_t)stride + (uint32_t)d) * (uint32_t)sizeof(T);
     }
-}
+
+    // Rows [r0, r0 + ROWS) of base; those from n on are zeros.
+    __device__ __forceinline__ void fill(T* tile, const T* base, int64_t stride, int r0, int n, int dim) const {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        T* to = tile + wave * L::KB;
+        const char* from = (const char*)(base + (int64_t)r0 * stride);
+        if (r0 + ROWS <= n && dim == L::PITCH) {  // the common case, without a test for each chunk
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k, from += (int64_t)STEP * stride * (int)sizeof(T))
+                send(from + offset, to + k * (STEP / L::KB_ROWS * L::KB));
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < STEPS; ++k, from += (int64_t)STEP * stride * (int)sizeof(T)) {
+                if (in && r0 + k * STEP + row0 < n) {
+                    send(from + offset, to);
+                } else {
+                    const u32v4 zero = {0, 0, 0, 0};
+                    *(u32v4*)(to + ((int)threadIdx.x & 63) * L::VEC) = zero;
+                }
+                to += STEP / L::KB_ROWS * L::KB;
+            }
+        }
+    }
+    __device__ __forceinline__ static void send(const char* from, T* to) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                         (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+    }
+};
+
+// Until the chunks that this thread has sent for have arrived.
+__device__ __forceinline__ void tile_wait() { __builtin_amdgcn_s_waitcnt(0x0F70); }  // vmcnt 0
+
+// Where a lane reads in a tile.  Its byte addresses are a few values that hold
+// for the whole kernel, one for each setting of the turned bits, plus constants;
+// they are kept from the compiler's sight, which would otherwise hold one
+// register for each read.
+template <int DT, int DP>
+struct Reader {
+    using T = storage_t<DT>;
+    using L = Tile<DT, DP>;
+    uint32_t row[4];  // row c = lane % 32, turned bits 0..3
+    uint32_t col[4];
+    int lane;
+
+    __device__ __forceinline__ explicit Reader(int lane_) : lane(lane_) {
+        const int c = lane & 31, g = lane >> 5;
+        const uint32_t row_at = (c / L::KB_ROWS * L::KB + c % L::KB_ROWS * L::PITCH) * sizeof(T);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (DT == DT_F32) {
+                // chunks 4k + 2g and the next
+                if (L::PITCH_BYTES == 256) row[v] = row_at + (((v ^ (c & 3)) << 2) + 2 * g) * 16;
+                else row[v] = row_at + (((v & 1) << 3 ^ L::turn(c)) + 2 * g) * 16;
+                // single elements of 32 columns, rows 4g + ..
+                const int q = (lane >> 4) & 1;
+                if (L::PITCH_BYTES == 256) col[v] = g * L::KB * 4 + ((q ^ (v & 1)) << 2) * 16 + (lane & 15) * 4;
+                else col[v] = 2 * g * L::KB * 4 + c * 4;
+            } else {
+                const int r = (lane & 15) >> 2, q = (lane >> 4) & 1, in = (lane & 3) >> 1;
+                if (L::PITCH_BYTES == 256) {
+                    row[v] = row_at + (((v ^ (c & 3)) << 2) + g) * 16;
+                    col[v] = g * L::KB * 2 + r * L::PITCH * 2 + (((v ^ r) << 2) + 2 * q + in) * 16 + (lane & 1) * 8;
+                } else {
+                    row[v] = row_at + ((v << 1 ^ L::turn(c)) + g) * 16;
+                    col[v] = (4 * g + r) * L::PITCH * 2 + ((((2 * v + q) << 1) ^ L::turn(4 * g + r)) + in) * 16 + (lane & 1) * 8;
+                }
+            }
+            asm volatile("" : "+v"(row[v]), "+v"(col[v]));
+        }
+    }
+
+    // Elements d = 16k + 8g .. +7 of row row0 + c (row0 a multiple of 32).
+    __device__ __forceinline__ frag_t<DT> row_frag(const T* tile, int row0, int k) const {
+        const char* base = (const char*)tile + row0 / L::KB_ROWS * L::KB * (int)sizeof(T);
+        if constexpr (DT == DT_F32) {
+            const char* at = L::PITCH_BYTES == 256 ? base + row[k & 3]
+                                                   : base + row[(k >> 1) & 1] + ((k >> 2) * 16 + (k & 1) * 4) * 16;
+            const f32x4 a = *(const f32x4*)at, b = *(const f32x4*)(at + 16);
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        } else {
+            const char* at = L::PITCH_BYTES == 256 ? base + row[k >> 1] + (k & 1) * 32 : base + row[k & 3];
+            return *(const frag_t<DT>*)at;
+        }
+    }
+
+    // Column d = 32 db + c of rows row0 + {4g .. 4g+3, 8+4g .. 8+4g+3} (row0 a
+    // multiple of 16).  In 16 bits each four come from one transposed read: of 16
+    // lanes, lane i gives the address of 4 elements of row i/4, columns
+    // 4(i%4) .., and receives column i of the four rows.
+    __device__ __forceinline__ frag_t<DT> col_frag(const T* tile, int row0, int db) const {
+        const char* base = (const char*)tile + row0 / L::KB_ROWS * L::KB * (int)sizeof(T);
+        if constexpr (DT == DT_F32) {
+            frag_t<DT> f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int r = 8 * (e >> 2) + (e & 3);  // + 4g
+                const char* at = base + r / L::KB_ROWS * L::KB * 4 + r % L::KB_ROWS * L::PITCH * 4;
+                f[e] = *(const float*)(L::PITCH_BYTES == 256
+                                           ? at + col[e & 1] + ((db ^ ((e >> 1) & 1)) * 8) * 16
+                                           : at + col[0] + (((db >> 1) * 16 + ((db ^ e) & 1) * 8)) * 16);
+            }
+            return f;
+        } else {
+            using lds_ptr = __attribute__((address_space(3))) s16x4*;
+            const char* at = base + col[db];
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)at);
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(s16x4*)(at + 8 / L::KB_ROWS * L::KB * 2));
+            return __builtin_bit_cast(frag_t<DT>, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        }
+    }
+};
 
 // Eight elements of a row in memory, d = 16c + 8g .., zeros past dim or if !in.
-template <int DT>
+// WHOLE: a chunk lies within dim or past it.
+template <int DT, bool WHOLE>
 __device__ __forceinline__ frag_t<DT> load_frag(const storage_t<DT>* row, int c, int g, int dim, bool in) {
     using T = storage_t<DT>;
     constexpr int N = Vec16<T>::N;
     frag_t<DT> f;
 #pragma unroll
     for (int k = 0; k < 8 / N; ++k) {
+        const int d = 16 * c + 8 * g + k * N;
         u32v4 v = {0, 0, 0, 0};
-        if (in) v = load_chunk(row, 16 * c + 8 * g + k * N, dim);
+        if (WHOLE) {
+            if (in && d < dim) v = *(const u32v4*)(row + d);
+        } else if (in) {
+            v = load_chunk(row, d, dim);
+        }
         const typename Vec16<T>::type t = __builtin_bit_cast(typename Vec16<T>::type, v);
 #pragma unroll
         for (int e = 0; e < N; ++e) f[k * N + e] = t[e];
@@ -178,6 +291,7 @@ __device__ __forceinline__ bool any_non_finite(frag_t<DT> f) {
 template <int DT>
 __device__ void mma_seen(f32x16& acc, frag_t<DT> a, frag_t<DT> b, int row0, int lo, int hi, int lane) {
     const int g = lane >> 5;
+#pragma unroll 1
     for (int n = 0; n < 32; ++n) {
         const int from = __builtin_amdgcn_readlane(lo, n), to = __builtin_amdgcn_readlane(hi, n);
         frag_t<DT> cut = a;
@@ -193,32 +307,31 @@ __device__ void mma_seen(f32x16& acc, frag_t<DT> a, frag_t<DT> b, int row0, int 
     }
 }
 
-// acc[db] += (rows [row0, row0 + 32) of the tile)^T b, b in two halves; with
-// `part` some (row, column) pairs are not seen, and the rows are looked through
-// for values that must not reach the columns that do not see them.
-template <int DT, int DP>
-__device__ __forceinline__ void mma_rows(f32x16 (&acc)[DP / 32], const storage_t<DT>* tile, int row0,
-                                         const frag_t<DT> (&b)[2], bool part, int lo, int hi, int lane) {
-    if (part) {
+// acc[db] += (rows [row0, row0 + 32) of the tile)^T b, b in two halves.  PART:
+// some (row, column) pairs are not seen, and the rows are looked through for
+// values that must not reach the columns that do not see them.
+template <int DT, int DP, bool PART>
+__device__ __forceinline__ void mma_rows(f32x16 (&acc)[DP / 32], const storage_t<DT>* tile, const Reader<DT, DP>& rd,
+                                         int row0, const frag_t<DT> (&b)[2], int lo, int hi) {
+    if (PART) {
         bool bad = false;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) bad |= any_non_finite<DT>(col_frag<DT, DP>(tile, row0 + 16 * j, db, lane));
+            for (int j = 0; j < 2; ++j) bad |= any_non_finite<DT>(rd.col_frag(tile, row0 + 16 * j, db));
         if (__any(bad)) {
 #pragma unroll
             for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    mma_seen<DT>(acc[db], col_frag<DT, DP>(tile, row0 + 16 * j, db, lane), j ? b[1] : b[0],
-                                 row0 + 16 * j, lo, hi, lane);
+                    mma_seen<DT>(acc[db], rd.col_frag(tile, row0 + 16 * j, db), b[j], row0 + 16 * j, lo, hi, rd.lane);
             return;
         }
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-            acc[db] = mma(col_frag<DT, DP>(tile, row0 + 16 * j, db, lane), b[j], acc[db]);
+        for (int db = 0; db < DP / 32; ++db) acc[db] = mma(rd.col_frag(tile, row0 + 16 * j, db), b[j], acc[db]);
 }
 
 // Elements d = 32 db + 8 q4 + 4 g .. +3 of a row of results.

@@ -117,8 +117,8 @@ template <int DT, int DP>
 __global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams p) {
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
-    __shared__ __align__(16) T qt[kQueries * L::PITCH];
-    __shared__ __align__(16) T dt[kQueries * L::PITCH];
+    __shared__ __align__(16) T qt[L::size(kQueries)];
+    __shared__ __align__(16) T dt[L::size(kQueries)];
     __shared__ __align__(16) float norm[kQueries], dots[kQueries], scratch[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
     const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams
     frag_t<DT> kf[DP / 16], vf[DP / 16];
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) {
-        kf[c] = load_frag<DT>(k, c, g, p.dim, live);
-        vf[c] = load_frag<DT>(v, c, g, p.dim, live);
+        kf[c] = load_frag<DT, false>(k, c, g, p.dim, live);
+        vf[c] = load_frag<DT, false>(v, c, g, p.dim, live);
     }
     // the queries that see a key: [sees(j), qlen)
     const auto sees = [&](int key) { return p.causal ? min(qlen, max(0, key - (klen - qlen))) : 0; };
@@ -144,6 +144,7 @@ __global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams
     const int wave_lo = wave_key < klen ? sees(wave_key) : qlen;
     const int wave_hi = sees(min(wave_key + 31, klen - 1));  // from here on every key of the wave is seen
 
+    const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
     for (int h = 0; h < p.group; ++h) {
@@ -166,8 +167,8 @@ __global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams
             f32x16 s = {}, t = {};
 #pragma unroll
             for (int c = 0; c < DP / 16; ++c) {
-                s = mma(row_frag<DT, DP>(qt, lane & 31, c, g), kf[c], s);
-                t = mma(row_frag<DT, DP>(dt, lane & 31, c, g), vf[c], t);
+                s = mma(rd.row_frag(qt, 0, c), kf[c], s);
+                t = mma(rd.row_frag(dt, 0, c), vf[c], t);
             }
             const bool part = i0 < wave_hi || i0 + kQueries > qlen || wave_key + 32 > klen;
 #pragma unroll
@@ -183,8 +184,13 @@ __global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams
                 }
             }
             const frag_t<DT> pf[2] = {narrow<DT>(s, 0), narrow<DT>(s, 1)}, tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
-            mma_rows<DT, DP>(dv, dt, 0, pf, part, lo - i0, qlen - i0, lane);
-            mma_rows<DT, DP>(dk, qt, 0, tf, part, lo - i0, qlen - i0, lane);
+            if (part) {
+                mma_rows<DT, DP, true>(dv, dt, rd, 0, pf, lo - i0, qlen - i0);
+                mma_rows<DT, DP, true>(dk, qt, rd, 0, tf, lo - i0, qlen - i0);
+            } else {
+                mma_rows<DT, DP, false>(dv, dt, rd, 0, pf, 0, 0);
+                mma_rows<DT, DP, false>(dk, qt, rd, 0, tf, 0, 0);
+            }
         }
     }
     if (j >= p.len_k) return;
@@ -201,8 +207,8 @@ template <int DT, int DP>
 __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnParams p) {
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
-    __shared__ __align__(16) T kt[kKeys * L::PITCH];
-    __shared__ __align__(16) T vt[kKeys * L::PITCH];
+    __shared__ __align__(16) T kt[L::size(kKeys)];
+    __shared__ __align__(16) T vt[L::size(kKeys)];
     __shared__ float scratch[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
     const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
@@ -228,14 +234,15 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
     frag_t<DT> qf[DP / 16], df[DP / 16];
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) {
-        qf[c] = load_frag<DT>(q, c, g, p.dim, live);
-        df[c] = load_frag<DT>(dout, c, g, p.dim, live);
+        qf[c] = load_frag<DT, false>(q, c, g, p.dim, live);
+        df[c] = load_frag<DT, false>(dout, c, g, p.dim, live);
     }
     const int64_t at_row = ((int64_t)at.b * p.heads + hq) * p.len_q + i;
     float lse = live ? p.lse[at_row] : 0.f;
     lse = lse == -INFINITY ? 0.f : lse * kLog2e;
     const float dot = live ? p.ws[at_row] : 0.f;
 
+    const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
     f32x16 dq[DP / 32] = {};
     for (int j0 = 0; j0 < end; j0 += kKeys) {
@@ -247,8 +254,8 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
         f32x16 s = {}, t = {};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
-            s = mma(row_frag<DT, DP>(kt, lane & 31, c, g), qf[c], s);
-            t = mma(row_frag<DT, DP>(vt, lane & 31, c, g), df[c], t);
+            s = mma(rd.row_frag(kt, 0, c), qf[c], s);
+            t = mma(rd.row_frag(vt, 0, c), df[c], t);
         }
         const bool part = j0 + kKeys > wave_all;
 #pragma unroll
@@ -258,7 +265,10 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
             t[r] = seen ? prob * (t[r] - dot) * t_scale : 0.f;
         }
         const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
-        mma_rows<DT, DP>(dq, kt, 0, tf, part, 0, lim - j0, lane);
+        if (part)
+            mma_rows<DT, DP, true>(dq, kt, rd, 0, tf, 0, lim - j0);
+        else
+            mma_rows<DT, DP, false>(dq, kt, rd, 0, tf, 0, 0);
     }
     if (!exists) return;
     store_column<DT, DP>((T*)p.dq.p + at.b * p.dq.sb + hq * p.dq.sh + i * p.dq.sl, dq, p.scale / t_scale, live, p.dim, g);

@@ -16,12 +16,108 @@ constexpr int kThreads = 256;
 constexpr int kRows = 128;  // query rows of a work-group
 constexpr int kKeys = 64;   // keys of a tile
 
-template <int DT, int DP>
-__global__ void __launch_bounds__(kThreads) attn_forward_kernel(AttnParams p) {
+// The softmax state of a lane's query over the tiles so far: terms are
+// exp(scale (s - m)).  In 16 bits m is a reference that follows the maximum only when a
+// term would pass 2^kSlack (scaling the sums takes as long as a quarter of a
+// tile's products), and next to l, the sum of the terms, there is the sum of the
+// rounded terms, those whose product with v is divided by it: where one term
+// outweighs the others, o is its v to the last bit.  In 32 bits m is the maximum.
+constexpr float kSlack = 8.f;
+struct Softmax {
+    float m = -INFINITY, l = 0.f, rounded = 0.f;
+};
+
+template <int DT>
+__device__ __forceinline__ float add_terms(frag_t<DT> f, float l) {
+    typedef storage_t<DT> two __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const two x = {f[e], f[e + 1]}, one = {(storage_t<DT>)1.f, (storage_t<DT>)1.f};
+        if constexpr (DT == DT_F16) l = __builtin_amdgcn_fdot2(x, one, l, false);
+        if constexpr (DT == DT_BF16) l = __builtin_amdgcn_fdot2_f32_bf16(x, one, l, false);
+    }
+    return l;
+}
+
+// The keys of one tile for 32 query rows of a wave.  PART: some (row, key)
+// pairs are not seen; the lane's row sees the tile's keys below hi.
+template <int DT, int DP, bool PART>
+__device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm, const frag_t<DT> (&qf)[DP / 16],
+                                             const storage_t<DT>* kt, const storage_t<DT>* vt, const Reader<DT, DP>& rd,
+                                             float to_log2, int hi) {
+    const int g = rd.lane >> 5;
+    float &m = sm.m, &l = sm.l;
+    const float ref = DT == DT_F32 || m == -INFINITY ? 0.f : -m;  // the products start from -m
+    f32x16 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = ref;
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) s[t] = mma(rd.row_frag(kt, 32 * t, c), qf[c], s[t]);
+    }
+    if (PART) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (32 * t + 8 * (r >> 2) + 4 * g + (r & 3) >= hi) s[t][r] = -INFINITY;
+    }
+    float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
+    top = fmaxf(top, other_half(top));
+    float shift = 0.f;  // taken from the scores
+    if constexpr (DT == DT_F32) {
+        const float now = fmaxf(m, top);
+        shift = now == -INFINITY ? 0.f : now;  // nothing seen yet: every term is 0
+        const float alpha = __builtin_amdgcn_exp2f((m - shift) * to_log2);
+        m = now;
+        l *= alpha;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+    } else {
+        const bool none = m == -INFINITY;
+        const bool move = none ? top > -INFINITY : top * to_log2 > kSlack;
+        if (__any(move)) {
+            const float now = move ? (none ? top : m + top) : m;
+            shift = move ? (none ? top : now - m) : 0.f;
+            const float alpha = none ? 1.f : __builtin_amdgcn_exp2f(-shift * to_log2);
+            m = now;
+            l *= alpha;
+            sm.rounded *= alpha;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[t][r] -= shift;
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[t][r] = __builtin_amdgcn_exp2f((DT == DT_F32 ? s[t][r] - shift : s[t][r]) * to_log2);
+            l += s[t][r];
+        }
+        const frag_t<DT> b[2] = {narrow<DT>(s[t], 0), narrow<DT>(s[t], 1)};
+        if (DT != DT_F32) sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
+        mma_rows<DT, DP, PART>(acc, vt, rd, 32 * t, b, 0, hi);
+    }
+}
+
+template <int DT, int DP, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_kernel(AttnParams p) {
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
-    __shared__ __align__(16) T kt[kKeys * L::PITCH];
-    __shared__ __align__(16) T vt[kKeys * L::PITCH];
+    using F = Filler<DT, DP, kKeys, kThreads>;
+    __shared__ __align__(16) T kt[2][L::size(kKeys)];
+    __shared__ __align__(16) T vt[2][L::size(kKeys)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
     const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
     const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
@@ -31,7 +127,8 @@ __global__ void __launch_bounds__(kThreads) attn_forward_kernel(AttnParams p) {
     const int64_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
     const bool exists = i < p.len_q, live = i < qlen;
-    const int wave_first = (int)((first + wave * 32) / p.group), wave_last = (int)((first + wave * 32 + 31) / p.group);
+    const int wave_first = __builtin_amdgcn_readfirstlane((int)((first + wave * 32) / p.group));
+    const int wave_last = __builtin_amdgcn_readfirstlane((int)((first + wave * 32 + 31) / p.group));
     const int block_last = (int)((first + kRows - 1) / p.group);
     const bool any = (int)(first / p.group) < qlen;
     const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
@@ -44,71 +141,48 @@ __global__ void __launch_bounds__(kThreads) attn_forward_kernel(AttnParams p) {
     const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh;
     frag_t<DT> qf[DP / 16];
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) qf[c] = load_frag<DT>(q, c, g, p.dim, live);
+    for (int c = 0; c < DP / 16; ++c) qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
+    const Reader<DT, DP> rd(lane);
+    const F fk(p.k.sl, p.dim), fv(p.v.sl, p.dim);
+    const auto fill = [&](int j0, int buf) {
+        if (WHOLE) {
+            fk.fill(kt[buf], k, p.k.sl, j0, klen, p.dim);
+            fv.fill(vt[buf], v, p.v.sl, j0, klen, p.dim);
+        } else {
+            stage<DT, DP, kKeys, kThreads>(kt[buf], k, p.k.sl, j0, klen, p.dim);
+            stage<DT, DP, kKeys, kThreads>(vt[buf], v, p.v.sl, j0, klen, p.dim);
+        }
+    };
 
     const float to_log2 = p.scale * kLog2e;
     f32x16 acc[DP / 32] = {};
-    float m = -INFINITY, l = 0.f;
-    for (int j0 = 0; j0 < end; j0 += kKeys) {
-        __syncthreads();
-        stage<DT, DP, kKeys, kThreads>(kt, k, p.k.sl, j0, klen, p.dim);
-        stage<DT, DP, kKeys, kThreads>(vt, v, p.v.sl, j0, klen, p.dim);
-        __syncthreads();
-        if (j0 >= wave_any) continue;
-        f32x16 s[2] = {};
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int c = 0; c < DP / 16; ++c) s[t] = mma(row_frag<DT, DP>(kt, 32 * t + (lane & 31), c, g), qf[c], s[t]);
-        const bool part = j0 + kKeys > wave_all;
-        if (part) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (j0 + 32 * t + 8 * (r >> 2) + 4 * g + (r & 3) >= lim) s[t][r] = -INFINITY;
-        }
-        float top = m;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[t][r]);
-        top = fmaxf(top, other_half(top));
-        // the difference before the scale: the largest term is 1 exactly
-        const float shift = top == -INFINITY ? 0.f : top;  // nothing seen yet: every term is 0
-        const float alpha = __builtin_amdgcn_exp2f((m - shift) * to_log2);
-        m = top;
-        l *= alpha;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[t][r] = __builtin_amdgcn_exp2f((s[t][r] - shift) * to_log2);
-                l += s[t][r];
-            }
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const frag_t<DT> b[2] = {narrow<DT>(s[t], 0), narrow<DT>(s[t], 1)};
-            mma_rows<DT, DP>(acc, vt, 32 * t, b, part, 0, lim - j0, lane);
-        }
+    Softmax sm;
+    if (end > 0) fill(0, 0);
+    for (int j0 = 0, buf = 0; j0 < end; j0 += kKeys, buf ^= 1) {
+        tile_wait();
+        __syncthreads();  // the tile is there, and the other one is read
+        if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
+        if (j0 + kKeys <= wave_all)
+            tile_forward<DT, DP, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+        else if (j0 < wave_any)
+            tile_forward<DT, DP, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0);
     }
     if (!exists) return;
-    l += other_half(l);
+    const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
     const bool some = live && l != 0.f;  // NaN too: it goes on to o
-    store_column<DT, DP>((T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl, acc, 1.f / l, some, p.dim, g);
+    store_column<DT, DP>((T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl, acc, 1.f / (DT == DT_F32 ? l : rounded), some, p.dim, g);
     if (g == 0)
         p.lse[((int64_t)at.b * p.heads + hq) * p.len_q + i] =
-            some ? fmaf(m, p.scale, kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
+            some ? fmaf(sm.m, p.scale, kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
 }
 
 template <int DT, int DP>
 hipError_t forward(const AttnParams& p, hipStream_t stream) {
     const int64_t blocks = ((int64_t)p.len_q * p.group + kRows - 1) / kRows * p.batch * p.kv_heads;
-    attn_forward_kernel<DT, DP><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(p);
+    if (p.whole)
+        attn_forward_kernel<DT, DP, true><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(p);
+    else
+        attn_forward_kernel<DT, DP, false><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(p);
     return hipGetLastError();
 }
 

@@ -70,6 +70,7 @@ struct AttnParams {
     int len_q, len_k, dim;
     float scale;
     int causal;
+    int whole;  // rows of q, k, v (and dout) are aligned to 16 bytes and made of 16-byte chunks
     float* ws;
 };
 

@@ -189,6 +189,15 @@ int check_rows(const char* call, const kb_tensor& x) {
 
 HeadView head_view(const kb_tensor* t) { return HeadView{t->data, t->strides[0], t->strides[1], t->strides[2]}; }
 
+// Rows that can be read in aligned 16-byte chunks, 64 of them within 2^31 bytes.
+bool whole_rows(const kb_tensor& t) {
+    const int64_t n = 16 / element_bytes(t.dtype);
+    if (((uintptr_t)t.data & 15u) || t.shape[3] % n) return false;
+    for (int i = 0; i < 3; ++i)
+        if (t.shape[i] > 1 && t.strides[i] % n) return false;
+    return t.shape[2] <= 1 || t.strides[2] < ((int64_t)1 << 25) / element_bytes(t.dtype);
+}
+
 constexpr int64_t kMaxLen = (int64_t)1 << 30;
 
 // Sizes of an attention call; false if q and k do not fit together.
@@ -349,6 +358,7 @@ int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, 
     if ((rc = check_apart(call, outs, 3, ins, 3))) return rc;
     if (is_empty(*q)) return KB_OK;
     p.o = head_view(o);
+    p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v);
     p.lse = lse;
     p.ws = (float*)workspace;
     const hipError_t e = launch_attn_forward(q->dtype, p, stream);
@@ -385,6 +395,7 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
     if ((rc = check_apart(call, outs, 4, ins, 6))) return rc;
     if (p.batch == 0 || p.kv_heads == 0 || p.heads == 0) return KB_OK;
     p.dout = head_view(dout);
+    p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v) && whole_rows(*dout);
     p.o = head_view(o);
     p.dq = head_view(dq);
     p.dk = head_view(dk);

@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
     const int wave_all = key_limit(min(wave_first, qlen - 1), qlen, klen, p.causal);  // keys that every row sees
     const int wave_any = wave_first < qlen ? key_limit(min(wave_last, qlen - 1), qlen, klen, p.causal) : 0;
+    const int block_all = any ? key_limit(min((int)(first / p.group), qlen - 1), qlen, klen, p.causal) : 0;
     const int end = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
 
     const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh + i * p.q.sl;
@@ -158,10 +159,19 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     f32x16 acc[DP / 32] = {};
     Softmax sm;
     if (end > 0) fill(0, 0);
-    for (int j0 = 0, buf = 0; j0 < end; j0 += kKeys, buf ^= 1) {
+    int j0 = 0, buf = 0;
+    const auto next = [&] {
         tile_wait();
         __syncthreads();  // the tile is there, and the other one is read
         if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
+    };
+    // first the tiles that every row of the work-group sees whole
+    for (; j0 + kKeys <= block_all; j0 += kKeys, buf ^= 1) {
+        next();
+        tile_forward<DT, DP, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+    }
+    for (; j0 < end; j0 += kKeys, buf ^= 1) {
+        next();
         if (j0 + kKeys <= wave_all)
             tile_forward<DT, DP, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
         else if (j0 < wave_any)

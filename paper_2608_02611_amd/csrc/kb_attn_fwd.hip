@@ -50,12 +50,13 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
     const float ref = DT == DT_F32 || m == -INFINITY ? 0.f : -m;  // the products start from -m
     f32x16 s[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[t][r] = ref;
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) s[t] = mma(rd.row_frag(kt, 32 * t, c), qf[c], s[t]);
-    }
+    for (int c = 0; c < DP / 16; ++c)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) s[t] = mma(rd.row_frag(kt, 32 * t, c), qf[c], s[t]);
     if (PART) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
@@ -63,10 +64,12 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
             for (int r = 0; r < 16; ++r)
                 if (32 * t + 8 * (r >> 2) + 4 * g + (r & 3) >= hi) s[t][r] = -INFINITY;
     }
-    float top = fmaxf(s[0][0], s[1][0]);
+    // a NaN among the scores makes top NaN, and the row's results are NaN whatever m is
+    float top = __builtin_elementwise_maximum(s[0][0], s[1][0]);
 #pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, fmaxf(s[0][r], s[1][r]));
-    top = fmaxf(top, other_half(top));
+    for (int r = 1; r < 16; ++r)
+        top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[0][r], s[1][r]), top);
+    top = __builtin_elementwise_maximum(top, other_half(top));
     float shift = 0.f;  // taken from the scores
     if constexpr (DT == DT_F32) {
         const float now = fmaxf(m, top);

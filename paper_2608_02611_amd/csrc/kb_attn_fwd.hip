@@ -57,6 +57,15 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
     for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
         for (int t = 0; t < 2; ++t) s[t] = mma(rd.row_frag(kt, 32 * t, c), qf[c], s[t]);
+    if (DT != DT_F32) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int k = 0; k < DP / 8 - 4; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    }
     if (PART) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)

@@ -269,25 +269,14 @@ __device__ __forceinline__ frag_t<DT> narrow(const f32x16& s, int j) {
     return f;
 }
 
-template <int DT>
-__device__ __forceinline__ bool any_non_finite(frag_t<DT> f) {
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        if constexpr (DT == DT_F32)
-            bad |= (__float_as_uint(f[e]) & 0x7F800000u) == 0x7F800000u;
-        else if constexpr (DT == DT_F16)
-            bad |= (__builtin_bit_cast(uint16_t, (_Float16)f[e]) & 0x7C00u) == 0x7C00u;
-        else
-            bad |= (__builtin_bit_cast(uint16_t, (__bf16)f[e]) & 0x7F80u) == 0x7F80u;
-    }
-    return bad;
-}
+// A product takes every row of a tile to every column, at 0 where the column
+// does not see the row.  That leaves nothing behind unless the row holds a NaN or
+// an infinity, which times 0 is NaN.  So a work-group whose sums end up with
+// such a value, and some of whose tiles were seen in part, computes them once
+// more (CAREFUL), with the rows that a column does not see cleared for it.
 
-// acc += A B over 16 rows of a tile where column n of B sees rows [lo, hi) of
-// it only (lo, hi: the lane's column's).  B is 0 elsewhere, and A's values
-// there drop out of the product as they are finite; where they are not, this
-// form is taken: a product for each column with A's other rows cleared.
+// acc += A B over 16 rows of a tile, column n of B seeing rows [lo, hi) of it
+// (lo, hi: the lane's column's): a product for each column.
 template <int DT>
 __device__ void mma_seen(f32x16& acc, frag_t<DT> a, frag_t<DT> b, int row0, int lo, int hi, int lane) {
     const int g = lane >> 5;
@@ -307,31 +296,29 @@ __device__ void mma_seen(f32x16& acc, frag_t<DT> a, frag_t<DT> b, int row0, int 
     }
 }
 
-// acc[db] += (rows [row0, row0 + 32) of the tile)^T b, b in two halves.  PART:
-// some (row, column) pairs are not seen, and the rows are looked through for
-// values that must not reach the columns that do not see them.
-template <int DT, int DP, bool PART>
+// acc[db] += (rows [row0, row0 + 32) of the tile)^T b, b in two halves; SEEN: by
+// mma_seen.
+template <int DT, int DP, bool SEEN>
 __device__ __forceinline__ void mma_rows(f32x16 (&acc)[DP / 32], const storage_t<DT>* tile, const Reader<DT, DP>& rd,
                                          int row0, const frag_t<DT> (&b)[2], int lo, int hi) {
-    if (PART) {
-        bool bad = false;
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) bad |= any_non_finite<DT>(rd.col_frag(tile, row0 + 16 * j, db));
-        if (__any(bad)) {
-#pragma unroll
-            for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    mma_seen<DT>(acc[db], rd.col_frag(tile, row0 + 16 * j, db), b[j], row0 + 16 * j, lo, hi, rd.lane);
-            return;
-        }
-    }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int db = 0; db < DP / 32; ++db) acc[db] = mma(rd.col_frag(tile, row0 + 16 * j, db), b[j], acc[db]);
+        for (int db = 0; db < DP / 32; ++db) {
+            const frag_t<DT> a = rd.col_frag(tile, row0 + 16 * j, db);
+            if (SEEN) mma_seen<DT>(acc[db], a, b[j], row0 + 16 * j, lo, hi, rd.lane);
+            else acc[db] = mma(a, b[j], acc[db]);
+        }
+}
+
+template <int N>
+__device__ __forceinline__ bool non_finite(const f32x16 (&acc)[N]) {
+    float z = 0.f;  // x 0 is 0, or NaN
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) z = fmaf(acc[k][r], 0.f, z);
+    return z != 0.f;
 }
 
 // Elements d = 32 db + 8 q4 + 4 g .. +3 of a row of results.

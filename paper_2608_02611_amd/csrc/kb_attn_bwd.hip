@@ -11,6 +11,8 @@
 // F16 holds p and t of a long row badly (its least normal number is 6e-5), so
 // they are scaled by powers of two before they are rounded: p, at most 1, by
 // 2^10; t, at most 2 |dout| |v|, so that this bound comes to at most 2^15.
+#include <type_traits>
+
 #include "kb_attn.hpp"
 
 namespace kb {
@@ -146,53 +148,55 @@ __global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams
 
     const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
-    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
-    for (int h = 0; h < p.group; ++h) {
-        const int hq = at.h * p.group + h;
-        const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh;
-        const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh;
-        const int64_t rows = ((int64_t)at.b * p.heads + hq) * p.len_q;
-        for (int i0 = start; i0 < qlen; i0 += kQueries) {
-            __syncthreads();
-            stage<DT, DP, kQueries, kThreads>(qt, q, p.q.sl, i0, qlen, p.dim);
-            stage<DT, DP, kQueries, kThreads>(dt, dout, p.dout.sl, i0, qlen, p.dim);
-            if (threadIdx.x < kQueries) {
-                const int i = i0 + (int)threadIdx.x;
-                const float lse = i < qlen ? p.lse[rows + i] : 0.f;
-                norm[threadIdx.x] = lse == -INFINITY ? 0.f : lse * kLog2e;
-                dots[threadIdx.x] = i < qlen ? p.ws[rows + i] : 0.f;
-            }
-            __syncthreads();
-            if (i0 + kQueries <= wave_lo) continue;
-            f32x16 s = {}, t = {};
+    f32x16 dk[DP / 32], dv[DP / 32];
+    const auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
-            for (int c = 0; c < DP / 16; ++c) {
-                s = mma(rd.row_frag(qt, 0, c), kf[c], s);
-                t = mma(rd.row_frag(dt, 0, c), vf[c], t);
-            }
-            const bool part = i0 < wave_hi || i0 + kQueries > qlen || wave_key + 32 > klen;
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                const f32x4 lse = *(const f32x4*)(norm + 8 * r4 + 4 * g), dot = *(const f32x4*)(dots + 8 * r4 + 4 * g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int r = 4 * r4 + e, i = i0 + 8 * r4 + 4 * g + e;
-                    const bool seen = !part || (i >= lo && i < qlen);
-                    const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse[e]));
-                    t[r] = seen ? prob * (t[r] - dot[e]) * t_scale : 0.f;
-                    s[r] = seen ? prob * p_scale : 0.f;
+        for (int db = 0; db < DP / 32; ++db) dk[db] = dv[db] = f32x16{};
+        for (int h = 0; h < p.group; ++h) {
+            const int hq = at.h * p.group + h;
+            const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh;
+            const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh;
+            const int64_t rows = ((int64_t)at.b * p.heads + hq) * p.len_q;
+            for (int i0 = start; i0 < qlen; i0 += kQueries) {
+                __syncthreads();
+                stage<DT, DP, kQueries, kThreads>(qt, q, p.q.sl, i0, qlen, p.dim);
+                stage<DT, DP, kQueries, kThreads>(dt, dout, p.dout.sl, i0, qlen, p.dim);
+                if (threadIdx.x < kQueries) {
+                    const int i = i0 + (int)threadIdx.x;
+                    const float lse = i < qlen ? p.lse[rows + i] : 0.f;
+                    norm[threadIdx.x] = lse == -INFINITY ? 0.f : lse * kLog2e;
+                    dots[threadIdx.x] = i < qlen ? p.ws[rows + i] : 0.f;
                 }
-            }
-            const frag_t<DT> pf[2] = {narrow<DT>(s, 0), narrow<DT>(s, 1)}, tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
-            if (part) {
-                mma_rows<DT, DP, true>(dv, dt, rd, 0, pf, lo - i0, qlen - i0);
-                mma_rows<DT, DP, true>(dk, qt, rd, 0, tf, lo - i0, qlen - i0);
-            } else {
-                mma_rows<DT, DP, false>(dv, dt, rd, 0, pf, 0, 0);
-                mma_rows<DT, DP, false>(dk, qt, rd, 0, tf, 0, 0);
+                __syncthreads();
+                if (i0 + kQueries <= wave_lo) continue;
+                f32x16 s = {}, t = {};
+#pragma unroll
+                for (int c = 0; c < DP / 16; ++c) {
+                    s = mma(rd.row_frag(qt, 0, c), kf[c], s);
+                    t = mma(rd.row_frag(dt, 0, c), vf[c], t);
+                }
+                const bool part = i0 < wave_hi || i0 + kQueries > qlen || wave_key + 32 > klen;
+#pragma unroll
+                for (int r4 = 0; r4 < 4; ++r4) {
+                    const f32x4 lse = *(const f32x4*)(norm + 8 * r4 + 4 * g), dot = *(const f32x4*)(dots + 8 * r4 + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int r = 4 * r4 + e, i = i0 + 8 * r4 + 4 * g + e;
+                        const bool seen = !part || (i >= lo && i < qlen);
+                        const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse[e]));
+                        t[r] = seen ? prob * (t[r] - dot[e]) * t_scale : 0.f;
+                        s[r] = seen ? prob * p_scale : 0.f;
+                    }
+                }
+                const frag_t<DT> pf[2] = {narrow<DT>(s, 0), narrow<DT>(s, 1)}, tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
+                mma_rows<DT, DP, CAREFUL>(dv, dt, rd, 0, pf, lo - i0, qlen - i0);
+                mma_rows<DT, DP, CAREFUL>(dk, qt, rd, 0, tf, lo - i0, qlen - i0);
             }
         }
-    }
+    };
+    pass(std::false_type{});
+    if (p.causal && __syncthreads_or(non_finite(dk) || non_finite(dv))) pass(std::true_type{});
     if (j >= p.len_k) return;
     store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, p.scale / t_scale, live, p.dim, g);
     store_column<DT, DP>((T*)p.dv.p + at.b * p.dv.sb + at.h * p.dv.sh + j * p.dv.sl, dv, 1.f / p_scale, live, p.dim, g);
@@ -244,32 +248,36 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
 
     const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
-    f32x16 dq[DP / 32] = {};
-    for (int j0 = 0; j0 < end; j0 += kKeys) {
-        __syncthreads();
-        stage<DT, DP, kKeys, kThreads>(kt, k, p.k.sl, j0, klen, p.dim);
-        stage<DT, DP, kKeys, kThreads>(vt, v, p.v.sl, j0, klen, p.dim);
-        __syncthreads();
-        if (j0 >= wave_any) continue;
-        f32x16 s = {}, t = {};
+    f32x16 dq[DP / 32];
+    const auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
-        for (int c = 0; c < DP / 16; ++c) {
-            s = mma(rd.row_frag(kt, 0, c), qf[c], s);
-            t = mma(rd.row_frag(vt, 0, c), df[c], t);
-        }
-        const bool part = j0 + kKeys > wave_all;
+        for (int db = 0; db < DP / 32; ++db) dq[db] = f32x16{};
+        for (int j0 = 0; j0 < end; j0 += kKeys) {
+            __syncthreads();
+            stage<DT, DP, kKeys, kThreads>(kt, k, p.k.sl, j0, klen, p.dim);
+            stage<DT, DP, kKeys, kThreads>(vt, v, p.v.sl, j0, klen, p.dim);
+            __syncthreads();
+            if (j0 >= wave_any) continue;
+            f32x16 s = {}, t = {};
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const bool seen = !part || j0 + 8 * (r >> 2) + 4 * g + (r & 3) < lim;
-            const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse));
-            t[r] = seen ? prob * (t[r] - dot) * t_scale : 0.f;
+            for (int c = 0; c < DP / 16; ++c) {
+                s = mma(rd.row_frag(kt, 0, c), qf[c], s);
+                t = mma(rd.row_frag(vt, 0, c), df[c], t);
+            }
+            const bool part = j0 + kKeys > wave_all;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool seen = !part || j0 + 8 * (r >> 2) + 4 * g + (r & 3) < lim;
+                const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse));
+                t[r] = seen ? prob * (t[r] - dot) * t_scale : 0.f;
+            }
+            const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
+            mma_rows<DT, DP, CAREFUL>(dq, kt, rd, 0, tf, 0, lim - j0);
         }
-        const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
-        if (part)
-            mma_rows<DT, DP, true>(dq, kt, rd, 0, tf, 0, lim - j0);
-        else
-            mma_rows<DT, DP, false>(dq, kt, rd, 0, tf, 0, 0);
-    }
+    };
+    pass(std::false_type{});
+    if (p.causal && __syncthreads_or(non_finite(dq))) pass(std::true_type{});
     if (!exists) return;
     store_column<DT, DP>((T*)p.dq.p + at.b * p.dq.sb + hq * p.dq.sh + i * p.dq.sl, dq, p.scale / t_scale, live, p.dim, g);
 }

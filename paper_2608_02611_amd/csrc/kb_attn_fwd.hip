@@ -7,6 +7,8 @@
 // before is scaled by exp(m_old - m).  A work-group takes 128 query rows, 32 a
 // wave; the query heads that share a key head are rows of the same work-group
 // (row = query * group + head), so that a tile of keys serves all of them.
+#include <type_traits>
+
 #include "kb_attn.hpp"
 
 namespace kb {
@@ -41,7 +43,7 @@ __device__ __forceinline__ float add_terms(frag_t<DT> f, float l) {
 
 // The keys of one tile for 32 query rows of a wave.  PART: some (row, key)
 // pairs are not seen; the lane's row sees the tile's keys below hi.
-template <int DT, int DP, bool PART>
+template <int DT, int DP, bool PART, bool CAREFUL>
 __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm, const frag_t<DT> (&qf)[DP / 16],
                                              const storage_t<DT>* kt, const storage_t<DT>* vt, const Reader<DT, DP>& rd,
                                              float to_log2, int hi) {
@@ -119,7 +121,7 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
         }
         const frag_t<DT> b[2] = {narrow<DT>(s[t], 0), narrow<DT>(s[t], 1)};
         if (DT != DT_F32) sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
-        mma_rows<DT, DP, PART>(acc, vt, rd, 32 * t, b, 0, hi);
+        mma_rows<DT, DP, PART && CAREFUL>(acc, vt, rd, 32 * t, b, 0, hi);
     }
 }
 
@@ -144,7 +146,6 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     const int block_last = (int)((first + kRows - 1) / p.group);
     const bool any = (int)(first / p.group) < qlen;
     const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
-    const int wave_all = key_limit(min(wave_first, qlen - 1), qlen, klen, p.causal);  // keys that every row sees
     const int wave_any = wave_first < qlen ? key_limit(min(wave_last, qlen - 1), qlen, klen, p.causal) : 0;
     const int block_all = any ? key_limit(min((int)(first / p.group), qlen - 1), qlen, klen, p.causal) : 0;
     const int end = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
@@ -168,27 +169,32 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     };
 
     const float to_log2 = p.scale * kLog2e;
-    f32x16 acc[DP / 32] = {};
+    f32x16 acc[DP / 32];
     Softmax sm;
-    if (end > 0) fill(0, 0);
-    int j0 = 0, buf = 0;
-    const auto next = [&] {
-        tile_wait();
-        __syncthreads();  // the tile is there, and the other one is read
-        if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
+    const auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db) acc[db] = f32x16{};
+        sm = Softmax{};
+        if (end > 0) fill(0, 0);
+        int j0 = 0, buf = 0;
+        const auto next = [&] {
+            tile_wait();
+            __syncthreads();  // the tile is there, and the other one is read
+            if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
+        };
+        // first the tiles that every row of the work-group sees whole
+        for (; j0 + kKeys <= block_all; j0 += kKeys, buf ^= 1) {
+            next();
+            tile_forward<DT, DP, false, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+        }
+        for (; j0 < end; j0 += kKeys, buf ^= 1) {
+            next();
+            if (j0 < wave_any) tile_forward<DT, DP, true, CAREFUL>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0);
+        }
     };
-    // first the tiles that every row of the work-group sees whole
-    for (; j0 + kKeys <= block_all; j0 += kKeys, buf ^= 1) {
-        next();
-        tile_forward<DT, DP, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
-    }
-    for (; j0 < end; j0 += kKeys, buf ^= 1) {
-        next();
-        if (j0 + kKeys <= wave_all)
-            tile_forward<DT, DP, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
-        else if (j0 < wave_any)
-            tile_forward<DT, DP, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0);
-    }
+    pass(std::false_type{});
+    if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
     if (!exists) return;
     const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
     const bool some = live && l != 0.f;  // NaN too: it goes on to o

@@ -15,8 +15,8 @@ namespace kb {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 128;  // query rows of a work-group
-constexpr int kKeys = 64;   // keys of a tile
+constexpr int kRows = kAttnRows;
+constexpr int kKeys = kAttnKeys;
 
 // The softmax state of a lane's query over the tiles so far: terms are
 // exp(scale (s - m)).  In 16 bits m is a reference that follows the maximum only when a
@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     __shared__ __align__(16) T kt[2][L::size(kKeys)];
     __shared__ __align__(16) T vt[2][L::size(kKeys)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+    const int part = (int)blockIdx.y;
     const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
     const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
     const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;  // causal: the longest first
@@ -148,7 +149,11 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
     const int wave_any = wave_first < qlen ? key_limit(min(wave_last, qlen - 1), qlen, klen, p.causal) : 0;
     const int block_all = any ? key_limit(min((int)(first / p.group), qlen - 1), qlen, klen, p.causal) : 0;
-    const int end = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
+    // the part's tiles of those that the work-group's rows see
+    const int all = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
+    const int tiles = (all + kKeys - 1) / kKeys;
+    const int start = (int)((int64_t)tiles * part / p.splits) * kKeys;
+    const int end = min(all, (int)((int64_t)tiles * (part + 1) / p.splits) * kKeys);
 
     const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh + i * p.q.sl;
     const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh;
@@ -176,15 +181,15 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) acc[db] = f32x16{};
         sm = Softmax{};
-        if (end > 0) fill(0, 0);
-        int j0 = 0, buf = 0;
+        if (start < end) fill(start, 0);
+        int j0 = start, buf = 0;
         const auto next = [&] {
             tile_wait();
             __syncthreads();  // the tile is there, and the other one is read
             if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
         };
         // first the tiles that every row of the work-group sees whole
-        for (; j0 + kKeys <= block_all; j0 += kKeys, buf ^= 1) {
+        for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
             tile_forward<DT, DP, false, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
         }
@@ -197,6 +202,17 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
     if (!exists) return;
     const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
+    if (p.splits > 1) {
+        float* to = p.ws + ((((int64_t)at.b * p.kv_heads + at.h) * p.len_q * p.group + row) * p.splits + part) * split_row(p);
+        if (g == 0) *(f32x4*)(to + split_row(p) - 4) = f32x4{live ? sm.m : -INFINITY, live ? l : 0.f, live ? rounded : 0.f, 0.f};
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                if (32 * db + 2 * r + 4 * g < p.dim)
+                    *(f32x4*)(to + 32 * db + 2 * r + 4 * g) = f32x4{acc[db][r], acc[db][r + 1], acc[db][r + 2], acc[db][r + 3]};
+        return;
+    }
     const bool some = live && l != 0.f;  // NaN too: it goes on to o
     store_column<DT, DP>((T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl, acc, 1.f / (DT == DT_F32 ? l : rounded), some, p.dim, g);
     if (g == 0)
@@ -204,13 +220,54 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
             some ? fmaf(sm.m, p.scale, kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
 }
 
+// The parts of a row joined: each part's sums are relative to its own m.  A
+// thread has four elements of a row.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnParams p) {
+    using T = storage_t<DT>;
+    const int quads = (p.dim + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t row = id / quads;  // [batch][key head][query][head of the group]
+    const int d = (int)(id % quads) * 4;
+    if (row >= (int64_t)p.batch * p.heads * p.len_q) return;
+    const int64_t stride = split_row(p);
+    const float* in = p.ws + row * p.splits * stride;
+    float m = -INFINITY;
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, in[s * stride + stride - 4]);
+    const float shift = m == -INFINITY ? 0.f : m, to_log2 = p.scale * kLog2e;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f, rounded = 0.f;
+    for (int s = 0; s < p.splits; ++s) {
+        const f32x4 stat = *(const f32x4*)(in + s * stride + stride - 4), x = *(const f32x4*)(in + s * stride + d);
+        const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * to_log2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+        l = fmaf(w, stat[1], l);
+        rounded = fmaf(w, stat[2], rounded);
+    }
+    const int64_t per_head = (int64_t)p.len_q * p.group;
+    const int pair = (int)(row / per_head), in_head = (int)(row % per_head);
+    const int b = pair / p.kv_heads, hq = pair % p.kv_heads * p.group + in_head % p.group, i = in_head / p.group;
+    const bool some = l != 0.f;
+    const float f = some ? 1.f / (DT == DT_F32 ? l : rounded) : 0.f;
+    store_quad<DT>((T*)p.o.p + b * p.o.sb + hq * p.o.sh + i * p.o.sl, d, p.dim, some ? acc[0] * f : 0.f,
+                   some ? acc[1] * f : 0.f, some ? acc[2] * f : 0.f, some ? acc[3] * f : 0.f);
+    if (d == 0)
+        p.lse[((int64_t)b * p.heads + hq) * p.len_q + i] = some ? fmaf(m, p.scale, kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
+}
+
 template <int DT, int DP>
 hipError_t forward(const AttnParams& p, hipStream_t stream) {
     const int64_t blocks = ((int64_t)p.len_q * p.group + kRows - 1) / kRows * p.batch * p.kv_heads;
+    const dim3 grid((unsigned)blocks, (unsigned)p.splits);
     if (p.whole)
-        attn_forward_kernel<DT, DP, true><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(p);
+        attn_forward_kernel<DT, DP, true><<<grid, kThreads, 0, stream>>>(p);
     else
-        attn_forward_kernel<DT, DP, false><<<dim3((unsigned)blocks), kThreads, 0, stream>>>(p);
+        attn_forward_kernel<DT, DP, false><<<grid, kThreads, 0, stream>>>(p);
+    if (p.splits > 1) {
+        const int64_t quads = (int64_t)p.batch * p.heads * p.len_q * ((p.dim + 3) / 4);
+        attn_join_kernel<DT><<<dim3((unsigned)((quads + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(p);
+    }
     return hipGetLastError();
 }
 

@@ -70,9 +70,32 @@ struct AttnParams {
     int len_q, len_k, dim;
     float scale;
     int causal;
+    int splits; // forward: parts of the keys
     int whole;  // rows of q, k, v (and dout) are aligned to 16 bytes and made of 16-byte chunks
     float* ws;
 };
+
+// Forward: query rows of a work-group and keys of a tile, and into how many parts
+// the keys are split so that few query rows still fill the device: up to kFill
+// work-groups (two for each of 256 CUs, and as many again, as parts of a ragged
+// batch end at different times), of no less than kSplitKeys keys each.
+constexpr int kAttnRows = 128;
+constexpr int kAttnKeys = 64;
+constexpr int64_t kFill = 1024;
+constexpr int64_t kSplitKeys = 512;
+inline int attn_splits(const AttnParams& p) {
+    const int64_t work_groups =
+        (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_q * p.group + kAttnRows - 1) / kAttnRows);
+    if (work_groups == 0 || 2 * work_groups > kFill) return 1;
+    const int64_t want = kFill / work_groups, most = p.len_k / kSplitKeys;
+    return (int)(want < most ? want : most > 1 ? most : 1);
+}
+// Workspace of a split forward pass, in floats: for each query row and part the
+// sums over its keys (dim rounded up to 4), then m, l and the rounded l.
+__host__ __device__ inline int64_t split_row(const AttnParams& p) { return (p.dim + 3) / 4 * 4 + 4; }
+inline int64_t split_floats(const AttnParams& p, int splits) {
+    return splits > 1 ? (int64_t)p.batch * p.heads * p.len_q * splits * split_row(p) : 0;
+}
 
 // Workspace of the backward pass, in floats: D_i for every query row, then
 // (F16) the largest squared norm of each block of kNormBlock rows of dout and

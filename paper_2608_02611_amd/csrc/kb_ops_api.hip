@@ -337,7 +337,7 @@ int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w
 size_t kb_attn_forward_workspace_bytes(const kb_tensor* q, const kb_tensor* k) {
     AttnParams p{};
     if (q == nullptr || k == nullptr || !attn_sizes(*q, *k, &p)) return 0;
-    return 0;
+    return (size_t)split_floats(p, attn_splits(p)) * sizeof(float);
 }
 
 int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, const kb_attn_opts* opts,
@@ -349,7 +349,8 @@ int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, 
     if ((rc = check_attn(call, q, k, v, opts, &p)) || (rc = check_view(call, "o", o, 4, true)) ||
         (rc = check_shape(call, "o", *o, "q", *q)) || (rc = check_lse(call, lse, *q)))
         return rc;
-    const size_t need = kb_attn_forward_workspace_bytes(q, k);
+    p.splits = attn_splits(p);
+    const size_t need = (size_t)split_floats(p, p.splits) * sizeof(float);
     if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
     const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
     const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));

@@ -19,17 +19,22 @@ namespace kb {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr float kProbScale = 1024.f;
+constexpr float kProbLog2 = 10.f;
 
-// Workspace: D, then the blocks' largest squared norms of dout and of v.
-__host__ __device__ __forceinline__ int64_t dout_norms_at(const AttnParams& p) {
+// Workspace: D, then lse in units of log 2, then the blocks' largest squared
+// norms of dout and of v.
+__host__ __device__ __forceinline__ int64_t lse_at(const AttnParams& p) {
     return (int64_t)p.batch * p.heads * p.len_q;
 }
+__host__ __device__ __forceinline__ int64_t dout_norms_at(const AttnParams& p) { return 2 * lse_at(p); }
 __host__ __device__ __forceinline__ int64_t v_norms_at(const AttnParams& p) {
     return dout_norms_at(p) + (int64_t)p.batch * p.heads * ((p.len_q + kNormBlock - 1) / kNormBlock);
 }
 
-// Before the products: D_i for 64 query rows a work-group, 16 lanes a row.  F16:
+// Before the products: D_i and lse_i / log 2 for 64 query rows a work-group, 16
+// lanes a row.  A row with no seen score has lse = -infinity, and its terms
+// exp(-infinity - lse) are to be 0: it gets 0.  A row of the padding gets
+// +infinity, which makes all its terms 0, and D = 0.  F16:
 // also the largest finite squared norm of the block's rows of dout, and, in
 // the work-groups after those, of 64 rows of v.
 template <int DT>
@@ -69,7 +74,12 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p) {
             dot += __shfl_xor(dot, s);
             sq += __shfl_xor(sq, s);
         }
-        if (!of_v && sub == 0 && i < p.len_q) p.ws[((int64_t)b * p.heads + h) * p.len_q + i] = dot;
+        if (!of_v && sub == 0 && i < p.len_q) {
+            const int64_t row = ((int64_t)b * p.heads + h) * p.len_q + i;
+            const float lse = p.lse[row];
+            p.ws[row] = dot;
+            p.ws[lse_at(p) + row] = i >= n ? INFINITY : lse == -INFINITY ? 0.f : lse * kLog2e;
+        }
         if (sq < INFINITY) top = fmaxf(top, sq);
     }
     if (DT != DT_F16) return;
@@ -89,7 +99,8 @@ __device__ __forceinline__ int bound_exponent(float sq) {
 }
 
 // F16: 2^(14 - e), |t| < 2^(1 + e) over the heads that share key head h of
-// sequence b; 1 for the other types.  Called by every thread of a work-group.
+// sequence b; 1 for the other types.  (The exponent stays within binary32: |x|
+// of an F16 row of 128 is under 2^20 and its smallest is 2^-24.)  Called by every thread of a work-group.
 template <int DT>
 __device__ __forceinline__ float score_scale(const AttnParams& p, int b, int h, float* shared) {
     if (DT != DT_F16) return 1.f;
@@ -110,109 +121,188 @@ __device__ __forceinline__ float score_scale(const AttnParams& p, int b, int h, 
     return __uint_as_float((uint32_t)(127 + 14 - bound_exponent(d) - bound_exponent(v)) << 23);
 }
 
-// dk and dv of 128 keys, 32 a wave, kept with their key and value rows in
-// registers while the query rows of every head of the group pass in tiles of 32.
+// dk and dv of 128 keys, 32 a wave.  The keys stay (key rows in registers, value
+// rows in LDS, which leaves registers for two waves a SIMD) while the query
+// rows of every head of the group pass in tiles of 32.
 constexpr int kKeyRows = 128;
 constexpr int kQueries = 32;
 
-template <int DT, int DP>
-__global__ void __launch_bounds__(kThreads) attn_backward_keys_kernel(AttnParams p) {
+// One tile of queries for a wave's 32 keys: s and t with a key a column.  PART:
+// the lane's key is seen by the tile's queries from lo on.
+template <int DT, int DP, bool PART, bool CAREFUL>
+__device__ __forceinline__ void tile_keys(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], const frag_t<DT> (&kf)[DP / 16],
+                                          const storage_t<DT>* vt, const storage_t<DT>* qt, const storage_t<DT>* dt,
+                                          const float* rows, const Reader<DT, DP>& rd, float to_log2, float t_over_p,
+                                          int lo) {
+    const int g = rd.lane >> 5;
+    f32x16 s = {}, t;
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {  // t starts from -D
+        const f32x4 dot = *(const f32x4*)(rows + 8 * r4 + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[4 * r4 + e] = -dot[e];
+    }
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        s = mma(rd.row_frag(qt, 0, c), kf[c], s);
+        t = mma(rd.row_frag(dt, 0, c), rd.row_frag(vt, 0, c), t);
+    }
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 lse = *(const f32x4*)(rows + kQueries + 8 * r4 + 4 * g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int r = 4 * r4 + e;
+            // F16: the power of two of p goes into its exponent
+            float x = fmaf(s[r], to_log2, DT == DT_F16 ? kProbLog2 - lse[e] : -lse[e]);
+            if (PART) x = 8 * r4 + 4 * g + e >= lo ? x : -INFINITY;
+            s[r] = __builtin_amdgcn_exp2f(x);
+            t[r] = s[r] * t[r];
+            if (DT == DT_F16) t[r] *= t_over_p;
+            if (PART) t[r] = 8 * r4 + 4 * g + e >= lo ? t[r] : 0.f;
+        }
+    }
+    const frag_t<DT> pf[2] = {narrow<DT>(s, 0), narrow<DT>(s, 1)}, tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
+    mma_rows<DT, DP, PART && CAREFUL>(dv, dt, rd, 0, pf, lo, kQueries);
+    mma_rows<DT, DP, PART && CAREFUL>(dk, qt, rd, 0, tf, lo, kQueries);
+}
+
+template <int DT, int DP, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_keys_kernel(AttnParams p) {
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
-    __shared__ __align__(16) T qt[L::size(kQueries)];
-    __shared__ __align__(16) T dt[L::size(kQueries)];
-    __shared__ __align__(16) float norm[kQueries], dots[kQueries], scratch[8];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+    using F = Filler<DT, DP, kQueries, kThreads>;
+    __shared__ __align__(16) T vt[L::size(kKeyRows)];
+    __shared__ __align__(16) T qt[2][L::size(kQueries)];
+    __shared__ __align__(16) T dt[2][L::size(kQueries)];
+    __shared__ __align__(16) float rows[2][2 * kQueries];  // D, lse
+    __shared__ float scratch[8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 5;
     const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
     const int first = at.block * kKeyRows, j = first + wave * 32 + (lane & 31);
     const bool live = j < klen;
-    const float t_scale = score_scale<DT>(p, at.b, at.h, scratch);
-    const float p_scale = DT == DT_F16 ? kProbScale : 1.f;
+    // F16: p is held 2^10 p
+    const float p_scale = DT == DT_F16 ? __uint_as_float((127u + (uint32_t)kProbLog2) << 23) : 1.f;
+    const float t_scale = score_scale<DT>(p, at.b, at.h, scratch), t_over_p = t_scale / p_scale;
 
     const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh + (int64_t)j * p.k.sl;
-    const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh + (int64_t)j * p.v.sl;
-    frag_t<DT> kf[DP / 16], vf[DP / 16];
+    const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh;
+    frag_t<DT> kf[DP / 16];
 #pragma unroll
-    for (int c = 0; c < DP / 16; ++c) {
-        kf[c] = load_frag<DT, false>(k, c, g, p.dim, live);
-        vf[c] = load_frag<DT, false>(v, c, g, p.dim, live);
-    }
+    for (int c = 0; c < DP / 16; ++c) kf[c] = load_frag<DT, WHOLE>(k, c, g, p.dim, live);
+    if (WHOLE) Filler<DT, DP, kKeyRows, kThreads>(p.v.sl, p.dim).fill(vt, v, p.v.sl, first, klen, p.dim);
+    else stage<DT, DP, kKeyRows, kThreads>(vt, v, p.v.sl, first, klen, p.dim);
+
     // the queries that see a key: [sees(j), qlen)
     const auto sees = [&](int key) { return p.causal ? min(qlen, max(0, key - (klen - qlen))) : 0; };
-    const int lo = live ? sees(j) : qlen;
-    const int wave_key = first + wave * 32;
+    const int lo = sees(j);
     const int start = first < klen ? sees(first) / kQueries * kQueries : qlen;
-    const int wave_lo = wave_key < klen ? sees(wave_key) : qlen;
-    const int wave_hi = sees(min(wave_key + 31, klen - 1));  // from here on every key of the wave is seen
+    const int wave_lo = sees(first + wave * 32), wave_hi = sees(first + wave * 32 + 31);
+    const int block_hi = sees(first + kKeyRows - 1);  // from here on every key is seen
+    const int steps = (qlen - start + kQueries - 1) / kQueries;  // tiles of one head
+
+    const F fq(p.q.sl, p.dim), fd(p.dout.sl, p.dim);
+    const T* q = (const T*)p.q.p + at.b * p.q.sb + at.h * p.group * p.q.sh;
+    const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + at.h * p.group * p.dout.sh;
+    const float* row_values = p.ws + ((int64_t)at.b * p.heads + at.h * p.group) * p.len_q;
+    const auto fill = [&](int h, int i0, int buf) {
+        if (WHOLE) {
+            fq.fill(qt[buf], q + h * p.q.sh, p.q.sl, i0, qlen, p.dim);
+            fd.fill(dt[buf], dout + h * p.dout.sh, p.dout.sl, i0, qlen, p.dim);
+        } else {
+            stage<DT, DP, kQueries, kThreads>(qt[buf], q + h * p.q.sh, p.q.sl, i0, qlen, p.dim);
+            stage<DT, DP, kQueries, kThreads>(dt[buf], dout + h * p.dout.sh, p.dout.sl, i0, qlen, p.dim);
+        }
+        if (wave == 0) {
+            const int i = i0 + (lane & 31);
+            if (i < qlen)
+                __builtin_amdgcn_global_load_lds(
+                    (const __attribute__((address_space(1))) void*)(row_values + (int64_t)h * p.len_q + i +
+                                                                    (lane < 32 ? 0 : lse_at(p))),
+                    (__attribute__((address_space(3))) void*)rows[buf], 4, 0, 0);
+            else
+                rows[buf][lane] = lane < 32 ? 0.f : INFINITY;
+        }
+    };
 
     const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
+    const T* v_rows = vt + wave * L::size(32);
     f32x16 dk[DP / 32], dv[DP / 32];
     const auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) dk[db] = dv[db] = f32x16{};
+        int buf = 0;
+        if (steps > 0) fill(0, start, 0);
         for (int h = 0; h < p.group; ++h) {
-            const int hq = at.h * p.group + h;
-            const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh;
-            const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh;
-            const int64_t rows = ((int64_t)at.b * p.heads + hq) * p.len_q;
-            for (int i0 = start; i0 < qlen; i0 += kQueries) {
-                __syncthreads();
-                stage<DT, DP, kQueries, kThreads>(qt, q, p.q.sl, i0, qlen, p.dim);
-                stage<DT, DP, kQueries, kThreads>(dt, dout, p.dout.sl, i0, qlen, p.dim);
-                if (threadIdx.x < kQueries) {
-                    const int i = i0 + (int)threadIdx.x;
-                    const float lse = i < qlen ? p.lse[rows + i] : 0.f;
-                    norm[threadIdx.x] = lse == -INFINITY ? 0.f : lse * kLog2e;
-                    dots[threadIdx.x] = i < qlen ? p.ws[rows + i] : 0.f;
-                }
-                __syncthreads();
-                if (i0 + kQueries <= wave_lo) continue;
-                f32x16 s = {}, t = {};
-#pragma unroll
-                for (int c = 0; c < DP / 16; ++c) {
-                    s = mma(rd.row_frag(qt, 0, c), kf[c], s);
-                    t = mma(rd.row_frag(dt, 0, c), vf[c], t);
-                }
-                const bool part = i0 < wave_hi || i0 + kQueries > qlen || wave_key + 32 > klen;
-#pragma unroll
-                for (int r4 = 0; r4 < 4; ++r4) {
-                    const f32x4 lse = *(const f32x4*)(norm + 8 * r4 + 4 * g), dot = *(const f32x4*)(dots + 8 * r4 + 4 * g);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int r = 4 * r4 + e, i = i0 + 8 * r4 + 4 * g + e;
-                        const bool seen = !part || (i >= lo && i < qlen);
-                        const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse[e]));
-                        t[r] = seen ? prob * (t[r] - dot[e]) * t_scale : 0.f;
-                        s[r] = seen ? prob * p_scale : 0.f;
-                    }
-                }
-                const frag_t<DT> pf[2] = {narrow<DT>(s, 0), narrow<DT>(s, 1)}, tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
-                mma_rows<DT, DP, CAREFUL>(dv, dt, rd, 0, pf, lo - i0, qlen - i0);
-                mma_rows<DT, DP, CAREFUL>(dk, qt, rd, 0, tf, lo - i0, qlen - i0);
+            int i0 = start;
+            const auto next = [&] {
+                tile_wait();
+                __syncthreads();  // the tile is there, and the other one is read
+                const bool last = i0 + kQueries >= qlen;
+                if (!last || h + 1 < p.group) fill(last ? h + 1 : h, last ? start : i0 + kQueries, buf ^ 1);
+            };
+            for (; i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1) {
+                next();
+                if (i0 >= wave_hi)
+                    tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
+                else if (i0 + kQueries > wave_lo)
+                    tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, lo - i0);
+            }
+            for (; i0 < qlen; i0 += kQueries, buf ^= 1) {
+                next();
+                tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
             }
         }
     };
     pass(std::false_type{});
     if (p.causal && __syncthreads_or(non_finite(dk) || non_finite(dv))) pass(std::true_type{});
     if (j >= p.len_k) return;
-    store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, p.scale / t_scale, live, p.dim, g);
+    store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, p.scale / t_scale, live,
+                         p.dim, g);
     store_column<DT, DP>((T*)p.dv.p + at.b * p.dv.sb + at.h * p.dv.sh + j * p.dv.sl, dv, 1.f / p_scale, live, p.dim, g);
 }
 
 // dq of 128 query rows (row = query * group + head, as in the forward pass),
-// 32 a wave, while the keys pass in tiles of 32.
-constexpr int kRows = 128;
-constexpr int kKeys = 32;
+// 32 a wave, while the keys pass in tiles of 64.
+constexpr int kRows = kAttnRows;
+constexpr int kKeys = kAttnKeys;
 
-template <int DT, int DP>
-__global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnParams p) {
+// One tile of keys for a wave's 32 query rows; PART: the lane's row sees the
+// tile's keys below hi.
+template <int DT, int DP, bool PART, bool CAREFUL>
+__device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t<DT> (&qf)[DP / 16],
+                                             const frag_t<DT> (&df)[DP / 16], const storage_t<DT>* kt,
+                                             const storage_t<DT>* vt, const Reader<DT, DP>& rd, float to_log2,
+                                             float lse, float dot, int hi) {
+    const int g = rd.lane >> 5;
+#pragma unroll
+    for (int u = 0; u < kKeys / 32; ++u) {
+        f32x16 s = {}, t = {};
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) {
+            s = mma(rd.row_frag(kt, 32 * u, c), qf[c], s);
+            t = mma(rd.row_frag(vt, 32 * u, c), df[c], t);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            t[r] = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse)) * (t[r] - dot);
+            if (PART) t[r] = 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) < hi ? t[r] : 0.f;
+        }
+        const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
+        mma_rows<DT, DP, PART && CAREFUL>(dq, kt, rd, 32 * u, tf, 0, hi);
+    }
+}
+
+template <int DT, int DP, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_queries_kernel(AttnParams p) {
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
-    __shared__ __align__(16) T kt[L::size(kKeys)];
-    __shared__ __align__(16) T vt[L::size(kKeys)];
+    using F = Filler<DT, DP, kKeys, kThreads>;
+    __shared__ __align__(16) T kt[2][L::size(kKeys)];
+    __shared__ __align__(16) T vt[2][L::size(kKeys)];
     __shared__ float scratch[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
     const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
@@ -224,12 +314,14 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
     const int64_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
     const bool exists = i < p.len_q, live = i < qlen;
-    const int wave_first = (int)((first + wave * 32) / p.group), wave_last = (int)((first + wave * 32 + 31) / p.group);
+    const int wave_first = __builtin_amdgcn_readfirstlane((int)((first + wave * 32) / p.group));
+    const int wave_last = __builtin_amdgcn_readfirstlane((int)((first + wave * 32 + 31) / p.group));
     const int block_last = (int)((first + kRows - 1) / p.group);
+    const bool any = (int)(first / p.group) < qlen;
     const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
-    const int wave_all = key_limit(min(wave_first, qlen - 1), qlen, klen, p.causal);
     const int wave_any = wave_first < qlen ? key_limit(min(wave_last, qlen - 1), qlen, klen, p.causal) : 0;
-    const int end = (int)(first / p.group) < qlen ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
+    const int block_all = any ? key_limit(min((int)(first / p.group), qlen - 1), qlen, klen, p.causal) : 0;
+    const int end = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
 
     const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh + i * p.q.sl;
     const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh + i * p.dout.sl;
@@ -238,14 +330,24 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
     frag_t<DT> qf[DP / 16], df[DP / 16];
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) {
-        qf[c] = load_frag<DT, false>(q, c, g, p.dim, live);
-        df[c] = load_frag<DT, false>(dout, c, g, p.dim, live);
+        qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
+        df[c] = load_frag<DT, WHOLE>(dout, c, g, p.dim, live);
     }
     const int64_t at_row = ((int64_t)at.b * p.heads + hq) * p.len_q + i;
-    float lse = live ? p.lse[at_row] : 0.f;
-    lse = lse == -INFINITY ? 0.f : lse * kLog2e;
+    // t_scale is a power of two: it goes into the exponent
+    const float lse = live ? p.ws[lse_at(p) + at_row] - __builtin_amdgcn_logf(t_scale) : INFINITY;
     const float dot = live ? p.ws[at_row] : 0.f;
 
+    const F fk(p.k.sl, p.dim), fv(p.v.sl, p.dim);
+    const auto fill = [&](int j0, int buf) {
+        if (WHOLE) {
+            fk.fill(kt[buf], k, p.k.sl, j0, klen, p.dim);
+            fv.fill(vt[buf], v, p.v.sl, j0, klen, p.dim);
+        } else {
+            stage<DT, DP, kKeys, kThreads>(kt[buf], k, p.k.sl, j0, klen, p.dim);
+            stage<DT, DP, kKeys, kThreads>(vt[buf], v, p.v.sl, j0, klen, p.dim);
+        }
+    };
     const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
     f32x16 dq[DP / 32];
@@ -253,27 +355,22 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
         constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) dq[db] = f32x16{};
-        for (int j0 = 0; j0 < end; j0 += kKeys) {
-            __syncthreads();
-            stage<DT, DP, kKeys, kThreads>(kt, k, p.k.sl, j0, klen, p.dim);
-            stage<DT, DP, kKeys, kThreads>(vt, v, p.v.sl, j0, klen, p.dim);
-            __syncthreads();
-            if (j0 >= wave_any) continue;
-            f32x16 s = {}, t = {};
-#pragma unroll
-            for (int c = 0; c < DP / 16; ++c) {
-                s = mma(rd.row_frag(kt, 0, c), qf[c], s);
-                t = mma(rd.row_frag(vt, 0, c), df[c], t);
-            }
-            const bool part = j0 + kKeys > wave_all;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const bool seen = !part || j0 + 8 * (r >> 2) + 4 * g + (r & 3) < lim;
-                const float prob = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse));
-                t[r] = seen ? prob * (t[r] - dot) * t_scale : 0.f;
-            }
-            const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
-            mma_rows<DT, DP, CAREFUL>(dq, kt, rd, 0, tf, 0, lim - j0);
+        if (end > 0) fill(0, 0);
+        int j0 = 0, buf = 0;
+        const auto next = [&] {
+            tile_wait();
+            __syncthreads();  // the tile is there, and the other one is read
+            if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
+        };
+        // first the tiles that every row of the work-group sees whole
+        for (; j0 + kKeys <= block_all; j0 += kKeys, buf ^= 1) {
+            next();
+            tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0);
+        }
+        for (; j0 < end; j0 += kKeys, buf ^= 1) {
+            next();
+            if (j0 < wave_any)
+                tile_queries<DT, DP, true, CAREFUL>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, lim - j0);
         }
     };
     pass(std::false_type{});
@@ -282,7 +379,7 @@ __global__ void __launch_bounds__(kThreads) attn_backward_queries_kernel(AttnPar
     store_column<DT, DP>((T*)p.dq.p + at.b * p.dq.sb + hq * p.dq.sh + i * p.dq.sl, dq, p.scale / t_scale, live, p.dim, g);
 }
 
-template <int DT, int DP>
+template <int DT, int DP, bool WHOLE>
 hipError_t backward(const AttnParams& p, hipStream_t stream) {
     const int64_t pairs = (int64_t)p.batch * p.kv_heads;
     const int64_t key_blocks = ((int64_t)p.len_k + kKeyRows - 1) / kKeyRows * pairs;
@@ -290,9 +387,14 @@ hipError_t backward(const AttnParams& p, hipStream_t stream) {
     const int64_t rows = (int64_t)p.batch * p.heads * norm_blocks(p.len_q) +
                          (DT == DT_F16 ? pairs * norm_blocks(p.len_k) : 0);
     if (rows > 0) attn_rows_kernel<DT><<<dim3((unsigned)rows), kThreads, 0, stream>>>(p);
-    if (key_blocks > 0) attn_backward_keys_kernel<DT, DP><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
-    if (row_blocks > 0) attn_backward_queries_kernel<DT, DP><<<dim3((unsigned)row_blocks), kThreads, 0, stream>>>(p);
+    if (key_blocks > 0) attn_backward_keys_kernel<DT, DP, WHOLE><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
+    if (row_blocks > 0) attn_backward_queries_kernel<DT, DP, WHOLE><<<dim3((unsigned)row_blocks), kThreads, 0, stream>>>(p);
     return hipGetLastError();
+}
+
+template <int DT, int DP>
+hipError_t backward(const AttnParams& p, hipStream_t stream) {
+    return p.whole ? backward<DT, DP, true>(p, stream) : backward<DT, DP, false>(p, stream);
 }
 
 template <int DT>

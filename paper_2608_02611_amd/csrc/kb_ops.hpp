@@ -97,7 +97,7 @@ inline int64_t split_floats(const AttnParams& p, int splits) {
     return splits > 1 ? (int64_t)p.batch * p.heads * p.len_q * splits * split_row(p) : 0;
 }
 
-// Workspace of the backward pass, in floats: D_i for every query row, then
+// Workspace of the backward pass, in floats: D_i and lse_i for every query row, then
 // (F16) the largest squared norm of each block of kNormBlock rows of dout and
 // of v.
 constexpr int kNormBlock = 64;

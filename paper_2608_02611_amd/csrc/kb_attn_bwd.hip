@@ -22,13 +22,17 @@ constexpr int kThreads = 256;
 constexpr float kProbLog2 = 10.f;
 
 // Workspace: D, then lse in units of log 2, then the blocks' largest squared
-// norms of dout and of v.
+// norms of dout and of v, then a mark for each work-group that has keys.
 __host__ __device__ __forceinline__ int64_t lse_at(const AttnParams& p) {
     return (int64_t)p.batch * p.heads * p.len_q;
 }
 __host__ __device__ __forceinline__ int64_t dout_norms_at(const AttnParams& p) { return 2 * lse_at(p); }
 __host__ __device__ __forceinline__ int64_t v_norms_at(const AttnParams& p) {
     return dout_norms_at(p) + (int64_t)p.batch * p.heads * ((p.len_q + kNormBlock - 1) / kNormBlock);
+}
+
+__host__ __device__ __forceinline__ int64_t marks_at(const AttnParams& p) {
+    return v_norms_at(p) + (int64_t)p.batch * p.kv_heads * ((p.len_k + kNormBlock - 1) / kNormBlock);
 }
 
 // Before the products: D_i and lse_i / log 2 for 64 query rows a work-group, 16
@@ -124,7 +128,7 @@ __device__ __forceinline__ float score_scale(const AttnParams& p, int b, int h, 
 // dk and dv of 128 keys, 32 a wave.  The keys stay (key rows in registers, value
 // rows in LDS, which leaves registers for two waves a SIMD) while the query
 // rows of every head of the group pass in tiles of 32.
-constexpr int kKeyRows = 128;
+constexpr int kKeyRows = kAttnKeyRows;
 constexpr int kQueries = 32;
 
 // One tile of queries for a wave's 32 keys: s and t with a key a column.  PART:
@@ -167,8 +171,12 @@ __device__ __forceinline__ void tile_keys(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP
     mma_rows<DT, DP, PART && CAREFUL>(dk, qt, rd, 0, tf, lo, kQueries);
 }
 
-template <int DT, int DP, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_keys_kernel(AttnParams p) {
+// CAREFUL: a launch of its own, for the work-groups that the first one marked (in
+// the same kernel it would cost the first pass the registers that it needs).
+template <int DT, int DP, bool WHOLE, bool CAREFUL>
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) attn_backward_keys_kernel(AttnParams p) {
+    uint32_t* mark = (uint32_t*)(p.ws + marks_at(p)) + blockIdx.x;
+    if (CAREFUL && *mark == 0) return;
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
     using F = Filler<DT, DP, kQueries, kThreads>;
@@ -198,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     const auto sees = [&](int key) { return p.causal ? min(qlen, max(0, key - (klen - qlen))) : 0; };
     const int lo = sees(j);
     const int start = first < klen ? sees(first) / kQueries * kQueries : qlen;
-    const int wave_lo = sees(first + wave * 32), wave_hi = sees(first + wave * 32 + 31);
+    const int wave_lo = sees(first + wave * 32);
     const int block_hi = sees(first + kKeyRows - 1);  // from here on every key is seen
     const int steps = (qlen - start + kQueries - 1) / kQueries;  // tiles of one head
 
@@ -229,36 +237,32 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
     const T* v_rows = vt + wave * L::size(32);
-    f32x16 dk[DP / 32], dv[DP / 32];
-    const auto pass = [&](auto careful) {
-        constexpr bool CAREFUL = decltype(careful)::value;
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db) dk[db] = dv[db] = f32x16{};
-        int buf = 0;
-        if (steps > 0) fill(0, start, 0);
-        for (int h = 0; h < p.group; ++h) {
-            int i0 = start;
-            const auto next = [&] {
-                tile_wait();
-                __syncthreads();  // the tile is there, and the other one is read
-                const bool last = i0 + kQueries >= qlen;
-                if (!last || h + 1 < p.group) fill(last ? h + 1 : h, last ? start : i0 + kQueries, buf ^ 1);
-            };
-            for (; i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1) {
-                next();
-                if (i0 >= wave_hi)
-                    tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
-                else if (i0 + kQueries > wave_lo)
-                    tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, lo - i0);
-            }
-            for (; i0 < qlen; i0 += kQueries, buf ^= 1) {
-                next();
-                tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
-            }
+    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    int buf = 0;
+    if (steps > 0) fill(0, start, 0);
+    for (int h = 0; h < p.group; ++h) {
+        int i0 = start;
+        const auto next = [&] {
+            tile_wait();
+            __syncthreads();  // the tile is there, and the other one is read
+            const bool last = i0 + kQueries >= qlen;
+            if (!last || h + 1 < p.group) fill(last ? h + 1 : h, last ? start : i0 + kQueries, buf ^ 1);
+        };
+        for (; i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1) {
+            next();
+            if (i0 + kQueries > wave_lo)
+                tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p,
+                                                 lo - i0);
         }
-    };
-    pass(std::false_type{});
-    if (p.causal && __syncthreads_or(non_finite(dk) || non_finite(dv))) pass(std::true_type{});
+        for (; i0 < qlen; i0 += kQueries, buf ^= 1) {
+            next();
+            tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
+        }
+    }
+    if (!CAREFUL && p.causal) {
+        const int bad = __syncthreads_or(non_finite(dk) || non_finite(dv));
+        if (threadIdx.x == 0) *mark = bad;
+    }
     if (j >= p.len_k) return;
     store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, p.scale / t_scale, live,
                          p.dim, g);
@@ -387,7 +391,11 @@ hipError_t backward(const AttnParams& p, hipStream_t stream) {
     const int64_t rows = (int64_t)p.batch * p.heads * norm_blocks(p.len_q) +
                          (DT == DT_F16 ? pairs * norm_blocks(p.len_k) : 0);
     if (rows > 0) attn_rows_kernel<DT><<<dim3((unsigned)rows), kThreads, 0, stream>>>(p);
-    if (key_blocks > 0) attn_backward_keys_kernel<DT, DP, WHOLE><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
+    if (key_blocks > 0) {
+        attn_backward_keys_kernel<DT, DP, WHOLE, false><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
+        if (p.causal)
+            attn_backward_keys_kernel<DT, DP, WHOLE, true><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
+    }
     if (row_blocks > 0) attn_backward_queries_kernel<DT, DP, WHOLE><<<dim3((unsigned)row_blocks), kThreads, 0, stream>>>(p);
     return hipGetLastError();
 }

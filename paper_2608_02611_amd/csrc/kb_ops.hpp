@@ -99,8 +99,9 @@ inline int64_t split_floats(const AttnParams& p, int splits) {
 
 // Workspace of the backward pass, in floats: D_i and lse_i for every query row, then
 // (F16) the largest squared norm of each block of kNormBlock rows of dout and
-// of v.
+// of v, then a word for each work-group of kAttnKeyRows keys.
 constexpr int kNormBlock = 64;
+constexpr int kAttnKeyRows = 128;
 inline int64_t norm_blocks(int64_t len) { return (len + kNormBlock - 1) / kNormBlock; }
 
 hipError_t launch_attn_forward(int dtype, const AttnParams& p, hipStream_t stream);

@@ -224,7 +224,8 @@ bool attn_sizes(const kb_tensor& q, const kb_tensor& k, AttnParams* p) {
 
 size_t attn_backward_bytes(const AttnParams& p) {
     const int64_t rows = (int64_t)p.batch * p.heads, pairs = (int64_t)p.batch * p.kv_heads;
-    const int64_t floats = 2 * rows * p.len_q + rows * norm_blocks(p.len_q) + pairs * norm_blocks(p.len_k);
+    const int64_t floats = 2 * rows * p.len_q + rows * norm_blocks(p.len_q) + pairs * norm_blocks(p.len_k) +
+                           pairs * (((int64_t)p.len_k + kAttnKeyRows - 1) / kAttnKeyRows);
     return ((size_t)floats * sizeof(float) + 15) & ~(size_t)15;
 }
 

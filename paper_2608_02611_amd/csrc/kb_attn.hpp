@@ -365,15 +365,21 @@ __device__ __forceinline__ int key_limit(int i, int qlen, int klen, int causal) 
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
 
-// Work-groups are numbered so that those of one key head follow each other at
-// a distance of all (batch, head) pairs: with a multiple of 8 pairs (the usual
-// case) a head's work-groups land on one XCD, whose L2 then holds its keys.
+// Work-group `id` of `blocks` blocks for each (batch, key head) pair, pair by
+// pair at the same block: with a multiple of 8 pairs (the usual case) a head's
+// work-groups land on one XCD, whose L2 then holds its keys.  Block 0 is to be
+// the longest.  A launch of two work-groups a CU or less has no later ones to
+// even out a causal mask's long and short blocks: there the second work-group
+// of a CU is the shorter, the longer the first one is.
 struct HeadBlock {
     int b, h, block;
 };
-__device__ __forceinline__ HeadBlock head_block(int kv_heads, int pairs) {
-    const int pair = (int)blockIdx.x % pairs;
-    return {pair / kv_heads, pair % kv_heads, (int)blockIdx.x / pairs};
+__device__ __forceinline__ HeadBlock head_block(int id, int kv_heads, int pairs, int blocks) {
+    constexpr int kCus = 256;
+    const int total = pairs * blocks;
+    if (total <= 2 * kCus && id >= kCus) id = total - 1 - (id - kCus);
+    const int pair = id % pairs;
+    return {pair / kv_heads, pair % kv_heads, id / pairs};
 }
 
 }  // namespace kb

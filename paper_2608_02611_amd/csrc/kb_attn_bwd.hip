@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     __shared__ __align__(16) float rows[2][2 * kQueries];  // D, lse
     __shared__ float scratch[8];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 5;
-    const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
+    const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, (p.len_k + kKeyRows - 1) / kKeyRows);
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
     const int first = at.block * kKeyRows, j = first + wave * 32 + (lane & 31);
     const bool live = j < klen;
@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     __shared__ __align__(16) T vt[2][L::size(kKeys)];
     __shared__ float scratch[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-    const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
     const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
+    const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, n_blocks);
     const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
     const float t_scale = score_scale<DT>(p, at.b, at.h, scratch);

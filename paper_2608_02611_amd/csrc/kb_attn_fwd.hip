@@ -134,8 +134,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     __shared__ __align__(16) T vt[2][L::size(kKeys)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
     const int part = (int)blockIdx.y;
-    const HeadBlock at = head_block(p.kv_heads, p.batch * p.kv_heads);
     const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
+    const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, n_blocks);
     const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;  // causal: the longest first
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
 

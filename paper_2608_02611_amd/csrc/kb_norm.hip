@@ -14,32 +14,308 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// Sums over the work-group, the same bits in every thread; s: one float per
-// wave and value.
+// Sums over the TPR threads of a row, the same bits in each of them; s: LDS for
+// one float per wave and value (rows of more than a wave).  The work-group meets
+// once, before the sums are read, so a call may not write the s of the call
+// before: the callers take two in turn.
+template <int TPR, int K>
+__device__ __forceinline__ void row_sum(float (&v)[K], float* s) {
+    if constexpr (TPR <= 16) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            v[k] += __uint_as_float(dpp_u32<DPP_QUAD_XOR1>(__float_as_uint(v[k])));
+            v[k] += __uint_as_float(dpp_u32<DPP_QUAD_XOR2>(__float_as_uint(v[k])));
+            v[k] += __uint_as_float(dpp_u32<DPP_ROW_HALF_MIRROR>(__float_as_uint(v[k])));
+            v[k] += __uint_as_float(dpp_u32<DPP_ROW_MIRROR>(__float_as_uint(v[k])));
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = wave_sum_f32(v[k]);
+    }
+    if constexpr (TPR > 64) {
+        constexpr int W = TPR / 64;  // waves of a row
+        const int wave = (int)threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) s[wave * K + k] = v[k];
+        }
+        __syncthreads();
+        const float* mine = s + wave / W * W * K;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float sum = mine[k];
+#pragma unroll
+            for (int w = 1; w < W; ++w) sum += mine[w * K + k];
+            v[k] = sum;
+        }
+    }
+}
+
+// A row in the registers of TPR threads, E elements each: vector i of a thread
+// is at column (i TPR + t) N.  Columns past the row are 0.
+template <int DT, int TPR, int E>
+struct RowRegs {
+    using T = storage_t<DT>;
+    static constexpr int N = Vec16<T>::N;
+    static constexpr int NV = E / N;
+    typename Vec16<T>::type v[NV];
+
+    __device__ __forceinline__ void load(const T* row, int t, int cols) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * N;
+            if (c + N <= cols) {
+                v[i] = *(const typename Vec16<T>::type*)(row + c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) v[i][e] = c + e < cols ? row[c + e] : (T)0.f;
+            }
+        }
+    }
+    __device__ __forceinline__ float at(int e) const { return (float)v[e / N][e % N]; }
+};
+
+// Threads of a row and elements of a thread: the fewest threads that hold the
+// row at 16 elements each (8 up to 512 columns), so that a wave or less has a
+// row where that is possible and its sums need no meeting.  More elements a
+// thread leave too few waves on a CU to cover HBM's latency.
+#define KB_NORM_DISPATCH(COLS, CALL)              \
+    ((COLS) <= 128     ? CALL<DT, WDT, 16, 8>     \
+     : (COLS) <= 512   ? CALL<DT, WDT, 64, 8>     \
+     : (COLS) <= 1024  ? CALL<DT, WDT, 64, 16>    \
+     : (COLS) <= 2048  ? CALL<DT, WDT, 128, 16>   \
+     : (COLS) <= 4096  ? CALL<DT, WDT, 256, 16>   \
+     : (COLS) <= 8192  ? CALL<DT, WDT, 512, 16>   \
+     : (COLS) <= 16384 ? CALL<DT, WDT, 1024, 16>  \
+                       : CALL##_long<DT, WDT>)
+
+constexpr int block_of(int tpr) { return tpr > kThreads ? tpr : kThreads; }
+
+// Work-groups of a launch that goes over the rows in strides.
+constexpr int64_t kForwardGroups = 2048;
+
+// Forward: the row stays in registers between its two sums and the result; the
+// next row is on its way meanwhile.
+template <int DT, int WDT, int TPR, int E>
+__global__ void __launch_bounds__(block_of(TPR)) norm_forward_rows_kernel(NormForwardParams p) {
+    using T = storage_t<DT>;
+    using W = storage_t<WDT>;
+    using R = RowRegs<DT, TPR, E>;
+    constexpr int N = R::N, ROWS = block_of(TPR) / TPR;
+    __shared__ float s[2][block_of(TPR) / 64];
+    const int t = (int)threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + (int)threadIdx.x / TPR;
+    const int64_t last = p.rows - 1;
+    const float inv = 1.f / (float)p.cols;
+    const auto column = [&](int e) { return (e / N * TPR + t) * N + e % N; };
+    float wf[E], bf[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int c = min(column(e), p.cols - 1);
+        wf[e] = p.w ? (float)((const W*)p.w)[c] : 1.f;
+        bf[e] = p.b ? (float)((const W*)p.b)[c] : 0.f;
+    }
+    R next;
+    next.load((const T*)p.x.p + min(row, last) * p.x.stride, t, p.cols);
+    for (int64_t base = (int64_t)blockIdx.x * ROWS; base < p.rows; base += step, row += step) {
+        const R x = next;
+        if (base + step < p.rows) next.load((const T*)p.x.p + min(row + step, last) * p.x.stride, t, p.cols);
+        float sum[1] = {0.f};
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[0] += x.at(e);
+        row_sum<TPR>(sum, s[0]);
+        const float mean = sum[0] * inv;
+        sum[0] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = column(e) < p.cols ? x.at(e) - mean : 0.f;
+            sum[0] = fmaf(d, d, sum[0]);
+        }
+        row_sum<TPR>(sum, s[1]);
+        const float rstd = 1.f / sqrtf(fmaf(sum[0], inv, p.eps));
+        if (row > last) continue;
+        if (t == 0) {
+            if (p.mean) p.mean[row] = mean;
+            if (p.rstd) p.rstd[row] = rstd;
+        }
+        T* y = (T*)p.y.p + row * p.y.stride;
+#pragma unroll
+        for (int i = 0; i < R::NV; ++i) {
+            float out[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) out[e] = fmaf((x.at(i * N + e) - mean) * rstd, wf[i * N + e], bf[i * N + e]);
+            const int c = (i * TPR + t) * N;
+            if (c < p.cols) store_vec(y + c, p.cols - c, out);
+        }
+    }
+}
+
+template <int DT, int WDT, int TPR, int E>
+hipError_t norm_forward_rows(const NormForwardParams& p, hipStream_t stream) {
+    constexpr int ROWS = block_of(TPR) / TPR;
+    const int64_t groups = (p.rows + ROWS - 1) / ROWS;
+    norm_forward_rows_kernel<DT, WDT, TPR, E>
+        <<<dim3((unsigned)(groups < kForwardGroups ? groups : kForwardGroups)), block_of(TPR), 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+// Backward: dy and x of a row in registers for the two sums and dx; dw and db of
+// the thread's columns add up over the rows that it sees.  At the end the row
+// groups of a work-group are added in LDS, in their order, and written as one
+// part.
+template <int DT, int WDT, int TPR, int E>
+__global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormBackwardParams p) {
+    using T = storage_t<DT>;
+    using W = storage_t<WDT>;
+    using R = RowRegs<DT, TPR, E>;
+    constexpr int N = R::N, ROWS = block_of(TPR) / TPR;
+    __shared__ float s[2][2 * block_of(TPR) / 64];
+    const int t = (int)threadIdx.x % TPR, group = (int)threadIdx.x / TPR;
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + group;
+    const int64_t last = p.rows - 1;
+    const float inv = 1.f / (float)p.cols;
+    const auto column = [&](int e) { return (e / N * TPR + t) * N + e % N; };
+    float wf[E], dw[E], db[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        wf[e] = p.w && column(e) < p.cols ? (float)((const W*)p.w)[column(e)] : 1.f;
+        dw[e] = db[e] = 0.f;
+    }
+    R next_dy, next_x;
+    next_dy.load((const T*)p.dy.p + min(row, last) * p.dy.stride, t, p.cols);
+    next_x.load((const T*)p.x.p + min(row, last) * p.x.stride, t, p.cols);
+    float next_mean = p.mean[min(row, last)], next_rstd = p.rstd[min(row, last)];
+    int turn = 0;
+    for (int64_t base = (int64_t)blockIdx.x * ROWS; base < p.rows; base += step, row += step, turn ^= 1) {
+        const R dy = next_dy, x = next_x;
+        const float mean = next_mean, rstd = next_rstd;
+        if (base + step < p.rows) {
+            const int64_t r = min(row + step, last);
+            next_dy.load((const T*)p.dy.p + r * p.dy.stride, t, p.cols);
+            next_x.load((const T*)p.x.p + r * p.x.stride, t, p.cols);
+            next_mean = p.mean[r];
+            next_rstd = p.rstd[r];
+        }
+        const bool live = row <= last;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = dy.at(e), g = d * wf[e];
+            // past the row dy is 0; z there is not, and may not be finite
+            const float z = column(e) < p.cols ? (x.at(e) - mean) * rstd : 0.f;
+            sum[0] += g;
+            sum[1] = fmaf(g, z, sum[1]);
+            if (live) {
+                dw[e] = fmaf(d, z, dw[e]);
+                db[e] += d;
+            }
+        }
+        if (!p.dx.p) continue;
+        row_sum<TPR>(sum, s[turn]);
+        if (!live) continue;
+        const float mg = sum[0] * inv, mgz = sum[1] * inv;
+        T* dx = (T*)p.dx.p + row * p.dx.stride;
+#pragma unroll
+        for (int i = 0; i < R::NV; ++i) {
+            float out[N];
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const float z = (x.at(i * N + e) - mean) * rstd;
+                out[e] = rstd * (fmaf(dy.at(i * N + e), wf[i * N + e], -mg) - z * mgz);
+            }
+            const int c = (i * TPR + t) * N;
+            if (c < p.cols) store_vec(dx + c, p.cols - c, out);
+        }
+    }
+    if (!p.dw && !p.db) return;
+    float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
+    if constexpr (ROWS > 1) {
+        __shared__ float sums[2][TPR * E];
+#pragma unroll 1
+        for (int k = 0; k < ROWS; ++k) {
+            if (group == k) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    sums[0][e * TPR + t] = k ? sums[0][e * TPR + t] + dw[e] : dw[e];
+                    sums[1][e * TPR + t] = k ? sums[1][e * TPR + t] + db[e] : db[e];
+                }
+            }
+            __syncthreads();
+        }
+        if (group > 0) return;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            dw[e] = sums[0][e * TPR + t];
+            db[e] = sums[1][e * TPR + t];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < R::NV; ++i) {
+        const int c = (i * TPR + t) * N;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (c + e < p.cols) {
+                part[c + e] = dw[i * N + e];
+                part[p.cols + c + e] = db[i * N + e];
+            }
+    }
+}
+
+// dw and db from the parts: a column a lane, the parts dealt out to 16 waves,
+// whose sums are added in their order.
+constexpr int kJoinWaves = 16;
+template <int WDT>
+__global__ void __launch_bounds__(64 * kJoinWaves) norm_backward_join_kernel(NormBackwardParams p, int parts) {
+    using W = storage_t<WDT>;
+    __shared__ float s[kJoinWaves][64];
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
+    const int64_t i = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)p.cols;
+    float sum = 0.f;
+    if (i < n) {
+#pragma unroll 8
+        for (int k = wave; k < parts; k += kJoinWaves) sum += p.part[(int64_t)k * n + i];
+    }
+    s[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || i >= n) return;
+#pragma unroll
+    for (int k = 1; k < kJoinWaves; ++k) sum += s[k][lane];
+    W* out = (W*)(i < p.cols ? p.dw : p.db);
+    if (out) out[i < p.cols ? i : i - p.cols] = (W)sum;
+}
+
+template <int WDT>
+hipError_t norm_backward_join(const NormBackwardParams& p, int parts, hipStream_t stream) {
+    norm_backward_join_kernel<WDT>
+        <<<dim3((unsigned)((2 * (int64_t)p.cols + 63) / 64)), 64 * kJoinWaves, 0, stream>>>(p, parts);
+    return hipGetLastError();
+}
+
+template <int DT, int WDT, int TPR, int E>
+hipError_t norm_backward_rows(const NormBackwardParams& p, hipStream_t stream) {
+    constexpr int ROWS = block_of(TPR) / TPR;
+    const int64_t groups = (p.rows + ROWS - 1) / ROWS;
+    const int parts = (int)(groups < kNormMaxParts ? groups : (int64_t)kNormMaxParts);
+    if (parts > 0)
+        norm_backward_rows_kernel<DT, WDT, TPR, E><<<dim3((unsigned)parts), block_of(TPR), 0, stream>>>(p);
+    return p.dw || p.db ? norm_backward_join<WDT>(p, parts, stream) : hipGetLastError();
+}
+
+// ------------------------------------------- rows of more than 16,384 columns --
+
+// Sums over a work-group of kThreads.
 template <int K>
 __device__ __forceinline__ void block_sum(float (&v)[K], float* s) {
-    constexpr int W = kThreads / 64;
-    const int wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = wave_sum_f32(v[k]);
-    if ((threadIdx.x & 63) == 0) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) s[k * W + wave] = v[k];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        v[k] = s[k * W];
-#pragma unroll
-        for (int w = 1; w < W; ++w) v[k] += s[k * W + w];
-    }
+    row_sum<kThreads>(v, s);
     __syncthreads();
 }
 
 // A row per work-group, read once for the mean, once for the deviations and
 // once for the result.
 template <int DT, int WDT>
-__global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormForwardParams p) {
+__global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForwardParams p) {
     using T = storage_t<DT>;
     using W = storage_t<WDT>;
     constexpr int N = Vec16<T>::N;
@@ -86,7 +362,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_kernel(NormForwardParam
 
 // dx: a row per work-group, read for the two sums and again for the result.
 template <int DT, int WDT>
-__global__ void __launch_bounds__(kThreads) norm_backward_dx_kernel(NormBackwardParams p) {
+__global__ void __launch_bounds__(kThreads) norm_backward_dx_long_kernel(NormBackwardParams p) {
     using T = storage_t<DT>;
     using W = storage_t<WDT>;
     constexpr int N = Vec16<T>::N;
@@ -127,7 +403,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_dx_kernel(NormBackward
 // Partial column sums: work-group (strip, part) adds the rows of its part over
 // a strip of kThreads vectors of columns.
 template <int DT>
-__global__ void __launch_bounds__(kThreads) norm_backward_part_kernel(NormBackwardParams p, int parts) {
+__global__ void __launch_bounds__(kThreads) norm_backward_part_long_kernel(NormBackwardParams p, int parts) {
     using T = storage_t<DT>;
     constexpr int N = Vec16<T>::N;
     const int c = (blockIdx.x * kThreads + threadIdx.x) * N;
@@ -154,37 +430,33 @@ __global__ void __launch_bounds__(kThreads) norm_backward_part_kernel(NormBackwa
         }
 }
 
-// dw and db: column sums of the partial sums, in the order of the parts.
-template <int WDT>
-__global__ void __launch_bounds__(kThreads) norm_backward_join_kernel(NormBackwardParams p, int parts) {
-    using W = storage_t<WDT>;
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    if (i >= 2 * (int64_t)p.cols) return;
-    float sum = 0.f;
-    for (int k = 0; k < parts; ++k) sum += p.part[(int64_t)k * 2 * p.cols + i];
-    W* out = (W*)(i < p.cols ? p.dw : p.db);
-    if (out) out[i < p.cols ? i : i - p.cols] = (W)sum;
+template <int DT, int WDT>
+hipError_t norm_forward_rows_long(const NormForwardParams& p, hipStream_t stream) {
+    norm_forward_long_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+template <int DT, int WDT>
+hipError_t norm_backward_rows_long(const NormBackwardParams& p, hipStream_t stream) {
+    if (p.dx.p && p.rows > 0)
+        norm_backward_dx_long_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
+    if (!p.dw && !p.db) return hipGetLastError();
+    const int parts = (int)(p.rows < kNormMaxParts ? p.rows : (int64_t)kNormMaxParts);
+    constexpr int strip = kThreads * Vec16<storage_t<DT>>::N;
+    if (parts > 0)
+        norm_backward_part_long_kernel<DT>
+            <<<dim3((unsigned)((p.cols + (int64_t)strip - 1) / strip), (unsigned)parts), kThreads, 0, stream>>>(p, parts);
+    return norm_backward_join<WDT>(p, parts, stream);
 }
 
 template <int DT, int WDT>
 hipError_t norm_forward(const NormForwardParams& p, hipStream_t stream) {
-    norm_forward_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
-    return hipGetLastError();
+    return KB_NORM_DISPATCH(p.cols, norm_forward_rows)(p, stream);
 }
 
 template <int DT, int WDT>
 hipError_t norm_backward(const NormBackwardParams& p, hipStream_t stream) {
-    if (p.dx.p && p.rows > 0) norm_backward_dx_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
-    if (p.dw || p.db) {
-        const int parts = (int)(p.rows < kNormMaxParts ? p.rows : (int64_t)kNormMaxParts);
-        constexpr int strip = kThreads * Vec16<storage_t<DT>>::N;
-        if (parts > 0)
-            norm_backward_part_kernel<DT>
-                <<<dim3((unsigned)((p.cols + (int64_t)strip - 1) / strip), (unsigned)parts), kThreads, 0, stream>>>(p, parts);
-        norm_backward_join_kernel<WDT>
-            <<<dim3((unsigned)((2 * (int64_t)p.cols + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(p, parts);
-    }
-    return hipGetLastError();
+    return KB_NORM_DISPATCH(p.cols, norm_backward_rows)(p, stream);
 }
 
 }  // namespace

@@ -63,13 +63,11 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p) {
             const T* x = (const T*)a.p + b * a.sb + h * a.sh + i * a.sl;
             const T* y = (const T*)p.o.p + b * p.o.sb + h * p.o.sh + i * p.o.sl;
             for (int d = sub * N; d < p.dim; d += 16 * N) {
-                float u[N], w[N];
-                load_vec(x + d, p.dim - d, u);
-                if (!of_v) load_vec(y + d, p.dim - d, w);
+                const auto u = load_vec(x, d, p.dim), w = load_vec(of_v ? x : y, d, p.dim);
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (!of_v) dot = fmaf(u[e], w[e], dot);
-                    sq = fmaf(u[e], u[e], sq);
+                    dot = fmaf((float)u[e], (float)w[e], dot);
+                    sq = fmaf((float)u[e], (float)u[e], sq);
                 }
             }
         }

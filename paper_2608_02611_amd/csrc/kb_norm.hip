@@ -64,12 +64,15 @@ struct RowRegs {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int c = (i * TPR + t) * N;
-            if (c + N <= cols) {
-                v[i] = *(const typename Vec16<T>::type*)(row + c);
-            } else {
+            if (c < cols) v[i] = fetch_vec(row, c, cols);
+            else v[i] = typename Vec16<T>::type{};
+        }
+    }
+    __device__ __forceinline__ void settle(int t, int cols) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) v[i][e] = c + e < cols ? row[c + e] : (T)0.f;
-            }
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + t) * N;
+            if (c < cols) v[i] = settle_vec<T>(v[i], c, cols);
         }
     }
     __device__ __forceinline__ float at(int e) const { return (float)v[e / N][e % N]; }
@@ -119,7 +122,8 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_forward_rows_kernel(NormFo
     R next;
     next.load((const T*)p.x.p + min(row, last) * p.x.stride, t, p.cols);
     for (int64_t base = (int64_t)blockIdx.x * ROWS; base < p.rows; base += step, row += step) {
-        const R x = next;
+        R x = next;
+        x.settle(t, p.cols);
         if (base + step < p.rows) next.load((const T*)p.x.p + min(row + step, last) * p.x.stride, t, p.cols);
         float sum[1] = {0.f};
 #pragma unroll
@@ -189,7 +193,9 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
     float next_mean = p.mean[min(row, last)], next_rstd = p.rstd[min(row, last)];
     int turn = 0;
     for (int64_t base = (int64_t)blockIdx.x * ROWS; base < p.rows; base += step, row += step, turn ^= 1) {
-        const R dy = next_dy, x = next_x;
+        R dy = next_dy, x = next_x;
+        dy.settle(t, p.cols);
+        x.settle(t, p.cols);
         const float mean = next_mean, rstd = next_rstd;
         if (base + step < p.rows) {
             const int64_t r = min(row + step, last);
@@ -305,6 +311,12 @@ hipError_t norm_backward_rows(const NormBackwardParams& p, hipStream_t stream) {
 
 // ------------------------------------------- rows of more than 16,384 columns --
 
+template <typename V, int N>
+__device__ __forceinline__ void widen(V v, float (&out)[N]) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) out[e] = (float)v[e];
+}
+
 // Sums over a work-group of kThreads.
 template <int K>
 __device__ __forceinline__ void block_sum(float (&v)[K], float* s) {
@@ -326,7 +338,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
     const float inv = 1.f / (float)p.cols;
     float acc[1] = {0.f}, v[N];
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
-        load_vec(x + c, p.cols - c, v);
+        widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[0] += v[e];
     }
@@ -334,7 +346,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
     const float mean = acc[0] * inv;
     acc[0] = 0.f;
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
-        load_vec(x + c, p.cols - c, v);
+        widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float d = c + e < p.cols ? v[e] - mean : 0.f;
@@ -348,7 +360,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
         if (p.rstd) p.rstd[row] = rstd;
     }
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
-        load_vec(x + c, p.cols - c, v);
+        widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const int col = min(c + e, p.cols - 1);
@@ -374,8 +386,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_dx_long_kernel(NormBac
     const float mean = p.mean[row], rstd = p.rstd[row], inv = 1.f / (float)p.cols;
     float acc[2] = {0.f, 0.f}, a[N], v[N];
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
-        load_vec(dy + c, p.cols - c, a);
-        load_vec(x + c, p.cols - c, v);
+        widen(load_vec(dy, c, p.cols), a);
+        widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const bool in = c + e < p.cols;
@@ -388,8 +400,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_dx_long_kernel(NormBac
     block_sum(acc, s);
     const float mg = acc[0] * inv, mgz = acc[1] * inv;
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
-        load_vec(dy + c, p.cols - c, a);
-        load_vec(x + c, p.cols - c, v);
+        widen(load_vec(dy, c, p.cols), a);
+        widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float g = a[e] * (p.w ? (float)((const W*)p.w)[min(c + e, p.cols - 1)] : 1.f);
@@ -412,8 +424,8 @@ __global__ void __launch_bounds__(kThreads) norm_backward_part_long_kernel(NormB
 #pragma unroll
     for (int e = 0; e < N; ++e) dw[e] = db[e] = 0.f;
     for (int64_t row = blockIdx.y; row < p.rows; row += parts) {
-        load_vec((const T*)p.dy.p + row * p.dy.stride + c, p.cols - c, a);
-        load_vec((const T*)p.x.p + row * p.x.stride + c, p.cols - c, v);
+        widen(load_vec((const T*)p.dy.p + row * p.dy.stride, c, p.cols), a);
+        widen(load_vec((const T*)p.x.p + row * p.x.stride, c, p.cols), v);
         const float mean = p.mean[row], rstd = p.rstd[row];
 #pragma unroll
         for (int e = 0; e < N; ++e) {

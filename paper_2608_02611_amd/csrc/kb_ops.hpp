@@ -126,6 +126,8 @@ struct Storage<DT_BF16> {
 template <int DT>
 using storage_t = typename Storage<DT>::type;
 
+typedef uint32_t u32v4 __attribute__((ext_vector_type(4)));
+
 // 16 bytes of elements, readable at any element's alignment (gfx950 loads
 // and stores dwords at any byte address).
 template <typename T>
@@ -134,32 +136,79 @@ struct Vec16 {
     typedef T type __attribute__((ext_vector_type(16 / sizeof(T)), aligned(sizeof(T))));
 };
 
-// Elements [0, n) of p as floats, 0 past them (n >= N: all).
+// 16 bytes without the first `drop` elements, zeros after the others.
 template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, int n, float (&out)[Vec16<T>::N]) {
-    constexpr int N = Vec16<T>::N;
-    if (n >= N) {
-        const typename Vec16<T>::type v = *(const typename Vec16<T>::type*)p;
+__device__ __forceinline__ u32v4 drop_elements(u32v4 v, int drop) {
+    const int bits = drop * 8 * (int)sizeof(T);
+    if (bits & 64) v = u32v4{v[2], v[3], 0, 0};
+    if (bits & 32) v = u32v4{v[1], v[2], v[3], 0};
+    if (sizeof(T) == 2) {
+        const uint32_t s = bits & 16;
 #pragma unroll
-        for (int e = 0; e < N; ++e) out[e] = (float)v[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) out[e] = e < n ? (float)p[e] : 0.f;
+        for (int k = 0; k < 4; ++k) v[k] = __builtin_amdgcn_alignbit(k < 3 ? v[k + 1] : 0, v[k], s);
     }
+    return v;
 }
 
+// 16 bytes of a row of n elements from element c < n on, zeros past its end.
+// The last ones of a row that is no multiple are read with the elements before
+// them, in the same instruction as every other lane's, and then moved down
+// (settle_vec, apart from the load so that nothing waits for one that is wanted
+// later): loads of single elements at the end of each row took a third of a
+// whole backward pass at 4095 columns of 2 bytes.
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::type fetch_vec(const T* row, int c, int n) {
+    using V = typename Vec16<T>::type;
+    constexpr int N = Vec16<T>::N;
+    if (n >= N) return *(const V*)(row + min(c, n - N));
+    V v;
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = c + e < n ? row[c + e] : (T)0.f;
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::type settle_vec(typename Vec16<T>::type v, int c, int n) {
+    using V = typename Vec16<T>::type;
+    constexpr int N = Vec16<T>::N;
+    if (c + N > n && n >= N) v = __builtin_bit_cast(V, drop_elements<T>(__builtin_bit_cast(u32v4, v), c + N - n));
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ typename Vec16<T>::type load_vec(const T* row, int c, int n) {
+    return settle_vec<T>(fetch_vec(row, c, n), c, n);
+}
+
+// The first n (at most N) of N elements, in at most three pieces.
 template <typename T>
 __device__ __forceinline__ void store_vec(T* p, int n, const float (&in)[Vec16<T>::N]) {
+    using V = typename Vec16<T>::type;
     constexpr int N = Vec16<T>::N;
+    V v;
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = (T)in[e];
     if (n >= N) {
-        typename Vec16<T>::type v;
-#pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = (T)in[e];
-        *(typename Vec16<T>::type*)p = v;
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (e < n) p[e] = (T)in[e];
+        *(V*)p = v;
+        return;
+    }
+    u32v4 u = __builtin_bit_cast(u32v4, v);
+    typedef T half __attribute__((ext_vector_type(N / 2), aligned(sizeof(T))));
+    typedef uint32_t u32v2 __attribute__((ext_vector_type(2)));
+    if (n & (N / 2)) {
+        *(half*)p = __builtin_bit_cast(half, u32v2{u[0], u[1]});
+        u = u32v4{u[2], u[3], 0, 0};
+        p += N / 2;
+    }
+    if constexpr (N == 8) {
+        typedef T two __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+        if (n & 2) {
+            *(two*)p = __builtin_bit_cast(two, u[0]);
+            u[0] = u[1];
+            p += 2;
+        }
+    }
+    if (n & 1) {
+        typedef T any __attribute__((ext_vector_type(4 / sizeof(T))));
+        *p = __builtin_bit_cast(any, u[0])[0];
     }
 }
 

@@ -78,19 +78,34 @@ struct RowRegs {
     __device__ __forceinline__ float at(int e) const { return (float)v[e / N][e % N]; }
 };
 
+// Elements c .. c + N - 1 of a weight [n], `other` past its end or without one.
+template <int N, typename W>
+__device__ __forceinline__ void load_weight(const W* w, int c, int n, float other, float* out) {
+    constexpr int M = Vec16<W>::N;
+#pragma unroll
+    for (int k = 0; k < N; k += M) {
+        if (w != nullptr && c + k < n) {
+            const typename Vec16<W>::type v = load_vec(w, c + k, n);
+#pragma unroll
+            for (int e = 0; e < M; ++e) out[k + e] = (float)v[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < M; ++e) out[k + e] = other;
+        }
+    }
+}
+
 // Threads of a row and elements of a thread: the fewest threads that hold the
 // row at 16 elements each (8 up to 512 columns), so that a wave or less has a
 // row where that is possible and its sums need no meeting.  More elements a
 // thread leave too few waves on a CU to cover HBM's latency.
-#define KB_NORM_DISPATCH(COLS, CALL)              \
-    ((COLS) <= 128     ? CALL<DT, WDT, 16, 8>     \
-     : (COLS) <= 512   ? CALL<DT, WDT, 64, 8>     \
-     : (COLS) <= 1024  ? CALL<DT, WDT, 64, 16>    \
-     : (COLS) <= 2048  ? CALL<DT, WDT, 128, 16>   \
-     : (COLS) <= 4096  ? CALL<DT, WDT, 256, 16>   \
-     : (COLS) <= 8192  ? CALL<DT, WDT, 512, 16>   \
-     : (COLS) <= 16384 ? CALL<DT, WDT, 1024, 16>  \
-                       : CALL##_long<DT, WDT>)
+#define KB_NORM_DISPATCH(COLS, CALL, LONGER)      \
+    ((COLS) <= 128    ? CALL<DT, WDT, 16, 8>      \
+     : (COLS) <= 512  ? CALL<DT, WDT, 64, 8>      \
+     : (COLS) <= 1024 ? CALL<DT, WDT, 64, 16>     \
+     : (COLS) <= 2048 ? CALL<DT, WDT, 128, 16>    \
+     : (COLS) <= 4096 ? CALL<DT, WDT, 256, 16>    \
+     : LONGER)
 
 constexpr int block_of(int tpr) { return tpr > kThreads ? tpr : kThreads; }
 
@@ -114,17 +129,16 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_forward_rows_kernel(NormFo
     const auto column = [&](int e) { return (e / N * TPR + t) * N + e % N; };
     float wf[E], bf[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int c = min(column(e), p.cols - 1);
-        wf[e] = p.w ? (float)((const W*)p.w)[c] : 1.f;
-        bf[e] = p.b ? (float)((const W*)p.b)[c] : 0.f;
+    for (int i = 0; i < R::NV; ++i) {
+        load_weight<N>((const W*)p.w, (i * TPR + t) * N, p.cols, 1.f, wf + i * N);
+        load_weight<N>((const W*)p.b, (i * TPR + t) * N, p.cols, 0.f, bf + i * N);
     }
     R next;
     next.load((const T*)p.x.p + min(row, last) * p.x.stride, t, p.cols);
     for (int64_t base = (int64_t)blockIdx.x * ROWS; base < p.rows; base += step, row += step) {
         R x = next;
-        x.settle(t, p.cols);
         if (base + step < p.rows) next.load((const T*)p.x.p + min(row + step, last) * p.x.stride, t, p.cols);
+        x.settle(t, p.cols);
         float sum[1] = {0.f};
 #pragma unroll
         for (int e = 0; e < E; ++e) sum[0] += x.at(e);
@@ -168,7 +182,10 @@ hipError_t norm_forward_rows(const NormForwardParams& p, hipStream_t stream) {
 // the thread's columns add up over the rows that it sees.  At the end the row
 // groups of a work-group are added in LDS, in their order, and written as one
 // part.
-template <int DT, int WDT, int TPR, int E>
+// SUMS: with dw and db.  They take two registers a column, too many for rows of
+// more than 8192 (spilled, 4096 x 16,384 f32 took 290 us): there a pass of its
+// own over dy and x adds the columns.
+template <int DT, int WDT, int TPR, int E, bool SUMS>
 __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormBackwardParams p) {
     using T = storage_t<DT>;
     using W = storage_t<WDT>;
@@ -181,12 +198,11 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
     const int64_t last = p.rows - 1;
     const float inv = 1.f / (float)p.cols;
     const auto column = [&](int e) { return (e / N * TPR + t) * N + e % N; };
-    float wf[E], dw[E], db[E];
+    float wf[E], dw[SUMS ? E : 1], db[SUMS ? E : 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        wf[e] = p.w && column(e) < p.cols ? (float)((const W*)p.w)[column(e)] : 1.f;
-        dw[e] = db[e] = 0.f;
-    }
+    for (int i = 0; i < R::NV; ++i) load_weight<N>((const W*)p.w, (i * TPR + t) * N, p.cols, 1.f, wf + i * N);
+#pragma unroll
+    for (int e = 0; e < (SUMS ? E : 1); ++e) dw[e] = db[e] = 0.f;
     R next_dy, next_x;
     next_dy.load((const T*)p.dy.p + min(row, last) * p.dy.stride, t, p.cols);
     next_x.load((const T*)p.x.p + min(row, last) * p.x.stride, t, p.cols);
@@ -194,8 +210,6 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
     int turn = 0;
     for (int64_t base = (int64_t)blockIdx.x * ROWS; base < p.rows; base += step, row += step, turn ^= 1) {
         R dy = next_dy, x = next_x;
-        dy.settle(t, p.cols);
-        x.settle(t, p.cols);
         const float mean = next_mean, rstd = next_rstd;
         if (base + step < p.rows) {
             const int64_t r = min(row + step, last);
@@ -204,6 +218,8 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
             next_mean = p.mean[r];
             next_rstd = p.rstd[r];
         }
+        dy.settle(t, p.cols);
+        x.settle(t, p.cols);
         const bool live = row <= last;
         float sum[2] = {0.f, 0.f};
 #pragma unroll
@@ -213,9 +229,9 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
             const float z = column(e) < p.cols ? (x.at(e) - mean) * rstd : 0.f;
             sum[0] += g;
             sum[1] = fmaf(g, z, sum[1]);
-            if (live) {
-                dw[e] = fmaf(d, z, dw[e]);
-                db[e] += d;
+            if (SUMS && live) {
+                dw[SUMS ? e : 0] = fmaf(d, z, dw[SUMS ? e : 0]);
+                db[SUMS ? e : 0] += d;
             }
         }
         if (!p.dx.p) continue;
@@ -227,45 +243,48 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
         for (int i = 0; i < R::NV; ++i) {
             float out[N];
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const float z = (x.at(i * N + e) - mean) * rstd;
-                out[e] = rstd * (fmaf(dy.at(i * N + e), wf[i * N + e], -mg) - z * mgz);
+            for (int k = 0; k < N; ++k) {
+                const int e = i * N + k;
+                const float z = (x.at(e) - mean) * rstd;
+                out[k] = rstd * (fmaf(dy.at(e), wf[e], -mg) - z * mgz);
             }
             const int c = (i * TPR + t) * N;
             if (c < p.cols) store_vec(dx + c, p.cols - c, out);
         }
     }
-    if (!p.dw && !p.db) return;
-    float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
-    if constexpr (ROWS > 1) {
-        __shared__ float sums[2][TPR * E];
+    if constexpr (SUMS) {
+        if (!p.dw && !p.db) return;
+        float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
+        if constexpr (ROWS > 1) {
+            __shared__ float sums[2][TPR * E];
 #pragma unroll 1
-        for (int k = 0; k < ROWS; ++k) {
-            if (group == k) {
+            for (int k = 0; k < ROWS; ++k) {
+                if (group == k) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    sums[0][e * TPR + t] = k ? sums[0][e * TPR + t] + dw[e] : dw[e];
-                    sums[1][e * TPR + t] = k ? sums[1][e * TPR + t] + db[e] : db[e];
+                    for (int e = 0; e < E; ++e) {
+                        sums[0][e * TPR + t] = k ? sums[0][e * TPR + t] + dw[e] : dw[e];
+                        sums[1][e * TPR + t] = k ? sums[1][e * TPR + t] + db[e] : db[e];
+                    }
                 }
+                __syncthreads();
             }
-            __syncthreads();
-        }
-        if (group > 0) return;
+            if (group > 0) return;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            dw[e] = sums[0][e * TPR + t];
-            db[e] = sums[1][e * TPR + t];
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < R::NV; ++i) {
-        const int c = (i * TPR + t) * N;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (c + e < p.cols) {
-                part[c + e] = dw[i * N + e];
-                part[p.cols + c + e] = db[i * N + e];
+            for (int e = 0; e < E; ++e) {
+                dw[e] = sums[0][e * TPR + t];
+                db[e] = sums[1][e * TPR + t];
             }
+        }
+#pragma unroll
+        for (int i = 0; i < R::NV; ++i) {
+            const int c = (i * TPR + t) * N;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (c + e < p.cols) {
+                    part[c + e] = dw[i * N + e];
+                    part[p.cols + c + e] = db[i * N + e];
+                }
+        }
     }
 }
 
@@ -303,13 +322,13 @@ template <int DT, int WDT, int TPR, int E>
 hipError_t norm_backward_rows(const NormBackwardParams& p, hipStream_t stream) {
     constexpr int ROWS = block_of(TPR) / TPR;
     const int64_t groups = (p.rows + ROWS - 1) / ROWS;
-    const int parts = (int)(groups < kNormMaxParts ? groups : (int64_t)kNormMaxParts);
+    const int parts = norm_parts(groups, (int64_t)p.cols * (int64_t)sizeof(storage_t<DT>));
     if (parts > 0)
-        norm_backward_rows_kernel<DT, WDT, TPR, E><<<dim3((unsigned)parts), block_of(TPR), 0, stream>>>(p);
+        norm_backward_rows_kernel<DT, WDT, TPR, E, true><<<dim3((unsigned)parts), block_of(TPR), 0, stream>>>(p);
     return p.dw || p.db ? norm_backward_join<WDT>(p, parts, stream) : hipGetLastError();
 }
 
-// ------------------------------------------- rows of more than 16,384 columns --
+// ------------------------------------- rows that do not fit in the registers --
 
 template <typename V, int N>
 __device__ __forceinline__ void widen(V v, float (&out)[N]) {
@@ -361,13 +380,11 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
     }
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
         widen(load_vec(x, c, p.cols), v);
+        float w[N], b[N];
+        load_weight<N>((const W*)p.w, c, p.cols, 1.f, w);
+        load_weight<N>((const W*)p.b, c, p.cols, 0.f, b);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const int col = min(c + e, p.cols - 1);
-            const float w = p.w ? (float)((const W*)p.w)[col] : 1.f;
-            const float b = p.b ? (float)((const W*)p.b)[col] : 0.f;
-            v[e] = fmaf((v[e] - mean) * rstd, w, b);
-        }
+        for (int e = 0; e < N; ++e) v[e] = fmaf((v[e] - mean) * rstd, w[e], b[e]);
         store_vec(y + c, p.cols - c, v);
     }
 }
@@ -388,11 +405,11 @@ __global__ void __launch_bounds__(kThreads) norm_backward_dx_long_kernel(NormBac
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
         widen(load_vec(dy, c, p.cols), a);
         widen(load_vec(x, c, p.cols), v);
+        float w[N];
+        load_weight<N>((const W*)p.w, c, p.cols, 1.f, w);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const bool in = c + e < p.cols;
-            const float g = in ? a[e] * (p.w ? (float)((const W*)p.w)[c + e] : 1.f) : 0.f;
-            const float z = in ? (v[e] - mean) * rstd : 0.f;
+            const float g = a[e] * w[e], z = c + e < p.cols ? (v[e] - mean) * rstd : 0.f;
             acc[0] += g;
             acc[1] = fmaf(g, z, acc[1]);
         }
@@ -402,10 +419,11 @@ __global__ void __launch_bounds__(kThreads) norm_backward_dx_long_kernel(NormBac
     for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
         widen(load_vec(dy, c, p.cols), a);
         widen(load_vec(x, c, p.cols), v);
+        float w[N];
+        load_weight<N>((const W*)p.w, c, p.cols, 1.f, w);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float g = a[e] * (p.w ? (float)((const W*)p.w)[min(c + e, p.cols - 1)] : 1.f);
-            const float z = (v[e] - mean) * rstd;
+            const float g = a[e] * w[e], z = (v[e] - mean) * rstd;
             v[e] = rstd * (g - mg - z * mgz);
         }
         store_vec(dx + c, p.cols - c, v);
@@ -423,6 +441,7 @@ __global__ void __launch_bounds__(kThreads) norm_backward_part_long_kernel(NormB
     float dw[N], db[N], a[N], v[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) dw[e] = db[e] = 0.f;
+#pragma unroll 4
     for (int64_t row = blockIdx.y; row < p.rows; row += parts) {
         widen(load_vec((const T*)p.dy.p + row * p.dy.stride, c, p.cols), a);
         widen(load_vec((const T*)p.x.p + row * p.x.stride, c, p.cols), v);
@@ -450,10 +469,15 @@ hipError_t norm_forward_rows_long(const NormForwardParams& p, hipStream_t stream
 
 template <int DT, int WDT>
 hipError_t norm_backward_rows_long(const NormBackwardParams& p, hipStream_t stream) {
-    if (p.dx.p && p.rows > 0)
-        norm_backward_dx_long_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
+    if (p.dx.p && p.rows > 0) {
+        if (p.cols <= 16384)
+            norm_backward_rows_kernel<DT, WDT, 1024, 16, false>
+                <<<dim3((unsigned)(p.rows < kForwardGroups ? p.rows : kForwardGroups)), 1024, 0, stream>>>(p);
+        else
+            norm_backward_dx_long_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
+    }
     if (!p.dw && !p.db) return hipGetLastError();
-    const int parts = (int)(p.rows < kNormMaxParts ? p.rows : (int64_t)kNormMaxParts);
+    const int parts = norm_parts(p.rows, INT64_MAX);
     constexpr int strip = kThreads * Vec16<storage_t<DT>>::N;
     if (parts > 0)
         norm_backward_part_long_kernel<DT>
@@ -463,12 +487,12 @@ hipError_t norm_backward_rows_long(const NormBackwardParams& p, hipStream_t stre
 
 template <int DT, int WDT>
 hipError_t norm_forward(const NormForwardParams& p, hipStream_t stream) {
-    return KB_NORM_DISPATCH(p.cols, norm_forward_rows)(p, stream);
+    return KB_NORM_DISPATCH(p.cols, norm_forward_rows, (p.cols <= 8192 ? norm_forward_rows<DT, WDT, 512, 16> : p.cols <= 16384 ? norm_forward_rows<DT, WDT, 1024, 16> : norm_forward_rows_long<DT, WDT>))(p, stream);
 }
 
 template <int DT, int WDT>
 hipError_t norm_backward(const NormBackwardParams& p, hipStream_t stream) {
-    return KB_NORM_DISPATCH(p.cols, norm_backward_rows)(p, stream);
+    return KB_NORM_DISPATCH(p.cols, norm_backward_rows, (p.cols <= 6144 ? norm_backward_rows<DT, WDT, 256, 24> : p.cols <= 8192 ? norm_backward_rows<DT, WDT, 512, 16> : norm_backward_rows_long<DT, WDT>))(p, stream);
 }
 
 }  // namespace

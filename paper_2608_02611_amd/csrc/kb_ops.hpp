@@ -41,10 +41,17 @@ struct NormBackwardParams {
     int cols;
 };
 
-// Row stripes whose column sums are kept apart (NormBackwardParams::part).
-constexpr int kNormMaxParts = 512;
+// Row stripes whose column sums are kept apart (NormBackwardParams::part): one
+// for each work-group.  Rows of 512 bytes to 2 KB get twice as many, as a
+// work-group has few bytes on their way (65,536 x 256 f32: 40 us, 73 with 512;
+// 16,384 x 1024 f32, longer rows: 49 us, 41 with 512).
+inline int norm_parts(int64_t rows, int64_t row_bytes) {
+    const int64_t most = row_bytes > 512 && row_bytes < 2048 ? 1024 : 512;
+    return (int)(rows < most ? rows : most);
+}
+// Enough for every type.
 inline size_t norm_part_bytes(int64_t rows, int64_t cols) {
-    const int64_t parts = rows < kNormMaxParts ? rows : (int64_t)kNormMaxParts;
+    const int64_t most = cols < 1024 ? 1024 : 512, parts = rows < most ? rows : most;
     return ((size_t)parts * 2 * (size_t)cols * sizeof(float) + 15) & ~(size_t)15;
 }
 

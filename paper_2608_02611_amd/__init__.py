@@ -774,31 +774,31 @@ def kb_gen_scatter(dst, ref, idx, mode, stream=None):
 
 _VIEW = struct.Struct("Pii16q")
 _OPTS = struct.Struct("fIPP")
-_ZEROS = tuple((0,) * n for n in range(KB_MAX_DIMS + 1))
 assert _VIEW.size == ctypes.sizeof(KbTensor) and _OPTS.size == 24
+# kb_tensor of n dimensions: the unused sizes and strides are pad bytes (zeros)
+_PACK = [struct.Struct("Pii%dq%dx%dq%dx" % (n, 8 * (KB_MAX_DIMS - n), n, 8 * (KB_MAX_DIMS - n))).pack
+         for n in range(KB_MAX_DIMS + 1)]
 
 
 def pack_view(t):
     """The kb_tensor descriptor of a device tensor as bytes (None: a NULL
-    pointer).  The same bytes as describe()'s, without a ctypes object: 1 us
+    pointer).  The same bytes as describe()'s, without a ctypes object: 0.8 us
     of host time instead of 3, for calls of up to nine tensors."""
     if t is None:
         return None
-    if not t.is_cuda:
-        raise ValueError("a tensor of the device is needed")
     shape = t.shape
     n = len(shape)
-    if n > KB_MAX_DIMS:
-        raise ValueError("more than %d dimensions" % KB_MAX_DIMS)
-    pad = _ZEROS[KB_MAX_DIMS - n]
-    return _VIEW.pack(t.data_ptr(), dtype_code(t), n, *shape, *pad, *t.stride(), *pad)
+    if n > KB_MAX_DIMS or not t.is_cuda:
+        raise ValueError("a device tensor of at most %d dimensions is needed" % KB_MAX_DIMS)
+    code = _dtype_codes.get(t.dtype)
+    return _PACK[n](t.data_ptr(), dtype_code(t) if code is None else code, n, *shape, *t.stride())
 
 
 def _floats(t, shape, name):
     """Address of a dense float32 device tensor of a shape (None: NULL)."""
     if t is None:
         return None
-    if t.dtype != _torch().float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or not t.is_cuda:
+    if t.shape != shape or _dtype_codes.get(t.dtype) != KB_F32 or not t.is_contiguous() or not t.is_cuda:
         raise ValueError("%s must be a contiguous float32 device tensor of shape %s" % (name, tuple(shape)))
     return t.data_ptr()
 
@@ -808,11 +808,10 @@ def _on(stream):
     return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
 
 
-def _scratch(workspace, nbytes, device):
-    """The caller's workspace, or a new one of nbytes (None for 0)."""
-    if workspace is None and nbytes:
-        workspace = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
-    return workspace
+def _scratch(nbytes, device):
+    """A workspace of nbytes (None for 0)."""
+    torch = _torch()
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 def _extent(t):
@@ -833,17 +832,19 @@ def kb_norm_forward(x, w, b, eps=1e-5, y=None, mean=None, rstd=None, stream=None
     """Layer norm over the last axis of x; w and b may be None.  Returns
     (y, mean, rstd), made here where not given; mean and rstd are float32 of
     x's other axes."""
-    torch = _torch()
-    with _on(stream):
-        if y is None:
-            y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if mean is None:
-            mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        if rstd is None:
-            rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _check(lib().kb_norm_forward(pack_view(_rows(x)), pack_view(w), pack_view(b), float(eps), pack_view(_rows(y)),
-                                 _floats(mean, x.shape[:-1], "mean"), _floats(rstd, x.shape[:-1], "rstd"),
-                                 _stream_handle(stream)))
+    outer = x.shape[:-1]
+    if y is None or mean is None or rstd is None:
+        torch = _torch()
+        with _on(stream):
+            if y is None:
+                y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            if mean is None:
+                mean = torch.empty(outer, dtype=torch.float32, device=x.device)
+            if rstd is None:
+                rstd = torch.empty(outer, dtype=torch.float32, device=x.device)
+    px = pack_view(_rows(x))  # (also makes _floats' dtype codes)
+    _check(lib().kb_norm_forward(px, pack_view(w), pack_view(b), eps, pack_view(_rows(y)), _floats(mean, outer, "mean"),
+                                 _floats(rstd, outer, "rstd"), _stream_handle(stream)))
     return y, mean, rstd
 
 
@@ -854,23 +855,25 @@ def kb_norm_backward_workspace_bytes(rows, cols):
 def kb_norm_backward(dy, x, w, mean, rstd, dx=None, dw=None, db=None, workspace=None, stream=None):
     """Gradients of kb_norm_forward: (dx, dw, db), made here where not given;
     dw and db of w's dtype (x's without a weight)."""
-    torch = _torch()
-    cols = x.shape[-1]
+    outer, cols = x.shape[:-1], x.shape[-1]
     L = lib()
-    with _on(stream):
-        if dx is None:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        if dw is None:
-            dw = torch.empty(cols, dtype=x.dtype if w is None else w.dtype, device=x.device)
-        if db is None:
-            db = torch.empty(cols, dtype=dw.dtype, device=x.device)
-        if workspace is None:
-            rows = x.numel() // cols if cols else 0
-            workspace = _scratch(None, L.kb_norm_backward_workspace_bytes(rows, cols), x.device)
+    if dx is None or dw is None or db is None or workspace is None:
+        torch = _torch()
+        with _on(stream):
+            if dx is None:
+                dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            if dw is None:
+                dw = torch.empty(cols, dtype=x.dtype if w is None else w.dtype, device=x.device)
+            if db is None:
+                db = torch.empty(cols, dtype=dw.dtype, device=x.device)
+            if workspace is None:
+                rows = x.numel() // cols if cols else 0
+                workspace = _scratch(L.kb_norm_backward_workspace_bytes(rows, cols), x.device)
     ws, nbytes = _extent(workspace)
-    _check(L.kb_norm_backward(pack_view(_rows(dy)), pack_view(_rows(x)), pack_view(w),
-                              _floats(mean, x.shape[:-1], "mean"), _floats(rstd, x.shape[:-1], "rstd"),
-                              pack_view(_rows(dx)), pack_view(dw), pack_view(db), ws, nbytes, _stream_handle(stream)))
+    px = pack_view(_rows(x))  # (also makes _floats' dtype codes)
+    _check(L.kb_norm_backward(pack_view(_rows(dy)), px, pack_view(w), _floats(mean, outer, "mean"),
+                              _floats(rstd, outer, "rstd"), pack_view(_rows(dx)), pack_view(dw), pack_view(db), ws,
+                              nbytes, _stream_handle(stream)))
     return dx, dw, db
 
 
@@ -901,17 +904,20 @@ def kb_attn_forward(q, k, v, scale=None, causal=False, q_lens=None, k_lens=None,
     [batch][kv_heads][len_k][dim], views of any strides with a contiguous last
     dimension; scale: dim^-1/2 if None; q_lens, k_lens: int32 [batch] device
     tensors of lengths.  Returns (o, lse), made here where not given."""
-    torch = _torch()
     L = lib()
     opts = _attn_opts(q, scale, causal, q_lens, k_lens)
     pq, pk = pack_view(q), pack_view(k)
-    with _on(stream):
-        if o is None:
-            o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if lse is None:
-            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
-        if workspace is None:
-            workspace = _scratch(None, L.kb_attn_forward_workspace_bytes(pq, pk), q.device)
+    if workspace is None:
+        nbytes = L.kb_attn_forward_workspace_bytes(pq, pk)
+    if o is None or lse is None or (workspace is None and nbytes):
+        torch = _torch()
+        with _on(stream):
+            if o is None:
+                o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if lse is None:
+                lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+            if workspace is None:
+                workspace = _scratch(nbytes, q.device)
     ws, nbytes = _extent(workspace)
     _check(L.kb_attn_forward(pq, pk, pack_view(v), opts, pack_view(o), _floats(lse, q.shape[:-1], "lse"), ws, nbytes,
                              _stream_handle(stream)))
@@ -938,7 +944,7 @@ def kb_attn_backward(dout, q, k, v, o, lse, scale=None, causal=False, q_lens=Non
         if dv is None:
             dv = torch.empty(k.shape, dtype=k.dtype, device=k.device)
         if workspace is None:
-            workspace = _scratch(None, L.kb_attn_backward_workspace_bytes(pq, pk), q.device)
+            workspace = _scratch(L.kb_attn_backward_workspace_bytes(pq, pk), q.device)
     ws, nbytes = _extent(workspace)
     _check(L.kb_attn_backward(pack_view(dout), pq, pk, pack_view(v), pack_view(o), _floats(lse, q.shape[:-1], "lse"),
                               opts, pack_view(dq), pack_view(dk), pack_view(dv), ws, nbytes, _stream_handle(stream)))

@@ -352,6 +352,17 @@ __device__ __forceinline__ void store_column(storage_t<DT>* row, const f32x16 (&
                            live ? acc[db][r + 3] * f : 0.f);
 }
 
+// The same as one part of a row's sums: binary32, at multiples of 4.
+template <int DP>
+__device__ __forceinline__ void store_part(float* row, const f32x16 (&acc)[DP / 32], int dim, int g) {
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4)
+            if (32 * db + 2 * r + 4 * g < dim)
+                *(f32x4*)(row + 32 * db + 2 * r + 4 * g) = f32x4{acc[db][r], acc[db][r + 1], acc[db][r + 2], acc[db][r + 3]};
+}
+
 // Lengths of sequence b.
 __device__ __forceinline__ int seq_len(const int32_t* lens, int b, int full) {
     return lens ? min(max(lens[b], 0), full) : full;

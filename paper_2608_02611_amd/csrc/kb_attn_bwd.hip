@@ -21,20 +21,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kProbLog2 = 10.f;
 
-// Workspace: D, then lse in units of log 2, then the blocks' largest squared
-// norms of dout and of v, then a mark for each work-group that has keys.
-__host__ __device__ __forceinline__ int64_t lse_at(const AttnParams& p) {
-    return (int64_t)p.batch * p.heads * p.len_q;
-}
-__host__ __device__ __forceinline__ int64_t dout_norms_at(const AttnParams& p) { return 2 * lse_at(p); }
-__host__ __device__ __forceinline__ int64_t v_norms_at(const AttnParams& p) {
-    return dout_norms_at(p) + (int64_t)p.batch * p.heads * ((p.len_q + kNormBlock - 1) / kNormBlock);
-}
-
-__host__ __device__ __forceinline__ int64_t marks_at(const AttnParams& p) {
-    return v_norms_at(p) + (int64_t)p.batch * p.kv_heads * ((p.len_k + kNormBlock - 1) / kNormBlock);
-}
-
 // Before the products: D_i and lse_i / log 2 for 64 query rows a work-group, 16
 // lanes a row.  A row with no seen score has lse = -infinity, and its terms
 // exp(-infinity - lse) are to be 0: it gets 0.  A row of the padding gets
@@ -42,7 +28,7 @@ __host__ __device__ __forceinline__ int64_t marks_at(const AttnParams& p) {
 // also the largest finite squared norm of the block's rows of dout, and, in
 // the work-groups after those, of 64 rows of v.
 template <int DT>
-__global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p) {
+__global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p, BackwardLayout l) {
     using T = storage_t<DT>;
     constexpr int N = Vec16<T>::N;
     __shared__ float largest[kThreads / 16];
@@ -80,7 +66,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p) {
             const int64_t row = ((int64_t)b * p.heads + h) * p.len_q + i;
             const float lse = p.lse[row];
             p.ws[row] = dot;
-            p.ws[lse_at(p) + row] = i >= n ? INFINITY : lse == -INFINITY ? 0.f : lse * kLog2e;
+            p.ws[l.lse + row] = i >= n ? INFINITY : lse == -INFINITY ? 0.f : lse * kLog2e;
         }
         if (sq < INFINITY) top = fmaxf(top, sq);
     }
@@ -89,7 +75,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p) {
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int k = 1; k < kThreads / 16; ++k) top = fmaxf(top, largest[k]);
-        p.ws[(of_v ? v_norms_at(p) : dout_norms_at(p)) + id] = top;
+        p.ws[(of_v ? l.v_norms : l.dout_norms) + id] = top;
     }
 }
 
@@ -104,11 +90,11 @@ __device__ __forceinline__ int bound_exponent(float sq) {
 // sequence b; 1 for the other types.  (The exponent stays within binary32: |x|
 // of an F16 row of 128 is under 2^20 and its smallest is 2^-24.)  Called by every thread of a work-group.
 template <int DT>
-__device__ __forceinline__ float score_scale(const AttnParams& p, int b, int h, float* shared) {
+__device__ __forceinline__ float score_scale(const AttnParams& p, const BackwardLayout& l, int b, int h, float* shared) {
     if (DT != DT_F16) return 1.f;
     const int q_blocks = (p.len_q + kNormBlock - 1) / kNormBlock, k_blocks = (p.len_k + kNormBlock - 1) / kNormBlock;
-    const float* dn = p.ws + dout_norms_at(p) + ((int64_t)b * p.heads + h * p.group) * q_blocks;
-    const float* vn = p.ws + v_norms_at(p) + ((int64_t)b * p.kv_heads + h) * k_blocks;
+    const float* dn = p.ws + l.dout_norms + ((int64_t)b * p.heads + h * p.group) * q_blocks;
+    const float* vn = p.ws + l.v_norms + ((int64_t)b * p.kv_heads + h) * k_blocks;
     float d = 0.f, v = 0.f;
     for (int64_t k = threadIdx.x; k < (int64_t)q_blocks * p.group; k += kThreads) d = fmaxf(d, dn[k]);
     for (int k = threadIdx.x; k < k_blocks; k += kThreads) v = fmaxf(v, vn[k]);
@@ -127,7 +113,7 @@ __device__ __forceinline__ float score_scale(const AttnParams& p, int b, int h, 
 // rows in LDS, which leaves registers for two waves a SIMD) while the query
 // rows of every head of the group pass in tiles of 32.
 constexpr int kKeyRows = kAttnKeyRows;
-constexpr int kQueries = 32;
+constexpr int kQueries = kAttnQueries;
 
 // One tile of queries for a wave's 32 keys: s and t with a key a column.  PART:
 // the lane's key is seen by the tile's queries from lo on.
@@ -172,8 +158,9 @@ __device__ __forceinline__ void tile_keys(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP
 // CAREFUL: a launch of its own, for the work-groups that the first one marked (in
 // the same kernel it would cost the first pass the registers that it needs).
 template <int DT, int DP, bool WHOLE, bool CAREFUL>
-__global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) attn_backward_keys_kernel(AttnParams p) {
-    uint32_t* mark = (uint32_t*)(p.ws + marks_at(p)) + blockIdx.x;
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) attn_backward_keys_kernel(AttnParams p, BackwardLayout l) {
+    const int part = (int)blockIdx.y;
+    uint32_t* mark = (uint32_t*)(p.ws + l.marks) + (int64_t)part * gridDim.x + blockIdx.x;
     if (CAREFUL && *mark == 0) return;
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
@@ -190,7 +177,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     const bool live = j < klen;
     // F16: p is held 2^10 p
     const float p_scale = DT == DT_F16 ? __uint_as_float((127u + (uint32_t)kProbLog2) << 23) : 1.f;
-    const float t_scale = score_scale<DT>(p, at.b, at.h, scratch), t_over_p = t_scale / p_scale;
+    const float t_scale = score_scale<DT>(p, l, at.b, at.h, scratch), t_over_p = t_scale / p_scale;
 
     const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh + (int64_t)j * p.k.sl;
     const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh;
@@ -225,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
             if (i < qlen)
                 __builtin_amdgcn_global_load_lds(
                     (const __attribute__((address_space(1))) void*)(row_values + (int64_t)h * p.len_q + i +
-                                                                    (lane < 32 ? 0 : lse_at(p))),
+                                                                    (lane < 32 ? 0 : l.lse)),
                     (__attribute__((address_space(3))) void*)rows[buf], 4, 0, 0);
             else
                 rows[buf][lane] = lane < 32 ? 0.f : INFINITY;
@@ -235,24 +222,27 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     const Reader<DT, DP> rd(lane);
     const float to_log2 = p.scale * kLog2e;
     const T* v_rows = vt + wave * L::size(32);
+    // the part's tiles of those of all heads, in their order
+    const int64_t tiles = (int64_t)steps * p.group;
+    const int64_t end = tiles * (part + 1) / p.key_parts;
+    int64_t tile = tiles * part / p.key_parts;
+    int h = steps ? (int)(tile / steps) : 0, i0 = steps ? start + (int)(tile % steps) * kQueries : 0, buf = 0;
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
-    int buf = 0;
-    if (steps > 0) fill(0, start, 0);
-    for (int h = 0; h < p.group; ++h) {
-        int i0 = start;
-        const auto next = [&] {
-            tile_wait();
-            __syncthreads();  // the tile is there, and the other one is read
-            const bool last = i0 + kQueries >= qlen;
-            if (!last || h + 1 < p.group) fill(last ? h + 1 : h, last ? start : i0 + kQueries, buf ^ 1);
-        };
-        for (; i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1) {
+    if (tile < end) fill(h, i0, 0);
+    const auto next = [&] {
+        tile_wait();
+        __syncthreads();  // the tile is there, and the other one is read
+        const bool last = i0 + kQueries >= qlen;
+        if (tile + 1 < end) fill(last ? h + 1 : h, last ? start : i0 + kQueries, buf ^ 1);
+    };
+    for (; tile < end; ++h, i0 = start) {
+        for (; tile < end && i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1, ++tile) {
             next();
             if (i0 + kQueries > wave_lo)
                 tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p,
                                                  lo - i0);
         }
-        for (; i0 < qlen; i0 += kQueries, buf ^= 1) {
+        for (; tile < end && i0 < qlen; i0 += kQueries, buf ^= 1, ++tile) {
             next();
             tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
         }
@@ -262,9 +252,24 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
         if (threadIdx.x == 0) *mark = bad;
     }
     if (j >= p.len_k) return;
-    store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, p.scale / t_scale, live,
-                         p.dim, g);
-    store_column<DT, DP>((T*)p.dv.p + at.b * p.dv.sb + at.h * p.dv.sh + j * p.dv.sl, dv, 1.f / p_scale, live, p.dim, g);
+    const float k_scale = p.scale / t_scale, v_scale = 1.f / p_scale;
+    if (p.key_parts > 1) {
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                dk[db][r] = live ? dk[db][r] * k_scale : 0.f;
+                dv[db][r] = live ? dv[db][r] * v_scale : 0.f;
+            }
+        const int64_t keys = (int64_t)p.batch * p.kv_heads * p.len_k, dim = part_dim(p);
+        const int64_t key = ((int64_t)at.b * p.kv_heads + at.h) * p.len_k + j;
+        float* to = p.ws + l.dkv + (key * p.key_parts + part) * dim;
+        store_part<DP>(to, dk, p.dim, g);
+        store_part<DP>(to + keys * p.key_parts * dim, dv, p.dim, g);
+        return;
+    }
+    store_column<DT, DP>((T*)p.dk.p + at.b * p.dk.sb + at.h * p.dk.sh + j * p.dk.sl, dk, k_scale, live, p.dim, g);
+    store_column<DT, DP>((T*)p.dv.p + at.b * p.dv.sb + at.h * p.dv.sh + j * p.dv.sl, dv, v_scale, live, p.dim, g);
 }
 
 // dq of 128 query rows (row = query * group + head, as in the forward pass),
@@ -299,7 +304,7 @@ __device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t
 }
 
 template <int DT, int DP, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_queries_kernel(AttnParams p) {
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_queries_kernel(AttnParams p, BackwardLayout l) {
     using T = storage_t<DT>;
     using L = Tile<DT, DP>;
     using F = Filler<DT, DP, kKeys, kThreads>;
@@ -311,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, n_blocks);
     const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
-    const float t_scale = score_scale<DT>(p, at.b, at.h, scratch);
+    const float t_scale = score_scale<DT>(p, l, at.b, at.h, scratch);
 
     const int64_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
@@ -323,7 +328,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     const int lim = key_limit(min(i, qlen - 1), qlen, klen, p.causal);
     const int wave_any = wave_first < qlen ? key_limit(min(wave_last, qlen - 1), qlen, klen, p.causal) : 0;
     const int block_all = any ? key_limit(min((int)(first / p.group), qlen - 1), qlen, klen, p.causal) : 0;
-    const int end = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
+    // the part's tiles of those that the work-group's rows see
+    const int part = (int)blockIdx.y;
+    const int all = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
+    const int tiles = (all + kKeys - 1) / kKeys;
+    const int start = (int)((int64_t)tiles * part / p.parts) * kKeys;
+    const int end = min(all, (int)((int64_t)tiles * (part + 1) / p.parts) * kKeys);
 
     const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh + i * p.q.sl;
     const T* dout = (const T*)p.dout.p + at.b * p.dout.sb + hq * p.dout.sh + i * p.dout.sl;
@@ -337,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     }
     const int64_t at_row = ((int64_t)at.b * p.heads + hq) * p.len_q + i;
     // t_scale is a power of two: it goes into the exponent
-    const float lse = live ? p.ws[lse_at(p) + at_row] - __builtin_amdgcn_logf(t_scale) : INFINITY;
+    const float lse = live ? p.ws[l.lse + at_row] - __builtin_amdgcn_logf(t_scale) : INFINITY;
     const float dot = live ? p.ws[at_row] : 0.f;
 
     const F fk(p.k.sl, p.dim), fv(p.v.sl, p.dim);
@@ -357,15 +367,15 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db) dq[db] = f32x16{};
-        if (end > 0) fill(0, 0);
-        int j0 = 0, buf = 0;
+        if (start < end) fill(start, 0);
+        int j0 = start, buf = 0;
         const auto next = [&] {
             tile_wait();
             __syncthreads();  // the tile is there, and the other one is read
             if (j0 + kKeys < end) fill(j0 + kKeys, buf ^ 1);
         };
         // first the tiles that every row of the work-group sees whole
-        for (; j0 + kKeys <= block_all; j0 += kKeys, buf ^= 1) {
+        for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
             tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0);
         }
@@ -378,23 +388,68 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     pass(std::false_type{});
     if (p.causal && __syncthreads_or(non_finite(dq))) pass(std::true_type{});
     if (!exists) return;
+    if (p.parts > 1) {
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[db][r] = live ? dq[db][r] * (p.scale / t_scale) : 0.f;
+        store_part<DP>(p.ws + l.dq + (at_row * p.parts + part) * part_dim(p), dq, p.dim, g);
+        return;
+    }
     store_column<DT, DP>((T*)p.dq.p + at.b * p.dq.sb + hq * p.dq.sh + i * p.dq.sl, dq, p.scale / t_scale, live, p.dim, g);
+}
+
+// Sums over the parts, in their order.  A thread has four elements of a row; the
+// rows of dq come first, then those of dk, then of dv.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) attn_backward_join_kernel(AttnParams p, BackwardLayout l) {
+    using T = storage_t<DT>;
+    const int quads = (p.dim + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    int64_t row = id / quads;
+    const int d = (int)(id % quads) * 4;
+    const int64_t q_rows = p.parts > 1 ? (int64_t)p.batch * p.heads * p.len_q : 0;
+    const int64_t k_rows = p.key_parts > 1 ? (int64_t)p.batch * p.kv_heads * p.len_k : 0;
+    if (row >= q_rows + 2 * k_rows) return;
+    const bool is_q = row < q_rows;
+    if (!is_q) row -= q_rows;
+    const bool is_v = !is_q && row >= k_rows;
+    const int parts = is_q ? p.parts : p.key_parts;
+    const float* in = p.ws + (is_q ? l.dq : l.dkv) + row * parts * part_dim(p) + d;
+    f32x4 sum = *(const f32x4*)in;
+    for (int k = 1; k < parts; ++k) {
+        const f32x4 x = *(const f32x4*)(in + k * part_dim(p));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += x[e];
+    }
+    if (is_v) row -= k_rows;
+    const int len = is_q ? p.len_q : p.len_k, heads = is_q ? p.heads : p.kv_heads;
+    const int i = (int)(row % len), h = (int)(row / len % heads), b = (int)(row / len / heads);
+    const HeadView& to = is_q ? p.dq : is_v ? p.dv : p.dk;
+    store_quad<DT>((T*)to.p + b * to.sb + h * to.sh + i * to.sl, d, p.dim, sum[0], sum[1], sum[2], sum[3]);
 }
 
 template <int DT, int DP, bool WHOLE>
 hipError_t backward(const AttnParams& p, hipStream_t stream) {
+    const BackwardLayout l = backward_layout(p);
     const int64_t pairs = (int64_t)p.batch * p.kv_heads;
-    const int64_t key_blocks = ((int64_t)p.len_k + kKeyRows - 1) / kKeyRows * pairs;
-    const int64_t row_blocks = ((int64_t)p.len_q * p.group + kRows - 1) / kRows * pairs;
-    const int64_t rows = (int64_t)p.batch * p.heads * norm_blocks(p.len_q) +
-                         (DT == DT_F16 ? pairs * norm_blocks(p.len_k) : 0);
-    if (rows > 0) attn_rows_kernel<DT><<<dim3((unsigned)rows), kThreads, 0, stream>>>(p);
-    if (key_blocks > 0) {
-        attn_backward_keys_kernel<DT, DP, WHOLE, false><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
-        if (p.causal)
-            attn_backward_keys_kernel<DT, DP, WHOLE, true><<<dim3((unsigned)key_blocks), kThreads, 0, stream>>>(p);
+    const auto blocks = [](int64_t n) { return (n + kNormBlock - 1) / kNormBlock; };
+    const int64_t rows = (int64_t)p.batch * p.heads * blocks(p.len_q) + (DT == DT_F16 ? pairs * blocks(p.len_k) : 0);
+    if (rows > 0) attn_rows_kernel<DT><<<dim3((unsigned)rows), kThreads, 0, stream>>>(p, l);
+    if (key_blocks(p) > 0) {
+        const dim3 grid((unsigned)key_blocks(p), (unsigned)p.key_parts);
+        attn_backward_keys_kernel<DT, DP, WHOLE, false><<<grid, kThreads, 0, stream>>>(p, l);
+        if (p.causal) attn_backward_keys_kernel<DT, DP, WHOLE, true><<<grid, kThreads, 0, stream>>>(p, l);
     }
-    if (row_blocks > 0) attn_backward_queries_kernel<DT, DP, WHOLE><<<dim3((unsigned)row_blocks), kThreads, 0, stream>>>(p);
+    if (row_blocks(p) > 0)
+        attn_backward_queries_kernel<DT, DP, WHOLE>
+            <<<dim3((unsigned)row_blocks(p), (unsigned)p.parts), kThreads, 0, stream>>>(p, l);
+    const int64_t join_rows = (p.parts > 1 ? (int64_t)p.batch * p.heads * p.len_q : 0) +
+                              (p.key_parts > 1 ? 2 * pairs * p.len_k : 0);
+    if (join_rows > 0) {
+        const int64_t quads = join_rows * ((p.dim + 3) / 4);
+        attn_backward_join_kernel<DT><<<dim3((unsigned)((quads + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(p, l);
+    }
     return hipGetLastError();
 }
 

@@ -152,8 +152,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     // the part's tiles of those that the work-group's rows see
     const int all = any ? key_limit(min(block_last, qlen - 1), qlen, klen, p.causal) : 0;
     const int tiles = (all + kKeys - 1) / kKeys;
-    const int start = (int)((int64_t)tiles * part / p.splits) * kKeys;
-    const int end = min(all, (int)((int64_t)tiles * (part + 1) / p.splits) * kKeys);
+    const int start = (int)((int64_t)tiles * part / p.parts) * kKeys;
+    const int end = min(all, (int)((int64_t)tiles * (part + 1) / p.parts) * kKeys);
 
     const T* q = (const T*)p.q.p + at.b * p.q.sb + hq * p.q.sh + i * p.q.sl;
     const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh;
@@ -202,15 +202,11 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
     if (!exists) return;
     const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
-    if (p.splits > 1) {
-        float* to = p.ws + ((((int64_t)at.b * p.kv_heads + at.h) * p.len_q * p.group + row) * p.splits + part) * split_row(p);
-        if (g == 0) *(f32x4*)(to + split_row(p) - 4) = f32x4{live ? sm.m : -INFINITY, live ? l : 0.f, live ? rounded : 0.f, 0.f};
-#pragma unroll
-        for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                if (32 * db + 2 * r + 4 * g < p.dim)
-                    *(f32x4*)(to + 32 * db + 2 * r + 4 * g) = f32x4{acc[db][r], acc[db][r + 1], acc[db][r + 2], acc[db][r + 3]};
+    if (p.parts > 1) {
+        const int64_t dim = part_dim(p);
+        float* to = p.ws + ((((int64_t)at.b * p.kv_heads + at.h) * p.len_q * p.group + row) * p.parts + part) * (dim + 4);
+        if (g == 0) *(f32x4*)(to + dim) = f32x4{live ? sm.m : -INFINITY, live ? l : 0.f, live ? rounded : 0.f, 0.f};
+        store_part<DP>(to, acc, p.dim, g);
         return;
     }
     const bool some = live && l != 0.f;  // NaN too: it goes on to o
@@ -230,14 +226,14 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnParams p) {
     const int64_t row = id / quads;  // [batch][key head][query][head of the group]
     const int d = (int)(id % quads) * 4;
     if (row >= (int64_t)p.batch * p.heads * p.len_q) return;
-    const int64_t stride = split_row(p);
-    const float* in = p.ws + row * p.splits * stride;
+    const int64_t stride = part_dim(p) + 4;
+    const float* in = p.ws + row * p.parts * stride;
     float m = -INFINITY;
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, in[s * stride + stride - 4]);
+    for (int s = 0; s < p.parts; ++s) m = fmaxf(m, in[s * stride + stride - 4]);
     const float shift = m == -INFINITY ? 0.f : m, to_log2 = p.scale * kLog2e;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f, rounded = 0.f;
-    for (int s = 0; s < p.splits; ++s) {
+    for (int s = 0; s < p.parts; ++s) {
         const f32x4 stat = *(const f32x4*)(in + s * stride + stride - 4), x = *(const f32x4*)(in + s * stride + d);
         const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * to_log2);
 #pragma unroll
@@ -259,12 +255,12 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnParams p) {
 template <int DT, int DP>
 hipError_t forward(const AttnParams& p, hipStream_t stream) {
     const int64_t blocks = ((int64_t)p.len_q * p.group + kRows - 1) / kRows * p.batch * p.kv_heads;
-    const dim3 grid((unsigned)blocks, (unsigned)p.splits);
+    const dim3 grid((unsigned)blocks, (unsigned)p.parts);
     if (p.whole)
         attn_forward_kernel<DT, DP, true><<<grid, kThreads, 0, stream>>>(p);
     else
         attn_forward_kernel<DT, DP, false><<<grid, kThreads, 0, stream>>>(p);
-    if (p.splits > 1) {
+    if (p.parts > 1) {
         const int64_t quads = (int64_t)p.batch * p.heads * p.len_q * ((p.dim + 3) / 4);
         attn_join_kernel<DT><<<dim3((unsigned)((quads + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(p);
     }

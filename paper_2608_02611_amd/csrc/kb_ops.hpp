@@ -77,39 +77,70 @@ struct AttnParams {
     int len_q, len_k, dim;
     float scale;
     int causal;
-    int splits; // forward: parts of the keys
+    int parts;      // forward, dq: parts of the keys
+    int key_parts;  // dk, dv: parts of the queries
     int whole;  // rows of q, k, v (and dout) are aligned to 16 bytes and made of 16-byte chunks
     float* ws;
 };
 
-// Forward: query rows of a work-group and keys of a tile, and into how many parts
-// the keys are split so that few query rows still fill the device: up to kFill
-// work-groups (two for each of 256 CUs, and as many again, as parts of a ragged
-// batch end at different times), of no less than kSplitKeys keys each.
+// Tiles: query rows of a work-group and keys that pass it at a time (forward, dq),
+// keys of a work-group and queries that pass it at a time (dk, dv).
 constexpr int kAttnRows = 128;
 constexpr int kAttnKeys = 64;
-constexpr int64_t kFill = 1024;
-constexpr int64_t kSplitKeys = 512;
-inline int attn_splits(const AttnParams& p) {
-    const int64_t work_groups =
-        (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_q * p.group + kAttnRows - 1) / kAttnRows);
-    if (work_groups == 0 || 2 * work_groups > kFill) return 1;
-    const int64_t want = kFill / work_groups, most = p.len_k / kSplitKeys;
+constexpr int kAttnKeyRows = 128;
+constexpr int kAttnQueries = 32;
+
+// What passes a work-group is split into parts, each with work-groups of its own
+// and joined afterwards, so that a few rows still fill the device: `fill`
+// work-groups, of `least` rows to pass or more.
+inline int attn_parts(int64_t work_groups, int64_t passing, int64_t fill, int64_t least) {
+    if (work_groups == 0 || 2 * work_groups > fill) return 1;
+    const int64_t want = fill / work_groups, most = passing / least;
     return (int)(want < most ? want : most > 1 ? most : 1);
 }
-// Workspace of a split forward pass, in floats: for each query row and part the
-// sums over its keys (dim rounded up to 4), then m, l and the rounded l.
-__host__ __device__ inline int64_t split_row(const AttnParams& p) { return (p.dim + 3) / 4 * 4 + 4; }
-inline int64_t split_floats(const AttnParams& p, int splits) {
-    return splits > 1 ? (int64_t)p.batch * p.heads * p.len_q * splits * split_row(p) : 0;
+inline int64_t row_blocks(const AttnParams& p) {
+    return (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_q * p.group + kAttnRows - 1) / kAttnRows);
+}
+inline int64_t key_blocks(const AttnParams& p) {
+    return (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_k + kAttnKeyRows - 1) / kAttnKeyRows);
+}
+// Forward: two work-groups for each of 256 CUs, and as many again, as the parts
+// of a ragged batch end at different times.
+inline int forward_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 1024, 512); }
+// Backward: one or two work-groups a CU.
+inline int row_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 512, 2 * kAttnKeys); }
+inline int key_parts(const AttnParams& p) {
+    return attn_parts(key_blocks(p), (int64_t)p.len_q * p.group, 512, 4 * kAttnQueries);
 }
 
-// Workspace of the backward pass, in floats: D_i and lse_i for every query row, then
-// (F16) the largest squared norm of each block of kNormBlock rows of dout and
-// of v, then a word for each work-group of kAttnKeyRows keys.
+// Workspace of the forward pass in parts, in floats: for each query row and part
+// the sums over its keys (dim rounded up to 4), then m, l and the rounded l.
+__host__ __device__ inline int64_t part_dim(const AttnParams& p) { return (p.dim + 3) / 4 * 4; }
+inline int64_t forward_floats(const AttnParams& p, int parts) {
+    return parts > 1 ? (int64_t)p.batch * p.heads * p.len_q * parts * (part_dim(p) + 4) : 0;
+}
+
+// Workspace of the backward pass, in floats: D_i and lse_i for every query row;
+// (F16) the largest squared norm of each block of kNormBlock rows of dout, and
+// of v; a word for each work-group of keys; then, each where it is in parts, dq
+// of every query row and part, and dk and dv of every key and part.
 constexpr int kNormBlock = 64;
-constexpr int kAttnKeyRows = 128;
-inline int64_t norm_blocks(int64_t len) { return (len + kNormBlock - 1) / kNormBlock; }
+struct BackwardLayout {
+    int64_t lse, dout_norms, v_norms, marks, dq, dkv, total;
+};
+inline BackwardLayout backward_layout(const AttnParams& p) {
+    const int64_t heads = (int64_t)p.batch * p.heads, pairs = (int64_t)p.batch * p.kv_heads;
+    const auto blocks = [](int64_t n) { return (n + kNormBlock - 1) / kNormBlock; };
+    BackwardLayout l;
+    l.lse = heads * p.len_q;
+    l.dout_norms = 2 * l.lse;
+    l.v_norms = l.dout_norms + heads * blocks(p.len_q);
+    l.marks = l.v_norms + pairs * blocks(p.len_k);
+    l.dq = (l.marks + key_blocks(p) * key_parts(p) + 3) / 4 * 4;
+    l.dkv = l.dq + (row_parts(p) > 1 ? heads * p.len_q * row_parts(p) * part_dim(p) : 0);
+    l.total = l.dkv + (key_parts(p) > 1 ? 2 * pairs * p.len_k * key_parts(p) * part_dim(p) : 0);
+    return l;
+}
 
 hipError_t launch_attn_forward(int dtype, const AttnParams& p, hipStream_t stream);
 hipError_t launch_attn_backward(int dtype, const AttnParams& p, hipStream_t stream);

@@ -222,12 +222,8 @@ bool attn_sizes(const kb_tensor& q, const kb_tensor& k, AttnParams* p) {
     return true;
 }
 
-size_t attn_backward_bytes(const AttnParams& p) {
-    const int64_t rows = (int64_t)p.batch * p.heads, pairs = (int64_t)p.batch * p.kv_heads;
-    const int64_t floats = 2 * rows * p.len_q + rows * norm_blocks(p.len_q) + pairs * norm_blocks(p.len_k) +
-                           pairs * (((int64_t)p.len_k + kAttnKeyRows - 1) / kAttnKeyRows);
-    return ((size_t)floats * sizeof(float) + 15) & ~(size_t)15;
-}
+size_t forward_bytes(const AttnParams& p) { return (size_t)forward_floats(p, forward_parts(p)) * sizeof(float); }
+size_t backward_bytes(const AttnParams& p) { return (size_t)(backward_layout(p).total + 3) / 4 * 16; }
 
 // q, k, v and what hangs on their sizes; fills p.
 int check_attn(const char* call, const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, const kb_attn_opts* opts,
@@ -338,7 +334,7 @@ int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w
 size_t kb_attn_forward_workspace_bytes(const kb_tensor* q, const kb_tensor* k) {
     AttnParams p{};
     if (q == nullptr || k == nullptr || !attn_sizes(*q, *k, &p)) return 0;
-    return (size_t)split_floats(p, attn_splits(p)) * sizeof(float);
+    return forward_bytes(p);
 }
 
 int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, const kb_attn_opts* opts,
@@ -350,8 +346,8 @@ int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, 
     if ((rc = check_attn(call, q, k, v, opts, &p)) || (rc = check_view(call, "o", o, 4, true)) ||
         (rc = check_shape(call, "o", *o, "q", *q)) || (rc = check_lse(call, lse, *q)))
         return rc;
-    p.splits = attn_splits(p);
-    const size_t need = (size_t)split_floats(p, p.splits) * sizeof(float);
+    p.parts = forward_parts(p);
+    const size_t need = forward_bytes(p);
     if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
     const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
     const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
@@ -370,7 +366,7 @@ int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, 
 size_t kb_attn_backward_workspace_bytes(const kb_tensor* q, const kb_tensor* k) {
     AttnParams p{};
     if (q == nullptr || k == nullptr || !attn_sizes(*q, *k, &p)) return 0;
-    return attn_backward_bytes(p);
+    return backward_bytes(p);
 }
 
 int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
@@ -388,7 +384,9 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
         (rc = check_view(call, "dk", dk, 4, true)) || (rc = check_shape(call, "dk", *dk, "k", *k)) ||
         (rc = check_view(call, "dv", dv, 4, true)) || (rc = check_shape(call, "dv", *dv, "k", *k)))
         return rc;
-    const size_t need = attn_backward_bytes(p);
+    p.parts = row_parts(p);
+    p.key_parts = key_parts(p);
+    const size_t need = backward_bytes(p);
     if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
     const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
     const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));

@@ -93,6 +93,11 @@ def test_workspace_bytes(L):
     for q, k in (((2, 6, 16, 64), K), (Q, (1, 4, 32, 64)), ((2, 8, 16, 200), (2, 4, 32, 200))):
         assert L.kb_attn_backward_workspace_bytes(view(1, q), view(1, k)) == 0
         assert L.kb_attn_forward_workspace_bytes(view(1, q), view(1, k)) == 0
+    # few rows on many keys: parts of their sums, binary32
+    q, k = (1, 2, 1, 61), (1, 1, 5000, 61)
+    assert L.kb_attn_forward_workspace_bytes(view(1, q), view(1, k)) == 4 * 2 * 9 * (64 + 4)
+    assert L.kb_attn_backward_workspace_bytes(view(1, q), view(1, k)) >= 4 * 2 * 39 * 64
+    assert L.kb_attn_forward_workspace_bytes(None, view(1, k)) == 0
 
 
 def test_gradients_as_columns_of_one_buffer(L):

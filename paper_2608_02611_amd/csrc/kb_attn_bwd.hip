@@ -21,61 +21,36 @@ namespace {
 constexpr int kThreads = 256;
 constexpr float kProbLog2 = 10.f;
 
-// Before the products: D_i and lse_i / log 2 for 64 query rows a work-group, 16
-// lanes a row.  A row with no seen score has lse = -infinity, and its terms
-// exp(-infinity - lse) are to be 0: it gets 0.  A row of the padding gets
-// +infinity, which makes all its terms 0, and D = 0.  F16:
-// also the largest finite squared norm of the block's rows of dout, and, in
-// the work-groups after those, of 64 rows of v.
+// F16, before all else: the largest finite squared norm of each block of
+// kNormBlock rows of v, 16 lanes a row.
 template <int DT>
-__global__ void __launch_bounds__(kThreads) attn_rows_kernel(AttnParams p, BackwardLayout l) {
+__global__ void __launch_bounds__(kThreads) attn_v_norms_kernel(AttnParams p, BackwardLayout l) {
     using T = storage_t<DT>;
     constexpr int N = Vec16<T>::N;
     __shared__ float largest[kThreads / 16];
-    const int q_blocks = (p.len_q + kNormBlock - 1) / kNormBlock, k_blocks = (p.len_k + kNormBlock - 1) / kNormBlock;
-    const int64_t q_total = (int64_t)p.batch * p.heads * q_blocks;
-    const bool of_v = (int64_t)blockIdx.x >= q_total;
-    const int64_t id = of_v ? (int64_t)blockIdx.x - q_total : (int64_t)blockIdx.x;
-    const int blocks = of_v ? k_blocks : q_blocks, heads = of_v ? p.kv_heads : p.heads;
-    const int block = (int)(id % blocks), h = (int)(id / blocks % heads), b = (int)(id / blocks / heads);
-    const int n = of_v ? seq_len(p.k_lens, b, p.len_k) : seq_len(p.q_lens, b, p.len_q);
-    const int sub = threadIdx.x & 15;
+    const int blocks = (p.len_k + kNormBlock - 1) / kNormBlock, id = (int)blockIdx.x;
+    const int block = id % blocks, h = id / blocks % p.kv_heads, b = id / blocks / p.kv_heads;
+    const int n = seq_len(p.k_lens, b, p.len_k), sub = threadIdx.x & 15;
     float top = 0.f;
+#pragma unroll
     for (int k = 0; k < kNormBlock / 16; ++k) {
-        const int i = block * kNormBlock + k * 16 + (threadIdx.x >> 4);
-        float dot = 0.f, sq = 0.f;
-        if (i < n) {
-            const HeadView& a = of_v ? p.v : p.dout;
-            const T* x = (const T*)a.p + b * a.sb + h * a.sh + i * a.sl;
-            const T* y = (const T*)p.o.p + b * p.o.sb + h * p.o.sh + i * p.o.sl;
-            for (int d = sub * N; d < p.dim; d += 16 * N) {
-                const auto u = load_vec(x, d, p.dim), w = load_vec(of_v ? x : y, d, p.dim);
+        const int j = block * kNormBlock + k * 16 + (threadIdx.x >> 4);
+        const T* x = (const T*)p.v.p + b * p.v.sb + h * p.v.sh + j * p.v.sl;
+        float sq = 0.f;
+        if (j < n && sub * N < p.dim) {
+            const auto u = load_vec(x, sub * N, p.dim);
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    dot = fmaf((float)u[e], (float)w[e], dot);
-                    sq = fmaf((float)u[e], (float)u[e], sq);
-                }
-            }
+            for (int e = 0; e < N; ++e) sq = fmaf((float)u[e], (float)u[e], sq);
         }
 #pragma unroll
-        for (int s = 1; s < 16; s <<= 1) {
-            dot += __shfl_xor(dot, s);
-            sq += __shfl_xor(sq, s);
-        }
-        if (!of_v && sub == 0 && i < p.len_q) {
-            const int64_t row = ((int64_t)b * p.heads + h) * p.len_q + i;
-            const float lse = p.lse[row];
-            p.ws[row] = dot;
-            p.ws[l.lse + row] = i >= n ? INFINITY : lse == -INFINITY ? 0.f : lse * kLog2e;
-        }
+        for (int s = 1; s < 16; s <<= 1) sq += __shfl_xor(sq, s);
         if (sq < INFINITY) top = fmaxf(top, sq);
     }
-    if (DT != DT_F16) return;
     if (sub == 0) largest[threadIdx.x >> 4] = top;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int k = 1; k < kThreads / 16; ++k) top = fmaxf(top, largest[k]);
-        p.ws[(of_v ? l.v_norms : l.dout_norms) + id] = top;
+        p.ws[l.v_norms + id] = top;
     }
 }
 
@@ -86,27 +61,24 @@ __device__ __forceinline__ int bound_exponent(float sq) {
     return ((ex + 1) >> 1) + ((ex + 1) & 1);
 }
 
-// F16: 2^(14 - e), |t| < 2^(1 + e) over the heads that share key head h of
-// sequence b; 1 for the other types.  (The exponent stays within binary32: |x|
-// of an F16 row of 128 is under 2^20 and its smallest is 2^-24.)  Called by every thread of a work-group.
-template <int DT>
-__device__ __forceinline__ float score_scale(const AttnParams& p, const BackwardLayout& l, int b, int h, float* shared) {
-    if (DT != DT_F16) return 1.f;
-    const int q_blocks = (p.len_q + kNormBlock - 1) / kNormBlock, k_blocks = (p.len_k + kNormBlock - 1) / kNormBlock;
-    const float* dn = p.ws + l.dout_norms + ((int64_t)b * p.heads + h * p.group) * q_blocks;
-    const float* vn = p.ws + l.v_norms + ((int64_t)b * p.kv_heads + h) * k_blocks;
-    float d = 0.f, v = 0.f;
-    for (int64_t k = threadIdx.x; k < (int64_t)q_blocks * p.group; k += kThreads) d = fmaxf(d, dn[k]);
-    for (int k = threadIdx.x; k < k_blocks; k += kThreads) v = fmaxf(v, vn[k]);
-    const uint32_t wd = wave_max_u32(__float_as_uint(d)), wv = wave_max_u32(__float_as_uint(v));
-    if ((threadIdx.x & 63) == 0) {
-        shared[threadIdx.x >> 6] = __uint_as_float(wd);
-        shared[4 + (threadIdx.x >> 6)] = __uint_as_float(wv);
-    }
+// The largest of n values that are not negative, in every thread of a
+// work-group; shared: a float for each wave.
+__device__ __forceinline__ float block_max(const float* x, int64_t n, float* shared) {
+    float top = 0.f;
+    for (int64_t k = threadIdx.x; k < n; k += kThreads) top = fmaxf(top, x[k]);
+    top = __uint_as_float(wave_max_u32(__float_as_uint(top)));
+    if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = top;
     __syncthreads();
-    d = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
-    v = fmaxf(fmaxf(shared[4], shared[5]), fmaxf(shared[6], shared[7]));
-    return __uint_as_float((uint32_t)(127 + 14 - bound_exponent(d) - bound_exponent(v)) << 23);
+    top = fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
+    __syncthreads();
+    return top;
+}
+
+// F16: 2^(14 - e), |t| < 2^(1 + e), from the squared norms of the rows of dout and
+// v that enter.  (The exponent stays within binary32: the norm of an F16 row of
+// 128 is under 2^20 and, if not 0, at least 2^-24.)
+__device__ __forceinline__ float score_scale(float dout_sq, float v_sq) {
+    return __uint_as_float((uint32_t)(127 + 14 - bound_exponent(dout_sq) - bound_exponent(v_sq)) << 23);
 }
 
 // dk and dv of 128 keys, 32 a wave.  The keys stay (key rows in registers, value
@@ -177,7 +149,15 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     const bool live = j < klen;
     // F16: p is held 2^10 p
     const float p_scale = DT == DT_F16 ? __uint_as_float((127u + (uint32_t)kProbLog2) << 23) : 1.f;
-    const float t_scale = score_scale<DT>(p, l, at.b, at.h, scratch), t_over_p = t_scale / p_scale;
+    float t_scale = 1.f;
+    if (DT == DT_F16) {
+        const int64_t pair = (int64_t)at.b * p.kv_heads + at.h;
+        const int64_t rows_of = ((int64_t)p.len_q * p.group + kAttnRows - 1) / kAttnRows;
+        const int64_t keys_of = (p.len_k + kNormBlock - 1) / kNormBlock;
+        const float dout_sq = block_max(p.ws + l.dout_norms + pair * rows_of, rows_of, scratch);
+        t_scale = score_scale(dout_sq, block_max(p.ws + l.v_norms + pair * keys_of, keys_of, scratch));
+    }
+    const float t_over_p = t_scale / p_scale;
 
     const T* k = (const T*)p.k.p + at.b * p.k.sb + at.h * p.k.sh + (int64_t)j * p.k.sl;
     const T* v = (const T*)p.v.p + at.b * p.v.sb + at.h * p.v.sh;
@@ -316,7 +296,6 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, n_blocks);
     const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
-    const float t_scale = score_scale<DT>(p, l, at.b, at.h, scratch);
 
     const int64_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
@@ -345,10 +324,44 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
         df[c] = load_frag<DT, WHOLE>(dout, c, g, p.dim, live);
     }
+    // D_i and lse_i / log 2, for here and for the keys' kernel.  A row with no
+    // seen score has lse = -infinity, and its terms exp(-infinity - lse) are to be
+    // 0: it gets 0.  A row of the padding gets +infinity, which makes its terms 0.
     const int64_t at_row = ((int64_t)at.b * p.heads + hq) * p.len_q + i;
-    // t_scale is a power of two: it goes into the exponent
-    const float lse = live ? p.ws[l.lse + at_row] - __builtin_amdgcn_logf(t_scale) : INFINITY;
-    const float dot = live ? p.ws[at_row] : 0.f;
+    const T* o = (const T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl;
+    float dot = 0.f, sq = 0.f;
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        const frag_t<DT> of = load_frag<DT, WHOLE>(o, c, g, p.dim, live);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            dot = fmaf((float)df[c][e], (float)of[e], dot);
+            if (DT == DT_F16) sq = fmaf((float)df[c][e], (float)df[c][e], sq);
+        }
+    }
+    dot += other_half(dot);
+    float lse = live ? p.lse[at_row] : INFINITY;
+    lse = lse == -INFINITY ? 0.f : lse * kLog2e;
+    if (part == 0 && exists && g == 0) {
+        p.ws[at_row] = dot;
+        p.ws[l.lse + at_row] = lse;
+    }
+    float t_scale = 1.f;
+    if (DT == DT_F16) {
+        const int64_t pair = (int64_t)at.b * p.kv_heads + at.h, keys_of = (p.len_k + kNormBlock - 1) / kNormBlock;
+        sq += other_half(sq);
+        sq = sq < INFINITY ? sq : 0.f;
+        t_scale = score_scale(sq, block_max(p.ws + l.v_norms + pair * keys_of, keys_of, scratch));
+        lse -= __builtin_amdgcn_logf(t_scale);  // a power of two: it goes into the exponent
+        if (part == 0) {
+            const float top = __uint_as_float(wave_max_u32(__float_as_uint(sq)));
+            if (lane == 0) scratch[wave] = top;
+            __syncthreads();
+            if (threadIdx.x == 0)
+                p.ws[l.dout_norms + pair * n_blocks + n_blocks - 1 - at.block] =
+                    fmaxf(fmaxf(scratch[0], scratch[1]), fmaxf(scratch[2], scratch[3]));
+        }
+    }
 
     const F fk(p.k.sl, p.dim), fv(p.v.sl, p.dim);
     const auto fill = [&](int j0, int buf) {
@@ -433,17 +446,16 @@ template <int DT, int DP, bool WHOLE>
 hipError_t backward(const AttnParams& p, hipStream_t stream) {
     const BackwardLayout l = backward_layout(p);
     const int64_t pairs = (int64_t)p.batch * p.kv_heads;
-    const auto blocks = [](int64_t n) { return (n + kNormBlock - 1) / kNormBlock; };
-    const int64_t rows = (int64_t)p.batch * p.heads * blocks(p.len_q) + (DT == DT_F16 ? pairs * blocks(p.len_k) : 0);
-    if (rows > 0) attn_rows_kernel<DT><<<dim3((unsigned)rows), kThreads, 0, stream>>>(p, l);
+    const int64_t v_blocks = pairs * ((p.len_k + (int64_t)kNormBlock - 1) / kNormBlock);
+    if (DT == DT_F16 && v_blocks > 0) attn_v_norms_kernel<DT><<<dim3((unsigned)v_blocks), kThreads, 0, stream>>>(p, l);
+    if (row_blocks(p) > 0)
+        attn_backward_queries_kernel<DT, DP, WHOLE>
+            <<<dim3((unsigned)row_blocks(p), (unsigned)p.parts), kThreads, 0, stream>>>(p, l);
     if (key_blocks(p) > 0) {
         const dim3 grid((unsigned)key_blocks(p), (unsigned)p.key_parts);
         attn_backward_keys_kernel<DT, DP, WHOLE, false><<<grid, kThreads, 0, stream>>>(p, l);
         if (p.causal) attn_backward_keys_kernel<DT, DP, WHOLE, true><<<grid, kThreads, 0, stream>>>(p, l);
     }
-    if (row_blocks(p) > 0)
-        attn_backward_queries_kernel<DT, DP, WHOLE>
-            <<<dim3((unsigned)row_blocks(p), (unsigned)p.parts), kThreads, 0, stream>>>(p, l);
     const int64_t join_rows = (p.parts > 1 ? (int64_t)p.batch * p.heads * p.len_q : 0) +
                               (p.key_parts > 1 ? 2 * pairs * p.len_k : 0);
     if (join_rows > 0) {

@@ -79,7 +79,7 @@ struct AttnParams {
     int causal;
     int parts;      // forward, dq: parts of the keys
     int key_parts;  // dk, dv: parts of the queries
-    int whole;  // rows of q, k, v (and dout) are aligned to 16 bytes and made of 16-byte chunks
+    int whole;  // rows of q, k, v (and o, dout) are aligned to 16 bytes and made of 16-byte chunks
     float* ws;
 };
 
@@ -107,10 +107,15 @@ inline int64_t key_blocks(const AttnParams& p) {
 // Forward: two work-groups for each of 256 CUs, and as many again, as the parts
 // of a ragged batch end at different times.
 inline int forward_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 1024, 512); }
-// Backward: one or two work-groups a CU.
-inline int row_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 512, 2 * kAttnKeys); }
+// Backward: one or two work-groups a CU, and as many again under a causal mask,
+// whose blocks are long and short (2 x 32 heads on 8 x 4096: 902 us with dk and
+// dv in two parts, 1086 in one).
+inline int64_t backward_fill(const AttnParams& p) { return p.causal ? 1024 : 512; }
+inline int row_parts(const AttnParams& p) {
+    return attn_parts(row_blocks(p), p.len_k, backward_fill(p), 2 * kAttnKeys);
+}
 inline int key_parts(const AttnParams& p) {
-    return attn_parts(key_blocks(p), (int64_t)p.len_q * p.group, 512, 4 * kAttnQueries);
+    return attn_parts(key_blocks(p), (int64_t)p.len_q * p.group, backward_fill(p), 4 * kAttnQueries);
 }
 
 // Workspace of the forward pass in parts, in floats: for each query row and part
@@ -121,8 +126,8 @@ inline int64_t forward_floats(const AttnParams& p, int parts) {
 }
 
 // Workspace of the backward pass, in floats: D_i and lse_i for every query row;
-// (F16) the largest squared norm of each block of kNormBlock rows of dout, and
-// of v; a word for each work-group of keys; then, each where it is in parts, dq
+// (F16) the largest squared norm of the rows of dout in each work-group of rows,
+// and of each block of kNormBlock rows of v; a word for each work-group of keys; then, each where it is in parts, dq
 // of every query row and part, and dk and dv of every key and part.
 constexpr int kNormBlock = 64;
 struct BackwardLayout {
@@ -130,12 +135,11 @@ struct BackwardLayout {
 };
 inline BackwardLayout backward_layout(const AttnParams& p) {
     const int64_t heads = (int64_t)p.batch * p.heads, pairs = (int64_t)p.batch * p.kv_heads;
-    const auto blocks = [](int64_t n) { return (n + kNormBlock - 1) / kNormBlock; };
     BackwardLayout l;
     l.lse = heads * p.len_q;
     l.dout_norms = 2 * l.lse;
-    l.v_norms = l.dout_norms + heads * blocks(p.len_q);
-    l.marks = l.v_norms + pairs * blocks(p.len_k);
+    l.v_norms = l.dout_norms + row_blocks(p);
+    l.marks = l.v_norms + pairs * ((p.len_k + (int64_t)kNormBlock - 1) / kNormBlock);
     l.dq = (l.marks + key_blocks(p) * key_parts(p) + 3) / 4 * 4;
     l.dkv = l.dq + (row_parts(p) > 1 ? heads * p.len_q * row_parts(p) * part_dim(p) : 0);
     l.total = l.dkv + (key_parts(p) > 1 ? 2 * pairs * p.len_k * key_parts(p) * part_dim(p) : 0);

@@ -223,7 +223,11 @@ bool attn_sizes(const kb_tensor& q, const kb_tensor& k, AttnParams* p) {
 }
 
 size_t forward_bytes(const AttnParams& p) { return (size_t)forward_floats(p, forward_parts(p)) * sizeof(float); }
-size_t backward_bytes(const AttnParams& p) { return (size_t)(backward_layout(p).total + 3) / 4 * 16; }
+// A causal mask takes the more parts.
+size_t backward_bytes(AttnParams p) {
+    p.causal = 1;
+    return (size_t)(backward_layout(p).total + 3) / 4 * 16;
+}
 
 // q, k, v and what hangs on their sizes; fills p.
 int check_attn(const char* call, const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, const kb_attn_opts* opts,
@@ -395,7 +399,7 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
     if ((rc = check_apart(call, outs, 4, ins, 6))) return rc;
     if (p.batch == 0 || p.kv_heads == 0 || p.heads == 0) return KB_OK;
     p.dout = head_view(dout);
-    p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v) && whole_rows(*dout);
+    p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v) && whole_rows(*dout) && whole_rows(*o);
     p.o = head_view(o);
     p.dq = head_view(dq);
     p.dk = head_view(dk);

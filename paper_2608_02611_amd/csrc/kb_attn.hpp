@@ -99,6 +99,21 @@ __device__ __forceinline__ void stage(storage_t<DT>* tile, const storage_t<DT>* 
     }
 }
 
+// Memory straight to LDS, BYTES a lane, in the order of the lanes: from the
+// address, the same in all lanes, plus two offsets, one a lane's.  As buffer loads: while
+// a global or flat one is under way, the compiler waits for all of a wave's LDS
+// reads wherever it needs the oldest (191 us of 4 x 32 heads x 2047 then).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t background(const void* address) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(address), 0, 0x7FFFFFFF, 0x00020000);
+}
+template <int BYTES>
+__device__ __forceinline__ void send(__amdgpu_buffer_rsrc_t from, uint32_t lane_offset, int offset, void* to) {
+    static_assert(BYTES == 4 || BYTES == 16, "a word or a chunk");
+    const auto lds = (__attribute__((address_space(3))) void*)to;
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 16, (int)lane_offset, offset, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, lds, 4, (int)lane_offset, offset, 0, 0);
+}
+
 // A tile filled in the background: each thread's 16-byte chunks go from memory
 // straight to LDS, with no register in between, and have arrived once the
 // thread has waited (tile_wait) and the work-group has met.  LDS takes a wave's
@@ -129,16 +144,16 @@ struct Filler {
     __device__ __forceinline__ void fill(T* tile, const T* base, int64_t stride, int r0, int n, int dim) const {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         T* to = tile + wave * L::KB;
-        const char* from = (const char*)(base + (int64_t)r0 * stride);
+        const auto from = background(base + (int64_t)r0 * stride);
+        const int step = STEP * (int)stride * (int)sizeof(T);  // (64 rows are within 2^31 bytes)
         if (r0 + ROWS <= n && dim == L::PITCH) {  // the common case, without a test for each chunk
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k, from += (int64_t)STEP * stride * (int)sizeof(T))
-                send(from + offset, to + k * (STEP / L::KB_ROWS * L::KB));
+            for (int k = 0; k < STEPS; ++k) send<16>(from, offset, k * step, to + k * (STEP / L::KB_ROWS * L::KB));
         } else {
 #pragma unroll 1
-            for (int k = 0; k < STEPS; ++k, from += (int64_t)STEP * stride * (int)sizeof(T)) {
+            for (int k = 0; k < STEPS; ++k) {
                 if (in && r0 + k * STEP + row0 < n) {
-                    send(from + offset, to);
+                    send<16>(from, offset, k * step, to);
                 } else {
                     const u32v4 zero = {0, 0, 0, 0};
                     *(u32v4*)(to + ((int)threadIdx.x & 63) * L::VEC) = zero;
@@ -146,10 +161,6 @@ struct Filler {
                 to += STEP / L::KB_ROWS * L::KB;
             }
         }
-    }
-    __device__ __forceinline__ static void send(const char* from, T* to) {
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                         (__attribute__((address_space(3))) void*)to, 16, 0, 0);
     }
 };
 

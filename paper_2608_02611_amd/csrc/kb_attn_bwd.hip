@@ -188,14 +188,10 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
             stage<DT, DP, kQueries, kThreads>(dt[buf], dout + h * p.dout.sh, p.dout.sl, i0, qlen, p.dim);
         }
         if (wave == 0) {
-            const int i = i0 + (lane & 31);
-            if (i < qlen)
-                __builtin_amdgcn_global_load_lds(
-                    (const __attribute__((address_space(1))) void*)(row_values + (int64_t)h * p.len_q + i +
-                                                                    (lane < 32 ? 0 : l.lse)),
-                    (__attribute__((address_space(3))) void*)rows[buf], 4, 0, 0);
-            else
-                rows[buf][lane] = lane < 32 ? 0.f : INFINITY;
+            const float* from = row_values + (int64_t)h * p.len_q + i0;
+            if (i0 + (lane & 31) >= qlen) rows[buf][lane] = lane < 32 ? 0.f : INFINITY;
+            else if (lane < 32) send<4>(background(from), lane * 4, 0, rows[buf]);
+            else send<4>(background(from + l.lse), (lane & 31) * 4, 0, rows[buf]);
         }
     };
 

@@ -18,16 +18,28 @@ constexpr int kThreads = 256;
 constexpr int kRows = kAttnRows;
 constexpr int kKeys = kAttnKeys;
 
-// The softmax state of a lane's query over the tiles so far: terms are
-// exp(scale (s - m)).  In 16 bits m is a reference that follows the maximum only when a
-// term would pass 2^kSlack (scaling the sums takes as long as a quarter of a
-// tile's products), and next to l, the sum of the terms, there is the sum of the
-// rounded terms, those whose product with v is divided by it: where one term
-// outweighs the others, o is its v to the last bit.  In 32 bits m is the maximum.
+// The softmax state of a lane's query over the tiles so far: terms are exp(scale
+// (s - m)).  In 32 bits m is the maximum.  In 16 bits it is a reference, held as
+// scale m / ln 2 (one instruction makes a term's exponent), that follows the
+// maximum only when a term would pass 2^kSlack (scaling the sums takes as long as
+// a quarter of a tile's products), and next to l, the sum of the terms, there is
+// the sum of the rounded terms, those whose product with v is divided by it:
+// where one term outweighs the others, o is its v to the last bit.
 constexpr float kSlack = 8.f;
 struct Softmax {
     float m = -INFINITY, l = 0.f, rounded = 0.f;
 };
+
+// What m is held in: log2 units of m, and natural ones.  (Scale over what the
+// scores are multiplied by: the rounding of that factor leaves lse again.)
+template <int DT>
+__device__ __forceinline__ float unit_log2(float scale) {
+    return DT == DT_F32 ? scale * kLog2e : 1.f;
+}
+template <int DT>
+__device__ __forceinline__ float unit_natural(float scale) {
+    return DT == DT_F32 ? scale : scale / (scale * kLog2e);
+}
 
 template <int DT>
 __device__ __forceinline__ float add_terms(frag_t<DT> f, float l) {
@@ -49,16 +61,20 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
                                              float to_log2, int hi) {
     const int g = rd.lane >> 5;
     float &m = sm.m, &l = sm.l;
-    const float ref = DT == DT_F32 || m == -INFINITY ? 0.f : -m;  // the products start from -m
-    f32x16 s[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][r] = ref;
+    f32x16 s[2] = {};
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
         for (int t = 0; t < 2; ++t) s[t] = mma(rd.row_frag(kt, 32 * t, c), qf[c], s[t]);
+    constexpr bool AHEAD = DT != DT_F32 && !(PART && CAREFUL);
+    constexpr int P = DP / 16;  // products with v for 32 keys
+    constexpr int F = 4;        // their values are read that many products ahead
+    frag_t<DT> a[F];
+    const auto values = [&](int n) { return rd.col_frag(vt, n / P * 32 + n % P / (DP / 32) * 16, n % (DP / 32)); };
+    if (AHEAD) {
+#pragma unroll
+        for (int n = 0; n < F; ++n) a[n] = values(n);
+    }
     if (DT != DT_F32) {
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -80,48 +96,67 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
 #pragma unroll
     for (int r = 1; r < 16; ++r)
         top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[0][r], s[1][r]), top);
-    top = __builtin_elementwise_maximum(top, other_half(top));
-    float shift = 0.f;  // taken from the scores
-    if constexpr (DT == DT_F32) {
-        const float now = fmaxf(m, top);
-        shift = now == -INFINITY ? 0.f : now;  // nothing seen yet: every term is 0
-        const float alpha = __builtin_amdgcn_exp2f((m - shift) * to_log2);
+    const auto follow = [&](float now, float alpha) {
         m = now;
         l *= alpha;
+        sm.rounded *= alpha;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
+    };
+    if constexpr (DT == DT_F32) {
+        const float now = fmaxf(m, __builtin_elementwise_maximum(top, other_half(top)));
+        follow(now, now == m ? 1.f : __builtin_amdgcn_exp2f((m - now) * to_log2));
     } else {
+        // either half of the row says alone whether the reference has to follow
         const bool none = m == -INFINITY;
-        const bool move = none ? top > -INFINITY : top * to_log2 > kSlack;
-        if (__any(move)) {
-            const float now = move ? (none ? top : m + top) : m;
-            shift = move ? (none ? top : now - m) : 0.f;
-            const float alpha = none ? 1.f : __builtin_amdgcn_exp2f(-shift * to_log2);
-            m = now;
-            l *= alpha;
-            sm.rounded *= alpha;
-#pragma unroll
-            for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[t][r] -= shift;
+        if (__any(none ? top > -INFINITY : fmaf(top, to_log2, -m) > kSlack)) {
+            top = __builtin_elementwise_maximum(top, other_half(top)) * to_log2;
+            const float now = top > (none ? m : m + kSlack) ? top : m;
+            follow(now, now == m ? 1.f : __builtin_amdgcn_exp2f(m - now));
         }
     }
+    const float ref = m == -INFINITY ? 0.f : m;  // nothing seen yet: every term is 0
+    const auto term = [&](float x) {
+        return __builtin_amdgcn_exp2f(DT == DT_F32 ? (x - ref) * to_log2 : fmaf(x, to_log2, -ref));
+    };
+    if constexpr (AHEAD) {
+        // The second 32 keys' terms are made between the first 32's products.
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+        for (int r = 0; r < 16; ++r) l += s[0][r] = term(s[0][r]);
+        frag_t<DT> b[2] = {narrow<DT>(s[0], 0), narrow<DT>(s[0], 1)};
+        sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[t][r] = __builtin_amdgcn_exp2f((DT == DT_F32 ? s[t][r] - shift : s[t][r]) * to_log2);
-            l += s[t][r];
+        for (int n = 0; n < 2 * P; ++n) {
+            if (n == P) {
+                b[0] = narrow<DT>(s[1], 0);
+                b[1] = narrow<DT>(s[1], 1);
+            }
+            acc[n % (DP / 32)] = mma(a[n % F], b[n % P / (DP / 32)], acc[n % (DP / 32)]);
+            if (n + F < 2 * P) a[n % F] = values(n + F);
+            if (n < P) {
+#pragma unroll
+                for (int r = n * 16 / P; r < (n + 1) * 16 / P; ++r) s[1][r] = term(s[1][r]);
+#pragma unroll
+                for (int r = (n - 1) * 16 / P; n > 0 && r < n * 16 / P; ++r) l += s[1][r];
+            } else if (n == P) {
+#pragma unroll
+                for (int r = (P - 1) * 16 / P; r < 16; ++r) l += s[1][r];
+                sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
-        const frag_t<DT> b[2] = {narrow<DT>(s[t], 0), narrow<DT>(s[t], 1)};
-        if (DT != DT_F32) sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
-        mma_rows<DT, DP, PART && CAREFUL>(acc, vt, rd, 32 * t, b, 0, hi);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) l += s[t][r] = term(s[t][r]);
+            const frag_t<DT> b[2] = {narrow<DT>(s[t], 0), narrow<DT>(s[t], 1)};
+            if (DT != DT_F32) sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
+            mma_rows<DT, DP, PART && CAREFUL>(acc, vt, rd, 32 * t, b, 0, hi);
+        }
     }
 }
 
@@ -213,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     store_column<DT, DP>((T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl, acc, 1.f / (DT == DT_F32 ? l : rounded), some, p.dim, g);
     if (g == 0)
         p.lse[((int64_t)at.b * p.heads + hq) * p.len_q + i] =
-            some ? fmaf(sm.m, p.scale, kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
+            some ? fmaf(sm.m, unit_natural<DT>(p.scale), kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
 }
 
 // The parts of a row joined: each part's sums are relative to its own m.  A
@@ -230,12 +265,12 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnParams p) {
     const float* in = p.ws + row * p.parts * stride;
     float m = -INFINITY;
     for (int s = 0; s < p.parts; ++s) m = fmaxf(m, in[s * stride + stride - 4]);
-    const float shift = m == -INFINITY ? 0.f : m, to_log2 = p.scale * kLog2e;
+    const float shift = m == -INFINITY ? 0.f : m;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f, rounded = 0.f;
     for (int s = 0; s < p.parts; ++s) {
         const f32x4 stat = *(const f32x4*)(in + s * stride + stride - 4), x = *(const f32x4*)(in + s * stride + d);
-        const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * to_log2);
+        const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * unit_log2<DT>(p.scale));
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
         l = fmaf(w, stat[1], l);
@@ -249,7 +284,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnParams p) {
     store_quad<DT>((T*)p.o.p + b * p.o.sb + hq * p.o.sh + i * p.o.sl, d, p.dim, some ? acc[0] * f : 0.f,
                    some ? acc[1] * f : 0.f, some ? acc[2] * f : 0.f, some ? acc[3] * f : 0.f);
     if (d == 0)
-        p.lse[((int64_t)b * p.heads + hq) * p.len_q + i] = some ? fmaf(m, p.scale, kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
+        p.lse[((int64_t)b * p.heads + hq) * p.len_q + i] = some ? fmaf(m, unit_natural<DT>(p.scale), kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
 }
 
 template <int DT, int DP>

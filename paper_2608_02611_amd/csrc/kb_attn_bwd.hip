@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     const auto sees = [&](int key) { return p.causal ? min(qlen, max(0, key - (klen - qlen))) : 0; };
     const int lo = sees(j);
     const int start = first < klen ? sees(first) / kQueries * kQueries : qlen;
+    const bool wave_live = first + wave * 32 < klen;
     const int wave_lo = sees(first + wave * 32);
     const int block_hi = sees(first + kKeyRows - 1);  // from here on every key is seen
     const int steps = (qlen - start + kQueries - 1) / kQueries;  // tiles of one head
@@ -214,13 +215,13 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     for (; tile < end; ++h, i0 = start) {
         for (; tile < end && i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1, ++tile) {
             next();
-            if (i0 + kQueries > wave_lo)
+            if (wave_live && i0 + kQueries > wave_lo)
                 tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p,
                                                  lo - i0);
         }
         for (; tile < end && i0 < qlen; i0 += kQueries, buf ^= 1, ++tile) {
             next();
-            tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
+            if (wave_live) tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
         }
     }
     if (!CAREFUL && p.causal) {
@@ -288,12 +289,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     __shared__ __align__(16) T vt[2][L::size(kKeys)];
     __shared__ float scratch[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
-    const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
+    const int n_blocks = pair_blocks(p);
     const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, n_blocks);
-    const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;
+    const uint32_t first = (uint32_t)(n_blocks - 1 - at.block) * kRows;
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
 
-    const int64_t row = first + wave * 32 + (lane & 31);
+    const uint32_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
     const bool exists = i < p.len_q, live = i < qlen;
     const int wave_first = __builtin_amdgcn_readfirstlane((int)((first + wave * 32) / p.group));
@@ -386,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         // first the tiles that every row of the work-group sees whole
         for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
-            tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0);
+            if (wave_any > 0) tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             next();

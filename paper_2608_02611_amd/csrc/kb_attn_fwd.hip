@@ -169,12 +169,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     __shared__ __align__(16) T vt[2][L::size(kKeys)];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
     const int part = (int)blockIdx.y;
-    const int n_blocks = (int)(((int64_t)p.len_q * p.group + kRows - 1) / kRows);
+    const int n_blocks = pair_blocks(p);
     const HeadBlock at = head_block(blockIdx.x, p.kv_heads, p.batch * p.kv_heads, n_blocks);
-    const int64_t first = (int64_t)(n_blocks - 1 - at.block) * kRows;  // causal: the longest first
+    const uint32_t first = (uint32_t)(n_blocks - 1 - at.block) * kRows;  // causal: the longest first
     const int qlen = seq_len(p.q_lens, at.b, p.len_q), klen = seq_len(p.k_lens, at.b, p.len_k);
 
-    const int64_t row = first + wave * 32 + (lane & 31);
+    const uint32_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / p.group), hq = at.h * p.group + (int)(row % p.group);
     const bool exists = i < p.len_q, live = i < qlen;
     const int wave_first = __builtin_amdgcn_readfirstlane((int)((first + wave * 32) / p.group));
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
         // first the tiles that every row of the work-group sees whole
         for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
-            tile_forward<DT, DP, false, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+            if (wave_any > 0) tile_forward<DT, DP, false, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             next();

@@ -77,6 +77,7 @@ struct AttnParams {
     int len_q, len_k, dim;
     float scale;
     int causal;
+    int f32;        // binary32 elements, whose products take eight times as long
     int parts;      // forward, dq: parts of the keys
     int key_parts;  // dk, dv: parts of the queries
     int whole;  // rows of q, k, v (and o, dout) are aligned to 16 bytes and made of 16-byte chunks
@@ -98,24 +99,31 @@ inline int attn_parts(int64_t work_groups, int64_t passing, int64_t fill, int64_
     const int64_t want = fill / work_groups, most = passing / least;
     return (int)(want < most ? want : most > 1 ? most : 1);
 }
-inline int64_t row_blocks(const AttnParams& p) {
-    return (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_q * p.group + kAttnRows - 1) / kAttnRows);
+// Blocks of query rows for each (batch, key head) pair: fewer than 2^24 over all
+// pairs, so that rows within one are numbered in 32 bits.
+__host__ __device__ inline int pair_blocks(const AttnParams& p) {
+    return (int)(((int64_t)p.len_q * p.group + kAttnRows - 1) / kAttnRows);
 }
+inline int64_t row_blocks(const AttnParams& p) { return (int64_t)p.batch * p.kv_heads * pair_blocks(p); }
 inline int64_t key_blocks(const AttnParams& p) {
     return (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_k + kAttnKeyRows - 1) / kAttnKeyRows);
 }
 // Forward: two work-groups for each of 256 CUs, and as many again, as the parts
-// of a ragged batch end at different times.
-inline int forward_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 1024, 512); }
+// of a ragged batch end at different times.  In 32 bits parts may be shorter (8
+// heads x 100 queries on 1000 keys: 43 us, 146 with parts of 512).
+inline int forward_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 1024, p.f32 ? 128 : 512); }
 // Backward: one or two work-groups a CU, and as many again under a causal mask,
 // whose blocks are long and short (2 x 32 heads on 8 x 4096: 902 us with dk and
-// dv in two parts, 1086 in one).
-inline int64_t backward_fill(const AttnParams& p) { return p.causal ? 1024 : 512; }
+// dv in two parts, 1086 in one).  In 32 bits a CU holds one work-group: a round of
+// them and a quarter more, as those of short sequences end at once (2 x 12 heads,
+// 513 x 257: 100 us, 116 with twice as many parts); but parts may be shorter, a
+// tile taking 6 us (8 heads x 300: 48 us, 62 with parts of 128).
+inline int64_t backward_fill(const AttnParams& p) { return (p.f32 ? 320 : 512) * (p.causal ? 2 : 1); }
 inline int row_parts(const AttnParams& p) {
-    return attn_parts(row_blocks(p), p.len_k, backward_fill(p), 2 * kAttnKeys);
+    return attn_parts(row_blocks(p), p.len_k, backward_fill(p), (p.f32 ? 1 : 2) * kAttnKeys);
 }
 inline int key_parts(const AttnParams& p) {
-    return attn_parts(key_blocks(p), (int64_t)p.len_q * p.group, backward_fill(p), 4 * kAttnQueries);
+    return attn_parts(key_blocks(p), (int64_t)p.len_q * p.group, backward_fill(p), (p.f32 ? 2 : 4) * kAttnQueries);
 }
 
 // Workspace of the forward pass in parts, in floats: for each query row and part

@@ -219,6 +219,7 @@ bool attn_sizes(const kb_tensor& q, const kb_tensor& k, AttnParams* p) {
     p->len_q = (int)q.shape[2];
     p->len_k = (int)k.shape[2];
     p->dim = (int)q.shape[3];
+    p->f32 = q.dtype == DT_F32;
     // a launch has fewer than 2^32 threads: 2^24 work-groups of 256
     const int64_t most = ((int64_t)1 << 24) - 1;
     const int64_t norm_blocks = q.shape[0] * k.shape[1] * ((k.shape[2] + kNormBlock - 1) / kNormBlock);

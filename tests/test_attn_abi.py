@@ -94,7 +94,7 @@ def test_workspace_bytes(L):
         assert L.kb_attn_forward_workspace_bytes(view(1, q), view(1, k)) == 0
     # few rows on many keys: parts of their sums, binary32
     q, k = (1, 2, 1, 61), (1, 1, 5000, 61)
-    assert L.kb_attn_forward_workspace_bytes(view(1, q), view(1, k)) == 4 * 2 * 9 * (64 + 4)
+    assert L.kb_attn_forward_workspace_bytes(view(1, q), view(1, k)) == 4 * 2 * 39 * (64 + 4)
     assert L.kb_attn_backward_workspace_bytes(view(1, q), view(1, k)) >= 4 * 2 * 39 * 64
     assert L.kb_attn_forward_workspace_bytes(None, view(1, k)) == 0
 

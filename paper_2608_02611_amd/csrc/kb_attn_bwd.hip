@@ -87,6 +87,19 @@ __device__ __forceinline__ float score_scale(float dout_sq, float v_sq) {
 constexpr int kKeyRows = kAttnKeyRows;
 constexpr int kQueries = kAttnQueries;
 
+// Order of N products, each with READS of its own: those of AHEAD products are
+// under way before the first product.
+template <int N, int AHEAD, int READS = 1>
+__device__ __forceinline__ void reads_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD * READS, 0);
+#pragma unroll
+    for (int k = 0; k < N - AHEAD; ++k) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 // One tile of queries for a wave's 32 keys: s and t with a key a column.  PART:
 // the lane's key is seen by the tile's queries from lo on.
 template <int DT, int DP, bool PART, bool CAREFUL>
@@ -270,6 +283,7 @@ __device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t
             s = mma(rd.row_frag(kt, 32 * u, c), qf[c], s);
             t = mma(rd.row_frag(vt, 32 * u, c), df[c], t);
         }
+        if (DT != DT_F32 && !(PART && CAREFUL)) reads_ahead<DP / 8, 4>();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             t[r] = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse)) * (t[r] - dot);
@@ -277,6 +291,10 @@ __device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t
         }
         const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
         mma_rows<DT, DP, PART && CAREFUL>(dq, kt, rd, 32 * u, tf, 0, hi);
+        if (DT != DT_F32 && !(PART && CAREFUL)) {
+            reads_ahead<DP / 16, 3, 2>();
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
 }
 

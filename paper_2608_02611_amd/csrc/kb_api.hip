@@ -12,6 +12,7 @@
 #include <vector>
 
 #include "kb_device.hpp"
+#include "kb_error.hpp"
 #include "kb_internal.hpp"
 #include "kb_rung.hpp"
 

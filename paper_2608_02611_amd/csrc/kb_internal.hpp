@@ -10,12 +10,6 @@
 
 namespace kb {
 
-// The calling thread's error text (kb_api.hip): fail() stores the message and
-// returns code, clear_error() empties it.
-int fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-int fail_hip(hipError_t e, const char* what);
-void clear_error();
-
 // One entry of the launch table.  The table holds the accepted candidates
 // in call order, then the rejected candidates: one entry per candidate.  (The
 // last candidate group is padded inside the kernel with the reference, which

@@ -4,6 +4,7 @@
 
 #include <cmath>
 
+#include "kb_error.hpp"
 #include "kb_internal.hpp"
 #include "kb_ops.hpp"
 

@@ -268,15 +268,16 @@ constexpr int kRows = kAttnRows;
 constexpr int kKeys = kAttnKeys;
 
 // One tile of keys for a wave's 32 query rows; PART: the lane's row sees the
-// tile's keys below hi.
+// tile's keys below hi, one of its rows those below seen.
 template <int DT, int DP, bool PART, bool CAREFUL>
 __device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t<DT> (&qf)[DP / 16],
                                              const frag_t<DT> (&df)[DP / 16], const storage_t<DT>* kt,
                                              const storage_t<DT>* vt, const Reader<DT, DP>& rd, float to_log2,
-                                             float lse, float dot, int hi) {
+                                             float lse, float dot, int hi, int seen) {
     const int g = rd.lane >> 5;
 #pragma unroll
     for (int u = 0; u < kKeys / 32; ++u) {
+        if (PART && 32 * u >= seen) break;
         f32x16 s = {}, t = {};
 #pragma unroll
         for (int c = 0; c < DP / 16; ++c) {
@@ -405,12 +406,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         // first the tiles that every row of the work-group sees whole
         for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
-            if (wave_any > 0) tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0);
+            if (wave_any > 0) tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0, 0);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             next();
             if (j0 < wave_any)
-                tile_queries<DT, DP, true, CAREFUL>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, lim - j0);
+                tile_queries<DT, DP, true, CAREFUL>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, lim - j0, wave_any - j0);
         }
     };
     pass(std::false_type{});

@@ -108,10 +108,13 @@ inline int64_t row_blocks(const AttnParams& p) { return (int64_t)p.batch * p.kv_
 inline int64_t key_blocks(const AttnParams& p) {
     return (int64_t)p.batch * p.kv_heads * (((int64_t)p.len_k + kAttnKeyRows - 1) / kAttnKeyRows);
 }
-// Forward: two work-groups for each of 256 CUs, and as many again, as the parts
-// of a ragged batch end at different times.  In 32 bits parts may be shorter (8
-// heads x 100 queries on 1000 keys: 43 us, 146 with parts of 512).
-inline int forward_parts(const AttnParams& p) { return attn_parts(row_blocks(p), p.len_k, 1024, p.f32 ? 128 : 512); }
+// Forward: two work-groups for each of 256 CUs; for sequences of different
+// lengths, whose parts end at different times, as many again (512 queries on
+// 16,384 keys of one sequence: 8 parts cost 15 us to join).  In 32 bits parts may
+// be shorter (8 heads x 100 queries on 1000 keys: 43 us, 146 with parts of 512).
+inline int forward_parts(const AttnParams& p) {
+    return attn_parts(row_blocks(p), p.len_k, p.q_lens || p.k_lens ? 1024 : 512, p.f32 ? 128 : 512);
+}
 // Backward: one or two work-groups a CU, and as many again under a causal mask,
 // whose blocks are long and short (2 x 32 heads on 8 x 4096: 902 us with dk and
 // dv in two parts, 1086 in one).  In 32 bits a CU holds one work-group: a round of

@@ -227,7 +227,12 @@ bool attn_sizes(const kb_tensor& q, const kb_tensor& k, AttnParams* p) {
     return row_blocks(*p) <= most && key_blocks(*p) <= most && norm_blocks <= most;
 }
 
-size_t forward_bytes(const AttnParams& p) { return (size_t)forward_floats(p, forward_parts(p)) * sizeof(float); }
+// Sequences of different lengths take the more parts.
+size_t forward_bytes(AttnParams p) {
+    static const int32_t len = 0;
+    p.k_lens = &len;
+    return (size_t)forward_floats(p, forward_parts(p)) * sizeof(float);
+}
 // A causal mask takes the more parts.
 size_t backward_bytes(AttnParams p) {
     p.causal = 1;

@@ -102,7 +102,8 @@ __device__ __forceinline__ void stage(storage_t<DT>* tile, const storage_t<DT>* 
 // Memory straight to LDS, BYTES a lane, in the order of the lanes: from the
 // address, the same in all lanes, plus two offsets, one a lane's.  As buffer loads: while
 // a global or flat one is under way, the compiler waits for all of a wave's LDS
-// reads wherever it needs the oldest (191 us of 4 x 32 heads x 2047 then).
+// reads wherever it needs the oldest (backward of 4 x 32 heads x 2047 f16: 612 us, 638
+// with global loads).
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t background(const void* address) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(address), 0, 0x7FFFFFFF, 0x00020000);
 }

@@ -11,6 +11,13 @@
 // F16 holds p and t of a long row badly (its least normal number is 6e-5), so
 // they are scaled by powers of two before they are rounded: p, at most 1, by
 // 2^10; t, at most 2 |dout| |v|, so that this bound comes to at most 2^15.
+//
+// Measured on an MI355X: 4 x 32 heads x 2047, dim 128, f16, causal: 590 us, of
+// which dk and dv take 330 and dq 241: 0.58 PFLOP/s of the 5 products, 0.81 of the 7
+// that are done, where a large library product reaches 1.2.  Of its time the kernel
+// for dk and dv has matrix instructions under way for 44% and LDS reads for 66%
+// (each product of 32 x 32 reads one or two operands there; twice as many keys a
+// wave would halve that, at 512 registers a lane).
 #include <type_traits>
 
 #include "kb_attn.hpp"

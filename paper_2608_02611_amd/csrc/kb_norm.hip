@@ -7,6 +7,10 @@
 // over the rows:      dw = S_rows(dy z), db = S_rows(dy).
 // Both move bytes: forward reads x and writes y, backward reads dy and x and
 // writes dx; the arithmetic is 8 to 14 operations an element.
+//
+// Measured on an MI355X, where a copy of 4 GB moves 4.8 TB/s: forward of 16,384 x
+// 4096 f16 53 us, 5.1 TB/s; backward of the same in bf16 85 us, 4.7 TB/s; backward of
+// 4095 x 4097 f32 56 us, 3.6 TB/s; 16 rows of 4096, a call's own time, 7 us.
 #include "kb_ops.hpp"
 
 namespace kb {

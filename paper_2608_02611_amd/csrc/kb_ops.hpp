@@ -116,8 +116,8 @@ inline int forward_parts(const AttnParams& p) {
     return attn_parts(row_blocks(p), p.len_k, p.q_lens || p.k_lens ? 1024 : 512, p.f32 ? 128 : 512);
 }
 // Backward: one or two work-groups a CU, and as many again under a causal mask,
-// whose blocks are long and short (2 x 32 heads on 8 x 4096: 902 us with dk and
-// dv in two parts, 1086 in one).  In 32 bits a CU holds one work-group: a round of
+// whose blocks are long and short (2 x 32 heads on 8 x 4096: 854 us with dk and
+// dv in two parts, 1005 in one).  In 32 bits a CU holds one work-group: a round of
 // them and a quarter more, as those of short sequences end at once (2 x 12 heads,
 // 513 x 257: 100 us, 116 with twice as many parts); but parts may be shorter, a
 // tile taking 6 us (8 heads x 300: 48 us, 62 with parts of 128).

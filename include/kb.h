@@ -727,7 +727,7 @@ typedef struct kb_attn_opts {
  * (which may be 0: then NULL will do); it needs no initialisation.
  * Errors: KB_ERR_INVALID_ARG (null descriptors or data, shapes that do not
  * fit, dim not in [1, KB_ATTN_MAX_DIM], strides, scale or flags out of
- * range), KB_ERR_DTYPE, KB_ERR_ALIGNMENT, KB_ERR_WORKSPACE, KB_ERR_HIP. */
+ * range, 2^24 or more blocks of 128 query rows or of 64 keys in all), KB_ERR_DTYPE, KB_ERR_ALIGNMENT, KB_ERR_WORKSPACE, KB_ERR_HIP. */
 size_t kb_attn_forward_workspace_bytes(const kb_tensor* q, const kb_tensor* k);
 int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
                     const kb_attn_opts* opts, const kb_tensor* o, float* lse, void* workspace,

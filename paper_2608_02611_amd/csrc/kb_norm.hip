@@ -184,8 +184,8 @@ hipError_t norm_forward_rows(const NormForwardParams& p, hipStream_t stream) {
 
 // Backward: dy and x of a row in registers for the two sums and dx; dw and db of
 // the thread's columns add up over the rows that it sees.  At the end the row
-// groups of a work-group are added in LDS, in their order, and written as one
-// part.
+// groups of a work-group meet in LDS and are added in their order, a column a
+// thread, as one part.
 // SUMS: with dw and db.  They take two registers a column, too many for rows of
 // more than 8192 (spilled, 4096 x 16,384 f32 took 290 us): there a pass of its
 // own over dy and x adds the columns.
@@ -259,35 +259,36 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
     if constexpr (SUMS) {
         if (!p.dw && !p.db) return;
         float* part = p.part + (int64_t)blockIdx.x * 2 * p.cols;
+        typedef float f32x4 __attribute__((ext_vector_type(4)));
         if constexpr (ROWS > 1) {
-            __shared__ float sums[2][TPR * E];
-#pragma unroll 1
-            for (int k = 0; k < ROWS; ++k) {
-                if (group == k) {
+            __shared__ __align__(16) float sums[2][ROWS][TPR * E];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        sums[0][e * TPR + t] = k ? sums[0][e * TPR + t] + dw[e] : dw[e];
-                        sums[1][e * TPR + t] = k ? sums[1][e * TPR + t] + db[e] : db[e];
-                    }
-                }
-                __syncthreads();
+            for (int e = 0; e < E; e += 4) {
+                const int c = (e / N * TPR + t) * N + e % N;
+                *(f32x4*)&sums[0][group][c] = f32x4{dw[e], dw[e + 1], dw[e + 2], dw[e + 3]};
+                *(f32x4*)&sums[1][group][c] = f32x4{db[e], db[e + 1], db[e + 2], db[e + 3]};
             }
-            if (group > 0) return;
+            __syncthreads();
+            for (int c = (int)threadIdx.x; c < p.cols; c += block_of(TPR)) {
+                float w = sums[0][0][c], b = sums[1][0][c];
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                dw[e] = sums[0][e * TPR + t];
-                db[e] = sums[1][e * TPR + t];
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < R::NV; ++i) {
-            const int c = (i * TPR + t) * N;
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (c + e < p.cols) {
-                    part[c + e] = dw[i * N + e];
-                    part[p.cols + c + e] = db[i * N + e];
+                for (int k = 1; k < ROWS; ++k) {
+                    w += sums[0][k][c];
+                    b += sums[1][k][c];
                 }
+                part[c] = w;
+                part[p.cols + c] = b;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; e += 4) {
+                const int c = (e / N * TPR + t) * N + e % N;
+                const float w[4] = {dw[e], dw[e + 1], dw[e + 2], dw[e + 3]}, b[4] = {db[e], db[e + 1], db[e + 2], db[e + 3]};
+                if (c < p.cols) {
+                    store_vec(part + c, p.cols - c, w);
+                    store_vec(part + p.cols + c, p.cols - c, b);
+                }
+            }
         }
     }
 }

@@ -9,8 +9,8 @@
 // writes dx; the arithmetic is 8 to 14 operations an element.
 //
 // Measured on an MI355X, where a copy of 4 GB moves 4.8 TB/s: forward of 16,384 x
-// 4096 f16 53 us, 5.1 TB/s; backward of the same in bf16 85 us, 4.7 TB/s; backward of
-// 4095 x 4097 f32 56 us, 3.6 TB/s; 16 rows of 4096, a call's own time, 7 us.
+// 4096 f16 54 us, 5.0 TB/s; backward of the same in bf16 80 us, 5.0 TB/s; backward of
+// 4095 x 4097 f32 53 us, 3.8 TB/s; 16 rows of 4096, a call's own time, 7 us.
 #include "kb_ops.hpp"
 
 namespace kb {
@@ -327,7 +327,7 @@ template <int DT, int WDT, int TPR, int E>
 hipError_t norm_backward_rows(const NormBackwardParams& p, hipStream_t stream) {
     constexpr int ROWS = block_of(TPR) / TPR;
     const int64_t groups = (p.rows + ROWS - 1) / ROWS;
-    const int parts = norm_parts(groups, (int64_t)p.cols * (int64_t)sizeof(storage_t<DT>));
+    const int parts = norm_parts(groups, p.cols, sizeof(storage_t<DT>));
     if (parts > 0)
         norm_backward_rows_kernel<DT, WDT, TPR, E, true><<<dim3((unsigned)parts), block_of(TPR), 0, stream>>>(p);
     return p.dw || p.db ? norm_backward_join<WDT>(p, parts, stream) : hipGetLastError();
@@ -482,7 +482,7 @@ hipError_t norm_backward_rows_long(const NormBackwardParams& p, hipStream_t stre
             norm_backward_dx_long_kernel<DT, WDT><<<dim3((unsigned)p.rows), kThreads, 0, stream>>>(p);
     }
     if (!p.dw && !p.db) return hipGetLastError();
-    const int parts = norm_parts(p.rows, INT64_MAX);
+    const int parts = norm_parts(p.rows, p.cols, sizeof(storage_t<DT>));
     constexpr int strip = kThreads * Vec16<storage_t<DT>>::N;
     if (parts > 0)
         norm_backward_part_long_kernel<DT>

@@ -42,17 +42,19 @@ struct NormBackwardParams {
 };
 
 // Row stripes whose column sums are kept apart (NormBackwardParams::part): one
-// for each work-group.  Rows of 512 bytes to 2 KB get twice as many, as a
-// work-group has few bytes on their way (65,536 x 256 f32: 40 us, 73 with 512;
-// 16,384 x 1024 f32, longer rows: 49 us, 41 with 512).
-inline int norm_parts(int64_t rows, int64_t row_bytes) {
-    const int64_t most = row_bytes > 512 && row_bytes < 2048 ? 1024 : 512;
-    return (int)(rows < most ? rows : most);
+// for each work-group.  Rows of more than 128 columns and at most 512 bytes get
+// twice as many, as a work-group of four such rows has few bytes on their way
+// (65,536 x 256 bf16: 32 us, 37 with 512 parts; 16,384 x 1024 bf16, longer rows: 26
+// us, 31 with 1024; 65,536 x 64, sixteen rows a work-group: 14 us, 15 with 1024).
+constexpr int64_t kNormParts = 512;
+inline int norm_parts(int64_t groups, int64_t cols, int64_t element_bytes) {
+    const int64_t most = cols > 128 && cols * element_bytes <= 512 ? 2 * kNormParts : kNormParts;
+    return (int)(groups < most ? groups : most);
 }
 // Enough for every type.
 inline size_t norm_part_bytes(int64_t rows, int64_t cols) {
-    const int64_t most = cols < 1024 ? 1024 : 512, parts = rows < most ? rows : most;
-    return ((size_t)parts * 2 * (size_t)cols * sizeof(float) + 15) & ~(size_t)15;
+    const size_t parts = (size_t)norm_parts(rows, cols, 2);
+    return (parts * 2 * (size_t)cols * sizeof(float) + 15) & ~(size_t)15;
 }
 
 // dtype: x's and y's; wdtype: w's, b's, dw's and db's (dtype or DT_F32).

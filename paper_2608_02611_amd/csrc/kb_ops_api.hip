@@ -407,7 +407,7 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
     const Named outs[] = {{"dq", dq}, {"dk", dk}, {"dv", dv}, {"the workspace", &tw}};
     const Named ins[] = {{"dout", dout}, {"q", q}, {"k", k}, {"v", v}, {"o", o}, {"lse", &tl}};
     if ((rc = check_apart(call, outs, 4, ins, 6))) return rc;
-    if (p.batch == 0 || p.kv_heads == 0 || p.heads == 0) return KB_OK;
+    if (row_blocks(p) == 0 && key_blocks(p) == 0) return KB_OK;  // (keys that no query head reads have gradients, of 0)
     p.dout = head_view(dout);
     p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v) && whole_rows(*dout) && whole_rows(*o);
     p.o = head_view(o);

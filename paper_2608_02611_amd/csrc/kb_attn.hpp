@@ -130,6 +130,7 @@ struct Filler {
     static constexpr int STEPS = ROWS / STEP;
     static_assert(NT % SLOTS == 0 && ROWS % STEP == 0, "a tile is filled in whole steps");
     static_assert(STEP % 8 == 0, "turn() is the same in every step");
+    static_assert(ROWS <= kAttnReach, "a tile's last row is within reach of its first");
     int row0;
     uint32_t offset;  // bytes from the step's first row to the lane's chunk
     bool in;          // the chunk lies within dim
@@ -146,7 +147,7 @@ struct Filler {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         T* to = tile + wave * L::KB;
         const auto from = background(base + (int64_t)r0 * stride);
-        const int step = STEP * (int)stride * (int)sizeof(T);  // (64 rows are within 2^31 bytes)
+        const int step = STEP * (int)stride * (int)sizeof(T);  // (ROWS of them are within 2^31 bytes)
         if (r0 + ROWS <= n && dim == L::PITCH) {  // the common case, without a test for each chunk
 #pragma unroll
             for (int k = 0; k < STEPS; ++k) send<16>(from, offset, k * step, to + k * (STEP / L::KB_ROWS * L::KB));

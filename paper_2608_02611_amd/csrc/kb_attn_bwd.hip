@@ -184,8 +184,13 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     frag_t<DT> kf[DP / 16];
 #pragma unroll
     for (int c = 0; c < DP / 16; ++c) kf[c] = load_frag<DT, WHOLE>(k, c, g, p.dim, live);
-    if (WHOLE) Filler<DT, DP, kKeyRows, kThreads>(p.v.sl, p.dim).fill(vt, v, p.v.sl, first, klen, p.dim);
-    else stage<DT, DP, kKeyRows, kThreads>(vt, v, p.v.sl, first, klen, p.dim);
+    if (WHOLE) {
+        const Filler<DT, DP, kAttnReach, kThreads> fv(p.v.sl, p.dim);
+#pragma unroll
+        for (int r = 0; r < kKeyRows; r += kAttnReach) fv.fill(vt + L::size(r), v, p.v.sl, first + r, klen, p.dim);
+    } else {
+        stage<DT, DP, kKeyRows, kThreads>(vt, v, p.v.sl, first, klen, p.dim);
+    }
 
     // the queries that see a key: [sees(j), qlen)
     const auto sees = [&](int key) { return p.causal ? min(qlen, max(0, key - (klen - qlen))) : 0; };

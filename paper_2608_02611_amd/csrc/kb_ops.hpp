@@ -92,6 +92,9 @@ constexpr int kAttnRows = 128;
 constexpr int kAttnKeys = 64;
 constexpr int kAttnKeyRows = 128;
 constexpr int kAttnQueries = 32;
+// Rows that one buffer descriptor of 2^31 bytes has to reach (AttnParams::whole
+// bounds their stride); what is longer is filled piece by piece.
+constexpr int kAttnReach = 64;
 
 // What passes a work-group is split into parts, each with work-groups of its own
 // and joined afterwards, so that a few rows still fill the device: `fill`

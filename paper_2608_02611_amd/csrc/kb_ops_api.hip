@@ -190,13 +190,14 @@ int check_rows(const char* call, const kb_tensor& x) {
 
 HeadView head_view(const kb_tensor* t) { return HeadView{t->data, t->strides[0], t->strides[1], t->strides[2]}; }
 
-// Rows that can be read in aligned 16-byte chunks, 64 of them within 2^31 bytes.
+// Rows that can be read in aligned 16-byte chunks, kAttnReach of them within 2^31
+// bytes.
 bool whole_rows(const kb_tensor& t) {
     const int64_t n = 16 / element_bytes(t.dtype);
     if (((uintptr_t)t.data & 15u) || t.shape[3] % n) return false;
     for (int i = 0; i < 3; ++i)
         if (t.shape[i] > 1 && t.strides[i] % n) return false;
-    return t.shape[2] <= 1 || t.strides[2] < ((int64_t)1 << 25) / element_bytes(t.dtype);
+    return t.shape[2] <= 1 || t.strides[2] < ((int64_t)1 << 31) / kAttnReach / element_bytes(t.dtype);
 }
 
 constexpr int64_t kMaxLen = (int64_t)1 << 30;

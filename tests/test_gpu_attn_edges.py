@@ -6,7 +6,7 @@ import torch
 
 import paper_2608_02611_amd as kb
 from tests.helpers import ensure_built
-from tests.test_gpu_attn import DT, heads
+from tests.test_gpu_attn import DT, heads, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,25 @@ def test_no_query_heads(dtype, causal, nq, nk):
     dk, dv = torch.full_like(k, 7.0), torch.full_like(v, 7.0)
     dq, _, _ = kb.kb_attn_backward(q, q, k, v, o, lse, causal=causal, dk=dk, dv=dv)
     assert dq.numel() == 0 and torch.all(dk == 0) and torch.all(dv == 0)
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 128), ("f16", 40), ("bf16", 80), ("f32", 64), ("f32", 128)])
+@pytest.mark.parametrize("step", [(1 << 24) + (1 << 20), (1 << 25) - 16, 1 << 25])
+def test_value_rows_far_apart(dtype, d, step):
+    """Blocks of 128 value rows that are longer than the 2^31 bytes which one buffer descriptor reaches: strides of just
+    over 2^31 / 128 bytes, of the largest that 64 rows allow, and of more.  As dense ones, to the bit."""
+    t = DT[dtype]
+    n, nq, elements = 130, 140, step // torch.finfo(t).bits * 8
+    buf = torch.empty(n * elements, dtype=t, device="cuda")
+    v = buf.as_strided((1, 1, n, d), (0, 0, elements, 1))
+    k = buf.as_strided((1, 1, n, d), (0, 0, elements, 1), 1024)
+    dense_k, dense_v = normal((1, 1, n, d), t, 1), normal((1, 1, n, d), t, 2)
+    k.copy_(dense_k)
+    v.copy_(dense_v)
+    q, do = normal((1, 2, nq, d), t, 3), normal((1, 2, nq, d), t, 4)
+    want = kb.kb_attn_forward(q, dense_k, dense_v, causal=True)
+    got = kb.kb_attn_forward(q, k, v, causal=True)
+    got += kb.kb_attn_backward(do, q, k, v, *want, causal=True)
+    want += kb.kb_attn_backward(do, q, dense_k, dense_v, *want, causal=True)
+    for a, c in zip(got, want):
+        assert torch.equal(a, c)

@@ -88,7 +88,7 @@ __device__ __forceinline__ void load_weight(const W* w, int c, int n, float othe
     constexpr int M = Vec16<W>::N;
 #pragma unroll
     for (int k = 0; k < N; k += M) {
-        if (w != nullptr && c + k < n) {
+        if (w != nullptr && k < n - c) {
             const typename Vec16<W>::type v = load_vec(w, c + k, n);
 #pragma unroll
             for (int e = 0; e < M; ++e) out[k + e] = (float)v[e];
@@ -294,32 +294,40 @@ __global__ void __launch_bounds__(block_of(TPR)) norm_backward_rows_kernel(NormB
 }
 
 // dw and db from the parts: a column a lane, the parts dealt out to 16 waves,
-// whose sums are added in their order.
+// whose sums are added in their order.  A launch has fewer than 2^32 threads, so
+// its work-groups are limited and go over longer rows in strides.
 constexpr int kJoinWaves = 16;
+constexpr int64_t kJoinGroups = (int64_t)1 << 21;
 template <int WDT>
 __global__ void __launch_bounds__(64 * kJoinWaves) norm_backward_join_kernel(NormBackwardParams p, int parts) {
     using W = storage_t<WDT>;
     __shared__ float s[kJoinWaves][64];
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
-    const int64_t i = (int64_t)blockIdx.x * 64 + lane, n = 2 * (int64_t)p.cols;
-    float sum = 0.f;
-    if (i < n) {
+    const int64_t n = 2 * (int64_t)p.cols, step = (int64_t)gridDim.x * 64;
+    for (int64_t first = (int64_t)blockIdx.x * 64; first < n; first += step) {
+        const int64_t i = first + lane;
+        float sum = 0.f;
+        if (i < n) {
 #pragma unroll 8
-        for (int k = wave; k < parts; k += kJoinWaves) sum += p.part[(int64_t)k * n + i];
-    }
-    s[wave][lane] = sum;
-    __syncthreads();
-    if (wave > 0 || i >= n) return;
+            for (int k = wave; k < parts; k += kJoinWaves) sum += p.part[(int64_t)k * n + i];
+        }
+        s[wave][lane] = sum;
+        __syncthreads();
+        if (wave == 0 && i < n) {
 #pragma unroll
-    for (int k = 1; k < kJoinWaves; ++k) sum += s[k][lane];
-    W* out = (W*)(i < p.cols ? p.dw : p.db);
-    if (out) out[i < p.cols ? i : i - p.cols] = (W)sum;
+            for (int k = 1; k < kJoinWaves; ++k) sum += s[k][lane];
+            W* out = (W*)(i < p.cols ? p.dw : p.db);
+            if (out) out[i < p.cols ? i : i - p.cols] = (W)sum;
+        }
+        if (first + step < n) __syncthreads();  // (the sums are read)
+    }
 }
 
 template <int WDT>
 hipError_t norm_backward_join(const NormBackwardParams& p, int parts, hipStream_t stream) {
+    const int64_t groups = (2 * (int64_t)p.cols + 63) / 64;
     norm_backward_join_kernel<WDT>
-        <<<dim3((unsigned)((2 * (int64_t)p.cols + 63) / 64)), 64 * kJoinWaves, 0, stream>>>(p, parts);
+        <<<dim3((unsigned)(groups < kJoinGroups ? groups : kJoinGroups)), 64 * kJoinWaves, 0, stream>>>(p, parts);
     return hipGetLastError();
 }
 
@@ -334,6 +342,7 @@ hipError_t norm_backward_rows(const NormBackwardParams& p, hipStream_t stream) {
 }
 
 // ------------------------------------- rows that do not fit in the registers --
+// A column is a uint32_t: the step past the last one may pass 2^31.
 
 template <typename V, int N>
 __device__ __forceinline__ void widen(V v, float (&out)[N]) {
@@ -361,7 +370,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
     T* y = (T*)p.y.p + row * p.y.stride;
     const float inv = 1.f / (float)p.cols;
     float acc[1] = {0.f}, v[N];
-    for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
+    for (uint32_t c = threadIdx.x * N; c < (uint32_t)p.cols; c += kThreads * N) {
         widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) acc[0] += v[e];
@@ -369,11 +378,11 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
     block_sum(acc, s);
     const float mean = acc[0] * inv;
     acc[0] = 0.f;
-    for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
+    for (uint32_t c = threadIdx.x * N; c < (uint32_t)p.cols; c += kThreads * N) {
         widen(load_vec(x, c, p.cols), v);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float d = c + e < p.cols ? v[e] - mean : 0.f;
+            const float d = e < p.cols - (int)c ? v[e] - mean : 0.f;
             acc[0] = fmaf(d, d, acc[0]);
         }
     }
@@ -383,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) norm_forward_long_kernel(NormForward
         if (p.mean) p.mean[row] = mean;
         if (p.rstd) p.rstd[row] = rstd;
     }
-    for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
+    for (uint32_t c = threadIdx.x * N; c < (uint32_t)p.cols; c += kThreads * N) {
         widen(load_vec(x, c, p.cols), v);
         float w[N], b[N];
         load_weight<N>((const W*)p.w, c, p.cols, 1.f, w);
@@ -407,21 +416,21 @@ __global__ void __launch_bounds__(kThreads) norm_backward_dx_long_kernel(NormBac
     T* dx = (T*)p.dx.p + row * p.dx.stride;
     const float mean = p.mean[row], rstd = p.rstd[row], inv = 1.f / (float)p.cols;
     float acc[2] = {0.f, 0.f}, a[N], v[N];
-    for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
+    for (uint32_t c = threadIdx.x * N; c < (uint32_t)p.cols; c += kThreads * N) {
         widen(load_vec(dy, c, p.cols), a);
         widen(load_vec(x, c, p.cols), v);
         float w[N];
         load_weight<N>((const W*)p.w, c, p.cols, 1.f, w);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float g = a[e] * w[e], z = c + e < p.cols ? (v[e] - mean) * rstd : 0.f;
+            const float g = a[e] * w[e], z = e < p.cols - (int)c ? (v[e] - mean) * rstd : 0.f;
             acc[0] += g;
             acc[1] = fmaf(g, z, acc[1]);
         }
     }
     block_sum(acc, s);
     const float mg = acc[0] * inv, mgz = acc[1] * inv;
-    for (int c = threadIdx.x * N; c < p.cols; c += kThreads * N) {
+    for (uint32_t c = threadIdx.x * N; c < (uint32_t)p.cols; c += kThreads * N) {
         widen(load_vec(dy, c, p.cols), a);
         widen(load_vec(x, c, p.cols), v);
         float w[N];
@@ -441,8 +450,8 @@ template <int DT>
 __global__ void __launch_bounds__(kThreads) norm_backward_part_long_kernel(NormBackwardParams p, int parts) {
     using T = storage_t<DT>;
     constexpr int N = Vec16<T>::N;
-    const int c = (blockIdx.x * kThreads + threadIdx.x) * N;
-    if (c >= p.cols) return;
+    const uint32_t c = (blockIdx.x * kThreads + threadIdx.x) * N;
+    if (c >= (uint32_t)p.cols) return;
     float dw[N], db[N], a[N], v[N];
 #pragma unroll
     for (int e = 0; e < N; ++e) dw[e] = db[e] = 0.f;
@@ -460,9 +469,9 @@ __global__ void __launch_bounds__(kThreads) norm_backward_part_long_kernel(NormB
     float* out = p.part + (int64_t)blockIdx.y * 2 * p.cols;
 #pragma unroll
     for (int e = 0; e < N; ++e)
-        if (c + e < p.cols) {
+        if (e < p.cols - (int)c) {
             out[c + e] = dw[e];
-            out[p.cols + c + e] = db[e];
+            out[(int64_t)p.cols + c + e] = db[e];
         }
 }
 

@@ -228,7 +228,7 @@ template <typename T>
 __device__ __forceinline__ typename Vec16<T>::type settle_vec(typename Vec16<T>::type v, int c, int n) {
     using V = typename Vec16<T>::type;
     constexpr int N = Vec16<T>::N;
-    if (c + N > n && n >= N) v = __builtin_bit_cast(V, drop_elements<T>(__builtin_bit_cast(u32v4, v), c + N - n));
+    if (n >= N && c > n - N) v = __builtin_bit_cast(V, drop_elements<T>(__builtin_bit_cast(u32v4, v), c - (n - N)));
     return v;
 }
 template <typename T>

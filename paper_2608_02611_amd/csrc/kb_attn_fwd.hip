@@ -29,11 +29,17 @@ constexpr int kKeys = kAttnKeys;
 // The softmax state of a lane's query over the tiles so far: terms are exp(scale
 // (s - m)).  In 32 bits m is the maximum.  In 16 bits it is a reference, held as
 // scale m / ln 2 (one instruction makes a term's exponent), that follows the
-// maximum only when a term would pass 2^kSlack (scaling the sums takes as long as
-// a quarter of a tile's products), and next to l, the sum of the terms, there is
-// the sum of the rounded terms, those whose product with v is divided by it:
-// where one term outweighs the others, o is its v to the last bit.
-constexpr float kSlack = 8.f;
+// maximum only when a term would pass 2^kSlack of the one that set it (scaling the
+// sums takes as long as a quarter of a tile's products), and next to l, the sum of
+// the terms, there is the sum of the rounded terms, those whose product with v is
+// divided by it: where one term outweighs the others, o is its v to the last bit.
+// F16 holds small terms badly (subnormal from 2^-14, nothing under 2^-25), so there
+// the reference is set 2^kBelow under the maximum: terms of up to 2^15, and what the
+// format takes from one is at most 2^-34 of the largest.
+template <int DT>
+constexpr float kSlack = DT == DT_F16 ? 6.f : 8.f;
+template <int DT>
+constexpr float kBelow = DT == DT_F16 ? 9.f : 0.f;
 struct Softmax {
     float m = -INFINITY, l = 0.f, rounded = 0.f;
 };
@@ -119,9 +125,12 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
     } else {
         // either half of the row says alone whether the reference has to follow
         const bool none = m == -INFINITY;
-        if (__any(none ? top > -INFINITY : fmaf(top, to_log2, -m) > kSlack)) {
-            top = __builtin_elementwise_maximum(top, other_half(top)) * to_log2;
-            const float now = top > (none ? m : m + kSlack) ? top : m;
+        const auto passes = [&](float x) {
+            return none ? x > -INFINITY : fmaf(x, to_log2, -m) > kSlack<DT> + kBelow<DT>;
+        };
+        if (__any(passes(top))) {
+            top = __builtin_elementwise_maximum(top, other_half(top));
+            const float now = passes(top) ? fmaf(top, to_log2, -kBelow<DT>) : m;
             follow(now, now == m ? 1.f : __builtin_amdgcn_exp2f(m - now));
         }
     }

@@ -50,3 +50,21 @@ def test_value_rows_far_apart(dtype, d, step):
     want += kb.kb_attn_backward(do, q, dense_k, dense_v, *want, causal=True)
     for a, c in zip(got, want):
         assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("apart", [16.0, 17.4])
+def test_long_flat_tails_in_f16(apart):
+    """One score above 2^17 equal ones, whose terms (2^-23 and 2^-25.1 of it) count together.  A term is rounded to
+    within 2^-11 of itself or, below f16's normal numbers, 2^-34 of the largest; a sum of 2^17 in 32 bits is off by at
+    most 2^17 2^-24 of it; the result is rounded once.  66,000 rows: the keys are not in parts."""
+    n, rows, d = 1 << 17, 66000, 64
+    q, k = torch.zeros((1, 1, rows, d), device="cuda").half(), torch.zeros((1, 1, n, d), device="cuda").half()
+    q[..., 0], k[:, :, 5, 0] = 1.0, apart
+    v = torch.ones_like(k)
+    v[:, :, 5] = 0.0
+    o, _ = kb.kb_attn_forward(q, k, v, 1.0)
+    assert kb.kb_attn_forward_workspace_bytes(q, k) == 0
+    top = k[0, 0, 5, 0].double().exp().item()
+    want = (n - 1) / (top + n - 1)
+    err = float((o.double() - want).abs().max())
+    assert err <= want * (2.0 ** -11 + 2.0 ** -11 + 2.0 ** -7) + n * 2.0 ** -34, (err, want)

@@ -739,10 +739,11 @@ int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
  *   dq_i = scale sum_j t_ij k_j,  dk_j = scale sum_i t_ij q_i,
  *   dv_j = sum_i p_ij dout_i,
  * dk and dv summed over the query heads that share the key head.  Padding has
- * gradient 0.  dout, o, dq: q's shape; dk, dv: k's; lse: the forward call's.
- * One dtype throughout.  With a 16-bit dtype p and t are rounded to it before
- * their products (F16: scaled by powers of two so that small ones keep their
- * bits).  workspace: 16-byte aligned, not less than
+ * gradient 0, and so has a query with |lse| of 2^24 ln 2 or more, whose p cannot
+ * be computed again in binary32.  dout, o, dq: q's shape; dk, dv: k's; lse: the
+ * forward call's.  One dtype throughout.  With a 16-bit dtype p and t are rounded
+ * to it before their products (F16: scaled by powers of two so that small ones
+ * keep their bits).  workspace: 16-byte aligned, not less than
  * kb_attn_backward_workspace_bytes; it needs no initialisation.
  * Errors as kb_attn_forward. */
 size_t kb_attn_backward_workspace_bytes(const kb_tensor* q, const kb_tensor* k);

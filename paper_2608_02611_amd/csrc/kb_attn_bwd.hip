@@ -354,7 +354,9 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     }
     // D_i and lse_i / log 2, for here and for the keys' kernel.  A row with no
     // seen score has lse = -infinity, and its terms exp(-infinity - lse) are to be
-    // 0: it gets 0.  A row of the padding gets +infinity, which makes its terms 0.
+    // 0: it gets 0.  A row of the padding gets +infinity, which makes its terms 0, and
+    // so does one whose lse is held too coarsely for a term to be known even to a
+    // factor of 2 (they would be 0 or infinite, and end up in the keys' gradients).
     const int64_t at_row = ((int64_t)at.b * p.heads + hq) * p.len_q + i;
     const T* o = (const T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl;
     float dot = 0.f, sq = 0.f;
@@ -370,6 +372,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     dot += other_half(dot);
     float lse = live ? p.lse[at_row] : INFINITY;
     lse = lse == -INFINITY ? 0.f : lse * kLog2e;
+    if (fabsf(lse) >= 16777216.f) lse = INFINITY;
     if (part == 0 && exists && g == 0) {
         p.ws[at_row] = dot;
         p.ws[l.lse + at_row] = lse;

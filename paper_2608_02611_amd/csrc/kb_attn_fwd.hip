@@ -15,6 +15,7 @@
 // for about as long.  512 queries on 16,384 keys: 152 us, 0.89 PFLOP/s.  Single tokens
 // (16 ragged sequences of up to 8191 keys, 32 heads on 8): 91 us, 4.4 TB/s, where a
 // large copy moves 4.8.
+#include <cfloat>
 #include <type_traits>
 
 #include "kb_attn.hpp"
@@ -42,7 +43,19 @@ template <int DT>
 constexpr float kBelow = DT == DT_F16 ? 9.f : 0.f;
 struct Softmax {
     float m = -INFINITY, l = 0.f, rounded = 0.f;
+    bool low = false;
 };
+
+// Binary32 holds a reference of 2^22 or more too coarsely for terms relative to
+// it: by the rounding of scale m / ln 2 alone they would be 0 or infinite.  So a
+// reference is not set by scores below -2^22 (the lowest numbers of bf16 in a row of
+// k, as a mask; they are noted in `low`), and a work-group with a row that ends up
+// with such scores alone, or with a larger reference, computes its sums once more
+// (CAREFUL), m being a score as in 32 bits.
+constexpr float kCoarse = 4194304.f;
+__device__ __forceinline__ bool too_coarse(const Softmax& sm) {
+    return sm.m == -INFINITY ? sm.low : fabsf(sm.m) >= kCoarse;
+}
 
 // What m is held in: log2 units of m, and natural ones.  (Scale over what the
 // scores are multiplied by: the rounding of that factor leaves lse again.)
@@ -68,11 +81,13 @@ __device__ __forceinline__ float add_terms(frag_t<DT> f, float l) {
 }
 
 // The keys of one tile for 32 query rows of a wave.  PART: some (row, key)
-// pairs are not seen; the lane's row sees the tile's keys below hi.
+// pairs are not seen; the lane's row sees the tile's keys below hi.  CAREFUL: m is
+// the largest score, as in 32 bits, and mma_seen for rows that are not seen.
 template <int DT, int DP, bool PART, bool CAREFUL>
 __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm, const frag_t<DT> (&qf)[DP / 16],
                                              const storage_t<DT>* kt, const storage_t<DT>* vt, const Reader<DT, DP>& rd,
                                              float to_log2, int hi) {
+    constexpr bool SCORE = DT == DT_F32 || CAREFUL;  // m is a score
     const int g = rd.lane >> 5;
     float &m = sm.m, &l = sm.l;
     f32x16 s[2] = {};
@@ -80,7 +95,7 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
     for (int c = 0; c < DP / 16; ++c)
 #pragma unroll
         for (int t = 0; t < 2; ++t) s[t] = mma(rd.row_frag(kt, 32 * t, c), qf[c], s[t]);
-    constexpr bool AHEAD = DT != DT_F32 && !(PART && CAREFUL);
+    constexpr bool AHEAD = !SCORE;
     constexpr int P = DP / 16;  // products with v for 32 keys
     constexpr int F = 4;        // their values are read that many products ahead
     frag_t<DT> a[F];
@@ -119,7 +134,7 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[db][r] *= alpha;
     };
-    if constexpr (DT == DT_F32) {
+    if constexpr (SCORE) {
         const float now = fmaxf(m, __builtin_elementwise_maximum(top, other_half(top)));
         follow(now, now == m ? 1.f : __builtin_amdgcn_exp2f((m - now) * to_log2));
     } else {
@@ -130,13 +145,17 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
         };
         if (__any(passes(top))) {
             top = __builtin_elementwise_maximum(top, other_half(top));
-            const float now = passes(top) ? fmaf(top, to_log2, -kBelow<DT>) : m;
+            float now = passes(top) ? fmaf(top, to_log2, -kBelow<DT>) : m;
+            if (now < -kCoarse) {
+                sm.low |= now > -INFINITY;
+                now = -INFINITY;  // (m is that, or passes() is false)
+            }
             follow(now, now == m ? 1.f : __builtin_amdgcn_exp2f(m - now));
         }
     }
     const float ref = m == -INFINITY ? 0.f : m;  // nothing seen yet: every term is 0
     const auto term = [&](float x) {
-        return __builtin_amdgcn_exp2f(DT == DT_F32 ? (x - ref) * to_log2 : fmaf(x, to_log2, -ref));
+        return __builtin_amdgcn_exp2f(SCORE ? fmaf(x - ref, to_log2, kBelow<DT>) : fmaf(x, to_log2, -ref));
     };
     if constexpr (AHEAD) {
         // The second 32 keys' terms are made between the first 32's products.
@@ -243,7 +262,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
         // first the tiles that every row of the work-group sees whole
         for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
-            if (wave_any > 0) tile_forward<DT, DP, false, false>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+            if (wave_any > 0)
+                tile_forward<DT, DP, false, CAREFUL && DT != DT_F32>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             next();
@@ -251,7 +271,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
         }
     };
     pass(std::false_type{});
-    if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
+    if constexpr (DT == DT_F32) {
+        if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
+    } else if (__syncthreads_or((p.causal && non_finite(acc)) || too_coarse(sm))) {
+        pass(std::true_type{});
+        if (sm.m > -INFINITY) sm.m = __builtin_amdgcn_fmed3f(fmaf(sm.m, to_log2, -kBelow<DT>), -FLT_MAX, FLT_MAX);
+    }
     if (!exists) return;
     const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
     if (p.parts > 1) {

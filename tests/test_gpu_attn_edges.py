@@ -6,7 +6,7 @@ import torch
 
 import paper_2608_02611_amd as kb
 from tests.helpers import ensure_built
-from tests.test_gpu_attn import DT, heads, normal
+from tests.test_gpu_attn import DT, U, heads, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -68,3 +68,70 @@ def test_long_flat_tails_in_f16(apart):
     want = (n - 1) / (top + n - 1)
     err = float((o.double() - want).abs().max())
     assert err <= want * (2.0 ** -11 + 2.0 ** -11 + 2.0 ** -7) + n * 2.0 ** -34, (err, want)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("scale", [0.125, 0.09, 0.3])
+@pytest.mark.parametrize("nq,nk", [(40, 200), (2, 3000)])
+def test_scores_of_the_types_lowest_value(dtype, scale, nq, nk):
+    """Keys that a column of the type's lowest number takes out of the softmax, first, in the middle and last: what is
+    left is as if they were not there.  Where they are all that a row has, their scores are equal: o is the mean of v
+    (a rounding of each term, which is exact, of the sum and of o), and gradients stay finite."""
+    t = DT[dtype]
+    q, k, v, do = heads(1, 4, nq, 64, t, 1), heads(1, 2, nk, 64, t, 2), heads(1, 2, nk, 64, t, 3), heads(1, 4, nq, 64, t, 4)
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    out = torch.zeros(nk, dtype=torch.bool, device="cuda")
+    out[:70], out[100:131], out[-5:] = True, True, True
+    k[:, :, out, 0] = torch.finfo(t).min
+    kept, vkept = k[:, :, ~out].contiguous(), v[:, :, ~out].contiguous()
+    o, lse = kb.kb_attn_forward(q, k, v, scale)
+    want, want_lse = kb.kb_attn_forward(q, kept, vkept, scale)
+    u = U[t]
+
+    def same(a, c, f):  # the same terms in other tiles: a rounding each, one of the result, 3000 of them summed in 32 bits
+        tol = (4 * u + 2 * 3000 * 2.0 ** -24) * f
+        assert float((a.double() - c.double()).abs().max()) <= tol, (float((a.double() - c.double()).abs().max()), tol)
+    same(o, want, float(v.abs().max()))
+    assert torch.allclose(lse, want_lse, rtol=1e-5, atol=1e-5)
+    dq, dk, dv = kb.kb_attn_backward(do, q, k, v, o, lse, scale)
+    _, dk1, dv1 = kb.kb_attn_backward(do, q, kept, vkept, o, lse, scale)
+    assert torch.all(dv[:, :, out] == 0) and torch.all(dk[:, :, out] == 0)
+    assert torch.allclose(dv[:, :, ~out].float(), dv1.float(), rtol=16 * u, atol=16 * u)
+    assert torch.allclose(dk[:, :, ~out].float(), dk1.float(), rtol=16 * u, atol=16 * u)
+    q[:, :2] = 0.0  # two of the heads, on the first key head, see nothing else
+    q[:, :2, :, 0] = 1.0
+    k[:, 0, :, 0] = torch.finfo(t).min
+    o, lse = kb.kb_attn_forward(q, k, v, scale)
+    mean = v[:, :1].double().mean(2, keepdim=True)
+    assert float((o[:, :2].double() - mean).abs().max()) <= (u + nk * 2.0 ** -24) * float(v.abs().max())
+    assert torch.isfinite(lse).all()
+    for grad in kb.kb_attn_backward(do, q, k, v, o, lse, scale):
+        assert torch.isfinite(grad.float()).all()
+
+
+@pytest.mark.parametrize("dtype,big", [("f32", 2.0 ** 50), ("f16", 2.0 ** 15), ("bf16", 2.0 ** 15), ("bf16", 2.0 ** 50)])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("nq,nk", [(100, 150), (3, 2500)])
+def test_scores_that_binary32_holds_coarsely(dtype, big, causal, nq, nk):
+    """Scores of up to 2^28 and 2^98 that differ by more than exp's range: o is the v of the largest one to the last
+    bit, and what follows from lse stays finite."""
+    t = DT[dtype]
+    q, k, v, do = heads(1, 2, nq, 64, t, 1), heads(1, 1, nk, 64, t, 2), heads(1, 1, nk, 64, t, 3), heads(1, 2, nq, 64, t, 4)
+    q[..., 1:], k[..., 1:] = 0.0, 0.0
+    q[..., 0] = torch.sign(q[..., 0]) * big
+    size = torch.randperm(nk, device="cuda") % 200 - 100
+    size[nk // 8], size[nk // 8 + 1] = 250, -250  # (whole numbers that bf16 holds)
+    k[..., 0] = size[None, None] * (big / 4096)
+    o, lse = kb.kb_attn_forward(q, k, v, 0.3, causal)
+    s = (q[..., :1].double() * k[..., 0].double()[:, :, None]) * 0.3
+    if causal:
+        s = torch.where(torch.ones((nq, nk), dtype=torch.bool, device="cuda").tril(nk - nq), s, float("-inf"))
+    top, at = s.max(-1)
+    gap = top - s.scatter(-1, at[..., None], float("-inf")).max(-1).values
+    clear = gap > 200
+    assert clear.all()
+    want = torch.gather(v.expand(1, 2, nk, 64), 2, at[..., None].expand(-1, -1, -1, 64))
+    assert torch.equal(o[clear], want[clear])
+    assert float(((lse.double() - top).abs() / top.abs())[clear].max()) <= 2.0 ** -22
+    for grad in kb.kb_attn_backward(do, q * 0 + 1, k / big, v, o, lse, 0.3, causal):
+        assert torch.isfinite(grad.float()).all()

@@ -107,12 +107,32 @@ __device__ __forceinline__ void reads_ahead() {
     __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
+// The exponent of a probability, in base 2, from a score s and the row's lse as
+// row_lse gives it.  In 32 bits the difference comes first and is rounded once, so
+// that its error does not grow with |lse| (scores near 5000: p to 7e-7 of itself,
+// 1.5e-4 with lse / ln 2 rounded beforehand; 2 x 12 heads, 513 x 257: 98 us, 96 with
+// that).  In 16 bits one instruction makes it, whose error, 2^-23 of |lse|, stays
+// under f16's rounding up to an lse of 2^12.
+template <int DT>
+__device__ __forceinline__ float row_lse(float lse) {
+    return DT == DT_F32 ? lse : lse * kLog2e;
+}
+template <int DT>
+__device__ __forceinline__ float score_factor(float scale) {
+    return DT == DT_F32 ? scale : scale * kLog2e;
+}
+template <int DT>
+__device__ __forceinline__ float exponent(float s, float factor, float lse) {
+    const float x = fmaf(s, factor, -lse);
+    return DT == DT_F32 ? x * kLog2e : x;
+}
+
 // One tile of queries for a wave's 32 keys: s and t with a key a column.  PART:
 // the lane's key is seen by the tile's queries from lo on.
 template <int DT, int DP, bool PART, bool CAREFUL>
 __device__ __forceinline__ void tile_keys(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP / 32], const frag_t<DT> (&kf)[DP / 16],
                                           const storage_t<DT>* vt, const storage_t<DT>* qt, const storage_t<DT>* dt,
-                                          const float* rows, const Reader<DT, DP>& rd, float to_log2, float t_over_p,
+                                          const float* rows, const Reader<DT, DP>& rd, float factor, float t_over_p,
                                           int lo) {
     const int g = rd.lane >> 5;
     f32x16 s = {}, t;
@@ -134,7 +154,7 @@ __device__ __forceinline__ void tile_keys(f32x16 (&dk)[DP / 32], f32x16 (&dv)[DP
         for (int e = 0; e < 4; ++e) {
             const int r = 4 * r4 + e;
             // F16: the power of two of p goes into its exponent
-            float x = fmaf(s[r], to_log2, DT == DT_F16 ? kProbLog2 - lse[e] : -lse[e]);
+            float x = exponent<DT>(s[r], factor, DT == DT_F16 ? lse[e] - kProbLog2 : lse[e]);
             if (PART) x = 8 * r4 + 4 * g + e >= lo ? x : -INFINITY;
             s[r] = __builtin_amdgcn_exp2f(x);
             t[r] = s[r] * t[r];
@@ -222,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
     };
 
     const Reader<DT, DP> rd(lane);
-    const float to_log2 = p.scale * kLog2e;
+    const float factor = score_factor<DT>(p.scale);
     const T* v_rows = vt + wave * L::size(32);
     // the part's tiles of those of all heads, in their order
     const int64_t tiles = (int64_t)steps * p.group;
@@ -241,12 +261,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || CAREFUL ? 1 : 2) att
         for (; tile < end && i0 < min(block_hi, qlen); i0 += kQueries, buf ^= 1, ++tile) {
             next();
             if (wave_live && i0 + kQueries > wave_lo)
-                tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p,
+                tile_keys<DT, DP, true, CAREFUL>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, factor, t_over_p,
                                                  lo - i0);
         }
         for (; tile < end && i0 < qlen; i0 += kQueries, buf ^= 1, ++tile) {
             next();
-            if (wave_live) tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, to_log2, t_over_p, 0);
+            if (wave_live) tile_keys<DT, DP, false, false>(dk, dv, kf, v_rows, qt[buf], dt[buf], rows[buf], rd, factor, t_over_p, 0);
         }
     }
     if (!CAREFUL && p.causal) {
@@ -284,7 +304,7 @@ constexpr int kKeys = kAttnKeys;
 template <int DT, int DP, bool PART, bool CAREFUL>
 __device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t<DT> (&qf)[DP / 16],
                                              const frag_t<DT> (&df)[DP / 16], const storage_t<DT>* kt,
-                                             const storage_t<DT>* vt, const Reader<DT, DP>& rd, float to_log2,
+                                             const storage_t<DT>* vt, const Reader<DT, DP>& rd, float factor,
                                              float lse, float dot, int hi, int seen) {
     const int g = rd.lane >> 5;
 #pragma unroll
@@ -299,7 +319,7 @@ __device__ __forceinline__ void tile_queries(f32x16 (&dq)[DP / 32], const frag_t
         if (DT != DT_F32 && !(PART && CAREFUL)) reads_ahead<DP / 8, 4>();
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-            t[r] = __builtin_amdgcn_exp2f(fmaf(s[r], to_log2, -lse)) * (t[r] - dot);
+            t[r] = __builtin_amdgcn_exp2f(exponent<DT>(s[r], factor, lse)) * (t[r] - dot);
             if (PART) t[r] = 32 * u + 8 * (r >> 2) + 4 * g + (r & 3) < hi ? t[r] : 0.f;
         }
         const frag_t<DT> tf[2] = {narrow<DT>(t, 0), narrow<DT>(t, 1)};
@@ -352,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
         df[c] = load_frag<DT, WHOLE>(dout, c, g, p.dim, live);
     }
-    // D_i and lse_i / log 2, for here and for the keys' kernel.  A row with no
+    // D_i and lse_i (row_lse), for here and for the keys' kernel.  A row with no
     // seen score has lse = -infinity, and its terms exp(-infinity - lse) are to be
     // 0: it gets 0.  A row of the padding gets +infinity, which makes its terms 0, and
     // so does one whose lse is held too coarsely for a term to be known even to a
@@ -371,8 +391,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
     }
     dot += other_half(dot);
     float lse = live ? p.lse[at_row] : INFINITY;
-    lse = lse == -INFINITY ? 0.f : lse * kLog2e;
-    if (fabsf(lse) >= 16777216.f) lse = INFINITY;
+    lse = lse == -INFINITY ? 0.f : row_lse<DT>(lse);
+    if (fabsf(lse) >= row_lse<DT>(kLn2 * 16777216.f)) lse = INFINITY;
     if (part == 0 && exists && g == 0) {
         p.ws[at_row] = dot;
         p.ws[l.lse + at_row] = lse;
@@ -405,7 +425,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         }
     };
     const Reader<DT, DP> rd(lane);
-    const float to_log2 = p.scale * kLog2e;
+    const float factor = score_factor<DT>(p.scale);
     f32x16 dq[DP / 32];
     const auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
@@ -421,12 +441,12 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_backward_
         // first the tiles that every row of the work-group sees whole
         for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
-            if (wave_any > 0) tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, 0, 0);
+            if (wave_any > 0) tile_queries<DT, DP, false, false>(dq, qf, df, kt[buf], vt[buf], rd, factor, lse, dot, 0, 0);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             next();
             if (j0 < wave_any)
-                tile_queries<DT, DP, true, CAREFUL>(dq, qf, df, kt[buf], vt[buf], rd, to_log2, lse, dot, lim - j0, wave_any - j0);
+                tile_queries<DT, DP, true, CAREFUL>(dq, qf, df, kt[buf], vt[buf], rd, factor, lse, dot, lim - j0, wave_any - j0);
         }
     };
     pass(std::false_type{});

@@ -135,3 +135,18 @@ def test_scores_that_binary32_holds_coarsely(dtype, big, causal, nq, nk):
     assert float(((lse.double() - top).abs() / top.abs())[clear].max()) <= 2.0 ** -22
     for grad in kb.kb_attn_backward(do, q * 0 + 1, k / big, v, o, lse, 0.3, causal):
         assert torch.isfinite(grad.float()).all()
+
+
+def test_large_scores_in_f32():
+    """Gradients where lse is far from 0 and the scores are exact (one element of q is not 0): for one query with
+    dout = 1, dv is p = exp(s - lse).  The difference is rounded once (2^-24 of up to 20), brought to base 2 (twice
+    2^-24 of it) and taken to a power (2^-22 or so): 3 x 20 x 2^-24 + 2^-22 = 3.9e-6."""
+    n, d = 300, 64
+    q, k = torch.zeros((1, 2, 1, d), device="cuda"), torch.zeros((1, 2, n, d), device="cuda")
+    q[..., 0] = 1.0
+    k[..., 0] = 5000.0 + normal((1, 2, n), torch.float32, 1, 2.0)
+    v, do = normal((1, 2, n, d), torch.float32, 2), torch.ones_like(q)
+    o, lse = kb.kb_attn_forward(q, k, v, 1.0)
+    _, _, dv = kb.kb_attn_backward(do, q, k, v, o, lse, 1.0)
+    want = (k[..., :1].double() - lse.double()[..., None]).exp()
+    assert float(((dv.double() - want).abs() / want).max()) <= 3.9e-6

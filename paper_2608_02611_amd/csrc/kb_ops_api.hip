@@ -94,8 +94,8 @@ void byte_range(const kb_tensor& t, uintptr_t* first, uintptr_t* last) {
 }
 
 // Whether two views can share memory: overlapping ranges, unless both walk the
-// memory with the same strides, at places that never meet (the q, k and v
-// columns of one projection).
+// memory with strides that keep them apart (the q, k and v columns of one
+// projection, its sequences any distance apart).
 bool may_overlap(const kb_tensor& a, const kb_tensor& b) {
     if (is_empty(a) || is_empty(b)) return false;
     uintptr_t a0, a1, b0, b1;
@@ -103,15 +103,17 @@ bool may_overlap(const kb_tensor& a, const kb_tensor& b) {
     byte_range(b, &b0, &b1);
     if (a1 < b0 || b1 < a0) return false;
     if (a.ndim != b.ndim || a.dtype != b.dtype) return true;
-    // the offset between them in strides, largest first, must place b's block
-    // beside a's along one dimension within one period of the next larger
     int64_t off = (int64_t)((a0 < b0 ? b0 - a0 : a0 - b0));
     if (off % element_bytes(a.dtype)) return true;
     off /= element_bytes(a.dtype);
     const kb_tensor& lo = a0 < b0 ? a : b;
     const kb_tensor& hi = a0 < b0 ? b : a;
-    // the common outer dimensions: those whose stride (equal in both) exceeds
-    // the offset plus the extent of everything inside
+    // The strides of both from the largest down.  Where the dimensions below a
+    // stride s stay within one period of s in both views, elements that coincide do
+    // so at the same place of a period: s and what is larger (multiples of s, or
+    // dealt with before) fall away, and the offset is taken modulo s.
+    int64_t pending[2 * KB_MAX_DIMS];  // larger strides that did not fall away
+    int n_pending = 0;
     for (int64_t bound = INT64_MAX;;) {
         // the largest stride below bound among the dimensions with more than one element
         int64_t s = -1;
@@ -125,16 +127,15 @@ bool may_overlap(const kb_tensor& a, const kb_tensor& b) {
             if (lo.shape[i] > 1 && lo.strides[i] < s) ext_lo += lo.strides[i] * (lo.shape[i] - 1);
             if (hi.shape[i] > 1 && hi.strides[i] < s) ext_hi += hi.strides[i] * (hi.shape[i] - 1);
         }
-        // modulo s the two blocks are [0, ext_lo) and [off mod s, off mod s + ext_hi)
         const int64_t at = off % s;
-        if (ext_lo <= s && ext_hi <= s && at >= ext_lo && at + ext_hi <= s) {
-            // apart modulo s: apart altogether if every larger stride is a multiple of s
-            bool multiple = true;
-            for (int i = 0; i < a.ndim; ++i) {
-                if (lo.shape[i] > 1 && lo.strides[i] > s && lo.strides[i] % s) multiple = false;
-                if (hi.shape[i] > 1 && hi.strides[i] > s && hi.strides[i] % s) multiple = false;
-            }
-            if (multiple) return false;
+        bool within = ext_lo <= s && at + ext_hi <= s;
+        for (int k = 0; k < n_pending; ++k) within = within && pending[k] % s == 0;
+        if (within) {
+            if (at >= ext_lo) return false;
+            off = at;
+            n_pending = 0;
+        } else {
+            pending[n_pending++] = s;
         }
         bound = s;
     }

@@ -1,12 +1,12 @@
 """Softmax attention where it can go wrong: heads without queries, wide strides,
-long flat tails, large scores, and keys in parts.  Against the formulas in 64
-bits with the tolerances of tests/test_gpu_attn.py, or those derived here."""
+long flat tails, large scores, and keys or queries in parts.  Against the formulas
+in 64 bits with the tolerances of tests/test_gpu_attn.py, or those derived here."""
 import pytest
 import torch
 
 import paper_2608_02611_amd as kb
 from tests.helpers import ensure_built
-from tests.test_gpu_attn import DT, U, heads, normal
+from tests.test_gpu_attn import DT, U, check, heads, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -150,3 +150,120 @@ def test_large_scores_in_f32():
     _, _, dv = kb.kb_attn_backward(do, q, k, v, o, lse, 1.0)
     want = (k[..., :1].double() - lse.double()[..., None]).exp()
     assert float(((dv.double() - want).abs() / want).max()) <= 3.9e-6
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [61, 97, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_parts_of_ragged_sequences(dtype, d, causal):
+    """Keys in parts, with padded queries, sequences of no key and of one, and dimensions that are no multiple of 4."""
+    nq, nk = 6, 2500
+    q, k = (torch.empty(s, dtype=DT[dtype], device="cuda") for s in ((5, 4, nq, d), (5, 2, nk, d)))
+    assert kb.kb_attn_forward_workspace_bytes(q, k) > 0
+    check(dtype, 5, 4, 2, nq, nk, d, causal, "bshd", [6, 3, 1, 0, 5], [2500, 0, 1, 2000, 1300])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [61, 72])
+def test_parts_of_queries_and_keys_backward(dtype, d):
+    """dq, dk and dv in parts at odd dimensions."""
+    check(dtype, 1, 2, 1, 700, 900, d, True, "bshd")
+    check(dtype, 2, 2, 2, 600, 40, d, False, "bhsd", [600, 1], [3, 40])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("nq,nk,d", [(4, 2100, 64), (1, 3000, 128), (130, 400, 80)])
+def test_rows_at_odd_addresses(dtype, nq, nk, d):
+    """Views that start one element into a wider buffer give the bits of dense ones."""
+    t = DT[dtype]
+
+    def odd(x):
+        wide = torch.full((*x.shape[:-1], x.shape[-1] + 3), 9.0, dtype=t, device="cuda")
+        view = wide[..., 1:1 + x.shape[-1]]
+        return view.copy_(x)
+    q, k, v, do = heads(2, 4, nq, d, t, 1), heads(2, 2, nk, d, t, 2), heads(2, 2, nk, d, t, 3), heads(2, 4, nq, d, t, 4)
+    want = kb.kb_attn_forward(q, k, v, causal=True)
+    got = kb.kb_attn_forward(odd(q), odd(k), odd(v), causal=True, o=odd(torch.zeros_like(q)))
+    wantg = kb.kb_attn_backward(do, q, k, v, *want, causal=True)
+    gotg = kb.kb_attn_backward(odd(do), odd(q), odd(k), odd(v), odd(want[0]), want[1], causal=True)
+    for a, c in zip(got + gotg, want + wantg):
+        assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("at", [3, 1500, 2995, 2999])
+def test_non_finite_values_in_one_part(dtype, bad, at):
+    """A value row that is not finite, in keys that pass in parts, reaches one column of the queries that see it; a NaN
+    key makes its queries NaN; the others keep their results (the same terms, maybe in another order: 16 u)."""
+    t = DT[dtype]
+    nq, nk, d = 8, 3000, 64
+    q, k, v = heads(1, 4, nq, d, t, 1, 0.5), heads(1, 2, nk, d, t, 2), heads(1, 2, nk, d, t, 3)
+    assert kb.kb_attn_forward_workspace_bytes(q, k) > 0
+    clean, clean_lse = kb.kb_attn_forward(q, k, v, causal=True)
+    tol = 16 * U[t]
+
+    def same(a, c):
+        assert torch.allclose(a.float(), c.float(), rtol=tol, atol=tol), float((a.float() - c.float()).abs().max())
+    v[:, :, at, 7] = bad
+    o, lse = kb.kb_attn_forward(q, k, v, causal=True)
+    seen = torch.arange(nq, device="cuda") + nk - nq >= at
+    other = [c for c in range(d) if c != 7]
+    same(lse, clean_lse)
+    same(o[..., other], clean[..., other])
+    same(o[:, :, ~seen], clean[:, :, ~seen])
+    assert not torch.isfinite(o[:, :, seen][..., 7].float()).any()
+    if bad != bad:
+        k[:, :, at, 2] = bad
+        o, lse = kb.kb_attn_forward(q, k, v, causal=True)
+        assert torch.isnan(o[:, :, seen]).all() and torch.isnan(lse[:, :, seen]).all()
+        same(o[:, :, ~seen], clean[:, :, ~seen])
+        same(lse[:, :, ~seen], clean_lse[:, :, ~seen])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_scores_of_minus_infinity_in_parts(dtype):
+    """Scores of -infinity over whole parts of the keys, and over all of them."""
+    t = DT[dtype]
+    nq, nk, d = 3, 4000, 64
+    q, k, v = heads(1, 2, nq, d, t, 1, 0.5), heads(1, 2, nk, d, t, 2), heads(1, 2, nk, d, t, 3)
+    q[..., 0] = 1.0
+    k[:, :, :1700, 0] = float("-inf")
+    o, lse = kb.kb_attn_forward(q, k, v)
+    want, want_lse = kb.kb_attn_forward(q, k[:, :, 1700:].contiguous(), v[:, :, 1700:].contiguous())
+    # the same terms in other tiles: a rounding each and one of the result on either side, 2300 of them summed in 32 bits
+    tol = 4 * U[t] + 2 * 2300 * 2.0 ** -24
+    assert float((o.double() - want.double()).abs().max()) <= tol * float(v.abs().max())
+    assert torch.allclose(lse, want_lse, rtol=1e-5, atol=1e-5)
+    k[..., 0] = float("-inf")
+    o, lse = kb.kb_attn_forward(q, k, v)
+    assert torch.all(o == 0) and torch.all(lse == float("-inf"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("at", [0, 300, 699])
+@pytest.mark.parametrize("which", ["q", "k", "v", "do"])
+def test_non_finite_values_backward_in_parts(dtype, at, which):
+    """A NaN at one position of a causal sequence whose queries and keys pass in parts: gradients that it does not reach
+    keep their values (the same terms, maybe in another order: 16 u)."""
+    t = DT[dtype]
+    n, d = 700, 64
+    x = dict(q=heads(1, 2, n, d, t, 1), k=heads(1, 1, n, d, t, 2), v=heads(1, 1, n, d, t, 3), do=heads(1, 2, n, d, t, 4))
+    o, lse = kb.kb_attn_forward(x["q"], x["k"], x["v"], causal=True)
+    clean = kb.kb_attn_backward(x["do"], x["q"], x["k"], x["v"], o, lse, causal=True)
+    x[which][:, :, at, 7] = float("nan")
+    o, lse = kb.kb_attn_forward(x["q"], x["k"], x["v"], causal=True)
+    dq, dk, dv = kb.kb_attn_backward(x["do"], x["q"], x["k"], x["v"], o, lse, causal=True)
+    tol = 16 * U[t]
+
+    def same(a, c):
+        assert torch.allclose(a.float(), c.float(), rtol=tol, atol=8 * tol), float((a.float() - c.float()).abs().max())
+    if which in ("k", "v"):
+        same(dq[:, :, :at], clean[0][:, :, :at])
+        assert torch.isnan(dq[:, :, at:]).all()
+    else:
+        others = [i for i in range(n) if i != at]
+        same(dq[:, :, others], clean[0][:, :, others])
+        assert torch.isnan(dq[:, :, at]).all() and torch.isnan(dk[:, :, :at + 1]).all()
+        same(dk[:, :, at + 1:], clean[1][:, :, at + 1:])
+        same(dv[:, :, at + 1:], clean[2][:, :, at + 1:])

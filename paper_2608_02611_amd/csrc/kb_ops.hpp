@@ -120,13 +120,15 @@ inline int64_t key_blocks(const AttnParams& p) {
 inline int forward_parts(const AttnParams& p) {
     return attn_parts(row_blocks(p), p.len_k, p.q_lens || p.k_lens ? 1024 : 512, p.f32 ? 128 : 512);
 }
-// Backward: one or two work-groups a CU, and as many again under a causal mask,
-// whose blocks are long and short (2 x 32 heads on 8 x 4096: 854 us with dk and
-// dv in two parts, 1005 in one).  In 32 bits a CU holds one work-group: a round of
-// them and a quarter more, as those of short sequences end at once (2 x 12 heads,
-// 513 x 257: 100 us, 116 with twice as many parts); but parts may be shorter, a
-// tile taking 6 us (8 heads x 300: 48 us, 62 with parts of 128).
-inline int64_t backward_fill(const AttnParams& p) { return (p.f32 ? 320 : 512) * (p.causal ? 2 : 1); }
+// Backward: the work-groups that the CUs hold at once, one each in 32 bits and two
+// in 16, and as many again under a causal mask, whose blocks are long and short (2 x
+// 32 heads on 8 x 4096 bf16: 854 us with dk and dv in two parts, 1005 in one).  In
+// 32 bits a few work-groups over a round cost a second one (256 / 320 at most: 2 x 12
+// heads x 384 59 / 84 us, the same of different lengths 60 / 79, 8 heads on 2 x 700
+// 157 / 214; 2 x 12 heads, 513 x 257 of different lengths 103 / 100; 512 at most: 71,
+// 170 and 115).  But parts may be shorter, a tile taking 6 us (8 heads x 300: 48 us,
+// 62 with parts of 128).
+inline int64_t backward_fill(const AttnParams& p) { return (p.f32 ? 256 : 512) * (p.causal ? 2 : 1); }
 inline int row_parts(const AttnParams& p) {
     return attn_parts(row_blocks(p), p.len_k, backward_fill(p), (p.f32 ? 1 : 2) * kAttnKeys);
 }

@@ -102,7 +102,8 @@ __device__ __forceinline__ void load_weight(const W* w, int c, int n, float othe
 // Threads of a row and elements of a thread: the fewest threads that hold the
 // row at 16 elements each (8 up to 512 columns), so that a wave or less has a
 // row where that is possible and its sums need no meeting.  More elements a
-// thread leave too few waves on a CU to cover HBM's latency.
+// thread leave too few waves on a CU to cover HBM's latency (backward makes one
+// exception, norm_backward).
 #define KB_NORM_DISPATCH(COLS, CALL, LONGER)      \
     ((COLS) <= 128    ? CALL<DT, WDT, 16, 8>      \
      : (COLS) <= 512  ? CALL<DT, WDT, 64, 8>      \
@@ -506,7 +507,13 @@ hipError_t norm_forward(const NormForwardParams& p, hipStream_t stream) {
 
 template <int DT, int WDT>
 hipError_t norm_backward(const NormBackwardParams& p, hipStream_t stream) {
-    return KB_NORM_DISPATCH(p.cols, norm_backward_rows, (p.cols <= 6144 ? norm_backward_rows<DT, WDT, 256, 24> : p.cols <= 8192 ? norm_backward_rows<DT, WDT, 512, 16> : norm_backward_rows_long<DT, WDT>))(p, stream);
+    // Rows of 16 bits of up to 5120 columns: 24 elements a thread leave fewer threads
+    // idle than 512 threads would (4096 x 4224 bf16: 33 us, 38 with 512 threads; x
+    // 5120: 36, 38; x 6144: 43, 41; 4096 x 4100 f32: 51, 48).
+    if constexpr (DT != DT_F32) {
+        if (p.cols > 4096 && p.cols <= 5120) return norm_backward_rows<DT, WDT, 256, 24>(p, stream);
+    }
+    return KB_NORM_DISPATCH(p.cols, norm_backward_rows, (p.cols <= 8192 ? norm_backward_rows<DT, WDT, 512, 16> : norm_backward_rows_long<DT, WDT>))(p, stream);
 }
 
 }  // namespace

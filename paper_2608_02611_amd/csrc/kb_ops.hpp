@@ -42,13 +42,14 @@ struct NormBackwardParams {
 };
 
 // Row stripes whose column sums are kept apart (NormBackwardParams::part): one
-// for each work-group.  Rows of more than 128 columns and at most 512 bytes get
+// for each work-group.  Rows of more than 128 columns and at most 768 bytes get
 // twice as many, as a work-group of four such rows has few bytes on their way
-// (65,536 x 256 bf16: 32 us, 37 with 512 parts; 16,384 x 1024 bf16, longer rows: 26
-// us, 31 with 1024; 65,536 x 64, sixteen rows a work-group: 14 us, 15 with 1024).
+// (65,536 rows, with 1024 / 512 parts: 136 x bf16 29 / 34 us, 256 31 / 37, 264 32 / 38,
+// 384 38 / 40, 512 45 / 44, 1024 92 / 77; f32 136 31 / 37, 192 37 / 39, 256 45 / 42;
+// sixteen rows a work-group: 64 x bf16 14.6 / 13.9, f32 128 24 / 23).
 constexpr int64_t kNormParts = 512;
 inline int norm_parts(int64_t groups, int64_t cols, int64_t element_bytes) {
-    const int64_t most = cols > 128 && cols * element_bytes <= 512 ? 2 * kNormParts : kNormParts;
+    const int64_t most = cols > 128 && cols * element_bytes <= 768 ? 2 * kNormParts : kNormParts;
     return (int)(groups < most ? groups : most);
 }
 // Enough for every type.

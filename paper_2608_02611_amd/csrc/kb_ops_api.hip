@@ -159,8 +159,8 @@ int check_apart(const char* call, const Named* outs, int n_outs, const Named* in
     return KB_OK;
 }
 
-// A dense float array as a view, for check_apart.
-kb_tensor float_array(const float* p, int64_t n) {
+// A dense array of 4-byte elements as a view, for check_apart.
+kb_tensor word_array(const void* p, int64_t n) {
     kb_tensor t{};
     t.data = p;
     t.dtype = DT_F32;
@@ -300,7 +300,7 @@ int kb_norm_forward(const kb_tensor* x, const kb_tensor* w, const kb_tensor* b, 
         return fail(KB_ERR_ALIGNMENT, "%s: mean or rstd not aligned to its element", call);
     if (is_empty(*x)) return KB_OK;
     const bool in_place = y->data == x->data && (x->shape[0] == 1 || y->strides[0] == x->strides[0]);
-    const kb_tensor tm = float_array(mean, x->shape[0]), tr = float_array(rstd, x->shape[0]);
+    const kb_tensor tm = word_array(mean, x->shape[0]), tr = word_array(rstd, x->shape[0]);
     const Named outs[] = {{"y", y}, {"mean", &tm}, {"rstd", &tr}};
     const Named ins[] = {{"w", w}, {"b", b}, {"x", x}};
     if ((rc = check_apart(call, outs, 1, ins, in_place ? 2 : 3)) || (rc = check_apart(call, outs, 3, ins, 2)) ||
@@ -335,8 +335,8 @@ int kb_norm_backward(const kb_tensor* dy, const kb_tensor* x, const kb_tensor* w
         return fail(KB_ERR_ALIGNMENT, "%s: mean or rstd not aligned to its element", call);
     const size_t need = dw || db ? norm_part_bytes(x->shape[0], x->shape[1]) : 0;
     if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
-    const kb_tensor tm = float_array(mean, x->shape[0]), tr = float_array(rstd, x->shape[0]);
-    const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
+    const kb_tensor tm = word_array(mean, x->shape[0]), tr = word_array(rstd, x->shape[0]);
+    const kb_tensor tw = word_array(need ? workspace : nullptr, (int64_t)(need / sizeof(float)));
     const Named outs[] = {{"dx", dx}, {"dw", dw}, {"db", db}, {"the workspace", &tw}};
     const Named ins[] = {{"dy", dy}, {"x", x}, {"w", w}, {"mean", &tm}, {"rstd", &tr}};
     if ((rc = check_apart(call, outs, 4, ins, 5))) return rc;
@@ -365,11 +365,12 @@ int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v, 
     p.parts = forward_parts(p);
     const size_t need = forward_bytes(p);
     if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
-    const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
-    const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
+    const kb_tensor tl = word_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
+    const kb_tensor tw = word_array(need ? workspace : nullptr, (int64_t)(need / sizeof(float)));
+    const kb_tensor ql = word_array(p.q_lens, p.batch), kl = word_array(p.k_lens, p.batch);
     const Named outs[] = {{"o", o}, {"lse", &tl}, {"the workspace", &tw}};
-    const Named ins[] = {{"q", q}, {"k", k}, {"v", v}};
-    if ((rc = check_apart(call, outs, 3, ins, 3))) return rc;
+    const Named ins[] = {{"q", q}, {"k", k}, {"v", v}, {"q_lens", &ql}, {"k_lens", &kl}};
+    if ((rc = check_apart(call, outs, 3, ins, 5))) return rc;
     if (is_empty(*q)) return KB_OK;
     p.o = head_view(o);
     p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v);
@@ -404,11 +405,12 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
     p.key_parts = key_parts(p);
     const size_t need = backward_bytes(p);
     if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
-    const kb_tensor tl = float_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
-    const kb_tensor tw = float_array((const float*)(need ? workspace : nullptr), (int64_t)(need / sizeof(float)));
+    const kb_tensor tl = word_array(lse, q->shape[0] * q->shape[1] * q->shape[2]);
+    const kb_tensor tw = word_array(need ? workspace : nullptr, (int64_t)(need / sizeof(float)));
+    const kb_tensor ql = word_array(p.q_lens, p.batch), kl = word_array(p.k_lens, p.batch);
     const Named outs[] = {{"dq", dq}, {"dk", dk}, {"dv", dv}, {"the workspace", &tw}};
-    const Named ins[] = {{"dout", dout}, {"q", q}, {"k", k}, {"v", v}, {"o", o}, {"lse", &tl}};
-    if ((rc = check_apart(call, outs, 4, ins, 6))) return rc;
+    const Named ins[] = {{"dout", dout}, {"q", q}, {"k", k}, {"v", v}, {"o", o}, {"lse", &tl}, {"q_lens", &ql}, {"k_lens", &kl}};
+    if ((rc = check_apart(call, outs, 4, ins, 8))) return rc;
     if (row_blocks(p) == 0 && key_blocks(p) == 0) return KB_OK;  // (keys that no query head reads have gradients, of 0)
     p.dout = head_view(dout);
     p.whole = whole_rows(*q) && whole_rows(*k) && whole_rows(*v) && whole_rows(*dout) && whole_rows(*o);

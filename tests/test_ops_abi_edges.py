@@ -8,7 +8,7 @@ import torch
 
 import paper_2608_02611_amd as kb
 from tests.helpers import ensure_built
-from tests.test_attn_abi import backward
+from tests.test_attn_abi import backward, forward, opts
 from tests.test_norm_abi import view
 
 pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="descriptors of memory that does not exist")
@@ -82,3 +82,16 @@ def test_overlap_of_views_of_three_strides(L):
             assert rc == HIP, (q, k, sq, sk, off)
         seen[0] += shares
     assert min(seen) > 200, seen
+
+
+def test_outputs_on_the_lengths(L):
+    """The lengths are inputs: an output or the workspace that holds them is refused."""
+    lens = dict(op=opts(q_lens=0xb00000, k_lens=0xb00100))
+    assert forward(L, **lens) == HIP and backward(L, **lens) == HIP
+    q = (2, 8, 16, 64)
+    assert forward(L, o=view(0xb00000 - 64, q), **lens) == ARG
+    assert forward(L, lse=0xb00100 - 4, **lens) == ARG
+    assert backward(L, dq=view(0xb00000 - 64, q), **lens) == ARG
+    assert backward(L, dk=view(0xb00104, (2, 4, 32, 64)), **lens) == ARG
+    assert backward(L, ws=0xb00100 - 256, **lens) == ARG
+    assert "q_lens" in kb.kb_last_error()

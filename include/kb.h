@@ -658,12 +658,14 @@ int kb_gen_scatter(void* dst, const void* ref, int dtype, uint64_t n, const uint
  *
  * All calls: tensors are device views whose last dimension is contiguous
  * (stride 1 where it has more than one element); the other strides are in
- * elements, at least 0, and for an output such that no two elements share
- * memory.  A data pointer is aligned to its element only, so rows and slices
- * of a larger tensor are valid views; an empty tensor's may be NULL.  `data`
- * of an output view is written.  An output must not overlap an input or
- * another output (kb_norm_forward's y may be x).  Asynchronous and
- * stream-ordered; on error nothing is launched. */
+ * elements, at least 0, and for an output at least the extent of the
+ * dimensions with smaller ones, so that no two elements share memory.  A data
+ * pointer is aligned to its element only, so rows and slices of a larger
+ * tensor are valid views; an empty tensor's may be NULL.  `data` of an output
+ * view is written.  An output must not overlap an input or another output
+ * (kb_norm_forward's y may be x); views that interleave, like the columns of
+ * one projection, are told apart by their strides where these are alike.
+ * Asynchronous and stream-ordered; on error nothing is launched. */
 
 /* Layer norm of the rows of x [rows][cols]:
  *   mean = sum_c x / cols,  rstd = 1 / sqrt(sum_c (x - mean)^2 / cols + eps),
@@ -721,13 +723,16 @@ typedef struct kb_attn_opts {
  * padding, has o = 0 and lse = -infinity.  A NaN or infinity reaches just the
  * queries that see it.  q, k, v, o: one dtype, F32, F16 or BF16.  lse: device
  * float[batch][heads][len_q], never NULL.  With a 16-bit dtype the softmax
- * terms are rounded to it before their product with v (as they are at most 1
- * before the division by their sum, by at most 2^-11 or 2^-8 of the largest).
+ * terms are rounded to it before their product with v and the sum that this is
+ * divided by, each by at most 2^-11 (F16) or 2^-8 (BF16) of itself, or, F16,
+ * by 2^-34 of the row's largest; a caller who wants them in binary32 passes F32
+ * copies of q, k and v.
  * workspace: 16-byte aligned, not less than kb_attn_forward_workspace_bytes
  * (which may be 0: then NULL will do); it needs no initialisation.
  * Errors: KB_ERR_INVALID_ARG (null descriptors or data, shapes that do not
- * fit, dim not in [1, KB_ATTN_MAX_DIM], strides, scale or flags out of
- * range, 2^24 or more blocks of 128 query rows or of 64 keys in all), KB_ERR_DTYPE, KB_ERR_ALIGNMENT, KB_ERR_WORKSPACE, KB_ERR_HIP. */
+ * fit, dim not in [1, KB_ATTN_MAX_DIM], strides, scale or flags out of range,
+ * 2^24 or more blocks of 128 query rows or of 64 keys in all), KB_ERR_DTYPE,
+ * KB_ERR_ALIGNMENT, KB_ERR_WORKSPACE, KB_ERR_HIP. */
 size_t kb_attn_forward_workspace_bytes(const kb_tensor* q, const kb_tensor* k);
 int kb_attn_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* v,
                     const kb_attn_opts* opts, const kb_tensor* o, float* lse, void* workspace,

@@ -13,11 +13,12 @@
 // 2^10; t, at most 2 |dout| |v|, so that this bound comes to at most 2^15.
 //
 // Measured on an MI355X: 4 x 32 heads x 2047, dim 128, f16, causal: 590 us, of
-// which dk and dv take 330 and dq 241: 0.58 PFLOP/s of the 5 products, 0.81 of the 7
-// that are done, where a large library product reaches 1.2.  Of its time the kernel
-// for dk and dv has matrix instructions under way for 44% and LDS reads for 66%
-// (each product of 32 x 32 reads one or two operands there; twice as many keys a
-// wave would halve that, at 512 registers a lane).
+// which, in the fastest passes of a trace, dk and dv take 336 and dq 241: 0.58
+// PFLOP/s of the 5 products, 0.82 of the 7 that are done, where a large library
+// product reaches 1.2.  Of its time the kernel for dk and dv has matrix instructions
+// under way for 43% and LDS reads (at 128 bytes a clock) for 66% (each product of
+// 32 x 32 reads one or two operands there; twice as many keys a wave would halve
+// that, at 512 registers a lane).
 #include <type_traits>
 
 #include "kb_attn.hpp"

@@ -8,11 +8,12 @@
 // wave; the query heads that share a key head are rows of the same work-group
 // (row = query * group + head), so that a tile of keys serves all of them.
 //
-// Measured on an MI355X: 4 x 32 heads x 2047, dim 128, f16, causal: 188 us, 0.73
+// Measured on an MI355X: 4 x 32 heads x 2047, dim 128, f16, causal: 183 us, 0.75
 // PFLOP/s, where a large library product of 16-bit matrices reaches 1.2 (both are
-// held back by power: on zeros 147 us, and 1.8 PFLOP/s).  Matrix instructions are
+// held back by power: on zeros 146 us, and 1.8 PFLOP/s).  Matrix instructions are
 // under way 43% of the time, vector ones and LDS reads (at 128 bytes a clock) each
-// for about as long.  512 queries on 16,384 keys: 152 us, 0.89 PFLOP/s.  Single tokens
+// for about as long: what is lost is the softmax that no product runs beside.  512
+// queries on 16,384 keys: 147 us, 0.92 PFLOP/s.  Single tokens
 // (16 ragged sequences of up to 8191 keys, 32 heads on 8): 91 us, 4.4 TB/s, where a
 // large copy moves 4.8.
 #include <cfloat>

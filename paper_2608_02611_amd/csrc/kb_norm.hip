@@ -9,8 +9,9 @@
 // writes dx; the arithmetic is 8 to 14 operations an element.
 //
 // Measured on an MI355X, where a copy of 4 GB moves 4.8 TB/s: forward of 16,384 x
-// 4096 f16 54 us, 5.0 TB/s; backward of the same in bf16 80 us, 5.0 TB/s; backward of
-// 4095 x 4097 f32 53 us, 3.8 TB/s; 16 rows of 4096, a call's own time, 7 us.
+// 4096 f16 53 us, 5.0 TB/s; backward of the same in bf16 81 us, 5.0 TB/s (part of it
+// from the 256 MB last-level cache); backward of 4095 x 4097 f32 47 us, 4.3 TB/s; 16
+// rows of 4096, a call's own time, 7 us.
 #include "kb_ops.hpp"
 
 namespace kb {

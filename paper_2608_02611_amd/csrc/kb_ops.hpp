@@ -146,8 +146,9 @@ inline int64_t forward_floats(const AttnParams& p, int parts) {
 
 // Workspace of the backward pass, in floats: D_i and lse_i for every query row;
 // (F16) the largest squared norm of the rows of dout in each work-group of rows,
-// and of each block of kNormBlock rows of v; a word for each work-group of keys; then, each where it is in parts, dq
-// of every query row and part, and dk and dv of every key and part.
+// and of each block of kNormBlock rows of v; a word for each work-group of keys;
+// then, each where it is in parts, dq of every query row and part, and dk and dv of
+// every key and part.
 constexpr int kNormBlock = 64;
 struct BackwardLayout {
     int64_t lse, dout_norms, v_norms, marks, dq, dkv, total;

@@ -33,7 +33,8 @@
  * promotion decision (kb_rung_stats, kb_rung_promote, kb_rung_survival),
  * kb_screen_noalloc for callers that cannot allocate, and operators whose
  * outputs serve as references (kb_norm_forward, kb_norm_backward,
- * kb_attn_forward, kb_attn_backward).
+ * kb_attn_forward, kb_attn_backward, kb_qk_norm_forward, kb_qk_norm_backward,
+ * kb_cache_write, kb_attn_paged).
  *
  * Conventions
  *   - Every function is extern "C" and returns an int status: KB_OK (0) or a
@@ -756,6 +757,118 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
                      const kb_tensor* o, const float* lse, const kb_attn_opts* opts,
                      const kb_tensor* dq, const kb_tensor* dk, const kb_tensor* dv, void* workspace,
                      size_t workspace_bytes, hipStream_t stream);
+
+/* What lies between an attention sublayer's projection and its output where keys
+ * and values are kept in pages: the head norms with the position rotation (and
+ * their gradients, for training), the write of new tokens into the pages, and the
+ * attention of new tokens over them. */
+
+/* Most heads and largest head dimension of these calls (kb_cache_write and
+ * kb_attn_paged: KB_ATTN_MAX_DIM). */
+#define KB_MAX_HEADS 65536
+#define KB_QK_MAX_DIM 256
+
+/* kb_qk_opts.flags */
+enum {
+    KB_QK_INTERLEAVED = 1u << 0 /* elements 2i and 2i + 1 rotate together; without it i and i + rot_dim / 2 */
+};
+
+/* What the two head norm calls share.  The first rot_dim elements of a row
+ * rotate (even, in [0, dim]; 0: none, and positions and freqs may be NULL).
+ * positions: device int32[tokens], any values.  freqs: device
+ * float[rot_dim / 2], radians per position: pair i of token t turns by
+ * positions[t] freqs[i], a product that is exact, whose cosine and sine are
+ * within 2^-23 of the exact ones up to 2^50 radians. */
+typedef struct kb_qk_opts {
+    float eps; /* finite and >= 0 */
+    uint32_t flags;
+    const int32_t* positions;
+    const float* freqs;
+    int32_t rot_dim;
+    int32_t reserved;
+} kb_qk_opts;
+
+/* Root mean square norm of every head row, then the rotation: for a row x of q
+ * [tokens][heads][dim] with weight wq, or of k [tokens][kv_heads][dim] with wk,
+ *   g = x w / sqrt(sum_c x^2 / dim + eps),
+ * and of each pair (a, b) of g's rotating elements
+ *   (a cos - b sin, b cos + a sin).
+ * q, k, q_out, k_out: one dtype, F32, F16 or BF16.  wq, wk: [dim], each NULL (1)
+ * or of q's dtype or F32, both the same.  q_out may be q, and k_out k.  Heads may
+ * be none of q's or k's.
+ * Errors: KB_ERR_INVALID_ARG (null descriptors or data, a shape, stride, head
+ * count, dim, eps, flags or rot_dim out of range), KB_ERR_DTYPE,
+ * KB_ERR_ALIGNMENT, KB_ERR_HIP. */
+int kb_qk_norm_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* wq, const kb_tensor* wk,
+                       const kb_qk_opts* opts, const kb_tensor* q_out, const kb_tensor* k_out,
+                       hipStream_t stream);
+
+/* Gradients of kb_qk_norm_forward from those of its outputs: with g the gradient
+ * turned the other way, r = 1 / sqrt(sum_c x^2 / dim + eps), z = x r and u = g w,
+ *   dx = r (u - z sum_c (u z) / dim),  dw = sum g z over tokens and heads.
+ * dq_out, dq: q's shape; dk_out, dk: k's; one dtype.  dwq, dwk: [dim], of q's
+ * dtype or F32, the weights and these all the same.  dq, dk, dwq and dwk may each
+ * be NULL (not computed); dwq and dwk of no row are 0.  workspace: 16-byte
+ * aligned, not less than kb_qk_norm_backward_workspace_bytes; it needs no
+ * initialisation and may be NULL when neither dwq nor dwk is wanted.
+ * Errors as kb_qk_norm_forward, and KB_ERR_WORKSPACE. */
+size_t kb_qk_norm_backward_workspace_bytes(int64_t dim);
+int kb_qk_norm_backward(const kb_tensor* dq_out, const kb_tensor* dk_out, const kb_tensor* q, const kb_tensor* k,
+                        const kb_tensor* wq, const kb_tensor* wk, const kb_qk_opts* opts, const kb_tensor* dq,
+                        const kb_tensor* dk, const kb_tensor* dwq, const kb_tensor* dwk, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream);
+
+/* Which keys of a paged cache a batch of sequences has.  Key j of sequence b lies
+ * in page table[b table_stride + j / page] at place j % page, the cache being a view
+ * [pages][kv_heads][page][dim].  A page number outside [0, pages) is no page: its
+ * keys are neither seen nor written.
+ *   table   device int32, rows of max_pages, table_stride apart;
+ *   lens    device int32[batch]: keys of each sequence, its new tokens included (a
+ *           value outside [0, max_pages page] counts as the nearer end);
+ *   starts  device int32[batch + 1], ascending: the tokens starts[b] .. starts[b+1]
+ *           of the call are sequence b's new ones, its last.  NULL: token b is
+ *           sequence b's, one each.  Tokens before starts[0] and from
+ *           starts[batch] on belong to no sequence.
+ * batch at most 2^20, max_pages page at most 2^30. */
+typedef struct kb_pages {
+    const int32_t* table;
+    int64_t table_stride;
+    const int32_t* lens;
+    const int32_t* starts;
+    int32_t batch;
+    int32_t max_pages;
+} kb_pages;
+
+/* The new tokens' rows of k and v [tokens][kv_heads][dim] into their places:
+ * token t of sequence b goes to place lens[b] - starts[b+1] + t.  A token of no
+ * sequence, with a place before the first or without a page is not written, and
+ * nothing else in the caches changes.  Places have to be distinct: where two
+ * tokens share one, each element is one of the two.  One dtype throughout, F32,
+ * F16 or BF16; the bits are copied.
+ * Errors: KB_ERR_INVALID_ARG (null descriptors or data, shapes that do not fit,
+ * sizes or strides out of range, starts NULL with other than batch tokens),
+ * KB_ERR_DTYPE, KB_ERR_ALIGNMENT, KB_ERR_HIP. */
+int kb_cache_write(const kb_tensor* k, const kb_tensor* v, const kb_pages* pages, const kb_tensor* k_cache,
+                   const kb_tensor* v_cache, hipStream_t stream);
+
+/* Softmax attention of new tokens over the cache.  q, o: [tokens][heads][dim];
+ * query head h reads key head h / (heads / kv_heads).  Query i of a sequence with
+ * Q new tokens and K keys sees all of its keys, or with KB_ATTN_CAUSAL in flags
+ * j <= i + K - Q, less those without a page; o and lse as kb_attn_forward's.  A
+ * query that sees no key has o = 0 and lse = -infinity; o and lse of tokens of no
+ * sequence are left as they are.  lse: device float[tokens][heads], may be NULL.
+ * One dtype, F32, F16 or BF16.  With a 16-bit dtype and more than 32 query rows
+ * (queries x heads / kv_heads) a sequence on average the softmax terms are rounded
+ * as kb_attn_forward's; with fewer they keep twice the dtype's digits.  workspace:
+ * 16-byte aligned, not less than kb_attn_paged_workspace_bytes (which may be 0:
+ * then NULL will do); it needs no initialisation.
+ * Errors: as kb_cache_write, and KB_ERR_INVALID_ARG for a scale or flags out of
+ * range, 2^30 or more (token, head) pairs, or 2^24 or more blocks of 128 query
+ * rows, and KB_ERR_WORKSPACE. */
+size_t kb_attn_paged_workspace_bytes(const kb_tensor* q, const kb_tensor* k_cache, const kb_pages* pages);
+int kb_attn_paged(const kb_tensor* q, const kb_tensor* k_cache, const kb_tensor* v_cache, const kb_pages* pages,
+                  float scale, uint32_t flags, const kb_tensor* o, float* lse, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream);
 
 /* ----------------------------------------------------------------- misc -- */
 

@@ -6,7 +6,8 @@ current stream.  The names mirror the C interface in include/kb.h:
 
     kb_policy_check, kb_screen_workspace_bytes, kb_screen_launch, kb_screen,
     kb_screen_stats, kb_gen_inputs, kb_norm_forward, kb_norm_backward,
-    kb_attn_forward, kb_attn_backward, kb_last_error, kb_version
+    kb_attn_forward, kb_attn_backward, kb_qk_norm_forward, kb_qk_norm_backward,
+    kb_cache_write, kb_attn_paged, kb_last_error, kb_version
 
 plus `screen(...)`, which chains the gate, the kernel and the readback for the
 common case.  The pass/fail verdict of each record comes from the library
@@ -37,6 +38,9 @@ KB_FAIL_FAST = 2
 KB_MAX_DIMS = 8
 KB_ATTN_CAUSAL = 1
 KB_ATTN_MAX_DIM = 128
+KB_QK_INTERLEAVED = 1
+KB_QK_MAX_DIM = 256
+KB_MAX_HEADS = 65536
 
 ERROR_NAMES = {KB_ERR_INVALID_ARG: "KB_ERR_INVALID_ARG", KB_ERR_DTYPE: "KB_ERR_DTYPE",
                KB_ERR_WORKSPACE: "KB_ERR_WORKSPACE", KB_ERR_ALIGNMENT: "KB_ERR_ALIGNMENT",
@@ -142,6 +146,8 @@ EXPORTS = ("kb_policy_check", "kb_screen_workspace_bytes", "kb_screen_positions_
            "kb_attn_forward", "kb_attn_forward_workspace_bytes",
            "kb_attn_backward", "kb_attn_backward_workspace_bytes",
            "kb_screen_noalloc", "kb_gen_softmax_rows", "kb_gen_indices", "kb_gen_perturb", "kb_gen_scatter",
+           "kb_qk_norm_forward", "kb_qk_norm_backward_workspace_bytes", "kb_qk_norm_backward",
+           "kb_cache_write", "kb_attn_paged_workspace_bytes", "kb_attn_paged",
            "kb_last_error", "kb_version")
 
 _lib = None
@@ -230,6 +236,18 @@ def lib():
         L.kb_attn_forward.restype = i32
         L.kb_attn_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
         L.kb_attn_backward.restype = i32
+        L.kb_qk_norm_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp]
+        L.kb_qk_norm_forward.restype = i32
+        L.kb_qk_norm_backward_workspace_bytes.argtypes = [i64]
+        L.kb_qk_norm_backward_workspace_bytes.restype = size
+        L.kb_qk_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, size, vp]
+        L.kb_qk_norm_backward.restype = i32
+        L.kb_cache_write.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.kb_cache_write.restype = i32
+        L.kb_attn_paged_workspace_bytes.argtypes = [vp, vp, vp]
+        L.kb_attn_paged_workspace_bytes.restype = size
+        L.kb_attn_paged.argtypes = [vp, vp, vp, vp, f32, ctypes.c_uint32, vp, vp, vp, size, vp]
+        L.kb_attn_paged.restype = i32
         L.kb_last_error.argtypes = []
         L.kb_last_error.restype = ctypes.c_char_p
         L.kb_version.argtypes = []
@@ -949,6 +967,154 @@ def kb_attn_backward(dout, q, k, v, o, lse, scale=None, causal=False, q_lens=Non
     _check(L.kb_attn_backward(pack_view(dout), pq, pk, pack_view(v), pack_view(o), _floats(lse, q.shape[:-1], "lse"),
                               opts, pack_view(dq), pack_view(dk), pack_view(dv), ws, nbytes, _stream_handle(stream)))
     return dq, dk, dv
+
+
+_QK_OPTS = struct.Struct("fIPPii")
+_PAGES = struct.Struct("PqPPii")
+assert _QK_OPTS.size == 32 and _PAGES.size == 40
+
+
+def _one_device(*tensors):
+    """Device addresses of another GPU than the current one are not this call's."""
+    here = _torch().cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            raise ValueError("a tensor is not on the current device, cuda:%d" % here)
+
+
+def _dense(t, dtype, shape, name):
+    """Address of a contiguous device tensor of a dtype and shape (None: NULL as 0)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError("%s must be a contiguous %s device tensor of shape %s" % (name, dtype, tuple(shape)))
+    return t.data_ptr()
+
+
+def _tokens(t):
+    """A tensor as [tokens][heads][dim] over its last two axes (a view, never a copy)."""
+    return t if t is None or t.dim() == 3 else t.view(-1, *t.shape[-2:])
+
+
+def _qk_opts(q, eps, positions, freqs, interleaved):
+    torch = _torch()
+    rot = 0 if freqs is None else 2 * freqs.numel()
+    at = _dense(positions, torch.int32, q.shape[:-2], "positions") if rot else 0
+    table = _dense(freqs, torch.float32, (rot // 2,), "freqs") if rot else 0
+    return _QK_OPTS.pack(eps, KB_QK_INTERLEAVED if interleaved else 0, at, table, rot, 0)
+
+
+def kb_qk_norm_forward(q, k, wq, wk, eps=1e-6, positions=None, freqs=None, interleaved=False, q_out=None, k_out=None,
+                       stream=None):
+    """Root mean square norm of each head row of q [..., heads, dim] and k
+    [..., kv_heads, dim] (views of any strides with a contiguous last dimension),
+    weights wq and wk [dim] (None: 1), then the rotation of the first 2 len(freqs)
+    elements by positions (int32, of q's leading shape) times freqs (float32,
+    radians per position; None: no rotation), as pairs (i, i + len(freqs)) or,
+    interleaved, (2i, 2i + 1).  Returns (q_out, k_out), made here where not given."""
+    if q_out is None or k_out is None:
+        torch = _torch()
+        with _on(stream):
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if k_out is None:
+                k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    _one_device(q, k, wq, wk, positions, freqs, q_out, k_out)
+    pq = pack_view(_tokens(q))
+    _check(lib().kb_qk_norm_forward(pq, pack_view(_tokens(k)), pack_view(wq), pack_view(wk),
+                                    _qk_opts(q, eps, positions, freqs, interleaved), pack_view(_tokens(q_out)),
+                                    pack_view(_tokens(k_out)), _stream_handle(stream)))
+    return q_out, k_out
+
+
+def kb_qk_norm_backward_workspace_bytes(dim):
+    return lib().kb_qk_norm_backward_workspace_bytes(dim)
+
+
+def kb_qk_norm_backward(dq_out, dk_out, q, k, wq, wk, eps=1e-6, positions=None, freqs=None, interleaved=False, dq=None,
+                        dk=None, dwq=None, dwk=None, workspace=None, stream=None):
+    """Gradients of kb_qk_norm_forward from those of its outputs: (dq, dk, dwq,
+    dwk), made here where not given; dwq and dwk of the weights' dtype (q's
+    without a weight)."""
+    torch = _torch()
+    L = lib()
+    weight = wq if wq is not None else wk
+    wdtype = q.dtype if weight is None else weight.dtype
+    with _on(stream):
+        if dq is None:
+            dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if dk is None:
+            dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        if dwq is None:
+            dwq = torch.empty(q.shape[-1], dtype=wdtype, device=q.device)
+        if dwk is None:
+            dwk = torch.empty(q.shape[-1], dtype=wdtype, device=q.device)
+        if workspace is None:
+            workspace = _scratch(L.kb_qk_norm_backward_workspace_bytes(q.shape[-1]), q.device)
+    _one_device(dq_out, dk_out, q, k, wq, wk, positions, freqs, dq, dk, dwq, dwk, workspace)
+    ws, nbytes = _extent(workspace)
+    pq = pack_view(_tokens(q))
+    _check(L.kb_qk_norm_backward(pack_view(_tokens(dq_out)), pack_view(_tokens(dk_out)), pq, pack_view(_tokens(k)),
+                                 pack_view(wq), pack_view(wk), _qk_opts(q, eps, positions, freqs, interleaved),
+                                 pack_view(_tokens(dq)), pack_view(_tokens(dk)), pack_view(dwq), pack_view(dwk), ws, nbytes,
+                                 _stream_handle(stream)))
+    return dq, dk, dwq, dwk
+
+
+def _pages(table, lens, starts):
+    """The kb_pages of a batch: table int32 [batch][max_pages] (rows may be apart), lens int32 [batch], starts int32
+    [batch + 1] or None."""
+    torch = _torch()
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be an int32 device tensor [batch][max_pages] with contiguous rows")
+    batch, width = table.shape
+    return _PAGES.pack(table.data_ptr(), table.stride(0), _dense(lens, torch.int32, (batch,), "lens"),
+                       _dense(starts, torch.int32, (batch + 1,), "starts"), batch, width)
+
+
+def kb_cache_write(k, v, k_cache, v_cache, table, lens, starts=None, stream=None):
+    """The rows of k and v [tokens][kv_heads][dim] to their places in the caches,
+    views [pages][kv_heads][page][dim]: of sequence b, with lens[b] keys, its last
+    ones, the tokens starts[b] .. starts[b + 1] (None: token b).  Key j lies in page
+    table[b][j / page].  Returns (k_cache, v_cache)."""
+    _one_device(k, v, k_cache, v_cache, table, lens, starts)
+    pk = pack_view(k)
+    _check(lib().kb_cache_write(pk, pack_view(v), _pages(table, lens, starts), pack_view(k_cache), pack_view(v_cache),
+                                _stream_handle(stream)))
+    return k_cache, v_cache
+
+
+def kb_attn_paged_workspace_bytes(q, k_cache, table, lens, starts=None):
+    return lib().kb_attn_paged_workspace_bytes(pack_view(q), pack_view(k_cache), _pages(table, lens, starts))
+
+
+def kb_attn_paged(q, k_cache, v_cache, table, lens, starts=None, scale=None, causal=True, o=None, lse=None,
+                  workspace=None, stream=None):
+    """Softmax attention of the new tokens q [tokens][heads][dim] over the pages of
+    their sequences (kb_cache_write's arguments); causal: a token sees the keys up
+    to its own; scale: dim^-1/2 if None.  Returns (o, lse), lse [tokens][heads],
+    made here where not given; rows of no sequence are left as they are."""
+    L = lib()
+    if scale is None:
+        scale = max(q.shape[-1], 1) ** -0.5
+    pages = _pages(table, lens, starts)
+    pq, pk = pack_view(q), pack_view(k_cache)
+    if workspace is None:
+        nbytes = L.kb_attn_paged_workspace_bytes(pq, pk, pages)
+    if o is None or lse is None or (workspace is None and nbytes):
+        torch = _torch()
+        with _on(stream):
+            if o is None:
+                o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if lse is None:
+                lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=q.device)
+            if workspace is None:
+                workspace = _scratch(nbytes, q.device)
+    _one_device(q, k_cache, v_cache, table, lens, starts, o, lse, workspace)
+    ws, nbytes = _extent(workspace)
+    _check(L.kb_attn_paged(pq, pk, pack_view(v_cache), pages, scale, KB_ATTN_CAUSAL if causal else 0, pack_view(o),
+                           _floats(lse, q.shape[:-1], "lse"), ws, nbytes, _stream_handle(stream)))
+    return o, lse
 
 
 def kb_summarize(records):

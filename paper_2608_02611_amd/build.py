@@ -13,7 +13,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkb.so")
 SOURCES = ["kb_api.hip", "kb_gen.hip", "kb_screen.hip", "kb_locate.hip", "kb_rung.hip",
-           "kb_ops_api.hip", "kb_norm.hip", "kb_attn_fwd.hip", "kb_attn_bwd.hip"]
+           "kb_ops_api.hip", "kb_norm.hip", "kb_attn_fwd.hip", "kb_attn_bwd.hip",
+           "kb_qk_norm.hip", "kb_cache.hip", "kb_attn_paged.hip"]
 ARCH = "gfx950"
 FLAGS = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH, "-ffp-contract=off",
          "-fhip-fp32-correctly-rounded-divide-sqrt",

@@ -1,0 +1,773 @@
+// kb_attn_paged.hip -- softmax attention of new tokens over a paged cache: query
+// i of a sequence's Q new tokens, with K keys in the cache, sees (causal) keys
+// j <= i + K - Q; s_j = scale q_i . k_j, lse = log S(exp s_j),
+// o = S(exp(s_j - lse) v_j).
+//
+// Few rows a sequence (rows: queries x heads of the group; single tokens): bound by
+// the bytes of the keys and values, each read once.  All tiles of 64 keys of all
+// (sequence, key head, block of rows) pairs are numbered one behind the other, and
+// each work-group takes the same number of them, whatever the sequences' lengths
+// are; the pairs that this cuts are joined by a second kernel.  Many rows: bound by
+// the matrix products; work-groups of 128 rows over tiles in LDS, as in the
+// attention over dense keys.
+#include <cfloat>
+#include <type_traits>
+
+#include "kb_attn_tile.hpp"
+#include "kb_paged.hpp"
+
+namespace kb {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kKeys = kPagedTile;
+static_assert(kKeys == 16 * kWaves, "a wave has 16 keys of a tile");
+
+// What a key's row is at: its page, or -1, and its place there.
+struct Place {
+    int page, at;
+};
+__device__ __forceinline__ Place place_of(const PagedParams& p, const int32_t* table, int key, int end) {
+    Place w{-1, 0};
+    if (key < end) {
+        const int n = page_of(p, key);
+        w.page = table[n];
+        w.at = key - n * p.page;
+    }
+    return w;
+}
+__device__ __forceinline__ bool in_cache(const PagedParams& p, int page) { return (uint32_t)page < (uint32_t)p.pages; }
+
+// ---------------------------------------------------------------- few rows --
+//
+// A wave has 16 keys of a tile and all 16 NB rows.  Scores are 16 x 16 products
+// K Q^T: lane l (c = l % 16, g = l / 16) gives key c's elements and has the scores
+// of row c with keys 4g .. 4g+3.  Those are, without moving, the right operand of
+// 16 x 16 products V^T P over 16 keys, whose left operand is of keys 4g .. 4g+3 at
+// element c: a lane reads VB elements of these four keys' rows and pairs them up in
+// registers; product e takes element VB c + e, so that a lane's results are 4 VB
+// elements of row c in a row.  Nothing passes through LDS, and no wave waits for
+// another, until a pair's sums are joined.
+
+template <int DT>
+__device__ __forceinline__ f32x4 mma16(frag_t<DT> a, frag_t<DT> b, f32x4 c) {
+    if constexpr (DT == DT_F16) return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+template <int DT>
+struct Four {
+    typedef storage_t<DT> type __attribute__((ext_vector_type(4)));
+};
+template <int DT>
+using four_t = typename Four<DT>::type;
+__device__ __forceinline__ f32x4 mma4(four_t<DT_F16> a, four_t<DT_F16> b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma4(four_t<DT_BF16> a, four_t<DT_BF16> b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, a), __builtin_bit_cast(s16x4, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mma4(four_t<DT_F32> a, four_t<DT_F32> b, f32x4 c) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], b[k], c, 0, 0, 0);
+    return c;
+}
+
+// N words of a row from element d on, zeros past dim or if !in.  WHOLE: rows are
+// aligned and these elements lie within dim or past it.
+template <int DT, int N, bool WHOLE>
+__device__ __forceinline__ void load_words(const storage_t<DT>* row, int d, int dim, bool in, uint32_t (&out)[N]) {
+    using T = storage_t<DT>;
+    constexpr int W = 4 / (int)sizeof(T), M = N < 4 ? N : 4;  // elements of a word, words of a load
+    typedef uint32_t words __attribute__((ext_vector_type(M), aligned(WHOLE ? 4 * M : sizeof(T))));
+    typedef T elements __attribute__((ext_vector_type(M * W)));
+#pragma unroll
+    for (int k = 0; k < N; k += M) {
+        const int at = d + k * W;
+        words v = {};
+        if (in && at + M * W <= dim) {
+            v = *(const words*)(row + at);
+        } else if (!WHOLE && in && at < dim) {
+            elements x = {};
+#pragma unroll
+            for (int e = 0; e < M * W; ++e)
+                if (at + e < dim) x[e] = row[at + e];
+            v = __builtin_bit_cast(words, x);
+        }
+#pragma unroll
+        for (int e = 0; e < M; ++e) out[k + e] = v[e];
+    }
+}
+
+// The 16 keys of a wave's step, in registers.
+template <int DT, int DP>
+struct Step {
+    using T = storage_t<DT>;
+    static constexpr int KB = 16 / (int)sizeof(T);  // elements of a key that a lane has in a row, 4 KB apart
+    static constexpr int KC = DP / (4 * KB);
+    static constexpr int VB = DP / 16;
+    static constexpr int VW = VB * (int)sizeof(T) / 4;
+    uint32_t k[KC][4], v[4][VW];
+    uint32_t seen;  // bit c: key c is there
+
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const PagedParams& p, const T* kc, const T* vc, Place w, int lane) {
+        const int c = lane & 15, g = lane >> 4;
+        const bool have = in_cache(p, w.page);
+        seen = (uint32_t)__ballot(have) & 0xFFFFu;
+        const T* kr = kc + (have ? w.page * p.cache[0].sb + w.at * p.cache[0].sl : 0);
+#pragma unroll
+        for (int n = 0; n < KC; ++n) load_words<DT, 4, WHOLE>(kr, (4 * n + g) * KB, p.dim, have, k[n]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int page = __shfl(w.page, 4 * g + j), at = __shfl(w.at, 4 * g + j);
+            const bool in = in_cache(p, page);
+            const T* vr = vc + (in ? page * p.cache[1].sb + at * p.cache[1].sl : 0);
+            load_words<DT, VW, WHOLE>(vr, VB * c, p.dim, in, v[j]);
+        }
+    }
+    // Element e of the four keys' pieces.
+    __device__ __forceinline__ four_t<DT> values(int e) const {
+        if constexpr (DT == DT_F32) {
+            return four_t<DT>{__uint_as_float(v[0][e]), __uint_as_float(v[1][e]), __uint_as_float(v[2][e]),
+                              __uint_as_float(v[3][e])};
+        } else {
+            const uint32_t pick = e & 1 ? 0x07060302u : 0x05040100u;  // the high halves of two words, or the low ones
+            typedef uint32_t two __attribute__((ext_vector_type(2)));
+            return __builtin_bit_cast(four_t<DT>, two{__builtin_amdgcn_perm(v[1][e / 2], v[0][e / 2], pick),
+                                                      __builtin_amdgcn_perm(v[3][e / 2], v[2][e / 2], pick)});
+        }
+    }
+};
+
+// Elements of a row of K or Q as an operand of their product.
+template <int DT>
+__device__ __forceinline__ f32x4 mma_scores(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c) {
+    const u32v4 x = {a[0], a[1], a[2], a[3]}, y = {b[0], b[1], b[2], b[3]};
+    if constexpr (DT == DT_F32) return mma4(__builtin_bit_cast(four_t<DT>, x), __builtin_bit_cast(four_t<DT>, y), c);
+    else return mma16<DT>(__builtin_bit_cast(frag_t<DT>, x), __builtin_bit_cast(frag_t<DT>, y), c);
+}
+
+// The softmax state of a lane's row, for each of the NB blocks of 16: terms are
+// exp(scale (s - m)), F16's 2^kBelow of that so that small ones keep their bits, m a
+// score that follows the maximum when a term would pass 2^kSlack; l: their sum over
+// the lane's keys.
+template <int NB>
+struct Rows {
+    float m[NB], l[NB];
+};
+
+template <int DT, int DP, int NB>
+__device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>& st,
+                                             const uint32_t (&q)[NB][Step<DT, DP>::KC][4],
+                                             const Step<DT, DP>& in, float to_log2, const int (&lim)[NB], int key0,
+                                             int every, int lane) {
+    using T = storage_t<DT>;
+    using S = Step<DT, DP>;
+    const int g = lane >> 4;
+    f32x4 s[NB] = {};
+#pragma unroll
+    for (int n = 0; n < S::KC; ++n)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = mma_scores<DT>(in.k[n], q[b][n], s[b]);
+    const bool full = in.seen == 0xFFFFu && key0 + 16 <= every;  // every row sees every key
+    if (!full) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (!(in.seen >> (4 * g + r) & 1) || key0 + 4 * g + r >= lim[b]) s[b][r] = -INFINITY;
+    }
+    four_t<DT> hi[NB], lo[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        float top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[b][0], s[b][1]),
+                                                  __builtin_elementwise_maximum(s[b][2], s[b][3]));
+        const auto passes = [&] { return st.m[b] == -INFINITY ? top > -INFINITY : (top - st.m[b]) * to_log2 > kSlack<DT>; };
+        if (__any(passes())) {
+            // a NaN makes the row's results NaN whatever m is
+            top = fmaxf(top, __shfl_xor(top, 16));
+            top = fmaxf(top, __shfl_xor(top, 32));
+            if (passes()) {
+                const float alpha = st.m[b] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((st.m[b] - top) * to_log2);
+                st.m[b] = top;
+                st.l[b] *= alpha;
+#pragma unroll
+                for (int e = 0; e < S::VB; ++e) acc[b][e] *= alpha;
+            }
+        }
+        const float ref = st.m[b] == -INFINITY ? 0.f : st.m[b];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float t = __builtin_amdgcn_exp2f(fmaf(s[b][r] - ref, to_log2, kBelow<DT>));
+            st.l[b] += t;
+            // 16 bits: the term in two parts, so that what it is rounded by is not lost
+            hi[b][r] = (T)t;
+            if constexpr (DT != DT_F32) lo[b][r] = (T)(t - (float)hi[b][r]);
+        }
+    }
+    // A product takes every key to every row, with 0 where a row does not see it, and
+    // 0 times NaN is NaN: a step with such values that some rows see and others do
+    // not goes row by row.
+    if (!full) {
+        float z = 0.f;
+#pragma unroll
+        for (int e = 0; e < S::VB; ++e) {
+            const four_t<DT> a = in.values(e);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z = fmaf((float)a[j], 0.f, z);
+        }
+        if (__any(z != 0.f)) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll 1
+                for (int n = 0; n < 16; ++n) {
+                    const int end = __builtin_amdgcn_readlane(lim[b], n);
+#pragma unroll
+                    for (int e = 0; e < S::VB; ++e) {
+                        four_t<DT> a = in.values(e);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+                            if (key0 + 4 * g + r >= end) a[r] = (T)0.f;
+                        f32x4 t = {};
+                        t = mma4(a, hi[b], t);
+                        if constexpr (DT != DT_F32) t = mma4(a, lo[b], t);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[b][e][r] = (lane & 15) == n ? acc[b][e][r] + t[r] : acc[b][e][r];
+                    }
+                }
+            return;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < S::VB; ++e) {
+        const four_t<DT> a = in.values(e);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            acc[b][e] = mma4(a, hi[b], acc[b][e]);
+            if constexpr (DT != DT_F32) acc[b][e] = mma4(a, lo[b], acc[b][e]);
+        }
+    }
+}
+
+// Units of sequence b, for one key head and block of rows: tiles, or 1.
+__device__ __forceinline__ int units_of(const PagedParams& p, int b) {
+    return p.pairs ? 1 : max(1, (paged_len(p, b) + kKeys - 1) / kKeys);
+}
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const PagedParams& p, int b) {
+    return (int)(((int64_t)tokens_of(p, b).n * p.group + ROWS - 1) / ROWS);
+}
+
+template <int DT, int DP, int NB, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) paged_few_kernel(PagedParams p) {
+    using T = storage_t<DT>;
+    using S = Step<DT, DP>;
+    constexpr int ROWS = 16 * NB, PITCH = DP + 4;
+    __shared__ __align__(16) float sums[kWaves][ROWS][PITCH];
+    __shared__ float stat_m[kWaves][ROWS], stat_l[kWaves][ROWS];
+    __shared__ int64_t wave_units[kWaves];
+    __shared__ int64_t start_units;
+    __shared__ int start_seq;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int me = (int)blockIdx.x;
+
+    // The units before each thread's sequences.
+    const int each = (p.batch + kThreads - 1) / kThreads, mine = (int)threadIdx.x * each;
+    int64_t units = 0;
+    for (int b = mine; b < min(mine + each, p.batch); ++b)
+        units += (int64_t)blocks_of<ROWS>(p, b) * p.kv_heads * units_of(p, b);
+    int64_t upto = units;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const int64_t before = __shfl_up(upto, m);
+        if (lane >= m) upto += before;
+    }
+    if (lane == 63) wave_units[wave] = upto;
+    __syncthreads();
+    int64_t all = 0, before = upto - units;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) before += wave_units[w];
+        all += wave_units[w];
+    }
+    const int64_t workers = min((int64_t)p.workers, all);
+    PagedHeader* header = (PagedHeader*)p.ws + me;
+    if (me >= workers) {
+        if (!p.pairs && threadIdx.x == 0) header->valid = 0;
+        return;
+    }
+    const int64_t first = all * me / workers, end = all * (me + 1) / workers;
+    if (before <= first && first < before + units) {
+        int b = mine;
+        int64_t at = before;
+        for (; b < p.batch - 1; ++b) {
+            const int64_t n = (int64_t)blocks_of<ROWS>(p, b) * p.kv_heads * units_of(p, b);
+            if (first < at + n) break;
+            at += n;
+        }
+        start_seq = b;
+        start_units = first - at;
+    }
+    __syncthreads();
+    int seq = __builtin_amdgcn_readfirstlane(start_seq);
+    int64_t in_seq = start_units;
+    if (!p.pairs && threadIdx.x == 0) header->valid = 0;
+
+    const float to_log2 = p.scale * kLog2e;
+    const auto slot = [&](int worker, int n) {
+        return p.ws + (int64_t)p.workers * (sizeof(PagedHeader) / sizeof(float)) +
+               ((int64_t)worker * 2 + n) * ROWS * PITCH;
+    };
+    for (int64_t unit = first; unit < end && seq < p.batch;) {
+        const int n_units = units_of(p, seq), klen = paged_len(p, seq);
+        const Tokens tok = tokens_of(p, seq);
+        const int n_blocks = blocks_of<ROWS>(p, seq);
+        if (n_blocks == 0) {  // (a sequence without new tokens has no unit)
+            ++seq;
+            in_seq = 0;
+            continue;
+        }
+        const int pair = __builtin_amdgcn_readfirstlane((int)(in_seq / n_units));
+        const int tile = __builtin_amdgcn_readfirstlane((int)(in_seq - (int64_t)pair * n_units));
+        const int block = pair / p.kv_heads, h = pair - block * p.kv_heads;
+        const int take = (int)min((int64_t)(n_units - tile), end - unit);
+
+        // the rows, and the keys that they see
+        int lim[NB];
+        uint32_t q[NB][S::KC][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const uint32_t row = (uint32_t)block * ROWS + b * 16 + c;
+            const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row - (uint32_t)i * p.group);
+            const bool live = i < tok.n;
+            lim[b] = live ? key_limit(i, tok.n, klen, p.causal) : 0;
+            const T* at = (const T*)p.q.p + (int64_t)(tok.first + (live ? i : 0)) * p.q.st + (live ? hq : 0) * p.q.sh;
+#pragma unroll
+            for (int n = 0; n < S::KC; ++n) load_words<DT, 4, WHOLE>(at, (4 * n + g) * S::KB, p.dim, live, q[b][n]);
+        }
+        const int row_first = (int)((uint32_t)block * ROWS / (uint32_t)p.group);
+        const int row_last = min(tok.n - 1, (int)(((uint32_t)block * ROWS + ROWS - 1) / (uint32_t)p.group));
+        const int every = key_limit(row_first, tok.n, klen, p.causal);  // what the first row sees, all others see
+        const int any = key_limit(row_last, tok.n, klen, p.causal);
+        const int key_end = p.pairs ? any : min(any, (tile + take) * kKeys);
+
+        f32x4 acc[NB][S::VB];
+        Rows<NB> st;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            st.m[b] = -INFINITY;
+            st.l[b] = 0.f;
+#pragma unroll
+            for (int e = 0; e < S::VB; ++e) acc[b][e] = f32x4{};
+        }
+        const int32_t* table = p.table + (int64_t)seq * p.table_stride;
+        const T* kc = (const T*)p.cache[0].p + h * p.cache[0].sh;
+        const T* vc = (const T*)p.cache[1].p + h * p.cache[1].sh;
+        const int key0 = tile * kKeys + 16 * wave;
+        {
+            // one step computed, the next one's keys on their way, the page of the one after that too
+            Step<DT, DP> a, b;
+            Place w = place_of(p, table, key0 + c, key_end);
+            Place next = place_of(p, table, key0 + kKeys + c, key_end);
+            a.template load<WHOLE>(p, kc, vc, w, lane);
+            for (int key = key0; key < key_end; key += 2 * kKeys) {
+                w = next;
+                next = place_of(p, table, key + 2 * kKeys + c, key_end);
+                b.template load<WHOLE>(p, kc, vc, w, lane);
+                step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
+                if (key + kKeys >= key_end) break;
+                w = next;
+                next = place_of(p, table, key + 3 * kKeys + c, key_end);
+                a.template load<WHOLE>(p, kc, vc, w, lane);
+                step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
+            }
+        }
+
+        // the waves' sums, joined through LDS
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            st.l[b] += __shfl_xor(st.l[b], 16);
+            st.l[b] += __shfl_xor(st.l[b], 32);
+            if (g == 0) {
+                stat_m[wave][b * 16 + c] = st.m[b];
+                stat_l[wave][b * 16 + c] = st.l[b];
+            }
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int e = 0; e < S::VB; e += 4)
+                    *(f32x4*)&sums[wave][b * 16 + c][S::VB * (4 * g + r) + e] =
+                        f32x4{acc[b][e][r], acc[b][e + 1][r], acc[b][e + 2][r], acc[b][e + 3][r]};
+        }
+        __syncthreads();
+        const bool begun = tile == 0, ended = tile + take == n_units;
+        const int rows = (int)min((int64_t)ROWS, (int64_t)tok.n * p.group - (int64_t)block * ROWS);
+        float* part = begun && ended ? nullptr : slot(me, begun ? 1 : 0);
+        for (int n = threadIdx.x; n < rows * (DP / 4); n += kThreads) {
+            const int r = n / (DP / 4), d = n % (DP / 4) * 4;
+            float m = stat_m[0][r];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat_m[w][r]);
+            const float ref = m == -INFINITY ? 0.f : m;
+            f32x4 o = {};
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f((stat_m[w][r] - ref) * to_log2);
+                const f32x4 x = *(const f32x4*)&sums[w][r][d];
+                l = fmaf(f, stat_l[w][r], l);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
+            }
+            if (part != nullptr) {
+                *(f32x4*)(part + r * PITCH + d) = o;
+                if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, 0.f, 0.f};
+                continue;
+            }
+            const uint32_t row = (uint32_t)block * ROWS + r;
+            const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row - (uint32_t)i * p.group);
+            const int64_t t = tok.first + i;
+            const bool some = l != 0.f;
+            const float f = 1.f / l;
+            store_quad<DT>((T*)p.o.p + t * p.o.st + hq * p.o.sh, d, p.dim, some ? o[0] * f : 0.f, some ? o[1] * f : 0.f,
+                           some ? o[2] * f : 0.f, some ? o[3] * f : 0.f);
+            if (d == 0 && p.lse != nullptr)
+                p.lse[t * p.heads + hq] =
+                    some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
+        }
+        if (begun && !ended && threadIdx.x == 0) {
+            // the worker that has the pair's last tile
+            const int64_t last = unit + (n_units - tile) - 1;
+            *header = PagedHeader{seq, block, h, (int)(((last + 1) * workers - 1) / all), 1, rows, {0, 0}};
+        }
+        unit += take;
+        in_seq += take;
+        if (in_seq == (int64_t)n_blocks * p.kv_heads * n_units) {
+            ++seq;
+            in_seq = 0;
+        }
+        __syncthreads();  // the sums are read
+    }
+}
+
+// A pair that work-groups share, joined: a work-group (x: the one that began the
+// pair, y: the row) has four waves, each with a quarter of the parts, two elements a
+// lane.
+template <int DT, int DP, int NB>
+__global__ void __launch_bounds__(kThreads) paged_few_join_kernel(PagedParams p) {
+    using T = storage_t<DT>;
+    constexpr int ROWS = 16 * NB, PITCH = DP + 4, E = DP / 64;
+    __shared__ float sums[kWaves][DP], stat_m[kWaves], stat_l[kWaves];
+    const int me = (int)blockIdx.x, r = (int)blockIdx.y;
+    const PagedHeader h = ((const PagedHeader*)p.ws)[me];
+    if (!h.valid || r >= h.rows) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float to_log2 = p.scale * kLog2e;
+    const float* base = p.ws + (int64_t)p.workers * (sizeof(PagedHeader) / sizeof(float)) + r * PITCH;
+    const int parts = h.last - me + 1;
+    const auto part = [&](int k) { return base + ((int64_t)(me + k) * 2 + (k == 0)) * ROWS * PITCH; };
+    float m = -INFINITY, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll 8
+    for (int k = wave; k < parts; k += kWaves) m = fmaxf(m, part(k)[DP]);
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll 8
+    for (int k = wave; k < parts; k += kWaves) {
+        const float* x = part(k);
+        const float f = __builtin_amdgcn_exp2f((x[DP] - ref) * to_log2);
+        l = fmaf(f, x[DP + 1], l);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = fmaf(f, x[lane * E + e], o[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = o[e];
+    if (lane == 0) {
+        stat_m[wave] = m;
+        stat_l[wave] = l;
+    }
+    __syncthreads();
+    const int d = threadIdx.x;
+    if (d >= p.dim) return;
+    m = stat_m[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat_m[w]);
+    const float all = m == -INFINITY ? 0.f : m;
+    float x = 0.f;
+    l = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        const float f = __builtin_amdgcn_exp2f((stat_m[w] - all) * to_log2);
+        l = fmaf(f, stat_l[w], l);
+        x = fmaf(f, sums[w][d], x);
+    }
+    const uint32_t row = (uint32_t)h.block * ROWS + r;
+    const int i = (int)(row / (uint32_t)p.group), hq = h.head * p.group + (int)(row - (uint32_t)i * p.group);
+    const int64_t t = tokens_of(p, h.seq).first + i;
+    const bool some = l != 0.f;
+    ((T*)p.o.p)[t * p.o.st + hq * p.o.sh + d] = (T)(some ? x / l : 0.f);
+    if (d == 0 && p.lse != nullptr)
+        p.lse[t * p.heads + hq] = some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
+}
+
+template <int DT, int DP, int NB>
+hipError_t few(const PagedParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)p.workers);
+    if (p.whole) paged_few_kernel<DT, DP, NB, true><<<grid, kThreads, 0, stream>>>(p);
+    else paged_few_kernel<DT, DP, NB, false><<<grid, kThreads, 0, stream>>>(p);
+    if (!p.pairs) {
+        const int64_t rows = (p.starts != nullptr ? (int64_t)p.tokens : 1) * p.group;
+        paged_few_join_kernel<DT, DP, NB>
+            <<<dim3((unsigned)p.workers, (unsigned)(rows < 16 * NB ? rows : 16 * NB)), kThreads, 0, stream>>>(p);
+    }
+    return hipGetLastError();
+}
+
+// --------------------------------------------------------------- many rows --
+
+constexpr int kRows = kAttnRows;
+
+// Where the rows of a tile lie: lane n of every wave knows of row n.
+struct TilePlace {
+    Place w;
+    uint64_t present;  // rows that are there
+};
+
+// Rows of a tile from their pages, in the background as Filler does it: one
+// descriptor for the rows that a wave fills at once, which are in one page.
+template <int DT, int DP>
+struct PagedFiller {
+    using T = storage_t<DT>;
+    using F = Filler<DT, DP, kKeys, kThreads>;
+    using L = Tile<DT, DP>;
+    static constexpr int SLOTS = F::SLOTS, STEP = F::STEP, STEPS = F::STEPS;
+    int row0;
+    uint32_t offset;
+    bool in;
+
+    __device__ __forceinline__ PagedFiller(int64_t stride, int dim) {
+        row0 = (int)threadIdx.x / SLOTS;
+        const int d = ((int)threadIdx.x % SLOTS ^ L::turn(row0)) * L::VEC;
+        in = d < dim;
+        offset = ((uint32_t)(((int)threadIdx.x & 63) / SLOTS) * (uint32_t)stride + (uint32_t)d) * (uint32_t)sizeof(T);
+    }
+    // base: the head's element 0 of page 0.
+    __device__ __forceinline__ void fill(T* tile, const T* base, const HeadView& c, const TilePlace& at) const {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        T* to = tile + wave * L::KB;
+#pragma unroll
+        for (int k = 0; k < STEPS; ++k) {
+            const int first = k * STEP + wave * L::KB_ROWS;  // of the wave's rows
+            const int page = __builtin_amdgcn_readlane(at.w.page, first), in_page = __builtin_amdgcn_readlane(at.w.at, first);
+            const bool have = (at.present >> (k * STEP + row0)) & 1;
+            const auto from = background(base + (at.present >> first & 1 ? page * c.sb + in_page * c.sl : 0));
+            if (in && have) {
+                send<16>(from, offset, 0, to);
+            } else {
+                const u32v4 zero = {0, 0, 0, 0};
+                *(u32v4*)(to + ((int)threadIdx.x & 63) * L::VEC) = zero;
+            }
+            to += STEP / L::KB_ROWS * L::KB;
+        }
+    }
+};
+
+// The same through registers: any page size, any alignment.
+template <int DT, int DP>
+__device__ __forceinline__ void paged_stage(storage_t<DT>* tile, const storage_t<DT>* base, const HeadView& c,
+                                            const TilePlace& at, int dim) {
+    using L = Tile<DT, DP>;
+    static_assert(kKeys * L::CHUNKS % kThreads == 0, "every thread has the same number of chunks");
+#pragma unroll
+    for (int k = 0; k < kKeys * L::CHUNKS / kThreads; ++k) {
+        const int idx = k * kThreads + (int)threadIdx.x, row = idx / L::CHUNKS, d = idx % L::CHUNKS * L::VEC;
+        const int page = __shfl(at.w.page, row), in_page = __shfl(at.w.at, row);
+        u32v4 v = {0, 0, 0, 0};
+        if (at.present >> row & 1) v = load_chunk(base + page * c.sb + in_page * c.sl, d, dim);
+        *(u32v4*)(tile + L::at(row, d)) = v;
+    }
+}
+
+template <int DT, int DP, bool WHOLE>
+__global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_kernel(PagedParams p) {
+    using T = storage_t<DT>;
+    using L = Tile<DT, DP>;
+    __shared__ __align__(16) T kt[2][L::size(kKeys)];
+    __shared__ __align__(16) T vt[2][L::size(kKeys)];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 5;
+    const int part = (int)blockIdx.y;
+    // the block's sequence: the last one whose first block is no later
+    const int h = (int)(blockIdx.x % (uint32_t)p.kv_heads);
+    const int64_t block = paged_blocks(p, kRows) - 1 - blockIdx.x / (uint32_t)p.kv_heads;
+    const auto first_block = [&](int b) {
+        return (int64_t)(p.starts ? min(max(p.starts[b], 0), p.tokens) : b) * p.group / kRows + b;
+    };
+    const int seq = __builtin_amdgcn_readfirstlane(count_up_to(p.batch, block, lane, first_block)) - 1;
+    if (seq < 0) return;
+    const int64_t block0 = first_block(seq);
+    const Tokens tok = tokens_of(p, seq);
+    const int64_t rows = (int64_t)tok.n * p.group;
+    if (block < block0 || (block - block0) * kRows >= rows) return;  // between two sequences
+    const uint32_t first = (uint32_t)(block - block0) * kRows;
+    const int klen = paged_len(p, seq);
+
+    const uint32_t row = first + wave * 32 + (lane & 31);
+    const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row % (uint32_t)p.group);
+    const bool live = i < tok.n;
+    const int wave_first = __builtin_amdgcn_readfirstlane((int)((first + wave * 32) / (uint32_t)p.group));
+    const int wave_last = __builtin_amdgcn_readfirstlane((int)((first + wave * 32 + 31) / (uint32_t)p.group));
+    const int block_last = (int)((first + kRows - 1) / (uint32_t)p.group);
+    const int lim = key_limit(min(i, tok.n - 1), tok.n, klen, p.causal);
+    const int wave_any = wave_first < tok.n ? key_limit(min(wave_last, tok.n - 1), tok.n, klen, p.causal) : 0;
+    const int block_all = key_limit((int)(first / (uint32_t)p.group), tok.n, klen, p.causal);
+    const int all = key_limit(min(block_last, tok.n - 1), tok.n, klen, p.causal);
+    const int tiles = (all + kKeys - 1) / kKeys;
+    const int start = (int)((int64_t)tiles * part / p.parts) * kKeys;
+    const int end = min(all, (int)((int64_t)tiles * (part + 1) / p.parts) * kKeys);
+
+    const int32_t* table = p.table + (int64_t)seq * p.table_stride;
+    const T* q = (const T*)p.q.p + (int64_t)(tok.first + (live ? i : 0)) * p.q.st + hq * p.q.sh;
+    const T* k = (const T*)p.cache[0].p + h * p.cache[0].sh;
+    const T* v = (const T*)p.cache[1].p + h * p.cache[1].sh;
+    frag_t<DT> qf[DP / 16];
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
+    const Reader<DT, DP> rd(lane);
+    const PagedFiller<DT, DP> fk(p.cache[0].sl, p.dim), fv(p.cache[1].sl, p.dim);
+    const auto fill = [&](const TilePlace& at, int buf) {
+        if (WHOLE) {
+            fk.fill(kt[buf], k, p.cache[0], at);
+            fv.fill(vt[buf], v, p.cache[1], at);
+        } else {
+            paged_stage<DT, DP>(kt[buf], k, p.cache[0], at, p.dim);
+            paged_stage<DT, DP>(vt[buf], v, p.cache[1], at, p.dim);
+        }
+    };
+    const auto look = [&](int j0) { return place_of(p, table, j0 + lane, end); };
+    const auto there = [&](Place w) { return TilePlace{w, __ballot(in_cache(p, w.page))}; };
+
+    const float to_log2 = p.scale * kLog2e;
+    f32x16 acc[DP / 32];
+    Softmax sm;
+    const auto pass = [&](auto careful) {
+        constexpr bool CAREFUL = decltype(careful)::value;
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db) acc[db] = f32x16{};
+        sm = Softmax{};
+        // a tile is used, the next one is filled, the pages of the one after that are looked up
+        TilePlace now = there(look(start)), ahead = now;
+        Place later = look(start + kKeys);
+        if (start < end) fill(now, 0);
+        int j0 = start, buf = 0;
+        const auto next = [&] {
+            tile_wait();
+            __syncthreads();  // the tile is there, and the other one is read
+            now = ahead;
+            if (j0 + kKeys < end) {
+                ahead = there(later);
+                later = look(j0 + 2 * kKeys);
+                fill(ahead, buf ^ 1);
+            }
+        };
+        for (; j0 < end; j0 += kKeys, buf ^= 1) {
+            next();
+            if (j0 >= wave_any) continue;
+            if (j0 + kKeys <= block_all && now.present == ~(uint64_t)0)  // every row of the work-group sees all of it
+                tile_forward<DT, DP, false, CAREFUL && DT != DT_F32>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+            else
+                tile_forward<DT, DP, true, CAREFUL, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0, now.present);
+        }
+    };
+    pass(std::false_type{});
+    if constexpr (DT == DT_F32) {
+        if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
+    } else if (__syncthreads_or((p.causal && non_finite(acc)) || too_coarse(sm))) {
+        pass(std::true_type{});
+        if (sm.m > -INFINITY) sm.m = __builtin_amdgcn_fmed3f(fmaf(sm.m, to_log2, -kBelow<DT>), -FLT_MAX, FLT_MAX);
+    }
+    if (!live) return;
+    const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
+    const int64_t t = tok.first + i;
+    if (p.parts > 1) {
+        const int64_t dim = (p.dim + 3) / 4 * 4;
+        float* to = p.ws + ((t * p.heads + hq) * p.parts + part) * (dim + 4);
+        if (g == 0) *(f32x4*)(to + dim) = f32x4{sm.m, l, rounded, 0.f};
+        store_part<DP>(to, acc, p.dim, g);
+        return;
+    }
+    const bool some = l != 0.f;  // NaN too: it goes on to o
+    store_column<DT, DP>((T*)p.o.p + t * p.o.st + hq * p.o.sh, acc, 1.f / (DT == DT_F32 ? l : rounded), some, p.dim, g);
+    if (g == 0 && p.lse != nullptr)
+        p.lse[t * p.heads + hq] = some ? fmaf(sm.m, unit_natural<DT>(p.scale), kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
+}
+
+// The parts of a row joined, four elements a thread.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) paged_many_join_kernel(PagedParams p) {
+    using T = storage_t<DT>;
+    const int quads = (p.dim + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    const int64_t row = id / quads;  // [token][head]
+    const int d = (int)(id % quads) * 4;
+    if (row >= (int64_t)p.tokens * p.heads) return;
+    const int64_t t = row / p.heads;
+    const int hq = (int)(row - t * p.heads);
+    if (p.starts != nullptr && (t < p.starts[0] || t >= p.starts[p.batch])) return;  // no sequence's
+    const int64_t dim = (p.dim + 3) / 4 * 4, stride = dim + 4;
+    const float* in = p.ws + row * p.parts * stride;
+    float m = -INFINITY;
+    for (int s = 0; s < p.parts; ++s) m = fmaxf(m, in[s * stride + dim]);
+    const float shift = m == -INFINITY ? 0.f : m;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float l = 0.f, rounded = 0.f;
+    for (int s = 0; s < p.parts; ++s) {
+        const f32x4 stat = *(const f32x4*)(in + s * stride + dim), x = *(const f32x4*)(in + s * stride + d);
+        const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * unit_log2<DT>(p.scale));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+        l = fmaf(w, stat[1], l);
+        rounded = fmaf(w, stat[2], rounded);
+    }
+    const bool some = l != 0.f;
+    const float f = some ? 1.f / (DT == DT_F32 ? l : rounded) : 0.f;
+    store_quad<DT>((T*)p.o.p + t * p.o.st + hq * p.o.sh, d, p.dim, some ? acc[0] * f : 0.f, some ? acc[1] * f : 0.f,
+                   some ? acc[2] * f : 0.f, some ? acc[3] * f : 0.f);
+    if (d == 0 && p.lse != nullptr)
+        p.lse[row] = some ? fmaf(m, unit_natural<DT>(p.scale), kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
+}
+
+template <int DT, int DP>
+hipError_t many(const PagedParams& p, hipStream_t stream) {
+    const dim3 grid((unsigned)(paged_blocks(p, kRows) * p.kv_heads), (unsigned)p.parts);
+    // rows that a wave fills at once lie in one page
+    if (p.whole && p.page % Tile<DT, DP>::KB_ROWS == 0) paged_many_kernel<DT, DP, true><<<grid, kThreads, 0, stream>>>(p);
+    else paged_many_kernel<DT, DP, false><<<grid, kThreads, 0, stream>>>(p);
+    if (p.parts > 1) {
+        const int64_t quads = (int64_t)p.tokens * p.heads * ((p.dim + 3) / 4);
+        paged_many_join_kernel<DT><<<dim3((unsigned)((quads + kThreads - 1) / kThreads)), kThreads, 0, stream>>>(p);
+    }
+    return hipGetLastError();
+}
+
+template <int DT>
+hipError_t paged(const PagedParams& p, hipStream_t stream) {
+    if (few_rows(p)) {
+        if (few_block(p) == 16) return p.dim <= 64 ? few<DT, 64, 1>(p, stream) : few<DT, 128, 1>(p, stream);
+        return p.dim <= 64 ? few<DT, 64, 2>(p, stream) : few<DT, 128, 2>(p, stream);
+    }
+    if (p.dim <= 64) return many<DT, 64>(p, stream);
+    if (p.dim <= 96) return many<DT, 96>(p, stream);
+    return many<DT, 128>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_attn_paged(int dtype, const PagedParams& p, hipStream_t stream) {
+    if (dtype == DT_F32) return paged<DT_F32>(p, stream);
+    if (dtype == DT_F16) return paged<DT_F16>(p, stream);
+    return paged<DT_BF16>(p, stream);
+}
+
+}  // namespace kb

@@ -1,11 +1,13 @@
-// kb_ops.hpp -- the reference operators (layer norm, attention): parameters
-// that the host fills in, launchers, and the device helpers they share.
+// kb_ops.hpp -- the reference operators (layer norm, head norms, cache writes,
+// attention): parameters that the host fills in, launchers, and the device
+// helpers they share.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/kb.h"
 #include "kb_device.hpp"
 
 namespace kb {
@@ -61,6 +63,38 @@ inline size_t norm_part_bytes(int64_t rows, int64_t cols) {
 // dtype: x's and y's; wdtype: w's, b's, dw's and db's (dtype or DT_F32).
 hipError_t launch_norm_forward(int dtype, int wdtype, const NormForwardParams& p, hipStream_t stream);
 hipError_t launch_norm_backward(int dtype, int wdtype, const NormBackwardParams& p, hipStream_t stream);
+
+// ------------------------------------------ head norms and their rotation --
+
+// A [tokens][heads][dim] view; strides in elements, dim contiguous.
+struct TokenView {
+    const void* p;
+    int64_t st, sh;
+};
+
+struct QkParams {
+    TokenView x[2], y[2];   // q and k; y: the forward call's outputs, the backward call's dx (y.p may be NULL there)
+    TokenView dy[2];        // backward
+    const void* w[2];       // each NULL: 1
+    void* dw[2];            // backward, each may be NULL
+    const int32_t* positions;
+    const float* freqs;
+    float* part;            // backward: partial sums of dw, [parts][2][dim]
+    int64_t tokens;
+    int heads[2];
+    int dim, rot;
+    float eps;
+    int interleaved;
+    int w_f32;              // w and dw are F32, not of x's type
+    int sums;               // backward: dw of q or of k is wanted
+};
+
+// Work-groups of the backward pass, each with sums of its own.
+constexpr int64_t kQkParts = 1024;
+inline int64_t qk_part_bytes(int64_t dim) { return kQkParts * 2 * dim * (int64_t)sizeof(float); }
+
+hipError_t launch_qk_norm_forward(int dtype, const QkParams& p, hipStream_t stream);
+hipError_t launch_qk_norm_backward(int dtype, const QkParams& p, hipStream_t stream);
 
 // -------------------------------------------------------------- attention --
 
@@ -168,6 +202,79 @@ inline BackwardLayout backward_layout(const AttnParams& p) {
 
 hipError_t launch_attn_forward(int dtype, const AttnParams& p, hipStream_t stream);
 hipError_t launch_attn_backward(int dtype, const AttnParams& p, hipStream_t stream);
+
+// ------------------------------------------------------------ paged cache --
+
+// A cache view [pages][heads][page][dim] is a HeadView: sb from page to page, sl
+// from place to place within one.
+struct PagedParams {
+    TokenView q, o;     // attention
+    TokenView rows[2];  // cache write: k and v
+    HeadView cache[2];  // k's and v's
+    const int32_t* table;  // [batch][width]
+    int64_t table_stride;
+    const int32_t* lens;
+    const int32_t* starts;  // NULL: token b is sequence b's
+    int batch, width;       // pages of a sequence at most
+    int pages, page;        // pages of the cache, keys of a page
+    uint32_t page_mul;      // n / page = n page_mul >> page_shift for n < 2^31
+    int page_shift;
+    int tokens, heads, kv_heads, group, dim;
+    float scale;
+    int causal;
+    int f32;
+    int whole;  // rows of q and of the caches are aligned to 16 bytes and made of 16-byte chunks
+    float* lse;  // [tokens][heads], may be NULL
+    float* ws;
+    int workers;  // few rows a sequence: work-groups
+    int pairs;    // and their units are (sequence, head, block) pairs, not tiles of keys
+    int parts;    // many rows: parts of the keys
+};
+
+// Query rows (query, head of the group) that a sequence has on average up to
+// which a work-group takes 16, or 32, at a time and its waves share the keys.
+constexpr int kFewRows = 32;
+constexpr int kPagedTile = 64;  // keys of a unit of work, 16 a wave
+constexpr int kPagedWorkers = 1024;
+constexpr int kPagedWhole = 512;  // sequences of no more keys are not split
+
+inline int64_t paged_keys(const PagedParams& p) { return (int64_t)p.width * p.page; }
+inline bool few_rows(const PagedParams& p) { return (int64_t)p.tokens * p.group <= (int64_t)kFewRows * p.batch; }
+inline int few_block(const PagedParams& p) { return (int64_t)p.tokens * p.group <= (int64_t)16 * p.batch ? 16 : 32; }
+// At most so many blocks of `rows` query rows have all sequences together: each
+// begins one, and a block numbered (rows before the sequence) / rows + sequence
+// leaves room for it.
+__host__ __device__ inline int64_t paged_blocks(const PagedParams& p, int rows) {
+    return (int64_t)p.tokens * p.group / rows + p.batch;
+}
+
+// Workspace of the attention over pages, in floats.  Few rows: for each
+// work-group a header of eight words, then the sums of its first and its last
+// pair.  Many rows: for each row and part the sums over its keys.
+struct PagedHeader {
+    int32_t seq, block, head, last;  // the pair that this work-group began and others went on with, the last of them
+    int32_t valid, rows, pad[2];
+};
+inline int paged_dim(const PagedParams& p) { return p.dim <= 64 ? 64 : 128; }
+inline int paged_workers(const PagedParams& p) {
+    const int64_t tiles = paged_keys(p) <= kPagedWhole ? 1 : (paged_keys(p) + kPagedTile - 1) / kPagedTile;
+    const int64_t pairs = paged_blocks(p, few_block(p)) * p.kv_heads;
+    return (int)(pairs >= kPagedWorkers || pairs * tiles >= kPagedWorkers ? kPagedWorkers : pairs * tiles);
+}
+inline int paged_parts(const PagedParams& p) {
+    return attn_parts(paged_blocks(p, kAttnRows) * p.kv_heads, paged_keys(p), 1024, p.f32 ? 128 : 512);
+}
+inline int64_t paged_floats(const PagedParams& p) {
+    if (few_rows(p))
+        return paged_keys(p) <= kPagedWhole
+                   ? 0
+                   : (int64_t)paged_workers(p) * (8 + 2 * (int64_t)few_block(p) * (paged_dim(p) + 4));
+    const int parts = paged_parts(p);
+    return parts > 1 ? (int64_t)p.tokens * p.heads * parts * ((p.dim + 3) / 4 * 4 + 4) : 0;
+}
+
+hipError_t launch_cache_write(int dtype, const PagedParams& p, hipStream_t stream);
+hipError_t launch_attn_paged(int dtype, const PagedParams& p, hipStream_t stream);
 
 // ------------------------------------------------------- storage <-> float --
 

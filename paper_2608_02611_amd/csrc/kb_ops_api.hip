@@ -272,6 +272,155 @@ int check_attn(const char* call, const kb_tensor* q, const kb_tensor* k, const k
     return KB_OK;
 }
 
+TokenView token_view(const kb_tensor* t) {
+    return t ? TokenView{t->data, t->strides[0], t->strides[1]} : TokenView{nullptr, 0, 0};
+}
+
+// A dense array of n words that a call reads or writes.
+int check_words(const char* call, const char* name, const void* p, int64_t n) {
+    if (p == nullptr && n > 0) return fail(KB_ERR_INVALID_ARG, "%s: null %s", call, name);
+    if ((uintptr_t)p & 3u) return fail(KB_ERR_ALIGNMENT, "%s: %s not aligned to its element", call, name);
+    return KB_OK;
+}
+
+// The weights' type: q's, or F32 for all of them.
+int check_weight(const char* call, const char* name, const kb_tensor* w, const kb_tensor& q, int* wdtype, bool output) {
+    if (w == nullptr) return KB_OK;
+    if (const int rc = check_view(call, name, w, 1, output)) return rc;
+    if (w->shape[0] != q.shape[2])
+        return fail(KB_ERR_INVALID_ARG, "%s: %s has %lld elements, not %lld", call, name, (long long)w->shape[0],
+                    (long long)q.shape[2]);
+    if (w->dtype != q.dtype && w->dtype != DT_F32)
+        return fail(KB_ERR_DTYPE, "%s: %s has dtype %d, neither q's nor F32", call, name, w->dtype);
+    if (*wdtype >= 0 && *wdtype != w->dtype)
+        return fail(KB_ERR_DTYPE, "%s: %s has dtype %d, another weight %d", call, name, w->dtype, *wdtype);
+    *wdtype = w->dtype;
+    return KB_OK;
+}
+
+// q, k, the weights and the options of the head norm calls; fills p.
+int check_qk(const char* call, const kb_tensor* q, const kb_tensor* k, const kb_tensor* wq, const kb_tensor* wk,
+             const kb_qk_opts* opts, QkParams* p, int* wdtype) {
+    int rc;
+    if ((rc = check_view(call, "q", q, 3, false)) || (rc = check_view(call, "k", k, 3, false))) return rc;
+    if (k->dtype != q->dtype) return fail(KB_ERR_DTYPE, "%s: k has dtype %d, q has %d", call, k->dtype, q->dtype);
+    if (k->shape[0] != q->shape[0] || k->shape[2] != q->shape[2])
+        return fail(KB_ERR_INVALID_ARG, "%s: q and k do not fit together", call);
+    if (q->shape[2] < 1 || q->shape[2] > KB_QK_MAX_DIM)
+        return fail(KB_ERR_INVALID_ARG, "%s: head dimension %lld not in [1, %d]", call, (long long)q->shape[2], KB_QK_MAX_DIM);
+    if (q->shape[1] > KB_MAX_HEADS || k->shape[1] > KB_MAX_HEADS)
+        return fail(KB_ERR_INVALID_ARG, "%s: more than %d heads", call, KB_MAX_HEADS);
+    if ((rc = check_weight(call, "wq", wq, *q, wdtype, false)) || (rc = check_weight(call, "wk", wk, *q, wdtype, false)))
+        return rc;
+    if (opts == nullptr) return fail(KB_ERR_INVALID_ARG, "%s: null opts", call);
+    if (!std::isfinite(opts->eps) || opts->eps < 0.f)
+        return fail(KB_ERR_INVALID_ARG, "%s: eps not finite and >= 0", call);
+    if (opts->flags & ~(uint32_t)KB_QK_INTERLEAVED)
+        return fail(KB_ERR_INVALID_ARG, "%s: unknown flags 0x%x", call, opts->flags);
+    if (opts->rot_dim < 0 || opts->rot_dim % 2 || opts->rot_dim > q->shape[2])
+        return fail(KB_ERR_INVALID_ARG, "%s: rot_dim %d is odd or not in [0, %lld]", call, opts->rot_dim,
+                    (long long)q->shape[2]);
+    if ((rc = check_words(call, "positions", opts->positions, opts->rot_dim ? q->shape[0] : 0)) ||
+        (rc = check_words(call, "freqs", opts->freqs, opts->rot_dim / 2)))
+        return rc;
+    p->x[0] = token_view(q);
+    p->x[1] = token_view(k);
+    p->w[0] = data_of(wq);
+    p->w[1] = data_of(wk);
+    p->positions = opts->positions;
+    p->freqs = opts->freqs;
+    p->tokens = q->shape[0];
+    p->heads[0] = (int)q->shape[1];
+    p->heads[1] = (int)k->shape[1];
+    p->dim = (int)q->shape[2];
+    p->rot = opts->rot_dim;
+    p->eps = opts->eps;
+    p->interleaved = (opts->flags & KB_QK_INTERLEAVED) != 0;
+    return KB_OK;
+}
+
+// The caches, which are outputs of a write, the page table and what hangs on
+// them; fills p.
+int check_pages(const char* call, const kb_tensor* k_cache, const kb_tensor* v_cache, const kb_pages* pages, bool output,
+                const kb_tensor& rows, PagedParams* p) {
+    int rc;
+    if ((rc = check_view(call, "k_cache", k_cache, 4, output)) || (rc = check_view(call, "v_cache", v_cache, 4, output)) ||
+        (rc = check_shape(call, "v_cache", *v_cache, "k_cache", *k_cache)))
+        return rc;
+    if (k_cache->dtype != rows.dtype)
+        return fail(KB_ERR_DTYPE, "%s: the caches have dtype %d, the tokens %d", call, k_cache->dtype, rows.dtype);
+    if (k_cache->shape[3] != rows.shape[2])
+        return fail(KB_ERR_INVALID_ARG, "%s: head dimension %lld in the caches, %lld in the tokens", call,
+                    (long long)k_cache->shape[3], (long long)rows.shape[2]);
+    if (rows.shape[2] < 1 || rows.shape[2] > KB_ATTN_MAX_DIM)
+        return fail(KB_ERR_INVALID_ARG, "%s: head dimension %lld not in [1, %d]", call, (long long)rows.shape[2],
+                    KB_ATTN_MAX_DIM);
+    if (rows.shape[1] > KB_MAX_HEADS || k_cache->shape[1] > KB_MAX_HEADS)
+        return fail(KB_ERR_INVALID_ARG, "%s: more than %d heads", call, KB_MAX_HEADS);
+    if (pages == nullptr) return fail(KB_ERR_INVALID_ARG, "%s: null pages", call);
+    const int64_t page = k_cache->shape[2], width = pages->max_pages, batch = pages->batch;
+    if (page < 1) return fail(KB_ERR_INVALID_ARG, "%s: pages of no key", call);
+    if (batch < 0 || width < 0 || batch > ((int64_t)1 << 20) || page * width > kMaxLen)
+        return fail(KB_ERR_INVALID_ARG, "%s: batch %d or max_pages %d out of range", call, pages->batch, pages->max_pages);
+    if (batch > 1 && (pages->table_stride < width || pages->table_stride > ((int64_t)1 << 40)))
+        return fail(KB_ERR_INVALID_ARG, "%s: table_stride %lld out of range", call, (long long)pages->table_stride);
+    if (rows.shape[0] > kMaxLen) return fail(KB_ERR_INVALID_ARG, "%s: %lld tokens", call, (long long)rows.shape[0]);
+    if (pages->starts == nullptr && rows.shape[0] != batch)
+        return fail(KB_ERR_INVALID_ARG, "%s: %lld tokens of %lld sequences without starts", call, (long long)rows.shape[0],
+                    (long long)batch);
+    if ((rc = check_words(call, "table", pages->table, batch * width)) || (rc = check_words(call, "lens", pages->lens, batch)) ||
+        (rc = check_words(call, "starts", pages->starts, 0)))
+        return rc;
+    p->cache[0] = head_view(k_cache);
+    p->cache[1] = head_view(v_cache);
+    p->table = pages->table;
+    p->table_stride = batch > 1 ? pages->table_stride : 0;
+    p->lens = pages->lens;
+    p->starts = pages->starts;
+    p->batch = (int)batch;
+    p->width = (int)width;
+    p->pages = (int)k_cache->shape[0];
+    p->page = (int)page;
+    int bits = 0;
+    while (((int64_t)1 << bits) < page) ++bits;
+    p->page_shift = 31 + bits;
+    p->page_mul = (uint32_t)(((uint64_t)1 << p->page_shift) / (uint64_t)page + 1);
+    p->tokens = (int)rows.shape[0];
+    p->kv_heads = (int)k_cache->shape[1];
+    p->dim = (int)rows.shape[2];
+    return KB_OK;
+}
+
+// The words of pages that a call reads, for check_apart: the table, rows apart, as
+// one range.
+struct PageWords {
+    kb_tensor table, lens, starts;
+};
+PageWords page_words(const PagedParams& p) {
+    const int64_t n = p.batch > 0 && p.width > 0 ? (int64_t)(p.batch - 1) * p.table_stride + p.width : 0;
+    return {word_array(p.table, n), word_array(p.lens, p.batch), word_array(p.starts, p.starts ? (int64_t)p.batch + 1 : 0)};
+}
+
+// Rows that can be read in aligned 16-byte chunks.
+bool whole_views(const kb_tensor& t) {
+    const int64_t n = 16 / element_bytes(t.dtype);
+    if (((uintptr_t)t.data & 15u) || t.shape[t.ndim - 1] % n) return false;
+    for (int i = 0; i < t.ndim - 1; ++i)
+        if (t.shape[i] > 1 && t.strides[i] % n) return false;
+    return true;
+}
+
+// Sizes of an attention call over pages; false if they are out of range.
+bool paged_sizes(const kb_tensor& q, PagedParams* p) {
+    if (p->kv_heads == 0 ? q.shape[1] != 0 : q.shape[1] % p->kv_heads != 0) return false;
+    p->heads = (int)q.shape[1];
+    p->group = p->kv_heads ? p->heads / p->kv_heads : 0;
+    p->f32 = q.dtype == DT_F32;
+    if ((int64_t)p->tokens * p->heads > kMaxLen) return false;
+    const int64_t most = ((int64_t)1 << 24) - 1;
+    return p->group == 0 || few_rows(*p) || paged_blocks(*p, kAttnRows) * p->kv_heads <= most;
+}
+
 int check_lse(const char* call, const float* lse, const kb_tensor& q) {
     if (lse == nullptr && q.shape[0] * q.shape[1] * q.shape[2] > 0)
         return fail(KB_ERR_INVALID_ARG, "%s: null lse", call);
@@ -422,6 +571,149 @@ int kb_attn_backward(const kb_tensor* dout, const kb_tensor* q, const kb_tensor*
     p.ws = (float*)workspace;
     const hipError_t e = launch_attn_backward(q->dtype, p, stream);
     return e == hipSuccess ? KB_OK : fail_hip(e, "kb_attn_backward: launch");
+}
+
+int kb_qk_norm_forward(const kb_tensor* q, const kb_tensor* k, const kb_tensor* wq, const kb_tensor* wk,
+                       const kb_qk_opts* opts, const kb_tensor* q_out, const kb_tensor* k_out, hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_qk_norm_forward";
+    QkParams p{};
+    int rc, wdtype = -1;
+    if ((rc = check_qk(call, q, k, wq, wk, opts, &p, &wdtype)) || (rc = check_view(call, "q_out", q_out, 3, true)) ||
+        (rc = check_shape(call, "q_out", *q_out, "q", *q)) || (rc = check_view(call, "k_out", k_out, 3, true)) ||
+        (rc = check_shape(call, "k_out", *k_out, "k", *k)))
+        return rc;
+    const auto in_place = [](const kb_tensor& y, const kb_tensor& x) {
+        return y.data == x.data && (x.shape[0] <= 1 || y.strides[0] == x.strides[0]) &&
+               (x.shape[1] <= 1 || y.strides[1] == x.strides[1]);
+    };
+    const kb_tensor tp = word_array(p.positions, p.rot ? p.tokens : 0), tf = word_array(p.freqs, p.rot / 2);
+    const Named qo[] = {{"q_out", q_out}}, ko[] = {{"k_out", k_out}}, both[] = {{"q_out", q_out}, {"k_out", k_out}};
+    const Named ins[] = {{"wq", wq}, {"wk", wk}, {"positions", &tp}, {"freqs", &tf}};
+    const Named q_in[] = {{"k", k}, {"q", q}}, k_in[] = {{"q", q}, {"k", k}};
+    if ((rc = check_apart(call, both, 2, ins, 4)) || (rc = check_apart(call, qo, 1, q_in, in_place(*q_out, *q) ? 1 : 2)) ||
+        (rc = check_apart(call, ko, 1, k_in, in_place(*k_out, *k) ? 1 : 2)))
+        return rc;
+    if (is_empty(*q) && is_empty(*k)) return KB_OK;
+    p.y[0] = token_view(q_out);
+    p.y[1] = token_view(k_out);
+    p.w_f32 = wdtype == DT_F32;
+    const hipError_t e = launch_qk_norm_forward(q->dtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_qk_norm_forward: launch");
+}
+
+size_t kb_qk_norm_backward_workspace_bytes(int64_t dim) {
+    return dim < 1 || dim > KB_QK_MAX_DIM ? 0 : (size_t)qk_part_bytes(dim);
+}
+
+int kb_qk_norm_backward(const kb_tensor* dq_out, const kb_tensor* dk_out, const kb_tensor* q, const kb_tensor* k,
+                        const kb_tensor* wq, const kb_tensor* wk, const kb_qk_opts* opts, const kb_tensor* dq,
+                        const kb_tensor* dk, const kb_tensor* dwq, const kb_tensor* dwk, void* workspace,
+                        size_t workspace_bytes, hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_qk_norm_backward";
+    QkParams p{};
+    int rc, wdtype = -1;
+    if ((rc = check_qk(call, q, k, wq, wk, opts, &p, &wdtype)) || (rc = check_view(call, "dq_out", dq_out, 3, false)) ||
+        (rc = check_shape(call, "dq_out", *dq_out, "q", *q)) || (rc = check_view(call, "dk_out", dk_out, 3, false)) ||
+        (rc = check_shape(call, "dk_out", *dk_out, "k", *k)) ||
+        (dq && ((rc = check_view(call, "dq", dq, 3, true)) || (rc = check_shape(call, "dq", *dq, "q", *q)))) ||
+        (dk && ((rc = check_view(call, "dk", dk, 3, true)) || (rc = check_shape(call, "dk", *dk, "k", *k)))) ||
+        (rc = check_weight(call, "dwq", dwq, *q, &wdtype, true)) || (rc = check_weight(call, "dwk", dwk, *q, &wdtype, true)))
+        return rc;
+    const size_t need = dwq || dwk ? (size_t)qk_part_bytes(p.dim) : 0;
+    if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
+    const kb_tensor tp = word_array(p.positions, p.rot ? p.tokens : 0), tf = word_array(p.freqs, p.rot / 2);
+    const kb_tensor tw = word_array(need ? workspace : nullptr, (int64_t)(need / sizeof(float)));
+    const Named outs[] = {{"dq", dq}, {"dk", dk}, {"dwq", dwq}, {"dwk", dwk}, {"the workspace", &tw}};
+    const Named ins[] = {{"dq_out", dq_out}, {"dk_out", dk_out}, {"q", q}, {"k", k}, {"wq", wq}, {"wk", wk},
+                         {"positions", &tp}, {"freqs", &tf}};
+    if ((rc = check_apart(call, outs, 5, ins, 8))) return rc;
+    if (is_empty(*q) && is_empty(*k)) p.tokens = 0;
+    if (p.tokens == 0 && !need) return KB_OK;
+    p.dy[0] = token_view(dq_out);
+    p.dy[1] = token_view(dk_out);
+    p.y[0] = token_view(dq);
+    p.y[1] = token_view(dk);
+    p.dw[0] = (void*)data_of(dwq);
+    p.dw[1] = (void*)data_of(dwk);
+    p.part = (float*)workspace;
+    p.sums = need != 0;
+    p.w_f32 = wdtype == DT_F32;
+    const hipError_t e = launch_qk_norm_backward(q->dtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_qk_norm_backward: launch");
+}
+
+int kb_cache_write(const kb_tensor* k, const kb_tensor* v, const kb_pages* pages, const kb_tensor* k_cache,
+                   const kb_tensor* v_cache, hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_cache_write";
+    PagedParams p{};
+    int rc;
+    if ((rc = check_view(call, "k", k, 3, false)) || (rc = check_view(call, "v", v, 3, false)) ||
+        (rc = check_shape(call, "v", *v, "k", *k)) || (rc = check_pages(call, k_cache, v_cache, pages, true, *k, &p)))
+        return rc;
+    if (k->shape[1] != p.kv_heads)
+        return fail(KB_ERR_INVALID_ARG, "%s: %lld heads, %d in the caches", call, (long long)k->shape[1], p.kv_heads);
+    const PageWords words = page_words(p);
+    const Named outs[] = {{"k_cache", k_cache}, {"v_cache", v_cache}};
+    const Named ins[] = {{"k", k}, {"v", v}, {"table", &words.table}, {"lens", &words.lens}, {"starts", &words.starts}};
+    if ((rc = check_apart(call, outs, 2, ins, 5))) return rc;
+    if (is_empty(*k) || is_empty(*k_cache) || p.batch == 0 || p.width == 0) return KB_OK;
+    p.rows[0] = token_view(k);
+    p.rows[1] = token_view(v);
+    const hipError_t e = launch_cache_write(k->dtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_cache_write: launch");
+}
+
+size_t kb_attn_paged_workspace_bytes(const kb_tensor* q, const kb_tensor* k_cache, const kb_pages* pages) {
+    clear_error();
+    PagedParams p{};
+    if (check_view("kb_attn_paged_workspace_bytes", "q", q, 3, false) ||
+        check_pages("kb_attn_paged_workspace_bytes", k_cache, k_cache, pages, false, *q, &p) || !paged_sizes(*q, &p) ||
+        is_empty(*q) || p.batch == 0)
+        return 0;
+    return (size_t)paged_floats(p) * sizeof(float);
+}
+
+int kb_attn_paged(const kb_tensor* q, const kb_tensor* k_cache, const kb_tensor* v_cache, const kb_pages* pages,
+                  float scale, uint32_t flags, const kb_tensor* o, float* lse, void* workspace, size_t workspace_bytes,
+                  hipStream_t stream) {
+    clear_error();
+    static const char* call = "kb_attn_paged";
+    PagedParams p{};
+    int rc;
+    if ((rc = check_view(call, "q", q, 3, false)) || (rc = check_pages(call, k_cache, v_cache, pages, false, *q, &p)) ||
+        (rc = check_view(call, "o", o, 3, true)) || (rc = check_shape(call, "o", *o, "q", *q)))
+        return rc;
+    if (!paged_sizes(*q, &p))
+        return fail(KB_ERR_INVALID_ARG, "%s: q and the caches do not fit together, or are too large", call);
+    if (!std::isfinite(scale) || !(scale > 0.f)) return fail(KB_ERR_INVALID_ARG, "%s: scale not finite and > 0", call);
+    if (flags & ~(uint32_t)KB_ATTN_CAUSAL) return fail(KB_ERR_INVALID_ARG, "%s: unknown flags 0x%x", call, flags);
+    if ((uintptr_t)lse & 3u) return fail(KB_ERR_ALIGNMENT, "%s: lse not aligned to its element", call);
+    const bool empty = is_empty(*q) || p.batch == 0;
+    const size_t need = empty ? 0 : (size_t)paged_floats(p) * sizeof(float);
+    if ((rc = check_workspace(call, workspace, workspace_bytes, need))) return rc;
+    const PageWords words = page_words(p);
+    const kb_tensor tl = word_array(lse, (int64_t)p.tokens * p.heads);
+    const kb_tensor tw = word_array(need ? workspace : nullptr, (int64_t)(need / sizeof(float)));
+    const Named outs[] = {{"o", o}, {"lse", &tl}, {"the workspace", &tw}};
+    const Named ins[] = {{"q", q}, {"k_cache", k_cache}, {"v_cache", v_cache}, {"table", &words.table},
+                         {"lens", &words.lens}, {"starts", &words.starts}};
+    if ((rc = check_apart(call, outs, 3, ins, 6))) return rc;
+    if (empty) return KB_OK;
+    p.q = token_view(q);
+    p.o = token_view(o);
+    p.scale = scale;
+    p.causal = (flags & KB_ATTN_CAUSAL) != 0;
+    p.whole = whole_views(*q) && whole_rows(*k_cache) && whole_rows(*v_cache);
+    p.lse = lse;
+    p.ws = (float*)workspace;
+    p.workers = paged_workers(p);
+    p.pairs = paged_keys(p) <= kPagedWhole;
+    p.parts = paged_parts(p);
+    const hipError_t e = launch_attn_paged(q->dtype, p, stream);
+    return e == hipSuccess ? KB_OK : fail_hip(e, "kb_attn_paged: launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,427 @@
+// kb_qk_norm.hip -- norms of query and key heads with the position rotation,
+// forward and backward.
+//
+// Forward, for each head row x of a token:  r = 1 / sqrt(S(x^2) / D + eps),
+//   g = x r w, and of the first `rot` elements each pair (a, b) becomes
+//   (a cos - b sin, b cos + a sin) of the token's angle for that pair.
+// Backward:  g = dy turned the other way, z = x r, u = g w,
+//   dx = r (u - z S(u z) / D), dw = S(g z) over tokens and heads.
+// Both move bytes: forward reads x and writes y, backward reads dy and x and
+// writes dx.  A token's angles are the same for all of its heads, so a wave takes
+// the head rows of one token and works the angles out once.
+#include "kb_ops.hpp"
+
+namespace kb {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxPairs = KB_QK_MAX_DIM / 2;
+
+// cos and sin of position * freq.  The angle is exact: the binary64 product of a
+// 31-bit and a 24-bit number, and what its rounding left.  In turns, less the
+// nearest quarter, it is off by less than 2^-56 up to angles of 2^50 (1 / (2 pi) in
+// two parts, the first product's rounding taken back by the fma); then Taylor's
+// series on [-pi/4, pi/4], whose first term left out is under 2^-28.
+__device__ __forceinline__ void turn_of(int position, float freq, float* cos_out, float* sin_out) {
+    constexpr double kInv = 0.15915494309189535, kInvLow = -9.8393350380770985e-18;  // 1 / (2 pi)
+    constexpr double kTwoPi = 6.283185307179586;
+    const double n = (double)position, f = (double)freq;
+    const double angle = n * f, left = fma(n, f, -angle);
+    const double quarters = rint(4.0 * (angle * kInv));
+    double t = fma(angle, kInv, -0.25 * quarters);
+    t = fma(angle, kInvLow, t);
+    t = fma(left, kInv, t);
+    const float r = (float)(t * kTwoPi), q = r * r;
+    float s = fmaf(q, 2.7557319e-6f, -1.9841270e-4f);
+    s = fmaf(q, s, 8.3333333e-3f);
+    s = fmaf(q, s, -1.6666667e-1f);
+    s = fmaf(r * q, s, r);
+    float c = fmaf(q, -2.7557319e-7f, 2.4801587e-5f);
+    c = fmaf(q, c, -1.3888889e-3f);
+    c = fmaf(q, c, 4.1666667e-2f);
+    c = fmaf(q, c, -0.5f);
+    c = fmaf(q, c, 1.f);
+    const int k = (int)(quarters - 4.0 * floor(quarters * 0.25));
+    const float a = k & 1 ? s : c, b = k & 1 ? c : s;
+    *cos_out = (k + 1) & 2 ? -a : a;
+    *sin_out = k & 2 ? -b : b;
+}
+
+// What a lane has of each head row: a unit of two vectors of V elements, at
+// `first` and `second`, that make V rotating pairs: elements i and V + i of the
+// unit, or 2i and 2i + 1 (NEAR).  Behind the rotating units come units of the
+// other elements; the last of them may lack its second vector.  A row is held by
+// `lanes` lanes, a power of two, so a wave has 64 / lanes rows at a time.
+template <int DT, int V>
+struct Vec {
+    typedef storage_t<DT> type __attribute__((ext_vector_type(V), aligned(sizeof(storage_t<DT>))));
+};
+
+template <int DT, int V, bool NEAR>
+struct Unit {
+    using T = storage_t<DT>;
+    using VT = typename Vec<DT, V>::type;
+    int first, second, pair;  // pair: the first of its V pairs
+    bool in, two, rotates;
+
+    __device__ __forceinline__ void set(int u, int dim, int rot) {
+        const int rotating = rot / (2 * V);
+        rotates = u < rotating;
+        pair = V * u;
+        if (rotates) {
+            first = NEAR ? 2 * V * u : V * u;
+            second = NEAR ? first + V : rot / 2 + V * u;
+        } else {
+            first = rot + 2 * V * (u - rotating);
+            second = first + V;
+        }
+        in = first < dim;
+        two = second < dim;
+    }
+    __device__ __forceinline__ void load(const T* row, bool live, VT (&v)[2]) const {
+        v[0] = v[1] = VT{};
+        if (live && in) v[0] = *(const VT*)(row + first);
+        if (live && two && in) v[1] = *(const VT*)(row + second);
+    }
+    __device__ __forceinline__ void store(T* row, bool live, const float (&x)[2 * V]) const {
+        VT v[2];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            v[0][e] = (T)x[e];
+            v[1][e] = (T)x[V + e];
+        }
+        if (live && in) *(VT*)(row + first) = v[0];
+        if (live && two && in) *(VT*)(row + second) = v[1];
+    }
+    // The pairs turned by (cos, sin); sign -1: the other way.
+    __device__ __forceinline__ void turn(float (&x)[2 * V], const float (&c)[V], const float (&s)[V], float sign) const {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int ia = NEAR ? 2 * i : i, ib = NEAR ? 2 * i + 1 : V + i;
+            const float a = x[ia], b = x[ib], si = sign * s[i];
+            x[ia] = rotates ? fmaf(a, c[i], -(b * si)) : a;
+            x[ib] = rotates ? fmaf(b, c[i], a * si) : b;
+        }
+    }
+    __device__ __forceinline__ void weight(const void* w, int w_f32, float (&out)[2 * V]) const {
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) {
+            const int d = e < V ? first + e : second + e - V;
+            const bool have = w != nullptr && in && (e < V || two);
+            out[e] = !have ? 1.f : w_f32 ? ((const float*)w)[d] : (float)((const T*)w)[d];
+        }
+    }
+};
+
+// Sum over the lanes of a row, the same bits in each.
+__device__ __forceinline__ float row_sum(float v, int lanes) {
+    if (lanes > 1) v += __uint_as_float(dpp_u32<DPP_QUAD_XOR1>(__float_as_uint(v)));
+    if (lanes > 2) v += __uint_as_float(dpp_u32<DPP_QUAD_XOR2>(__float_as_uint(v)));
+    if (lanes > 4) v += __uint_as_float(dpp_u32<DPP_ROW_HALF_MIRROR>(__float_as_uint(v)));
+    if (lanes > 8) v += __uint_as_float(dpp_u32<DPP_ROW_MIRROR>(__float_as_uint(v)));
+    if (lanes > 16) v += __shfl_xor(v, 16);
+    if (lanes > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// The token's angles, by all lanes of a wave into its own LDS, and from there
+// those of the lane's unit.
+template <int V, int E>
+__device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, int lane, float (*turns)[kMaxPairs],
+                                            const int (&pair)[E], const bool (&rotates)[E], float (&c)[E][V],
+                                            float (&s)[E][V]) {
+    const int position = p.positions[token];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int i = lane; i < p.rot / 2; i += 64) turn_of(position, p.freqs[i], &turns[0][i], &turns[1][i]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int n = 0; n < E; ++n)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            c[n][i] = rotates[n] ? turns[0][pair[n] + i] : 1.f;
+            s[n][i] = rotates[n] ? turns[1][pair[n] + i] : 0.f;
+        }
+}
+
+// A wave's passes over a token: `per` rows of q, or of k, in each.
+struct Passes {
+    int per, of_q, all;
+    __device__ __forceinline__ Passes(const QkParams& p, int lanes) {
+        per = 64 / lanes;
+        of_q = (p.heads[0] + per - 1) / per;
+        all = of_q + (p.heads[1] + per - 1) / per;
+    }
+};
+
+template <int DT, int V, int E, bool NEAR>
+__global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p, int lanes, int passes_each) {
+    using T = storage_t<DT>;
+    using U = Unit<DT, V, NEAR>;
+    __shared__ __align__(16) float turns[kWaves][2][kMaxPairs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const Passes ps(p, lanes);
+    const int in_row = lane & (lanes - 1), row0 = lane / lanes;
+    const int from = (int)blockIdx.y * passes_each, to = min(ps.all, from + passes_each);
+    const float inv = 1.f / (float)p.dim;
+    U unit[E];
+#pragma unroll
+    for (int n = 0; n < E; ++n) unit[n].set(in_row + n * lanes, p.dim, p.rot);
+    int pair[E];
+    bool rotates[E];
+    float w[2][E][2 * V];
+#pragma unroll
+    for (int n = 0; n < E; ++n) {
+        pair[n] = unit[n].pair;
+        rotates[n] = unit[n].rotates;
+        unit[n].weight(p.w[0], p.w_f32, w[0][n]);
+        unit[n].weight(p.w[1], p.w_f32, w[1][n]);
+    }
+    const int64_t step = (int64_t)gridDim.x * kWaves;
+    for (int64_t token = (int64_t)blockIdx.x * kWaves + wave; token < p.tokens; token += step) {
+        typename U::VT next[E][2];
+        const auto fetch = [&](int pass) {
+            const int t = pass >= ps.of_q, row = (t ? pass - ps.of_q : pass) * ps.per + row0;
+            const T* x = (const T*)p.x[t].p + token * p.x[t].st + row * p.x[t].sh;
+#pragma unroll
+            for (int n = 0; n < E; ++n) unit[n].load(x, row < p.heads[t], next[n]);
+        };
+        fetch(from);
+        float c[E][V], s[E][V];
+        if (p.rot > 0) token_turns<V, E>(p, token, lane, turns[wave], pair, rotates, c, s);
+        for (int pass = from; pass < to; ++pass) {
+            float x[E][2 * V], sum = 0.f;
+#pragma unroll
+            for (int n = 0; n < E; ++n)
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) {
+                    x[n][e] = (float)next[n][e / V][e % V];
+                    sum = fmaf(x[n][e], x[n][e], sum);
+                }
+            if (pass + 1 < to) fetch(pass + 1);
+            const float r = 1.f / sqrtf(fmaf(row_sum(sum, lanes), inv, p.eps));
+            const int t = pass >= ps.of_q, row = (t ? pass - ps.of_q : pass) * ps.per + row0;
+            T* y = (T*)p.y[t].p + token * p.y[t].st + row * p.y[t].sh;
+#pragma unroll
+            for (int n = 0; n < E; ++n) {
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) x[n][e] = x[n][e] * r * (t ? w[1][n][e] : w[0][n][e]);
+                if (p.rot > 0) unit[n].turn(x[n], c[n], s[n], 1.f);
+                unit[n].store(y, row < p.heads[t], x[n]);
+            }
+        }
+    }
+}
+
+template <int DT, int V, int E, bool NEAR>
+__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkParams p, int lanes, int passes_each) {
+    using T = storage_t<DT>;
+    using U = Unit<DT, V, NEAR>;
+    __shared__ __align__(16) float turns[kWaves][2][kMaxPairs];
+    __shared__ float sums[kWaves][2][KB_QK_MAX_DIM];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const Passes ps(p, lanes);
+    const int in_row = lane & (lanes - 1), row0 = lane / lanes;
+    const int chunks = (ps.all + passes_each - 1) / passes_each;
+    const float inv = 1.f / (float)p.dim;
+    U unit[E];
+#pragma unroll
+    for (int n = 0; n < E; ++n) unit[n].set(in_row + n * lanes, p.dim, p.rot);
+    int pair[E];
+    bool rotates[E];
+    float w[2][E][2 * V], dw[2][E][2 * V];
+#pragma unroll
+    for (int n = 0; n < E; ++n) {
+        pair[n] = unit[n].pair;
+        rotates[n] = unit[n].rotates;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            unit[n].weight(p.w[t], p.w_f32, w[t][n]);
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) dw[t][n][e] = 0.f;
+        }
+    }
+    const int64_t step = (int64_t)gridDim.x * kWaves, items = p.tokens * chunks;
+    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += step) {
+        const int64_t token = chunks == 1 ? item : item / chunks;
+        const int from = (int)(item - token * chunks) * passes_each, to = min(ps.all, from + passes_each);
+        typename U::VT next[E][2], next_dy[E][2];
+        const auto fetch = [&](int pass) {
+            const int t = pass >= ps.of_q, row = (t ? pass - ps.of_q : pass) * ps.per + row0;
+            const T* x = (const T*)p.x[t].p + token * p.x[t].st + row * p.x[t].sh;
+            const T* dy = (const T*)p.dy[t].p + token * p.dy[t].st + row * p.dy[t].sh;
+#pragma unroll
+            for (int n = 0; n < E; ++n) {
+                unit[n].load(x, row < p.heads[t], next[n]);
+                unit[n].load(dy, row < p.heads[t], next_dy[n]);
+            }
+        };
+        fetch(from);
+        float c[E][V], s[E][V];
+        if (p.rot > 0) token_turns<V, E>(p, token, lane, turns[wave], pair, rotates, c, s);
+        for (int pass = from; pass < to; ++pass) {
+            const int t = pass >= ps.of_q, row = (t ? pass - ps.of_q : pass) * ps.per + row0;
+            float x[E][2 * V], g[E][2 * V], sum = 0.f, dot = 0.f;
+#pragma unroll
+            for (int n = 0; n < E; ++n)
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) {
+                    x[n][e] = (float)next[n][e / V][e % V];
+                    g[n][e] = (float)next_dy[n][e / V][e % V];
+                }
+            if (pass + 1 < to) fetch(pass + 1);
+#pragma unroll
+            for (int n = 0; n < E; ++n) {
+                if (p.rot > 0) unit[n].turn(g[n], c[n], s[n], -1.f);
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) {
+                    sum = fmaf(x[n][e], x[n][e], sum);
+                    dot = fmaf(g[n][e] * (t ? w[1][n][e] : w[0][n][e]), x[n][e], dot);
+                }
+            }
+            const float r = 1.f / sqrtf(fmaf(row_sum(sum, lanes), inv, p.eps));
+            const float mean = row_sum(dot, lanes) * r * inv;  // S(u z) / D
+            const bool live = row < p.heads[t];
+            T* dx = (T*)p.y[t].p + token * p.y[t].st + row * p.y[t].sh;
+#pragma unroll
+            for (int n = 0; n < E; ++n) {
+#pragma unroll
+                for (int e = 0; e < 2 * V; ++e) {
+                    const float z = x[n][e] * r, gz = g[n][e] * z;
+                    if (live) {
+                        if (t) dw[1][n][e] += gz;
+                        else dw[0][n][e] += gz;
+                    }
+                    x[n][e] = r * (g[n][e] * (t ? w[1][n][e] : w[0][n][e]) - z * mean);
+                }
+                unit[n].store(dx, live && p.y[t].p != nullptr, x[n]);
+            }
+        }
+    }
+    if (!p.sums) return;
+    // the wave's rows, then the work-group's waves, in their order
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int n = 0; n < E; ++n)
+#pragma unroll
+            for (int e = 0; e < 2 * V; ++e) {
+                float v = dw[t][n][e];
+                for (int m = lanes; m < 64; m *= 2) v += __shfl_xor(v, m);
+                const int d = e < V ? unit[n].first + e : unit[n].second + e - V;
+                if (row0 == 0 && unit[n].in && (e < V || unit[n].two)) sums[wave][t][d] = v;
+            }
+    __syncthreads();
+    float* part = p.part + (int64_t)blockIdx.x * 2 * p.dim;
+    for (int i = threadIdx.x; i < 2 * p.dim; i += kThreads) {
+        const int t = i >= p.dim, d = i - t * p.dim;
+        float v = sums[0][t][d];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k) v += sums[k][t][d];
+        part[i] = v;
+    }
+}
+
+// The parts of dw added up: a work-group has 16 of the 2 dim sums and 64 threads
+// for each, whose parts it joins in a fixed order.
+constexpr int kJoinColumns = 16;
+constexpr int kJoinThreads = 1024;
+template <int WDT>
+__global__ void __launch_bounds__(kJoinThreads) qk_join_kernel(QkParams p, int parts) {
+    constexpr int K = kJoinThreads / kJoinColumns;
+    __shared__ float s[K][kJoinColumns + 1];
+    const int c = threadIdx.x % kJoinColumns, k = threadIdx.x / kJoinColumns;
+    const int i = (int)blockIdx.x * kJoinColumns + c;
+    float v = 0.f;
+    if (i < 2 * p.dim) {
+#pragma unroll 4
+        for (int n = k; n < parts; n += K) v += p.part[(int64_t)n * 2 * p.dim + i];
+    }
+    s[k][c] = v;
+    __syncthreads();
+#pragma unroll
+    for (int m = K / 2; m > 0; m /= 2) {
+        if (k < m) s[k][c] += s[k + m][c];
+        __syncthreads();
+    }
+    if (k > 0 || i >= 2 * p.dim) return;
+    const int t = i >= p.dim;
+    if (p.dw[t] != nullptr) ((storage_t<WDT>*)p.dw[t])[i - t * p.dim] = (storage_t<WDT>)s[0][c];
+}
+
+// The launch: passes that a wave makes over its token.  All of them, so that the
+// angles are worked out once, where there are tokens enough for the device.
+struct Plan {
+    int lanes, passes_each, chunks;
+};
+Plan plan_of(const QkParams& p, int v, int e) {
+    const int units = p.rot / (2 * v) + (p.dim - p.rot + 2 * v - 1) / (2 * v);
+    Plan plan{1, 1, 1};
+    while (plan.lanes * e < units) plan.lanes *= 2;
+    const int per = 64 / plan.lanes;
+    const int64_t all = (p.heads[0] + (int64_t)per - 1) / per + (p.heads[1] + (int64_t)per - 1) / per;
+    constexpr int64_t kWavesWanted = 256 * 16;
+    int64_t each = p.tokens * all / kWavesWanted;
+    each = each < 1 ? 1 : each > all ? all : each;
+    if ((all + each - 1) / each > 65535) each = (all + 65534) / 65535;
+    plan.passes_each = (int)each;
+    plan.chunks = (int)((all + each - 1) / each);
+    return plan;
+}
+
+template <int DT, int V, int E, bool NEAR>
+hipError_t forward(const QkParams& p, hipStream_t stream) {
+    const Plan plan = plan_of(p, V, E);
+    const int64_t groups = (p.tokens + kWaves - 1) / kWaves;
+    const dim3 grid((unsigned)(groups < 8192 ? groups : 8192), (unsigned)plan.chunks);
+    qk_forward_kernel<DT, V, E, NEAR><<<grid, kThreads, 0, stream>>>(p, plan.lanes, plan.passes_each);
+    return hipGetLastError();
+}
+
+template <int DT, int V, int E, bool NEAR>
+hipError_t backward(const QkParams& p, hipStream_t stream) {
+    const Plan plan = plan_of(p, V, E);
+    const int64_t groups = (p.tokens * plan.chunks + kWaves - 1) / kWaves;
+    const int parts = (int)(groups < kQkParts ? groups : kQkParts);
+    if (parts > 0)
+        qk_backward_kernel<DT, V, E, NEAR><<<dim3((unsigned)parts), kThreads, 0, stream>>>(p, plan.lanes, plan.passes_each);
+    if (p.sums) {
+        const dim3 grid((unsigned)((2 * p.dim + kJoinColumns - 1) / kJoinColumns));
+        if (DT == DT_F32 || p.w_f32) qk_join_kernel<DT_F32><<<grid, kJoinThreads, 0, stream>>>(p, parts);
+        else qk_join_kernel<DT><<<grid, kJoinThreads, 0, stream>>>(p, parts);
+    }
+    return hipGetLastError();
+}
+
+// The widest vectors that rotating pairs and rows are made of.
+template <int DT, bool FORWARD, bool NEAR>
+hipError_t widest(const QkParams& p, hipStream_t stream) {
+    const auto fits = [&](int v) { return p.rot % (2 * v) == 0 && p.dim % v == 0; };
+    if constexpr (DT != DT_F32) {
+        if (fits(8)) return FORWARD ? forward<DT, 8, 1, NEAR>(p, stream) : backward<DT, 8, 1, NEAR>(p, stream);
+    }
+    if (fits(4)) return FORWARD ? forward<DT, 4, 1, NEAR>(p, stream) : backward<DT, 4, 1, NEAR>(p, stream);
+    if (fits(2)) return FORWARD ? forward<DT, 2, 1, NEAR>(p, stream) : backward<DT, 2, 1, NEAR>(p, stream);
+    return FORWARD ? forward<DT, 1, 2, NEAR>(p, stream) : backward<DT, 1, 2, NEAR>(p, stream);
+}
+template <bool FORWARD>
+hipError_t launch(int dtype, const QkParams& p, hipStream_t stream) {
+    if (dtype == DT_F32)
+        return p.interleaved ? widest<DT_F32, FORWARD, true>(p, stream) : widest<DT_F32, FORWARD, false>(p, stream);
+    if (dtype == DT_F16)
+        return p.interleaved ? widest<DT_F16, FORWARD, true>(p, stream) : widest<DT_F16, FORWARD, false>(p, stream);
+    return p.interleaved ? widest<DT_BF16, FORWARD, true>(p, stream) : widest<DT_BF16, FORWARD, false>(p, stream);
+}
+
+}  // namespace
+
+hipError_t launch_qk_norm_forward(int dtype, const QkParams& p, hipStream_t stream) {
+    return launch<true>(dtype, p, stream);
+}
+
+hipError_t launch_qk_norm_backward(int dtype, const QkParams& p, hipStream_t stream) {
+    return launch<false>(dtype, p, stream);
+}
+
+}  // namespace kb

@@ -99,6 +99,14 @@ __device__ __forceinline__ void load_words(const storage_t<DT>* row, int d, int 
     }
 }
 
+// A pointer that is the same in all lanes, so that the compiler sees it.
+__device__ __forceinline__ void* uniform_pointer(const void* at) {
+    const uint64_t u = (uint64_t)at;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
+    return (void*)((uint64_t)hi << 32 | lo);
+}
+
 // The 16 keys of a wave's step, in registers.
 template <int DT, int DP>
 struct Step {
@@ -110,21 +118,52 @@ struct Step {
     uint32_t k[KC][4], v[4][VW];
     uint32_t seen;  // bit c: key c is there
 
-    template <bool WHOLE>
+    // The keys of 16 places, lane c knowing key c's.
     __device__ __forceinline__ void load(const PagedParams& p, const T* kc, const T* vc, Place w, int lane) {
         const int c = lane & 15, g = lane >> 4;
         const bool have = in_cache(p, w.page);
         seen = (uint32_t)__ballot(have) & 0xFFFFu;
         const T* kr = kc + (have ? w.page * p.cache[0].sb + w.at * p.cache[0].sl : 0);
 #pragma unroll
-        for (int n = 0; n < KC; ++n) load_words<DT, 4, WHOLE>(kr, (4 * n + g) * KB, p.dim, have, k[n]);
+        for (int n = 0; n < KC; ++n) load_words<DT, 4, false>(kr, (4 * n + g) * KB, p.dim, have, k[n]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int page = __shfl(w.page, 4 * g + j), at = __shfl(w.at, 4 * g + j);
             const bool in = in_cache(p, page);
             const T* vr = vc + (in ? page * p.cache[1].sb + at * p.cache[1].sl : 0);
-            load_words<DT, VW, WHOLE>(vr, VB * c, p.dim, in, v[j]);
+            load_words<DT, VW, false>(vr, VB * c, p.dim, in, v[j]);
         }
+    }
+    // The same where the 16 keys lie in one page: kr, vr: row 0 of them, of which
+    // `rows` are there; at: where the lane reads (StepPlaces).  The bounds of a buffer
+    // descriptor make zeros of the other rows.
+    __device__ __forceinline__ void load_page(const T* kr, const T* vr, int rows, uint32_t k_row, uint32_t v_row,
+                                              const uint32_t (&k_at)[KC], const uint32_t (&v_at)[4][(VW + 3) / 4]) {
+        rows = __builtin_amdgcn_readfirstlane(rows);
+        seen = (1u << rows) - 1u;
+        const auto kd = __builtin_amdgcn_make_buffer_rsrc(uniform_pointer(kr), 0, rows * k_row, 0x00020000);
+        const auto vd = __builtin_amdgcn_make_buffer_rsrc(uniform_pointer(vr), 0, rows * v_row, 0x00020000);
+#pragma unroll
+        for (int n = 0; n < KC; ++n) {
+            const u32v4 x = __builtin_bit_cast(u32v4, __builtin_amdgcn_raw_buffer_load_b128(kd, (int)k_at[n], 0, 0));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) k[n][e] = x[e];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int n = 0; n < (VW + 3) / 4; ++n) {
+                if constexpr (VW >= 4) {
+                    const u32v4 x = __builtin_bit_cast(u32v4, __builtin_amdgcn_raw_buffer_load_b128(vd, (int)v_at[j][n], 0, 0));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[j][4 * n + e] = x[e];
+                } else {
+                    typedef uint32_t two __attribute__((ext_vector_type(2)));
+                    const two x = __builtin_bit_cast(two, __builtin_amdgcn_raw_buffer_load_b64(vd, (int)v_at[j][n], 0, 0));
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) v[j][e] = x[e];
+                }
+            }
     }
     // Element e of the four keys' pieces.
     __device__ __forceinline__ four_t<DT> values(int e) const {
@@ -206,39 +245,6 @@ __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>
             if constexpr (DT != DT_F32) lo[b][r] = (T)(t - (float)hi[b][r]);
         }
     }
-    // A product takes every key to every row, with 0 where a row does not see it, and
-    // 0 times NaN is NaN: a step with such values that some rows see and others do
-    // not goes row by row.
-    if (!full) {
-        float z = 0.f;
-#pragma unroll
-        for (int e = 0; e < S::VB; ++e) {
-            const four_t<DT> a = in.values(e);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) z = fmaf((float)a[j], 0.f, z);
-        }
-        if (__any(z != 0.f)) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll 1
-                for (int n = 0; n < 16; ++n) {
-                    const int end = __builtin_amdgcn_readlane(lim[b], n);
-#pragma unroll
-                    for (int e = 0; e < S::VB; ++e) {
-                        four_t<DT> a = in.values(e);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r)
-                            if (key0 + 4 * g + r >= end) a[r] = (T)0.f;
-                        f32x4 t = {};
-                        t = mma4(a, hi[b], t);
-                        if constexpr (DT != DT_F32) t = mma4(a, lo[b], t);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[b][e][r] = (lane & 15) == n ? acc[b][e][r] + t[r] : acc[b][e][r];
-                    }
-                }
-            return;
-        }
-    }
 #pragma unroll
     for (int e = 0; e < S::VB; ++e) {
         const four_t<DT> a = in.values(e);
@@ -250,16 +256,22 @@ __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>
     }
 }
 
-// Units of sequence b, for one key head and block of rows: tiles, or 1.
-__device__ __forceinline__ int units_of(const PagedParams& p, int b) {
-    return p.pairs ? 1 : max(1, (paged_len(p, b) + kKeys - 1) / kKeys);
+// Tiles of sequence b, for one key head and block of rows, and its units: beginning
+// a pair takes as long as kBegin tiles, so that a work-group with many short ones has
+// no more to do than others.  (Or one for all of it.)
+constexpr int kBegin = 3;
+__device__ __forceinline__ int tiles_of(const PagedParams& p, int b) {
+    return max(1, (paged_len(p, b) + kKeys - 1) / kKeys);
 }
+__device__ __forceinline__ int units_of(const PagedParams& p, int b) { return p.pairs ? 1 : tiles_of(p, b) + kBegin; }
 template <int ROWS>
 __device__ __forceinline__ int blocks_of(const PagedParams& p, int b) {
     return (int)(((int64_t)tokens_of(p, b).n * p.group + ROWS - 1) / ROWS);
 }
 
-template <int DT, int DP, int NB, bool WHOLE>
+// ONE_PAGE: rows are read in aligned 16-byte chunks, and a wave's 16 keys lie in one
+// page (its size is a multiple of 16).
+template <int DT, int DP, int NB, bool ONE_PAGE>
 __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) paged_few_kernel(PagedParams p) {
     using T = storage_t<DT>;
     using S = Step<DT, DP>;
@@ -293,11 +305,9 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
         all += wave_units[w];
     }
     const int64_t workers = min((int64_t)p.workers, all);
-    PagedHeader* header = (PagedHeader*)p.ws + me;
-    if (me >= workers) {
-        if (!p.pairs && threadIdx.x == 0) header->valid = 0;
-        return;
-    }
+    PagedHeader* headers = (PagedHeader*)p.ws;
+    if (!p.pairs && !p.by_pair && threadIdx.x == 0) headers[me].valid = 0;
+    if (me >= workers) return;
     const int64_t first = all * me / workers, end = all * (me + 1) / workers;
     if (before <= first && first < before + units) {
         int b = mine;
@@ -313,15 +323,31 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
     __syncthreads();
     int seq = __builtin_amdgcn_readfirstlane(start_seq);
     int64_t in_seq = start_units;
-    if (!p.pairs && threadIdx.x == 0) header->valid = 0;
 
     const float to_log2 = p.scale * kLog2e;
+    // Where a lane reads in 16 rows of one page, in bytes; past dim: nowhere.
+    constexpr uint32_t kNowhere = 0x7FFFFFF0u;
+    constexpr int PIECE = S::VW >= 4 ? S::KB : S::VB;  // elements of a load of V
+    const uint32_t k_row = (uint32_t)p.cache[0].sl * (uint32_t)sizeof(T), v_row = (uint32_t)p.cache[1].sl * (uint32_t)sizeof(T);
+    uint32_t k_at[S::KC], v_at[4][(S::VW + 3) / 4];
+#pragma unroll
+    for (int n = 0; n < S::KC; ++n) {
+        const int d = (4 * n + g) * S::KB;
+        k_at[n] = d < p.dim ? c * k_row + d * (int)sizeof(T) : kNowhere;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int n = 0; n < (S::VW + 3) / 4; ++n) {
+            const int d = S::VB * c + n * PIECE;
+            v_at[j][n] = d < p.dim ? (4 * g + j) * v_row + d * (int)sizeof(T) : kNowhere;
+        }
     const auto slot = [&](int worker, int n) {
-        return p.ws + (int64_t)p.workers * (sizeof(PagedHeader) / sizeof(float)) +
+        return p.ws + (int64_t)p.headers * (sizeof(PagedHeader) / sizeof(float)) +
                ((int64_t)worker * 2 + n) * ROWS * PITCH;
     };
     for (int64_t unit = first; unit < end && seq < p.batch;) {
-        const int n_units = units_of(p, seq), klen = paged_len(p, seq);
+        const int n_tiles = tiles_of(p, seq), n_units = units_of(p, seq), klen = paged_len(p, seq);
         const Tokens tok = tokens_of(p, seq);
         const int n_blocks = blocks_of<ROWS>(p, seq);
         if (n_blocks == 0) {  // (a sequence without new tokens has no unit)
@@ -330,9 +356,23 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
             continue;
         }
         const int pair = __builtin_amdgcn_readfirstlane((int)(in_seq / n_units));
-        const int tile = __builtin_amdgcn_readfirstlane((int)(in_seq - (int64_t)pair * n_units));
-        const int block = pair / p.kv_heads, h = pair - block * p.kv_heads;
-        const int take = (int)min((int64_t)(n_units - tile), end - unit);
+        const int in_pair = (int)(in_seq - (int64_t)pair * n_units);
+        const int take = (int)min((int64_t)(n_units - in_pair), end - unit);
+        const int tile = __builtin_amdgcn_readfirstlane(p.pairs ? 0 : max(0, in_pair - kBegin));
+        const int tile_end = __builtin_amdgcn_readfirstlane(p.pairs ? n_tiles : max(0, in_pair + take - kBegin));
+        const auto advance = [&] {
+            unit += take;
+            in_seq += take;
+            if (in_seq == (int64_t)n_blocks * p.kv_heads * n_units) {
+                ++seq;
+                in_seq = 0;
+            }
+        };
+        if (tile == tile_end) {  // no more than a pair's beginning
+            advance();
+            continue;
+        }
+        const int block = __builtin_amdgcn_readfirstlane(pair / p.kv_heads), h = pair - block * p.kv_heads;
 
         // the rows, and the keys that they see
         int lim[NB];
@@ -345,13 +385,23 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
             lim[b] = live ? key_limit(i, tok.n, klen, p.causal) : 0;
             const T* at = (const T*)p.q.p + (int64_t)(tok.first + (live ? i : 0)) * p.q.st + (live ? hq : 0) * p.q.sh;
 #pragma unroll
-            for (int n = 0; n < S::KC; ++n) load_words<DT, 4, WHOLE>(at, (4 * n + g) * S::KB, p.dim, live, q[b][n]);
+            for (int n = 0; n < S::KC; ++n) load_words<DT, 4, ONE_PAGE>(at, (4 * n + g) * S::KB, p.dim, live, q[b][n]);
         }
         const int row_first = (int)((uint32_t)block * ROWS / (uint32_t)p.group);
         const int row_last = min(tok.n - 1, (int)(((uint32_t)block * ROWS + ROWS - 1) / (uint32_t)p.group));
         const int every = key_limit(row_first, tok.n, klen, p.causal);  // what the first row sees, all others see
         const int any = key_limit(row_last, tok.n, klen, p.causal);
-        const int key_end = p.pairs ? any : min(any, (tile + take) * kKeys);
+        const int take_end = min(any, tile_end * kKeys);
+        const int rows = (int)min((int64_t)ROWS, (int64_t)tok.n * p.group - (int64_t)block * ROWS);
+
+        // A product takes every key to every row, with 0 where a row does not see it,
+        // and 0 times NaN is NaN.  So rows of several queries whose sums end up with
+        // such a value are computed once more, query by query, each with its own keys
+        // alone (only >= 0).
+        int only = -1;
+        for (;;) {
+        const int key_end = __builtin_amdgcn_readfirstlane(
+            only < 0 ? take_end : min(take_end, key_limit(only, tok.n, klen, p.causal)));
 
         f32x4 acc[NB][S::VB];
         Rows<NB> st;
@@ -362,26 +412,64 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
 #pragma unroll
             for (int e = 0; e < S::VB; ++e) acc[b][e] = f32x4{};
         }
-        const int32_t* table = p.table + (int64_t)seq * p.table_stride;
+        const int32_t* table = p.table + (int64_t)__builtin_amdgcn_readfirstlane(seq) * p.table_stride;
         const T* kc = (const T*)p.cache[0].p + h * p.cache[0].sh;
         const T* vc = (const T*)p.cache[1].p + h * p.cache[1].sh;
         const int key0 = tile * kKeys + 16 * wave;
-        {
-            // one step computed, the next one's keys on their way, the page of the one after that too
-            Step<DT, DP> a, b;
+        // one step is computed while the next one's keys are on their way
+        Step<DT, DP> a, b;
+        if constexpr (ONE_PAGE) {
+            // the pages of 64 steps, one a lane
+            int pages = 0;
+            const auto load = [&](Step<DT, DP>& to, int n) {
+                const int key = key0 + n * kKeys;
+                if (n % 64 == 0) {
+                    const int of_lane = key + lane * kKeys;
+                    pages = of_lane < key_end ? table[page_of(p, of_lane)] : -1;
+                }
+                const int page = __builtin_amdgcn_readlane(pages, n % 64);
+                const int at = key - page_of(p, key) * p.page;
+                const int rows = in_cache(p, page) ? min(max(key_end - key, 0), 16) : 0;
+                to.load_page(kc + (int64_t)page * p.cache[0].sb + (int64_t)at * p.cache[0].sl,
+                             vc + (int64_t)page * p.cache[1].sb + (int64_t)at * p.cache[1].sl, rows, k_row, v_row, k_at, v_at);
+            };
+            load(a, 0);
+#pragma unroll 1
+            for (int n = 0, key = key0; key < key_end; n += 2, key += 2 * kKeys) {  // (a step without a key adds nothing)
+                load(b, n + 1);
+                step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
+                load(a, n + 2);
+                step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
+            }
+        } else {
+            // and the places of the one after that
             Place w = place_of(p, table, key0 + c, key_end);
             Place next = place_of(p, table, key0 + kKeys + c, key_end);
-            a.template load<WHOLE>(p, kc, vc, w, lane);
+            a.load(p, kc, vc, w, lane);
+#pragma unroll 1
             for (int key = key0; key < key_end; key += 2 * kKeys) {
                 w = next;
                 next = place_of(p, table, key + 2 * kKeys + c, key_end);
-                b.template load<WHOLE>(p, kc, vc, w, lane);
+                b.load(p, kc, vc, w, lane);
                 step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
-                if (key + kKeys >= key_end) break;
                 w = next;
                 next = place_of(p, table, key + 3 * kKeys + c, key_end);
-                a.template load<WHOLE>(p, kc, vc, w, lane);
+                a.load(p, kc, vc, w, lane);
                 step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
+            }
+        }
+
+        if (only < 0 && p.causal && row_first < row_last) {
+            float z = 0.f;  // x 0 is 0, or NaN
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < S::VB; ++e)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z = fmaf(acc[b][e][r], 0.f, z);
+            if (__syncthreads_or(z != 0.f)) {
+                only = row_first;
+                continue;
             }
         }
 
@@ -402,11 +490,13 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
                         f32x4{acc[b][e][r], acc[b][e + 1][r], acc[b][e + 2][r], acc[b][e + 3][r]};
         }
         __syncthreads();
-        const bool begun = tile == 0, ended = tile + take == n_units;
-        const int rows = (int)min((int64_t)ROWS, (int64_t)tok.n * p.group - (int64_t)block * ROWS);
+        const bool begun = tile == 0, ended = tile_end == n_tiles;
         float* part = begun && ended ? nullptr : slot(me, begun ? 1 : 0);
         for (int n = threadIdx.x; n < rows * (DP / 4); n += kThreads) {
             const int r = n / (DP / 4), d = n % (DP / 4) * 4;
+            const uint32_t row = (uint32_t)block * ROWS + r;
+            const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row - (uint32_t)i * p.group);
+            if (only >= 0 && i != only) continue;
             float m = stat_m[0][r];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat_m[w][r]);
@@ -426,8 +516,6 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
                 if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, 0.f, 0.f};
                 continue;
             }
-            const uint32_t row = (uint32_t)block * ROWS + r;
-            const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row - (uint32_t)i * p.group);
             const int64_t t = tok.first + i;
             const bool some = l != 0.f;
             const float f = 1.f / l;
@@ -437,90 +525,132 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
                 p.lse[t * p.heads + hq] =
                     some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
         }
-        if (begun && !ended && threadIdx.x == 0) {
+        if (threadIdx.x == 0 && !p.pairs && begun && (p.by_pair || !ended)) {
             // the worker that has the pair's last tile
-            const int64_t last = unit + (n_units - tile) - 1;
-            *header = PagedHeader{seq, block, h, (int)(((last + 1) * workers - 1) / all), 1, rows, {0, 0}};
-        }
-        unit += take;
-        in_seq += take;
-        if (in_seq == (int64_t)n_blocks * p.kv_heads * n_units) {
-            ++seq;
-            in_seq = 0;
+            const int64_t last = unit + (n_units - in_pair) - 1;
+            headers[p.by_pair ? (block_before<ROWS>(p, seq) + block) * p.kv_heads + h : me] =
+                PagedHeader{seq, block, h, me, (int)(((last + 1) * workers - 1) / all), !ended, rows, 0};
         }
         __syncthreads();  // the sums are read
+        if (only < 0 || ++only > row_last) break;
+        }
+        advance();
     }
 }
 
-// A pair that work-groups share, joined: a work-group (x: the one that began the
-// pair, y: the row) has four waves, each with a quarter of the parts, two elements a
-// lane.
-template <int DT, int DP, int NB>
-__global__ void __launch_bounds__(kThreads) paged_few_join_kernel(PagedParams p) {
+// A pair that work-groups share, joined.  WAVES waves have a row, each every
+// WAVES-th part of it, DP / 64 elements a lane; up to AHEAD of a wave's parts are on
+// their way together.
+constexpr int kJoinThreads = 512;
+template <int DT, int DP, int NB, int WAVES>
+__global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParams p) {
     using T = storage_t<DT>;
-    constexpr int ROWS = 16 * NB, PITCH = DP + 4, E = DP / 64;
-    __shared__ float sums[kWaves][DP], stat_m[kWaves], stat_l[kWaves];
-    const int me = (int)blockIdx.x, r = (int)blockIdx.y;
-    const PagedHeader h = ((const PagedHeader*)p.ws)[me];
+    constexpr int ROWS = 16 * NB, PITCH = DP + 4, E = DP / 64, AHEAD = 8, EACH = kJoinThreads / 64 / WAVES;
+    __shared__ float sums[WAVES][DP], stat_m[WAVES], stat_l[WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WAVES;
+    const int r = (int)blockIdx.y * EACH + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WAVES;
+    if (p.by_pair) {
+        // a pair's number may be no pair's
+        const int64_t block = blockIdx.x / (uint32_t)p.kv_heads;
+        const auto first_block = [&](int b) { return block_before<ROWS>(p, b); };
+        const int seq = count_up_to(p.batch, block, lane, first_block) - 1;
+        if (seq < 0 || (block - first_block(seq)) * ROWS >= (int64_t)tokens_of(p, seq).n * p.group) return;
+    }
+    const PagedHeader h = ((const PagedHeader*)p.ws)[blockIdx.x];
     if (!h.valid || r >= h.rows) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int me = h.first;
     const float to_log2 = p.scale * kLog2e;
-    const float* base = p.ws + (int64_t)p.workers * (sizeof(PagedHeader) / sizeof(float)) + r * PITCH;
+    const float* base = p.ws + (int64_t)p.headers * (sizeof(PagedHeader) / sizeof(float)) + r * PITCH;
     const int parts = h.last - me + 1;
     const auto part = [&](int k) { return base + ((int64_t)(me + k) * 2 + (k == 0)) * ROWS * PITCH; };
     float m = -INFINITY, l = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 8
-    for (int k = wave; k < parts; k += kWaves) m = fmaxf(m, part(k)[DP]);
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 8
-    for (int k = wave; k < parts; k += kWaves) {
-        const float* x = part(k);
-        const float f = __builtin_amdgcn_exp2f((x[DP] - ref) * to_log2);
-        l = fmaf(f, x[DP + 1], l);
+    for (int k0 = wave; k0 < parts; k0 += WAVES * AHEAD) {
+        float x[AHEAD][E], xm[AHEAD], xl[AHEAD];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = fmaf(f, x[lane * E + e], o[e]);
-    }
+        for (int n = 0; n < AHEAD; ++n) {
+            const int k = k0 + n * WAVES;
+            xm[n] = -INFINITY;
+            if (k < parts) {
+                const float* at = part(k);
+                xm[n] = at[DP];
+                xl[n] = at[DP + 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = o[e];
-    if (lane == 0) {
-        stat_m[wave] = m;
-        stat_l[wave] = l;
-    }
-    __syncthreads();
-    const int d = threadIdx.x;
-    if (d >= p.dim) return;
-    m = stat_m[0];
+                for (int e = 0; e < E; ++e) x[n][e] = at[lane * E + e];
+            }
+        }
+        float now = m;
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat_m[w]);
-    const float all = m == -INFINITY ? 0.f : m;
-    float x = 0.f;
-    l = 0.f;
+        for (int n = 0; n < AHEAD; ++n) now = fmaxf(now, xm[n]);
+        const float ref = now == -INFINITY ? 0.f : now;
+        float f = __builtin_amdgcn_exp2f((m - ref) * to_log2);
+        l *= f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f((stat_m[w] - all) * to_log2);
-        l = fmaf(f, stat_l[w], l);
-        x = fmaf(f, sums[w][d], x);
+        for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n) {
+            if (k0 + n * WAVES >= parts) continue;
+            f = __builtin_amdgcn_exp2f((xm[n] - ref) * to_log2);
+            l = fmaf(f, xl[n], l);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(f, x[n][e], o[e]);
+        }
+        m = now;
     }
     const uint32_t row = (uint32_t)h.block * ROWS + r;
     const int i = (int)(row / (uint32_t)p.group), hq = h.head * p.group + (int)(row - (uint32_t)i * p.group);
     const int64_t t = tokens_of(p, h.seq).first + i;
-    const bool some = l != 0.f;
-    ((T*)p.o.p)[t * p.o.st + hq * p.o.sh + d] = (T)(some ? x / l : 0.f);
-    if (d == 0 && p.lse != nullptr)
-        p.lse[t * p.heads + hq] = some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
+    const auto write = [&](int d, float x) {
+        const bool some = l != 0.f;
+        if (d < p.dim) ((T*)p.o.p)[t * p.o.st + hq * p.o.sh + d] = (T)(some ? x / l : 0.f);
+        if (d == 0 && p.lse != nullptr)
+            p.lse[t * p.heads + hq] = some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
+    };
+    if constexpr (WAVES == 1) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) write(lane * E + e, o[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = o[e];
+        if (lane == 0) {
+            stat_m[wave] = m;
+            stat_l[wave] = l;
+        }
+        __syncthreads();
+        const int d = threadIdx.x;
+        if (d >= p.dim) return;
+        m = stat_m[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, stat_m[w]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float x = 0.f;
+        l = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float f = __builtin_amdgcn_exp2f((stat_m[w] - ref) * to_log2);
+            l = fmaf(f, stat_l[w], l);
+            x = fmaf(f, sums[w][d], x);
+        }
+        write(d, x);
+    }
 }
 
 template <int DT, int DP, int NB>
 hipError_t few(const PagedParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)p.workers);
-    if (p.whole) paged_few_kernel<DT, DP, NB, true><<<grid, kThreads, 0, stream>>>(p);
+    if (p.whole && p.page % 16 == 0) paged_few_kernel<DT, DP, NB, true><<<grid, kThreads, 0, stream>>>(p);
     else paged_few_kernel<DT, DP, NB, false><<<grid, kThreads, 0, stream>>>(p);
     if (!p.pairs) {
-        const int64_t rows = (p.starts != nullptr ? (int64_t)p.tokens : 1) * p.group;
-        paged_few_join_kernel<DT, DP, NB>
-            <<<dim3((unsigned)p.workers, (unsigned)(rows < 16 * NB ? rows : 16 * NB)), kThreads, 0, stream>>>(p);
+        const int64_t most = (p.starts != nullptr ? (int64_t)p.tokens : 1) * p.group;
+        const int rows = (int)(most < 16 * NB ? most : 16 * NB);
+        // eight waves a row where a pair is likely to have more parts than a wave reads at once
+        if (p.by_pair && p.workers > 8 * p.headers)
+            paged_few_join_kernel<DT, DP, NB, 8>
+                <<<dim3((unsigned)p.headers, (unsigned)rows), kJoinThreads, 0, stream>>>(p);
+        else
+            paged_few_join_kernel<DT, DP, NB, 1>
+                <<<dim3((unsigned)p.headers, (unsigned)((rows + 7) / 8)), kJoinThreads, 0, stream>>>(p);
     }
     return hipGetLastError();
 }
@@ -529,11 +659,18 @@ hipError_t few(const PagedParams& p, hipStream_t stream) {
 
 constexpr int kRows = kAttnRows;
 
-// Where the rows of a tile lie: lane n of every wave knows of row n.
-struct TilePlace {
-    Place w;
-    uint64_t present;  // rows that are there
+// The pages of a tile's rows, lane n of every wave knowing row n's, and the rows
+// that are there.
+struct TilePages {
+    int first;  // key of row 0
+    int page;
+    uint64_t present;
 };
+// The table by buffer loads, for the reason that tiles are filled by them; past its
+// end they give 0, which place_in_table's caller does not use.
+__device__ __forceinline__ int page_in_table(const PagedParams& p, __amdgpu_buffer_rsrc_t table, int key) {
+    return (int)__builtin_amdgcn_raw_buffer_load_b32(table, page_of(p, key) * 4, 0, 0);
+}
 
 // Rows of a tile from their pages, in the background as Filler does it: one
 // descriptor for the rows that a wave fills at once, which are in one page.
@@ -543,49 +680,56 @@ struct PagedFiller {
     using F = Filler<DT, DP, kKeys, kThreads>;
     using L = Tile<DT, DP>;
     static constexpr int SLOTS = F::SLOTS, STEP = F::STEP, STEPS = F::STEPS;
-    int row0;
     uint32_t offset;
     bool in;
 
     __device__ __forceinline__ PagedFiller(int64_t stride, int dim) {
-        row0 = (int)threadIdx.x / SLOTS;
-        const int d = ((int)threadIdx.x % SLOTS ^ L::turn(row0)) * L::VEC;
+        const int d = ((int)threadIdx.x % SLOTS ^ L::turn((int)threadIdx.x / SLOTS)) * L::VEC;
         in = d < dim;
         offset = ((uint32_t)(((int)threadIdx.x & 63) / SLOTS) * (uint32_t)stride + (uint32_t)d) * (uint32_t)sizeof(T);
     }
     // base: the head's element 0 of page 0.
-    __device__ __forceinline__ void fill(T* tile, const T* base, const HeadView& c, const TilePlace& at) const {
+    __device__ __forceinline__ void fill(T* tile, const T* base, const PagedParams& p, const HeadView& c,
+                                         const TilePages& at) const {
         const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         T* to = tile + wave * L::KB;
+        const auto from = [&](int row) {
+            const int key = at.first + row, page = __builtin_amdgcn_readlane(at.page, row);
+            return background(base + (int64_t)page * c.sb + (int64_t)(key - page_of(p, key) * p.page) * c.sl);
+        };
+        if (at.present == ~(uint64_t)0 && p.dim == L::PITCH) {
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) {
-            const int first = k * STEP + wave * L::KB_ROWS;  // of the wave's rows
-            const int page = __builtin_amdgcn_readlane(at.w.page, first), in_page = __builtin_amdgcn_readlane(at.w.at, first);
-            const bool have = (at.present >> (k * STEP + row0)) & 1;
-            const auto from = background(base + (at.present >> first & 1 ? page * c.sb + in_page * c.sl : 0));
-            if (in && have) {
-                send<16>(from, offset, 0, to);
-            } else {
-                const u32v4 zero = {0, 0, 0, 0};
-                *(u32v4*)(to + ((int)threadIdx.x & 63) * L::VEC) = zero;
+            for (int k = 0; k < STEPS; ++k)
+                send<16>(from(k * STEP + wave * L::KB_ROWS), offset, 0, to + k * (STEP / L::KB_ROWS * L::KB));
+        } else {
+#pragma unroll 1
+            for (int k = 0; k < STEPS; ++k) {
+                const int row = k * STEP + wave * L::KB_ROWS;  // the wave's first; if it is not there, none is
+                if (in && (at.present >> (row + ((int)threadIdx.x & 63) / SLOTS) & 1)) {
+                    send<16>(from(row), offset, 0, to);
+                } else {
+                    const u32v4 zero = {0, 0, 0, 0};
+                    *(u32v4*)(to + ((int)threadIdx.x & 63) * L::VEC) = zero;
+                }
+                to += STEP / L::KB_ROWS * L::KB;
             }
-            to += STEP / L::KB_ROWS * L::KB;
         }
     }
 };
 
 // The same through registers: any page size, any alignment.
 template <int DT, int DP>
-__device__ __forceinline__ void paged_stage(storage_t<DT>* tile, const storage_t<DT>* base, const HeadView& c,
-                                            const TilePlace& at, int dim) {
+__device__ __forceinline__ void paged_stage(storage_t<DT>* tile, const storage_t<DT>* base, const PagedParams& p,
+                                            const HeadView& c, const TilePages& at) {
     using L = Tile<DT, DP>;
     static_assert(kKeys * L::CHUNKS % kThreads == 0, "every thread has the same number of chunks");
 #pragma unroll
     for (int k = 0; k < kKeys * L::CHUNKS / kThreads; ++k) {
         const int idx = k * kThreads + (int)threadIdx.x, row = idx / L::CHUNKS, d = idx % L::CHUNKS * L::VEC;
-        const int page = __shfl(at.w.page, row), in_page = __shfl(at.w.at, row);
+        const int key = at.first + row, page = __shfl(at.page, row);
         u32v4 v = {0, 0, 0, 0};
-        if (at.present >> row & 1) v = load_chunk(base + page * c.sb + in_page * c.sl, d, dim);
+        if (at.present >> row & 1)
+            v = load_chunk(base + (int64_t)page * c.sb + (int64_t)(key - page_of(p, key) * p.page) * c.sl, d, p.dim);
         *(u32v4*)(tile + L::at(row, d)) = v;
     }
 }
@@ -601,9 +745,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     // the block's sequence: the last one whose first block is no later
     const int h = (int)(blockIdx.x % (uint32_t)p.kv_heads);
     const int64_t block = paged_blocks(p, kRows) - 1 - blockIdx.x / (uint32_t)p.kv_heads;
-    const auto first_block = [&](int b) {
-        return (int64_t)(p.starts ? min(max(p.starts[b], 0), p.tokens) : b) * p.group / kRows + b;
-    };
+    const auto first_block = [&](int b) { return block_before<kRows>(p, b); };
     const int seq = __builtin_amdgcn_readfirstlane(count_up_to(p.batch, block, lane, first_block)) - 1;
     if (seq < 0) return;
     const int64_t block0 = first_block(seq);
@@ -627,7 +769,6 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     const int start = (int)((int64_t)tiles * part / p.parts) * kKeys;
     const int end = min(all, (int)((int64_t)tiles * (part + 1) / p.parts) * kKeys);
 
-    const int32_t* table = p.table + (int64_t)seq * p.table_stride;
     const T* q = (const T*)p.q.p + (int64_t)(tok.first + (live ? i : 0)) * p.q.st + hq * p.q.sh;
     const T* k = (const T*)p.cache[0].p + h * p.cache[0].sh;
     const T* v = (const T*)p.cache[1].p + h * p.cache[1].sh;
@@ -636,17 +777,21 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     for (int c = 0; c < DP / 16; ++c) qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
     const Reader<DT, DP> rd(lane);
     const PagedFiller<DT, DP> fk(p.cache[0].sl, p.dim), fv(p.cache[1].sl, p.dim);
-    const auto fill = [&](const TilePlace& at, int buf) {
+    const auto rows_of = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(p.table + (int64_t)seq * p.table_stride), 0,
+                                                           (uint32_t)p.width * 4u, 0x00020000);
+    const auto look = [&](int j0) { return page_in_table(p, rows_of, j0 + lane); };
+    // Fills the tile from key j0 on; which of its rows are there.
+    const auto fill = [&](int j0, int page, int buf) {
+        const TilePages at{j0, page, __ballot(in_cache(p, page) && j0 + lane < end)};
         if (WHOLE) {
-            fk.fill(kt[buf], k, p.cache[0], at);
-            fv.fill(vt[buf], v, p.cache[1], at);
+            fk.fill(kt[buf], k, p, p.cache[0], at);
+            fv.fill(vt[buf], v, p, p.cache[1], at);
         } else {
-            paged_stage<DT, DP>(kt[buf], k, p.cache[0], at, p.dim);
-            paged_stage<DT, DP>(vt[buf], v, p.cache[1], at, p.dim);
+            paged_stage<DT, DP>(kt[buf], k, p, p.cache[0], at);
+            paged_stage<DT, DP>(vt[buf], v, p, p.cache[1], at);
         }
+        return at.present;
     };
-    const auto look = [&](int j0) { return place_of(p, table, j0 + lane, end); };
-    const auto there = [&](Place w) { return TilePlace{w, __ballot(in_cache(p, w.page))}; };
 
     const float to_log2 = p.scale * kLog2e;
     f32x16 acc[DP / 32];
@@ -657,27 +802,34 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
         for (int db = 0; db < DP / 32; ++db) acc[db] = f32x16{};
         sm = Softmax{};
         // a tile is used, the next one is filled, the pages of the one after that are looked up
-        TilePlace now = there(look(start)), ahead = now;
-        Place later = look(start + kKeys);
-        if (start < end) fill(now, 0);
+        uint64_t now = 0, ahead = 0;
+        int page = look(start);
+        if (start < end) ahead = fill(start, page, 0);
+        page = look(start + kKeys);
         int j0 = start, buf = 0;
         const auto next = [&] {
             tile_wait();
             __syncthreads();  // the tile is there, and the other one is read
             now = ahead;
             if (j0 + kKeys < end) {
-                ahead = there(later);
-                later = look(j0 + 2 * kKeys);
-                fill(ahead, buf ^ 1);
+                ahead = fill(j0 + kKeys, page, buf ^ 1);
+                page = look(j0 + 2 * kKeys);
             }
         };
-        for (; j0 < end; j0 += kKeys, buf ^= 1) {
+        // first the tiles that every row of the work-group sees whole, up to a key without a page
+        bool ready = false;
+        for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
-            if (j0 >= wave_any) continue;
-            if (j0 + kKeys <= block_all && now.present == ~(uint64_t)0)  // every row of the work-group sees all of it
+            ready = now != ~(uint64_t)0;
+            if (ready) break;
+            if (wave_any > 0)
                 tile_forward<DT, DP, false, CAREFUL && DT != DT_F32>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
-            else
-                tile_forward<DT, DP, true, CAREFUL, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0, now.present);
+        }
+        for (; j0 < end; j0 += kKeys, buf ^= 1) {
+            if (!ready) next();
+            ready = false;
+            if (j0 < wave_any)
+                tile_forward<DT, DP, true, CAREFUL, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0, now);
         }
     };
     pass(std::false_type{});

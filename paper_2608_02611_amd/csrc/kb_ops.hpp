@@ -228,6 +228,8 @@ struct PagedParams {
     float* ws;
     int workers;  // few rows a sequence: work-groups
     int pairs;    // and their units are (sequence, head, block) pairs, not tiles of keys
+    int headers;  // of the workspace: one a worker, or (by_pair) one a pair's number
+    int by_pair;
     int parts;    // many rows: parts of the keys
 };
 
@@ -235,7 +237,6 @@ struct PagedParams {
 // which a work-group takes 16, or 32, at a time and its waves share the keys.
 constexpr int kFewRows = 32;
 constexpr int kPagedTile = 64;  // keys of a unit of work, 16 a wave
-constexpr int kPagedWorkers = 1024;
 constexpr int kPagedWhole = 512;  // sequences of no more keys are not split
 
 inline int64_t paged_keys(const PagedParams& p) { return (int64_t)p.width * p.page; }
@@ -248,19 +249,27 @@ __host__ __device__ inline int64_t paged_blocks(const PagedParams& p, int rows) 
     return (int64_t)p.tokens * p.group / rows + p.batch;
 }
 
-// Workspace of the attention over pages, in floats.  Few rows: for each
-// work-group a header of eight words, then the sums of its first and its last
-// pair.  Many rows: for each row and part the sums over its keys.
+// Workspace of the attention over pages, in floats.  Few rows: headers of eight
+// words that say which work-groups share a pair, then for each work-group the sums
+// of its first and its last pair.  Many rows: for each row and part the sums over
+// its keys.
 struct PagedHeader {
-    int32_t seq, block, head, last;  // the pair that this work-group began and others went on with, the last of them
-    int32_t valid, rows, pad[2];
+    int32_t seq, block, head;
+    int32_t first, last;  // work-groups
+    int32_t valid, rows, pad;
 };
 inline int paged_dim(const PagedParams& p) { return p.dim <= 64 ? 64 : 128; }
 inline int paged_workers(const PagedParams& p) {
+    const int64_t most = p.f32 || few_block(p) == 32 ? 512 : 768;  // as many as the CUs hold at once
     const int64_t tiles = paged_keys(p) <= kPagedWhole ? 1 : (paged_keys(p) + kPagedTile - 1) / kPagedTile;
     const int64_t pairs = paged_blocks(p, few_block(p)) * p.kv_heads;
-    return (int)(pairs >= kPagedWorkers || pairs * tiles >= kPagedWorkers ? kPagedWorkers : pairs * tiles);
+    return (int)(pairs >= most || pairs * tiles >= most ? most : pairs * tiles);
 }
+// A header for each pair where there are fewer of them than work-groups, so that
+// the second kernel has no work-groups without a pair.
+inline int64_t paged_pairs(const PagedParams& p) { return paged_blocks(p, few_block(p)) * p.kv_heads; }
+inline bool paged_by_pair(const PagedParams& p) { return paged_pairs(p) <= paged_workers(p); }
+inline int paged_headers(const PagedParams& p) { return paged_by_pair(p) ? (int)paged_pairs(p) : paged_workers(p); }
 inline int paged_parts(const PagedParams& p) {
     return attn_parts(paged_blocks(p, kAttnRows) * p.kv_heads, paged_keys(p), 1024, p.f32 ? 128 : 512);
 }
@@ -268,7 +277,7 @@ inline int64_t paged_floats(const PagedParams& p) {
     if (few_rows(p))
         return paged_keys(p) <= kPagedWhole
                    ? 0
-                   : (int64_t)paged_workers(p) * (8 + 2 * (int64_t)few_block(p) * (paged_dim(p) + 4));
+                   : (int64_t)paged_headers(p) * 8 + (int64_t)paged_workers(p) * 2 * few_block(p) * (paged_dim(p) + 4);
     const int parts = paged_parts(p);
     return parts > 1 ? (int64_t)p.tokens * p.heads * parts * ((p.dim + 3) / 4 * 4 + 4) : 0;
 }

@@ -26,6 +26,12 @@ __device__ __forceinline__ Tokens tokens_of(const PagedParams& p, int b) {
     return {first, max(0, end - first)};
 }
 
+// Number of the first block of `ROWS` query rows of sequence b (paged_blocks).
+template <int ROWS>
+__device__ __forceinline__ int64_t block_before(const PagedParams& p, int b) {
+    return (int64_t)(p.starts ? min(max(p.starts[b], 0), p.tokens) : b) * p.group / ROWS + b;
+}
+
 // How many of `n` ascending values f(0 .. n - 1) are at most x: 64 are looked at
 // at once, one a lane.
 template <typename F>

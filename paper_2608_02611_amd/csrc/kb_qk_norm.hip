@@ -104,13 +104,20 @@ struct Unit {
             x[ib] = rotates ? fmaf(b, c[i], a * si) : b;
         }
     }
-    __device__ __forceinline__ void weight(const void* w, int w_f32, float (&out)[2 * V]) const {
+    template <typename W>
+    __device__ __forceinline__ void weight_as(const W* w, float (&out)[2 * V]) const {
+        typedef W vec __attribute__((ext_vector_type(V), aligned(sizeof(W))));
+        vec v[2];
 #pragma unroll
-        for (int e = 0; e < 2 * V; ++e) {
-            const int d = e < V ? first + e : second + e - V;
-            const bool have = w != nullptr && in && (e < V || two);
-            out[e] = !have ? 1.f : w_f32 ? ((const float*)w)[d] : (float)((const T*)w)[d];
-        }
+        for (int e = 0; e < V; ++e) v[0][e] = v[1][e] = (W)1.f;
+        if (w != nullptr && in) v[0] = *(const vec*)(w + first);
+        if (w != nullptr && in && two) v[1] = *(const vec*)(w + second);
+#pragma unroll
+        for (int e = 0; e < 2 * V; ++e) out[e] = (float)v[e / V][e % V];
+    }
+    __device__ __forceinline__ void weight(const void* w, int w_f32, float (&out)[2 * V]) const {
+        if (DT == DT_F32 || w_f32) weight_as((const float*)w, out);
+        else weight_as((const T*)w, out);
     }
 };
 

@@ -123,14 +123,14 @@ struct Step {
         const int c = lane & 15, g = lane >> 4;
         const bool have = in_cache(p, w.page);
         seen = (uint32_t)__ballot(have) & 0xFFFFu;
-        const T* kr = kc + (have ? w.page * p.cache[0].sb + w.at * p.cache[0].sl : 0);
+        const T* kr = kc + (have ? row_offset(p.cache[0], w.page, w.at) : 0);
 #pragma unroll
         for (int n = 0; n < KC; ++n) load_words<DT, 4, false>(kr, (4 * n + g) * KB, p.dim, have, k[n]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int page = __shfl(w.page, 4 * g + j), at = __shfl(w.at, 4 * g + j);
             const bool in = in_cache(p, page);
-            const T* vr = vc + (in ? page * p.cache[1].sb + at * p.cache[1].sl : 0);
+            const T* vr = vc + (in ? row_offset(p.cache[1], page, at) : 0);
             load_words<DT, VW, false>(vr, VB * c, p.dim, in, v[j]);
         }
     }
@@ -430,8 +430,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
                 const int page = __builtin_amdgcn_readlane(pages, n % 64);
                 const int at = key - page_of(p, key) * p.page;
                 const int rows = in_cache(p, page) ? min(max(key_end - key, 0), 16) : 0;
-                to.load_page(kc + (int64_t)page * p.cache[0].sb + (int64_t)at * p.cache[0].sl,
-                             vc + (int64_t)page * p.cache[1].sb + (int64_t)at * p.cache[1].sl, rows, k_row, v_row, k_at, v_at);
+                to.load_page(kc + row_offset(p.cache[0], page, at), vc + row_offset(p.cache[1], page, at), rows, k_row, v_row,
+                             k_at, v_at);
             };
             load(a, 0);
 #pragma unroll 1
@@ -659,11 +659,10 @@ hipError_t few(const PagedParams& p, hipStream_t stream) {
 
 constexpr int kRows = kAttnRows;
 
-// The pages of a tile's rows, lane n of every wave knowing row n's, and the rows
-// that are there.
+// Where a tile's rows are, lane n of every wave knowing row n's page and its place
+// there, and which of them are there.
 struct TilePages {
-    int first;  // key of row 0
-    int page;
+    int page, in_page;
     uint64_t present;
 };
 // The table by buffer loads, for the reason that tiles are filled by them; past its
@@ -688,15 +687,13 @@ struct PagedFiller {
         in = d < dim;
         offset = ((uint32_t)(((int)threadIdx.x & 63) / SLOTS) * (uint32_t)stride + (uint32_t)d) * (uint32_t)sizeof(T);
     }
-    // base: the head's element 0 of page 0.
+    // base: the head's element 0 of page 0; lane n knows row n's address.
     __device__ __forceinline__ void fill(T* tile, const T* base, const PagedParams& p, const HeadView& c,
                                          const TilePages& at) const {
-        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         T* to = tile + wave * L::KB;
-        const auto from = [&](int row) {
-            const int key = at.first + row, page = __builtin_amdgcn_readlane(at.page, row);
-            return background(base + (int64_t)page * c.sb + (int64_t)(key - page_of(p, key) * p.page) * c.sl);
-        };
+        const uint64_t address = (uint64_t)(base + row_offset(c, at.page, at.in_page));
+        const auto from = [&](int row) { return background((const void*)readlane_u64(address, row)); };
         if (at.present == ~(uint64_t)0 && p.dim == L::PITCH) {
 #pragma unroll
             for (int k = 0; k < STEPS; ++k)
@@ -705,11 +702,11 @@ struct PagedFiller {
 #pragma unroll 1
             for (int k = 0; k < STEPS; ++k) {
                 const int row = k * STEP + wave * L::KB_ROWS;  // the wave's first; if it is not there, none is
-                if (in && (at.present >> (row + ((int)threadIdx.x & 63) / SLOTS) & 1)) {
+                if (in && (at.present >> (row + lane / SLOTS) & 1)) {
                     send<16>(from(row), offset, 0, to);
                 } else {
                     const u32v4 zero = {0, 0, 0, 0};
-                    *(u32v4*)(to + ((int)threadIdx.x & 63) * L::VEC) = zero;
+                    *(u32v4*)(to + lane * L::VEC) = zero;
                 }
                 to += STEP / L::KB_ROWS * L::KB;
             }
@@ -726,10 +723,9 @@ __device__ __forceinline__ void paged_stage(storage_t<DT>* tile, const storage_t
 #pragma unroll
     for (int k = 0; k < kKeys * L::CHUNKS / kThreads; ++k) {
         const int idx = k * kThreads + (int)threadIdx.x, row = idx / L::CHUNKS, d = idx % L::CHUNKS * L::VEC;
-        const int key = at.first + row, page = __shfl(at.page, row);
+        const int page = __shfl(at.page, row), in_page = __shfl(at.in_page, row);
         u32v4 v = {0, 0, 0, 0};
-        if (at.present >> row & 1)
-            v = load_chunk(base + (int64_t)page * c.sb + (int64_t)(key - page_of(p, key) * p.page) * c.sl, d, p.dim);
+        if (at.present >> row & 1) v = load_chunk(base + row_offset(c, page, in_page), d, p.dim);
         *(u32v4*)(tile + L::at(row, d)) = v;
     }
 }
@@ -782,7 +778,8 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     const auto look = [&](int j0) { return page_in_table(p, rows_of, j0 + lane); };
     // Fills the tile from key j0 on; which of its rows are there.
     const auto fill = [&](int j0, int page, int buf) {
-        const TilePages at{j0, page, __ballot(in_cache(p, page) && j0 + lane < end)};
+        const int key = j0 + lane;
+        const TilePages at{page, key - page_of(p, key) * p.page, __ballot(in_cache(p, page) && key < end)};
         if (WHOLE) {
             fk.fill(kt[buf], k, p, p.cache[0], at);
             fv.fill(vt[buf], v, p, p.cache[1], at);

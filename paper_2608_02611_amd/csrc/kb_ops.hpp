@@ -217,8 +217,8 @@ struct PagedParams {
     const int32_t* starts;  // NULL: token b is sequence b's
     int batch, width;       // pages of a sequence at most
     int pages, page;        // pages of the cache, keys of a page
-    uint32_t page_mul;      // n / page = n page_mul >> page_shift for n < 2^31
-    int page_shift;
+    uint32_t page_mul;      // n / page = (n + page_add) page_mul / 2^32 >> page_shift for n < 2^31
+    int page_shift, page_add;
     int tokens, heads, kv_heads, group, dim;
     float scale;
     int causal;

@@ -381,10 +381,14 @@ int check_pages(const char* call, const kb_tensor* k_cache, const kb_tensor* v_c
     p->width = (int)width;
     p->pages = (int)k_cache->shape[0];
     p->page = (int)page;
+    // 2^(32 + s) / page, rounded up, with 2^s < page <= 2^(s + 1): what it is too large
+    // by, times n < 2^31, stays under the 2^(32 + s) / page of the next quotient.  Pages
+    // of one key: (n + 1) (2^32 - 1) / 2^32 = n.
     int bits = 0;
-    while (((int64_t)1 << bits) < page) ++bits;
-    p->page_shift = 31 + bits;
-    p->page_mul = (uint32_t)(((uint64_t)1 << p->page_shift) / (uint64_t)page + 1);
+    while (((int64_t)2 << bits) < page) ++bits;
+    p->page_shift = page > 1 ? bits : 0;
+    p->page_add = page == 1;
+    p->page_mul = page > 1 ? (uint32_t)((((uint64_t)1 << (32 + bits)) + (uint64_t)page - 1) / (uint64_t)page) : 0xFFFFFFFFu;
     p->tokens = (int)rows.shape[0];
     p->kv_heads = (int)k_cache->shape[1];
     p->dim = (int)rows.shape[2];

@@ -8,7 +8,13 @@ namespace kb {
 
 // n / p.page for 0 <= n < 2^31.
 __device__ __forceinline__ int page_of(const PagedParams& p, int n) {
-    return (int)(((uint64_t)(uint32_t)n * p.page_mul) >> p.page_shift);
+    return (int)(__umulhi((uint32_t)(n + p.page_add), p.page_mul) >> p.page_shift);
+}
+
+// Elements from page 0's first row to that of place `at` in a page.
+__device__ __forceinline__ int64_t row_offset(const HeadView& c, int page, int at) {
+    const uint64_t of_page = (uint64_t)(uint32_t)page * (uint32_t)c.sb + ((uint64_t)((uint32_t)page * (uint32_t)((uint64_t)c.sb >> 32)) << 32);
+    return (int64_t)(of_page + (uint64_t)(uint32_t)at * (uint32_t)c.sl + ((uint64_t)((uint32_t)at * (uint32_t)((uint64_t)c.sl >> 32)) << 32));
 }
 
 // Keys of sequence b, its new tokens' included.

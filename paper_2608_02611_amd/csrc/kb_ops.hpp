@@ -79,7 +79,7 @@ struct QkParams {
     void* dw[2];            // backward, each may be NULL
     const int32_t* positions;
     const float* freqs;
-    float* part;            // backward: partial sums of dw, [parts][2][dim]
+    float* part;            // backward: partial sums of dw, [parts of q's, then of k's][dim]
     int64_t tokens;
     int heads[2];
     int dim, rot;
@@ -89,9 +89,9 @@ struct QkParams {
     int sums;               // backward: dw of q or of k is wanted
 };
 
-// Work-groups of the backward pass, each with sums of its own.
+// Work-groups of the backward pass, each with sums of its own, and what they need.
 constexpr int64_t kQkParts = 1024;
-inline int64_t qk_part_bytes(int64_t dim) { return kQkParts * 2 * dim * (int64_t)sizeof(float); }
+inline int64_t qk_part_bytes(int64_t dim) { return (kQkParts + 1) * dim * (int64_t)sizeof(float) / 16 * 16 + 16; }
 
 hipError_t launch_qk_norm_forward(int dtype, const QkParams& p, hipStream_t stream);
 hipError_t launch_qk_norm_backward(int dtype, const QkParams& p, hipStream_t stream);

@@ -68,7 +68,7 @@ struct Unit {
     __device__ __forceinline__ void set(int u, int dim, int rot) {
         const int rotating = rot / (2 * V);
         rotates = u < rotating;
-        pair = V * u;
+        pair = rotates ? V * u : 0;
         if (rotates) {
             first = NEAR ? 2 * V * u : V * u;
             second = NEAR ? first + V : rot / 2 + V * u;
@@ -134,6 +134,13 @@ __device__ __forceinline__ float row_sum(float v, int lanes) {
 
 // The token's angles, by all lanes of a wave into its own LDS, and from there
 // those of the lane's unit.
+__device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, int lane, float (*turns)[kMaxPairs]) {
+    const int position = p.positions[token];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    for (int i = lane; i < p.rot / 2; i += 64) turn_of(position, p.freqs[i], &turns[0][i], &turns[1][i]);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 template <int V, int E>
 __device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, int lane, float (*turns)[kMaxPairs],
                                             const int (&pair)[E], const bool (&rotates)[E], float (&c)[E][V],
@@ -151,6 +158,12 @@ __device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, in
             s[n][i] = rotates[n] ? turns[1][pair[n] + i] : 0.f;
         }
 }
+
+// Backward: lanes of a row, passes over a token that a wave makes at a time, and the
+// work-groups of q and of k.
+struct BackwardPlan {
+    int lanes, passes_each, parts[2];
+};
 
 // A wave's passes over a token: `per` rows of q, or of k, in each.
 struct Passes {
@@ -221,54 +234,54 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p, int la
     }
 }
 
+// Backward: a work-group has rows of q alone, or of k, so that its waves hold one
+// weight and the sums of one gradient.
 template <int DT, int V, int E, bool NEAR>
-__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkParams p, int lanes, int passes_each) {
+__global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkParams p, BackwardPlan plan) {
     using T = storage_t<DT>;
     using U = Unit<DT, V, NEAR>;
     __shared__ __align__(16) float turns[kWaves][2][kMaxPairs];
-    __shared__ float sums[kWaves][2][KB_QK_MAX_DIM];
+    __shared__ float sums[kWaves][KB_QK_MAX_DIM];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const Passes ps(p, lanes);
+    const int t = (int)blockIdx.x >= plan.parts[0];
+    const int part = (int)blockIdx.x - t * plan.parts[0], parts = t ? plan.parts[1] : plan.parts[0];
+    const int heads = t ? p.heads[1] : p.heads[0], lanes = plan.lanes, per = 64 / lanes;
+    const int all = (heads + per - 1) / per, each = min(all, plan.passes_each), chunks = (all + each - 1) / each;
     const int in_row = lane & (lanes - 1), row0 = lane / lanes;
-    const int chunks = (ps.all + passes_each - 1) / passes_each;
     const float inv = 1.f / (float)p.dim;
+    const TokenView vx = t ? p.x[1] : p.x[0], vdy = t ? p.dy[1] : p.dy[0], vdx = t ? p.y[1] : p.y[0];
     U unit[E];
-#pragma unroll
-    for (int n = 0; n < E; ++n) unit[n].set(in_row + n * lanes, p.dim, p.rot);
     int pair[E];
     bool rotates[E];
-    float w[2][E][2 * V], dw[2][E][2 * V];
+    float w[E][2 * V], dw[E][2 * V];
 #pragma unroll
     for (int n = 0; n < E; ++n) {
+        unit[n].set(in_row + n * lanes, p.dim, p.rot);
         pair[n] = unit[n].pair;
         rotates[n] = unit[n].rotates;
+        unit[n].weight(t ? p.w[1] : p.w[0], p.w_f32, w[n]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            unit[n].weight(p.w[t], p.w_f32, w[t][n]);
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) dw[t][n][e] = 0.f;
-        }
+        for (int e = 0; e < 2 * V; ++e) dw[n][e] = 0.f;
     }
-    const int64_t step = (int64_t)gridDim.x * kWaves, items = p.tokens * chunks;
-    for (int64_t item = (int64_t)blockIdx.x * kWaves + wave; item < items; item += step) {
+    const int64_t step = (int64_t)parts * kWaves, items = p.tokens * chunks;
+    for (int64_t item = (int64_t)part * kWaves + wave; item < items; item += step) {
         const int64_t token = chunks == 1 ? item : item / chunks;
-        const int from = (int)(item - token * chunks) * passes_each, to = min(ps.all, from + passes_each);
+        const int from = (int)(item - token * chunks) * each, to = min(all, from + each);
         typename U::VT next[E][2], next_dy[E][2];
         const auto fetch = [&](int pass) {
-            const int t = pass >= ps.of_q, row = (t ? pass - ps.of_q : pass) * ps.per + row0;
-            const T* x = (const T*)p.x[t].p + token * p.x[t].st + row * p.x[t].sh;
-            const T* dy = (const T*)p.dy[t].p + token * p.dy[t].st + row * p.dy[t].sh;
+            const int row = pass * per + row0;
+            const T* x = (const T*)vx.p + token * vx.st + row * vx.sh;
+            const T* dy = (const T*)vdy.p + token * vdy.st + row * vdy.sh;
 #pragma unroll
             for (int n = 0; n < E; ++n) {
-                unit[n].load(x, row < p.heads[t], next[n]);
-                unit[n].load(dy, row < p.heads[t], next_dy[n]);
+                unit[n].load(x, row < heads, next[n]);
+                unit[n].load(dy, row < heads, next_dy[n]);
             }
         };
         fetch(from);
-        float c[E][V], s[E][V];
-        if (p.rot > 0) token_turns<V, E>(p, token, lane, turns[wave], pair, rotates, c, s);
+        if (p.rot > 0) token_turns(p, token, lane, turns[wave]);
         for (int pass = from; pass < to; ++pass) {
-            const int t = pass >= ps.of_q, row = (t ? pass - ps.of_q : pass) * ps.per + row0;
+            const int row = pass * per + row0;
             float x[E][2 * V], g[E][2 * V], sum = 0.f, dot = 0.f;
 #pragma unroll
             for (int n = 0; n < E; ++n)
@@ -280,70 +293,74 @@ __global__ void __launch_bounds__(kThreads) qk_backward_kernel(QkParams p, int l
             if (pass + 1 < to) fetch(pass + 1);
 #pragma unroll
             for (int n = 0; n < E; ++n) {
-                if (p.rot > 0) unit[n].turn(g[n], c[n], s[n], -1.f);
+                if (p.rot > 0) {
+                    asm volatile("" ::: "memory");  // read where they are used: 16 registers less
+                    float c[V], s[V];
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        c[i] = turns[wave][0][pair[n] + i];
+                        s[i] = turns[wave][1][pair[n] + i];
+                    }
+                    unit[n].turn(g[n], c, s, -1.f);
+                }
 #pragma unroll
                 for (int e = 0; e < 2 * V; ++e) {
                     sum = fmaf(x[n][e], x[n][e], sum);
-                    dot = fmaf(g[n][e] * (t ? w[1][n][e] : w[0][n][e]), x[n][e], dot);
+                    dot = fmaf(g[n][e] * w[n][e], x[n][e], dot);
                 }
             }
             const float r = 1.f / sqrtf(fmaf(row_sum(sum, lanes), inv, p.eps));
             const float mean = row_sum(dot, lanes) * r * inv;  // S(u z) / D
-            const bool live = row < p.heads[t];
-            T* dx = (T*)p.y[t].p + token * p.y[t].st + row * p.y[t].sh;
+            const bool live = row < heads;
+            T* dx = (T*)vdx.p + token * vdx.st + row * vdx.sh;
 #pragma unroll
             for (int n = 0; n < E; ++n) {
 #pragma unroll
                 for (int e = 0; e < 2 * V; ++e) {
-                    const float z = x[n][e] * r, gz = g[n][e] * z;
-                    if (live) {
-                        if (t) dw[1][n][e] += gz;
-                        else dw[0][n][e] += gz;
-                    }
-                    x[n][e] = r * (g[n][e] * (t ? w[1][n][e] : w[0][n][e]) - z * mean);
+                    const float z = x[n][e] * r;
+                    if (live) dw[n][e] = fmaf(g[n][e], z, dw[n][e]);
+                    x[n][e] = r * (g[n][e] * w[n][e] - z * mean);
                 }
-                unit[n].store(dx, live && p.y[t].p != nullptr, x[n]);
+                unit[n].store(dx, live && vdx.p != nullptr, x[n]);
             }
         }
     }
     if (!p.sums) return;
     // the wave's rows, then the work-group's waves, in their order
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int n = 0; n < E; ++n)
 #pragma unroll
-        for (int n = 0; n < E; ++n)
-#pragma unroll
-            for (int e = 0; e < 2 * V; ++e) {
-                float v = dw[t][n][e];
-                for (int m = lanes; m < 64; m *= 2) v += __shfl_xor(v, m);
-                const int d = e < V ? unit[n].first + e : unit[n].second + e - V;
-                if (row0 == 0 && unit[n].in && (e < V || unit[n].two)) sums[wave][t][d] = v;
-            }
+        for (int e = 0; e < 2 * V; ++e) {
+            float v = dw[n][e];
+            for (int m = lanes; m < 64; m *= 2) v += __shfl_xor(v, m);
+            const int d = e < V ? unit[n].first + e : unit[n].second + e - V;
+            if (row0 == 0 && unit[n].in && (e < V || unit[n].two)) sums[wave][d] = v;
+        }
     __syncthreads();
-    float* part = p.part + (int64_t)blockIdx.x * 2 * p.dim;
-    for (int i = threadIdx.x; i < 2 * p.dim; i += kThreads) {
-        const int t = i >= p.dim, d = i - t * p.dim;
-        float v = sums[0][t][d];
+    for (int d = threadIdx.x; d < p.dim; d += kThreads) {
+        float v = sums[0][d];
 #pragma unroll
-        for (int k = 1; k < kWaves; ++k) v += sums[k][t][d];
-        part[i] = v;
+        for (int k = 1; k < kWaves; ++k) v += sums[k][d];
+        p.part[(int64_t)blockIdx.x * p.dim + d] = v;
     }
 }
 
-// The parts of dw added up: a work-group has 16 of the 2 dim sums and 64 threads
-// for each, whose parts it joins in a fixed order.
+// The parts of dw added up: a work-group has 16 columns of q's or of k's and 64
+// threads for each, whose parts it joins in a fixed order.
 constexpr int kJoinColumns = 16;
 constexpr int kJoinThreads = 1024;
 template <int WDT>
-__global__ void __launch_bounds__(kJoinThreads) qk_join_kernel(QkParams p, int parts) {
+__global__ void __launch_bounds__(kJoinThreads) qk_join_kernel(QkParams p, BackwardPlan plan) {
     constexpr int K = kJoinThreads / kJoinColumns;
     __shared__ float s[K][kJoinColumns + 1];
-    const int c = threadIdx.x % kJoinColumns, k = threadIdx.x / kJoinColumns;
-    const int i = (int)blockIdx.x * kJoinColumns + c;
+    const int c = threadIdx.x % kJoinColumns, k = threadIdx.x / kJoinColumns, t = (int)blockIdx.y;
+    const int d = (int)blockIdx.x * kJoinColumns + c;
+    const int parts = t ? plan.parts[1] : plan.parts[0];
+    const float* part = p.part + (int64_t)(t ? plan.parts[0] : 0) * p.dim;
     float v = 0.f;
-    if (i < 2 * p.dim) {
-#pragma unroll 4
-        for (int n = k; n < parts; n += K) v += p.part[(int64_t)n * 2 * p.dim + i];
+    if (d < p.dim) {
+#pragma unroll 8
+        for (int n = k; n < parts; n += K) v += part[(int64_t)n * p.dim + d];
     }
     s[k][c] = v;
     __syncthreads();
@@ -352,9 +369,8 @@ __global__ void __launch_bounds__(kJoinThreads) qk_join_kernel(QkParams p, int p
         if (k < m) s[k][c] += s[k + m][c];
         __syncthreads();
     }
-    if (k > 0 || i >= 2 * p.dim) return;
-    const int t = i >= p.dim;
-    if (p.dw[t] != nullptr) ((storage_t<WDT>*)p.dw[t])[i - t * p.dim] = (storage_t<WDT>)s[0][c];
+    void* dw = t ? p.dw[1] : p.dw[0];
+    if (k == 0 && d < p.dim && dw != nullptr) ((storage_t<WDT>*)dw)[d] = (storage_t<WDT>)s[0][c];
 }
 
 // The launch: passes that a wave makes over its token.  All of them, so that the
@@ -389,14 +405,23 @@ hipError_t forward(const QkParams& p, hipStream_t stream) {
 template <int DT, int V, int E, bool NEAR>
 hipError_t backward(const QkParams& p, hipStream_t stream) {
     const Plan plan = plan_of(p, V, E);
-    const int64_t groups = (p.tokens * plan.chunks + kWaves - 1) / kWaves;
-    const int parts = (int)(groups < kQkParts ? groups : kQkParts);
-    if (parts > 0)
-        qk_backward_kernel<DT, V, E, NEAR><<<dim3((unsigned)parts), kThreads, 0, stream>>>(p, plan.lanes, plan.passes_each);
+    BackwardPlan b{plan.lanes, plan.passes_each, {0, 0}};
+    // work-groups in the proportion of q's and k's rows, as many as have something to do
+    const int64_t per = 64 / plan.lanes;
+    const int64_t passes[2] = {(p.heads[0] + per - 1) / per, (p.heads[1] + per - 1) / per};
+    for (int t = 0; t < 2; ++t) {
+        if (passes[t] == 0 || p.tokens == 0) continue;
+        const int64_t each = passes[t] < plan.passes_each ? passes[t] : plan.passes_each;
+        const int64_t groups = (p.tokens * ((passes[t] + each - 1) / each) + kWaves - 1) / kWaves;
+        const int64_t share = (kQkParts - 1) * passes[t] / (passes[0] + passes[1]) + (t == 0 || passes[0] > 0);
+        b.parts[t] = (int)(groups < share ? groups : share > 0 ? share : 1);
+    }
+    if (b.parts[0] + b.parts[1] > 0)
+        qk_backward_kernel<DT, V, E, NEAR><<<dim3((unsigned)(b.parts[0] + b.parts[1])), kThreads, 0, stream>>>(p, b);
     if (p.sums) {
-        const dim3 grid((unsigned)((2 * p.dim + kJoinColumns - 1) / kJoinColumns));
-        if (DT == DT_F32 || p.w_f32) qk_join_kernel<DT_F32><<<grid, kJoinThreads, 0, stream>>>(p, parts);
-        else qk_join_kernel<DT><<<grid, kJoinThreads, 0, stream>>>(p, parts);
+        const dim3 grid((unsigned)((p.dim + kJoinColumns - 1) / kJoinColumns), 2);
+        if (DT == DT_F32 || p.w_f32) qk_join_kernel<DT_F32><<<grid, kJoinThreads, 0, stream>>>(p, b);
+        else qk_join_kernel<DT><<<grid, kJoinThreads, 0, stream>>>(p, b);
     }
     return hipGetLastError();
 }

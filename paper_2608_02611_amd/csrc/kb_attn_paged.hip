@@ -99,12 +99,11 @@ __device__ __forceinline__ void load_words(const storage_t<DT>* row, int d, int 
     }
 }
 
-// A pointer that is the same in all lanes, so that the compiler sees it.
-__device__ __forceinline__ void* uniform_pointer(const void* at) {
-    const uint64_t u = (uint64_t)at;
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)u);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(u >> 32));
-    return (void*)((uint64_t)hi << 32 | lo);
+// What is the same in all lanes, so that the compiler sees it.
+__device__ __forceinline__ int64_t uniform(int64_t v) {
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)((uint64_t)v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
 // The 16 keys of a wave's step, in registers.
@@ -141,8 +140,8 @@ struct Step {
                                               const uint32_t (&k_at)[KC], const uint32_t (&v_at)[4][(VW + 3) / 4]) {
         rows = __builtin_amdgcn_readfirstlane(rows);
         seen = (1u << rows) - 1u;
-        const auto kd = __builtin_amdgcn_make_buffer_rsrc(uniform_pointer(kr), 0, rows * k_row, 0x00020000);
-        const auto vd = __builtin_amdgcn_make_buffer_rsrc(uniform_pointer(vr), 0, rows * v_row, 0x00020000);
+        const auto kd = __builtin_amdgcn_make_buffer_rsrc((void*)uniform((int64_t)kr), 0, rows * k_row, 0x00020000);
+        const auto vd = __builtin_amdgcn_make_buffer_rsrc((void*)uniform((int64_t)vr), 0, rows * v_row, 0x00020000);
 #pragma unroll
         for (int n = 0; n < KC; ++n) {
             const u32v4 x = __builtin_bit_cast(u32v4, __builtin_amdgcn_raw_buffer_load_b128(kd, (int)k_at[n], 0, 0));
@@ -259,20 +258,22 @@ __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>
 // Tiles of sequence b, for one key head and block of rows, and its units: beginning
 // a pair takes as long as kBegin tiles, so that a work-group with many short ones has
 // no more to do than others.  (Or one for all of it.)
-constexpr int kBegin = 3;
-__device__ __forceinline__ int tiles_of(const PagedParams& p, int b) {
-    return max(1, (paged_len(p, b) + kKeys - 1) / kKeys);
-}
-__device__ __forceinline__ int units_of(const PagedParams& p, int b) { return p.pairs ? 1 : tiles_of(p, b) + kBegin; }
 template <int ROWS>
-__device__ __forceinline__ int blocks_of(const PagedParams& p, int b) {
-    return (int)(((int64_t)tokens_of(p, b).n * p.group + ROWS - 1) / ROWS);
+constexpr int kBegin = ROWS == 16 ? 2 : 5;
+__device__ __forceinline__ int tiles_of(int len) { return max(1, (len + kKeys - 1) / kKeys); }
+template <int ROWS>
+__device__ __forceinline__ int units_of(const PagedParams& p, int len) {
+    return p.pairs ? 1 : tiles_of(len) + kBegin<ROWS>;
+}
+template <int ROWS>
+__device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
+    return (int)(((uint32_t)n * (uint32_t)p.group + ROWS - 1) / ROWS);
 }
 
 // ONE_PAGE: rows are read in aligned 16-byte chunks, and a wave's 16 keys lie in one
 // page (its size is a multiple of 16).
 template <int DT, int DP, int NB, bool ONE_PAGE>
-__global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) paged_few_kernel(PagedParams p) {
+__global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(PagedParams p) {
     using T = storage_t<DT>;
     using S = Step<DT, DP>;
     constexpr int ROWS = 16 * NB, PITCH = DP + 4;
@@ -281,48 +282,90 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
     __shared__ int64_t wave_units[kWaves];
     __shared__ int64_t start_units;
     __shared__ int start_seq;
+    __shared__ Sequence sequences[64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int me = (int)blockIdx.x;
 
-    // The units before each thread's sequences.
-    const int each = (p.batch + kThreads - 1) / kThreads, mine = (int)threadIdx.x * each;
-    int64_t units = 0;
-    for (int b = mine; b < min(mine + each, p.batch); ++b)
-        units += (int64_t)blocks_of<ROWS>(p, b) * p.kv_heads * units_of(p, b);
-    int64_t upto = units;
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-        const int64_t before = __shfl_up(upto, m);
-        if (lane >= m) upto += before;
-    }
-    if (lane == 63) wave_units[wave] = upto;
-    __syncthreads();
-    int64_t all = 0, before = upto - units;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += wave_units[w];
-        all += wave_units[w];
-    }
-    const int64_t workers = min((int64_t)p.workers, all);
+    // Where this work-group's units begin: in_seq units into sequence seq.
     PagedHeader* headers = (PagedHeader*)p.ws;
     if (!p.pairs && !p.by_pair && threadIdx.x == 0) headers[me].valid = 0;
-    if (me >= workers) return;
-    const int64_t first = all * me / workers, end = all * (me + 1) / workers;
-    if (before <= first && first < before + units) {
-        int b = mine;
-        int64_t at = before;
-        for (; b < p.batch - 1; ++b) {
-            const int64_t n = (int64_t)blocks_of<ROWS>(p, b) * p.kv_heads * units_of(p, b);
-            if (first < at + n) break;
-            at += n;
+    int64_t all, workers, first, end, in_seq;
+    int seq;
+    if (p.small) {
+        // Each wave for itself, a sequence a lane, in 32 bits.  The quotients are exact: of
+        // products under 2^41, held in binary64, they are no nearer to the next integer
+        // than 1 / workers.
+        int units = 0;
+        if (lane < p.batch) {
+            const Sequence s = sequence_of(p, lane);
+            units = blocks_of<ROWS>(p, s.n) * p.kv_heads * units_of<ROWS>(p, s.len);
+            sequences[lane] = s;  // (every wave writes the same, and reads what it has written)
         }
-        start_seq = b;
-        start_units = first - at;
+        int upto = units;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const int before = __shfl_up(upto, m);
+            if (lane >= m) upto += before;
+        }
+        const int sum = __builtin_amdgcn_readlane(upto, 63);
+        all = sum;
+        workers = min(p.workers, sum);
+        if (me >= workers) return;
+        const auto share = [&](int n) { return (int)((double)sum * (double)n / (double)(int)workers); };
+        first = share(me);
+        end = share(me + 1);
+        seq = __popcll(__ballot(upto <= (int)first));
+        in_seq = (int)first - __builtin_amdgcn_readlane(upto - units, seq);
+    } else {
+        // The units before each thread's sequences.
+        const auto units_at = [&](int b) {
+            const Sequence s = sequence_of(p, b);
+            return (int64_t)blocks_of<ROWS>(p, s.n) * p.kv_heads * units_of<ROWS>(p, s.len);
+        };
+        const int each = (p.batch + kThreads - 1) / kThreads, mine = (int)threadIdx.x * each;
+        int64_t units = 0;
+        for (int b = mine; b < min(mine + each, p.batch); ++b) units += units_at(b);
+        int64_t upto = units;
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) {
+            const int64_t before = __shfl_up(upto, m);
+            if (lane >= m) upto += before;
+        }
+        if (lane == 63) wave_units[wave] = upto;
+        __syncthreads();
+        int64_t before = upto - units;
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += wave_units[w];
+            all += wave_units[w];
+        }
+        workers = min((int64_t)p.workers, all);
+        if (me >= workers) return;
+        first = all * me / workers;
+        end = all * (me + 1) / workers;
+        if (before <= first && first < before + units) {
+            int b = mine;
+            int64_t at = before;
+            for (; b < p.batch - 1; ++b) {
+                const int64_t n = units_at(b);
+                if (first < at + n) break;
+                at += n;
+            }
+            start_seq = b;
+            start_units = first - at;
+        }
+        __syncthreads();
+        seq = start_seq;
+        in_seq = start_units;
     }
-    __syncthreads();
-    int seq = __builtin_amdgcn_readfirstlane(start_seq);
-    int64_t in_seq = start_units;
+    seq = __builtin_amdgcn_readfirstlane(seq);
+    all = uniform(all);
+    workers = uniform(workers);
+    first = uniform(first);
+    end = uniform(end);
+    in_seq = uniform(in_seq);
 
     const float to_log2 = p.scale * kLog2e;
     // Where a lane reads in 16 rows of one page, in bytes; past dim: nowhere.
@@ -347,19 +390,22 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
                ((int64_t)worker * 2 + n) * ROWS * PITCH;
     };
     for (int64_t unit = first; unit < end && seq < p.batch;) {
-        const int n_tiles = tiles_of(p, seq), n_units = units_of(p, seq), klen = paged_len(p, seq);
-        const Tokens tok = tokens_of(p, seq);
-        const int n_blocks = blocks_of<ROWS>(p, seq);
+        Sequence tok = p.small ? sequences[seq] : sequence_of(p, seq);
+        tok = Sequence{__builtin_amdgcn_readfirstlane(tok.first), __builtin_amdgcn_readfirstlane(tok.n),
+                       __builtin_amdgcn_readfirstlane(tok.len)};
+        const int klen = tok.len, n_tiles = tiles_of(klen), n_units = units_of<ROWS>(p, klen);
+        const int n_blocks = blocks_of<ROWS>(p, tok.n);
         if (n_blocks == 0) {  // (a sequence without new tokens has no unit)
             ++seq;
             in_seq = 0;
             continue;
         }
-        const int pair = __builtin_amdgcn_readfirstlane((int)(in_seq / n_units));
+        const int pair = __builtin_amdgcn_readfirstlane(p.small ? (int)((uint32_t)in_seq / (uint32_t)n_units)
+                                                                : (int)(in_seq / n_units));
         const int in_pair = (int)(in_seq - (int64_t)pair * n_units);
         const int take = (int)min((int64_t)(n_units - in_pair), end - unit);
-        const int tile = __builtin_amdgcn_readfirstlane(p.pairs ? 0 : max(0, in_pair - kBegin));
-        const int tile_end = __builtin_amdgcn_readfirstlane(p.pairs ? n_tiles : max(0, in_pair + take - kBegin));
+        const int tile = __builtin_amdgcn_readfirstlane(p.pairs ? 0 : max(0, in_pair - kBegin<ROWS>));
+        const int tile_end = __builtin_amdgcn_readfirstlane(p.pairs ? n_tiles : max(0, in_pair + take - kBegin<ROWS>));
         const auto advance = [&] {
             unit += take;
             in_seq += take;
@@ -528,8 +574,10 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 || NB == 2 ? 2 : 3) pag
         if (threadIdx.x == 0 && !p.pairs && begun && (p.by_pair || !ended)) {
             // the worker that has the pair's last tile
             const int64_t last = unit + (n_units - in_pair) - 1;
-            headers[p.by_pair ? (block_before<ROWS>(p, seq) + block) * p.kv_heads + h : me] =
-                PagedHeader{seq, block, h, me, (int)(((last + 1) * workers - 1) / all), !ended, rows, 0};
+            headers[p.by_pair ? (block_before<ROWS>(p, seq) + block) * p.kv_heads + h : me] = PagedHeader{
+                seq, block, h, me,
+                p.small ? (int)((double)((last + 1) * workers - 1) / (double)all) : (int)(((last + 1) * workers - 1) / all),
+                !ended, rows, 0};
         }
         __syncthreads();  // the sums are read
         if (only < 0 || ++only > row_last) break;

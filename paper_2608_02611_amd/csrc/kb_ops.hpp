@@ -230,6 +230,7 @@ struct PagedParams {
     int pairs;    // and their units are (sequence, head, block) pairs, not tiles of keys
     int headers;  // of the workspace: one a worker, or (by_pair) one a pair's number
     int by_pair;
+    int small;    // 64 sequences at most, and units that 32 bits number
     int parts;    // many rows: parts of the keys
 };
 
@@ -260,10 +261,16 @@ struct PagedHeader {
 };
 inline int paged_dim(const PagedParams& p) { return p.dim <= 64 ? 64 : 128; }
 inline int paged_workers(const PagedParams& p) {
-    const int64_t most = p.f32 || few_block(p) == 32 ? 512 : 768;  // as many as the CUs hold at once
+    const int64_t most = 512;  // two a CU
     const int64_t tiles = paged_keys(p) <= kPagedWhole ? 1 : (paged_keys(p) + kPagedTile - 1) / kPagedTile;
     const int64_t pairs = paged_blocks(p, few_block(p)) * p.kv_heads;
     return (int)(pairs >= most || pairs * tiles >= most ? most : pairs * tiles);
+}
+// (Units: tiles and what the beginning of a pair counts for, a few.  Every sequence
+// could say that all tokens are its own.)
+inline bool paged_small(const PagedParams& p) {
+    return p.batch <= 64 && ((int64_t)p.tokens * p.group / 16 + 1) * p.batch * p.kv_heads <
+                                ((int64_t)1 << 31) / (paged_keys(p) / kPagedTile + 16);
 }
 // A header for each pair where there are fewer of them than work-groups, so that
 // the second kernel has no work-groups without a pair.

@@ -717,6 +717,7 @@ int kb_attn_paged(const kb_tensor* q, const kb_tensor* k_cache, const kb_tensor*
     p.pairs = paged_keys(p) <= kPagedWhole;
     p.headers = paged_headers(p);
     p.by_pair = paged_by_pair(p);
+    p.small = paged_small(p);
     p.parts = paged_parts(p);
     const hipError_t e = launch_attn_paged(q->dtype, p, stream);
     return e == hipSuccess ? KB_OK : fail_hip(e, "kb_attn_paged: launch");

@@ -32,6 +32,15 @@ __device__ __forceinline__ Tokens tokens_of(const PagedParams& p, int b) {
     return {first, max(0, end - first)};
 }
 
+// Its tokens and its keys.
+struct Sequence {
+    int first, n, len;
+};
+__device__ __forceinline__ Sequence sequence_of(const PagedParams& p, int b) {
+    const Tokens t = tokens_of(p, b);
+    return {t.first, t.n, paged_len(p, b)};
+}
+
 // Number of the first block of `ROWS` query rows of sequence b (paged_blocks).
 template <int ROWS>
 __device__ __forceinline__ int64_t block_before(const PagedParams& p, int b) {

@@ -743,9 +743,17 @@ struct PagedFiller {
         const uint64_t address = (uint64_t)(base + row_offset(c, at.page, at.in_page));
         const auto from = [&](int row) { return background((const void*)readlane_u64(address, row)); };
         if (at.present == ~(uint64_t)0 && p.dim == L::PITCH) {
+            if (p.page % kKeys == 0) {  // all of the tile in one page
+                const auto whole = from(0);
+                const int row = (int)c.sl * (int)sizeof(T);  // (kKeys of them are within 2^31 bytes)
 #pragma unroll
-            for (int k = 0; k < STEPS; ++k)
-                send<16>(from(k * STEP + wave * L::KB_ROWS), offset, 0, to + k * (STEP / L::KB_ROWS * L::KB));
+                for (int k = 0; k < STEPS; ++k)
+                    send<16>(whole, offset, (k * STEP + wave * L::KB_ROWS) * row, to + k * (STEP / L::KB_ROWS * L::KB));
+            } else {
+#pragma unroll
+                for (int k = 0; k < STEPS; ++k)
+                    send<16>(from(k * STEP + wave * L::KB_ROWS), offset, 0, to + k * (STEP / L::KB_ROWS * L::KB));
+            }
         } else {
 #pragma unroll 1
             for (int k = 0; k < STEPS; ++k) {
@@ -789,15 +797,28 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     // the block's sequence: the last one whose first block is no later
     const int h = (int)(blockIdx.x % (uint32_t)p.kv_heads);
     const int64_t block = paged_blocks(p, kRows) - 1 - blockIdx.x / (uint32_t)p.kv_heads;
-    const auto first_block = [&](int b) { return block_before<kRows>(p, b); };
-    const int seq = __builtin_amdgcn_readfirstlane(count_up_to(p.batch, block, lane, first_block)) - 1;
-    if (seq < 0) return;
-    const int64_t block0 = first_block(seq);
-    const Tokens tok = tokens_of(p, seq);
-    const int64_t rows = (int64_t)tok.n * p.group;
-    if (block < block0 || (block - block0) * kRows >= rows) return;  // between two sequences
+    int seq, klen;
+    Tokens tok;
+    int64_t block0;
+    if (p.batch <= 64) {  // a sequence a lane: all that is asked of them on its way at once
+        Sequence mine{0, 0, 0};
+        if (lane < p.batch) mine = sequence_of(p, lane);
+        const int of_lane = (int)((uint32_t)mine.first * (uint32_t)p.group / kRows) + lane;  // block_before
+        seq = __popcll(__ballot(lane < p.batch && of_lane <= block)) - 1;
+        if (seq < 0) return;
+        tok = {__builtin_amdgcn_readlane(mine.first, seq), __builtin_amdgcn_readlane(mine.n, seq)};
+        klen = __builtin_amdgcn_readlane(mine.len, seq);
+        block0 = __builtin_amdgcn_readlane(of_lane, seq);
+    } else {
+        const auto first_block = [&](int b) { return block_before<kRows>(p, b); };
+        seq = __builtin_amdgcn_readfirstlane(count_up_to(p.batch, block, lane, first_block)) - 1;
+        if (seq < 0) return;
+        tok = tokens_of(p, seq);
+        klen = paged_len(p, seq);
+        block0 = first_block(seq);
+    }
+    if (block < block0 || (block - block0) * kRows >= (int64_t)tok.n * p.group) return;  // between two sequences
     const uint32_t first = (uint32_t)(block - block0) * kRows;
-    const int klen = paged_len(p, seq);
 
     const uint32_t row = first + wave * 32 + (lane & 31);
     const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row % (uint32_t)p.group);

@@ -39,14 +39,30 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(PagedParams p) {
         for (int n = 0; n < kAhead; ++n)
             if (n * 64 + lane < all) v[n] = fetch(n * 64 + lane);
 
-        int b = (int)token;
-        if (p.starts != nullptr) {
-            b = count_up_to(p.batch, token, lane, [&](int i) { return (int64_t)p.starts[i + 1]; });
-            if (b >= p.batch || token < p.starts[b]) continue;  // no sequence's
+        // its sequence, and the token after that one's last
+        int b = (int)token, len;
+        int64_t end = token + 1;
+        if (p.starts != nullptr && p.batch <= 64) {  // a sequence a lane: all that is asked of them on its way at once
+            int first = 0, last = 0, keys = 0;
+            if (lane < p.batch) {
+                first = p.starts[lane];
+                last = p.starts[lane + 1];
+                keys = paged_len(p, lane);
+            }
+            b = __popcll(__ballot(lane < p.batch && last <= token));
+            if (b >= p.batch || token < __builtin_amdgcn_readlane(first, b)) continue;  // no sequence's
+            end = __builtin_amdgcn_readlane(last, b);
+            len = __builtin_amdgcn_readlane(keys, b);
+        } else {
+            if (p.starts != nullptr) {
+                b = count_up_to(p.batch, token, lane, [&](int i) { return (int64_t)p.starts[i + 1]; });
+                if (b >= p.batch || token < p.starts[b]) continue;
+                end = p.starts[b + 1];
+            }
+            len = paged_len(p, b);
         }
-        const int64_t end = p.starts != nullptr ? (int64_t)p.starts[b + 1] : token + 1;
-        const int64_t place = (int64_t)paged_len(p, b) - end + token;
-        if (place < 0 || place >= paged_len(p, b)) continue;
+        const int64_t place = (int64_t)len - end + token;
+        if (place < 0 || place >= len) continue;
         const int at = page_of(p, (int)place), in_page = (int)place - at * p.page;
         const int page = p.table[b * p.table_stride + at];
         if (page < 0 || page >= p.pages) continue;  // no page

@@ -273,7 +273,7 @@ __device__ __forceinline__ int blocks_of(const PagedParams& p, int n) {
 // ONE_PAGE: rows are read in aligned 16-byte chunks, and a wave's 16 keys lie in one
 // page (its size is a multiple of 16).
 template <int DT, int DP, int NB, bool ONE_PAGE>
-__global__ void __launch_bounds__(kThreads, 2) paged_few_kernel(PagedParams p) {
+__global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 ? 4 : 2) paged_few_kernel(PagedParams p) {
     using T = storage_t<DT>;
     using S = Step<DT, DP>;
     constexpr int ROWS = 16 * NB, PITCH = DP + 4;
@@ -742,7 +742,8 @@ struct PagedFiller {
         T* to = tile + wave * L::KB;
         const uint64_t address = (uint64_t)(base + row_offset(c, at.page, at.in_page));
         const auto from = [&](int row) { return background((const void*)readlane_u64(address, row)); };
-        if (at.present == ~(uint64_t)0 && p.dim == L::PITCH) {
+        if (at.present == ~(uint64_t)0) {
+            if (!in) return;  // (zeros from the beginning)
             if (p.page % kKeys == 0) {  // all of the tile in one page
                 const auto whole = from(0);
                 const int row = (int)c.sl * (int)sizeof(T);  // (kKeys of them are within 2^31 bytes)
@@ -842,6 +843,14 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     for (int c = 0; c < DP / 16; ++c) qf[c] = load_frag<DT, WHOLE>(q, c, g, p.dim, live);
     const Reader<DT, DP> rd(lane);
     const PagedFiller<DT, DP> fk(p.cache[0].sl, p.dim), fv(p.cache[1].sl, p.dim);
+    if (WHOLE && p.dim != L::PITCH) {  // what no tile's rows fill
+        for (int n = threadIdx.x * L::VEC; n < 2 * L::size(kKeys); n += kThreads * L::VEC) {
+            const u32v4 zero = {0, 0, 0, 0};
+            *(u32v4*)(&kt[0][0] + n) = zero;
+            *(u32v4*)(&vt[0][0] + n) = zero;
+        }
+        __syncthreads();
+    }
     const auto rows_of = __builtin_amdgcn_make_buffer_rsrc(const_cast<int32_t*>(p.table + (int64_t)seq * p.table_stride), 0,
                                                            (uint32_t)p.width * 4u, 0x00020000);
     const auto look = [&](int j0) { return page_in_table(p, rows_of, j0 + lane); };
@@ -972,8 +981,11 @@ hipError_t many(const PagedParams& p, hipStream_t stream) {
 template <int DT>
 hipError_t paged(const PagedParams& p, hipStream_t stream) {
     if (few_rows(p)) {
-        if (few_block(p) == 16) return p.dim <= 64 ? few<DT, 64, 1>(p, stream) : few<DT, 128, 1>(p, stream);
-        return p.dim <= 64 ? few<DT, 64, 2>(p, stream) : few<DT, 128, 2>(p, stream);
+        if (p.dim <= 64) return few_block(p) == 16 ? few<DT, 64, 1>(p, stream) : few<DT, 64, 2>(p, stream);
+        if constexpr (DT != DT_F32) {
+            if (few_block(p) == 32) return few<DT, 128, 2>(p, stream);
+        }
+        return few<DT, 128, 1>(p, stream);
     }
     if (p.dim <= 64) return many<DT, 64>(p, stream);
     if (p.dim <= 96) return many<DT, 96>(p, stream);

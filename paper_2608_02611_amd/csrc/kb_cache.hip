@@ -12,10 +12,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kAhead = 4;  // vectors of a lane that are on their way during the search
 
-// Elements are moved as bits, V of them at once (V divides the rows).
-template <typename B, int V>
+// Elements are moved as bits, V of them at once (V divides the rows).  AHEAD: vectors
+// of a lane that are on their way during the search.
+template <typename B, int V, int AHEAD>
 __global__ void __launch_bounds__(kThreads) cache_write_kernel(PagedParams p) {
     typedef B VT __attribute__((ext_vector_type(V), aligned(sizeof(B))));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -34,9 +34,9 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(PagedParams p) {
             const TokenView& x = t ? p.rows[1] : p.rows[0];
             return *(const VT*)((const B*)x.p + token * x.st + head * x.sh + d);
         };
-        VT v[kAhead];
+        VT v[AHEAD];
 #pragma unroll
-        for (int n = 0; n < kAhead; ++n)
+        for (int n = 0; n < AHEAD; ++n)
             if (n * 64 + lane < all) v[n] = fetch(n * 64 + lane);
 
         // its sequence, and the token after that one's last
@@ -74,16 +74,19 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(PagedParams p) {
             *(VT*)((B*)c.p + page * c.sb + head * c.sh + in_page * c.sl + d) = x;
         };
 #pragma unroll
-        for (int n = 0; n < kAhead; ++n)
+        for (int n = 0; n < AHEAD; ++n)
             if (n * 64 + lane < all) put(n * 64 + lane, v[n]);
-        for (int i = kAhead * 64 + lane; i < all; i += 64) put(i, fetch(i));
+        for (int i = AHEAD * 64 + lane; i < all; i += 64) put(i, fetch(i));
     }
 }
 
 template <typename B, int V>
 hipError_t write(const PagedParams& p, hipStream_t stream) {
     const int64_t groups = ((int64_t)p.tokens + kWaves - 1) / kWaves;
-    cache_write_kernel<B, V><<<dim3((unsigned)(groups < 16384 ? groups : 16384)), kThreads, 0, stream>>>(p);
+    const dim3 grid((unsigned)(groups < 16384 ? groups : 16384));
+    // tokens of a vector a lane need fewer registers, and latency is what bounds them
+    if (2 * (int64_t)p.kv_heads * (p.dim / V) <= 64) cache_write_kernel<B, V, 1><<<grid, kThreads, 0, stream>>>(p);
+    else cache_write_kernel<B, V, 4><<<grid, kThreads, 0, stream>>>(p);
     return hipGetLastError();
 }
 

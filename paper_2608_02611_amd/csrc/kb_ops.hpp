@@ -242,7 +242,9 @@ constexpr int kPagedWhole = 512;  // sequences of no more keys are not split
 
 inline int64_t paged_keys(const PagedParams& p) { return (int64_t)p.width * p.page; }
 inline bool few_rows(const PagedParams& p) { return (int64_t)p.tokens * p.group <= (int64_t)kFewRows * p.batch; }
-inline int few_block(const PagedParams& p) { return (int64_t)p.tokens * p.group <= (int64_t)16 * p.batch ? 16 : 32; }
+inline int few_block(const PagedParams& p) {
+    return (int64_t)p.tokens * p.group <= (int64_t)16 * p.batch || (p.f32 && p.dim > 64) ? 16 : 32;
+}
 // At most so many blocks of `rows` query rows have all sequences together: each
 // begins one, and a block numbered (rows before the sequence) / rows + sequence
 // leaves room for it.
@@ -261,7 +263,7 @@ struct PagedHeader {
 };
 inline int paged_dim(const PagedParams& p) { return p.dim <= 64 ? 64 : 128; }
 inline int paged_workers(const PagedParams& p) {
-    const int64_t most = 512;  // two a CU
+    const int64_t most = p.dim <= 64 && few_block(p) == 16 ? 1024 : 512;
     const int64_t tiles = paged_keys(p) <= kPagedWhole ? 1 : (paged_keys(p) + kPagedTile - 1) / kPagedTile;
     const int64_t pairs = paged_blocks(p, few_block(p)) * p.kv_heads;
     return (int)(pairs >= most || pairs * tiles >= most ? most : pairs * tiles);

@@ -1036,21 +1036,22 @@ def kb_qk_norm_backward(dq_out, dk_out, q, k, wq, wk, eps=1e-6, positions=None, 
     """Gradients of kb_qk_norm_forward from those of its outputs: (dq, dk, dwq,
     dwk), made here where not given; dwq and dwk of the weights' dtype (q's
     without a weight)."""
-    torch = _torch()
     L = lib()
-    weight = wq if wq is not None else wk
-    wdtype = q.dtype if weight is None else weight.dtype
-    with _on(stream):
-        if dq is None:
-            dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        if dk is None:
-            dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        if dwq is None:
-            dwq = torch.empty(q.shape[-1], dtype=wdtype, device=q.device)
-        if dwk is None:
-            dwk = torch.empty(q.shape[-1], dtype=wdtype, device=q.device)
-        if workspace is None:
-            workspace = _scratch(L.kb_qk_norm_backward_workspace_bytes(q.shape[-1]), q.device)
+    if dq is None or dk is None or dwq is None or dwk is None or workspace is None:
+        torch = _torch()
+        weight = wq if wq is not None else wk
+        wdtype = q.dtype if weight is None else weight.dtype
+        with _on(stream):
+            if dq is None:
+                dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            if dk is None:
+                dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+            if dwq is None:
+                dwq = torch.empty(q.shape[-1], dtype=wdtype, device=q.device)
+            if dwk is None:
+                dwk = torch.empty(q.shape[-1], dtype=wdtype, device=q.device)
+            if workspace is None:
+                workspace = _scratch(L.kb_qk_norm_backward_workspace_bytes(q.shape[-1]), q.device)
     _one_device(dq_out, dk_out, q, k, wq, wk, positions, freqs, dq, dk, dwq, dwk, workspace)
     ws, nbytes = _extent(workspace)
     pq = pack_view(_tokens(q))

@@ -446,141 +446,142 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
         // alone (only >= 0).
         int only = -1;
         for (;;) {
-        const int key_end = __builtin_amdgcn_readfirstlane(
-            only < 0 ? take_end : min(take_end, key_limit(only, tok.n, klen, p.causal)));
+            const int key_end = __builtin_amdgcn_readfirstlane(
+                only < 0 ? take_end : min(take_end, key_limit(only, tok.n, klen, p.causal)));
 
-        f32x4 acc[NB][S::VB];
-        Rows<NB> st;
+            f32x4 acc[NB][S::VB];
+            Rows<NB> st;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            st.m[b] = -INFINITY;
-            st.l[b] = 0.f;
+            for (int b = 0; b < NB; ++b) {
+                st.m[b] = -INFINITY;
+                st.l[b] = 0.f;
 #pragma unroll
-            for (int e = 0; e < S::VB; ++e) acc[b][e] = f32x4{};
-        }
-        const int32_t* table = p.table + (int64_t)__builtin_amdgcn_readfirstlane(seq) * p.table_stride;
-        const T* kc = (const T*)p.cache[0].p + h * p.cache[0].sh;
-        const T* vc = (const T*)p.cache[1].p + h * p.cache[1].sh;
-        const int key0 = tile * kKeys + 16 * wave;
-        // one step is computed while the next one's keys are on their way
-        Step<DT, DP> a, b;
-        if constexpr (ONE_PAGE) {
-            // the pages of 64 steps, one a lane
-            int pages = 0;
-            const auto load = [&](Step<DT, DP>& to, int n) {
-                const int key = key0 + n * kKeys;
-                if (n % 64 == 0) {
-                    const int of_lane = key + lane * kKeys;
-                    pages = of_lane < key_end ? table[page_of(p, of_lane)] : -1;
+                for (int e = 0; e < S::VB; ++e) acc[b][e] = f32x4{};
+            }
+            const int32_t* table = p.table + (int64_t)__builtin_amdgcn_readfirstlane(seq) * p.table_stride;
+            const T* kc = (const T*)p.cache[0].p + h * p.cache[0].sh;
+            const T* vc = (const T*)p.cache[1].p + h * p.cache[1].sh;
+            const int key0 = tile * kKeys + 16 * wave;
+            // one step is computed while the next one's keys are on their way
+            Step<DT, DP> a, b;
+            if constexpr (ONE_PAGE) {
+                // the pages of 64 steps, one a lane
+                int pages = 0;
+                const auto load = [&](Step<DT, DP>& to, int n) {
+                    const int key = key0 + n * kKeys;
+                    if (n % 64 == 0) {
+                        const int of_lane = key + lane * kKeys;
+                        pages = of_lane < key_end ? table[page_of(p, of_lane)] : -1;
+                    }
+                    const int page = __builtin_amdgcn_readlane(pages, n % 64);
+                    const int at = key - page_of(p, key) * p.page;
+                    const int rows = in_cache(p, page) ? min(max(key_end - key, 0), 16) : 0;
+                    const int some = rows ? page : 0;
+                    to.load_page(kc + row_offset(p.cache[0], some, at), vc + row_offset(p.cache[1], some, at), rows, k_row, v_row,
+                                 k_at, v_at);
+                };
+                load(a, 0);
+#pragma unroll 1
+                for (int n = 0, key = key0; key < key_end; n += 2, key += 2 * kKeys) {  // (a step without a key adds nothing)
+                    load(b, n + 1);
+                    step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
+                    load(a, n + 2);
+                    step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
                 }
-                const int page = __builtin_amdgcn_readlane(pages, n % 64);
-                const int at = key - page_of(p, key) * p.page;
-                const int rows = in_cache(p, page) ? min(max(key_end - key, 0), 16) : 0;
-                to.load_page(kc + row_offset(p.cache[0], page, at), vc + row_offset(p.cache[1], page, at), rows, k_row, v_row,
-                             k_at, v_at);
-            };
-            load(a, 0);
-#pragma unroll 1
-            for (int n = 0, key = key0; key < key_end; n += 2, key += 2 * kKeys) {  // (a step without a key adds nothing)
-                load(b, n + 1);
-                step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
-                load(a, n + 2);
-                step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
-            }
-        } else {
-            // and the places of the one after that
-            Place w = place_of(p, table, key0 + c, key_end);
-            Place next = place_of(p, table, key0 + kKeys + c, key_end);
-            a.load(p, kc, vc, w, lane);
-#pragma unroll 1
-            for (int key = key0; key < key_end; key += 2 * kKeys) {
-                w = next;
-                next = place_of(p, table, key + 2 * kKeys + c, key_end);
-                b.load(p, kc, vc, w, lane);
-                step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
-                w = next;
-                next = place_of(p, table, key + 3 * kKeys + c, key_end);
+            } else {
+                // and the places of the one after that
+                Place w = place_of(p, table, key0 + c, key_end);
+                Place next = place_of(p, table, key0 + kKeys + c, key_end);
                 a.load(p, kc, vc, w, lane);
-                step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
+#pragma unroll 1
+                for (int key = key0; key < key_end; key += 2 * kKeys) {
+                    w = next;
+                    next = place_of(p, table, key + 2 * kKeys + c, key_end);
+                    b.load(p, kc, vc, w, lane);
+                    step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
+                    w = next;
+                    next = place_of(p, table, key + 3 * kKeys + c, key_end);
+                    a.load(p, kc, vc, w, lane);
+                    step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
+                }
             }
-        }
 
-        if (only < 0 && p.causal && row_first < row_last) {
-            float z = 0.f;  // x 0 is 0, or NaN
+            if (only < 0 && p.causal && row_first < row_last) {
+                float z = 0.f;  // x 0 is 0, or NaN
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+                for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int e = 0; e < S::VB; ++e)
+                    for (int e = 0; e < S::VB; ++e)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) z = fmaf(acc[b][e][r], 0.f, z);
-            if (__syncthreads_or(z != 0.f)) {
-                only = row_first;
-                continue;
+                        for (int r = 0; r < 4; ++r) z = fmaf(acc[b][e][r], 0.f, z);
+                if (__syncthreads_or(z != 0.f)) {
+                    only = row_first;
+                    continue;
+                }
             }
-        }
 
-        // the waves' sums, joined through LDS
+            // the waves' sums, joined through LDS
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            st.l[b] += __shfl_xor(st.l[b], 16);
-            st.l[b] += __shfl_xor(st.l[b], 32);
-            if (g == 0) {
-                stat_m[wave][b * 16 + c] = st.m[b];
-                stat_l[wave][b * 16 + c] = st.l[b];
+            for (int b = 0; b < NB; ++b) {
+                st.l[b] += __shfl_xor(st.l[b], 16);
+                st.l[b] += __shfl_xor(st.l[b], 32);
+                if (g == 0) {
+                    stat_m[wave][b * 16 + c] = st.m[b];
+                    stat_l[wave][b * 16 + c] = st.l[b];
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < S::VB; e += 4)
+                        *(f32x4*)&sums[wave][b * 16 + c][S::VB * (4 * g + r) + e] =
+                            f32x4{acc[b][e][r], acc[b][e + 1][r], acc[b][e + 2][r], acc[b][e + 3][r]};
             }
+            __syncthreads();
+            const bool begun = tile == 0, ended = tile_end == n_tiles;
+            float* part = begun && ended ? nullptr : slot(me, begun ? 1 : 0);
+            for (int n = threadIdx.x; n < rows * (DP / 4); n += kThreads) {
+                const int r = n / (DP / 4), d = n % (DP / 4) * 4;
+                const uint32_t row = (uint32_t)block * ROWS + r;
+                const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row - (uint32_t)i * p.group);
+                if (only >= 0 && i != only) continue;
+                float m = stat_m[0][r];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+                for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat_m[w][r]);
+                const float ref = m == -INFINITY ? 0.f : m;
+                f32x4 o = {};
+                float l = 0.f;
 #pragma unroll
-                for (int e = 0; e < S::VB; e += 4)
-                    *(f32x4*)&sums[wave][b * 16 + c][S::VB * (4 * g + r) + e] =
-                        f32x4{acc[b][e][r], acc[b][e + 1][r], acc[b][e + 2][r], acc[b][e + 3][r]};
-        }
-        __syncthreads();
-        const bool begun = tile == 0, ended = tile_end == n_tiles;
-        float* part = begun && ended ? nullptr : slot(me, begun ? 1 : 0);
-        for (int n = threadIdx.x; n < rows * (DP / 4); n += kThreads) {
-            const int r = n / (DP / 4), d = n % (DP / 4) * 4;
-            const uint32_t row = (uint32_t)block * ROWS + r;
-            const int i = (int)(row / (uint32_t)p.group), hq = h * p.group + (int)(row - (uint32_t)i * p.group);
-            if (only >= 0 && i != only) continue;
-            float m = stat_m[0][r];
+                for (int w = 0; w < kWaves; ++w) {
+                    const float f = __builtin_amdgcn_exp2f((stat_m[w][r] - ref) * to_log2);
+                    const f32x4 x = *(const f32x4*)&sums[w][r][d];
+                    l = fmaf(f, stat_l[w][r], l);
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) m = fmaxf(m, stat_m[w][r]);
-            const float ref = m == -INFINITY ? 0.f : m;
-            f32x4 o = {};
-            float l = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f((stat_m[w][r] - ref) * to_log2);
-                const f32x4 x = *(const f32x4*)&sums[w][r][d];
-                l = fmaf(f, stat_l[w][r], l);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
+                    for (int e = 0; e < 4; ++e) o[e] = fmaf(f, x[e], o[e]);
+                }
+                if (part != nullptr) {
+                    *(f32x4*)(part + r * PITCH + d) = o;
+                    if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, 0.f, 0.f};
+                    continue;
+                }
+                const int64_t t = tok.first + i;
+                const bool some = l != 0.f;
+                const float f = 1.f / l;
+                store_quad<DT>((T*)p.o.p + t * p.o.st + hq * p.o.sh, d, p.dim, some ? o[0] * f : 0.f, some ? o[1] * f : 0.f,
+                               some ? o[2] * f : 0.f, some ? o[3] * f : 0.f);
+                if (d == 0 && p.lse != nullptr)
+                    p.lse[t * p.heads + hq] =
+                        some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
             }
-            if (part != nullptr) {
-                *(f32x4*)(part + r * PITCH + d) = o;
-                if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, 0.f, 0.f};
-                continue;
+            if (threadIdx.x == 0 && !p.pairs && begun && (p.by_pair || !ended)) {
+                // the worker that has the pair's last tile
+                const int64_t last = unit + (n_units - in_pair) - 1;
+                headers[p.by_pair ? (block_before<ROWS>(p, seq) + block) * p.kv_heads + h : me] = PagedHeader{
+                    seq, block, h, me,
+                    p.small ? (int)((double)((last + 1) * workers - 1) / (double)all) : (int)(((last + 1) * workers - 1) / all),
+                    !ended, rows, 0};
             }
-            const int64_t t = tok.first + i;
-            const bool some = l != 0.f;
-            const float f = 1.f / l;
-            store_quad<DT>((T*)p.o.p + t * p.o.st + hq * p.o.sh, d, p.dim, some ? o[0] * f : 0.f, some ? o[1] * f : 0.f,
-                           some ? o[2] * f : 0.f, some ? o[3] * f : 0.f);
-            if (d == 0 && p.lse != nullptr)
-                p.lse[t * p.heads + hq] =
-                    some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
-        }
-        if (threadIdx.x == 0 && !p.pairs && begun && (p.by_pair || !ended)) {
-            // the worker that has the pair's last tile
-            const int64_t last = unit + (n_units - in_pair) - 1;
-            headers[p.by_pair ? (block_before<ROWS>(p, seq) + block) * p.kv_heads + h : me] = PagedHeader{
-                seq, block, h, me,
-                p.small ? (int)((double)((last + 1) * workers - 1) / (double)all) : (int)(((last + 1) * workers - 1) / all),
-                !ended, rows, 0};
-        }
-        __syncthreads();  // the sums are read
-        if (only < 0 || ++only > row_last) break;
+            __syncthreads();  // the sums are read
+            if (only < 0 || ++only > row_last) break;
         }
         advance();
     }

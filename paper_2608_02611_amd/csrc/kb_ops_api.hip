@@ -360,7 +360,8 @@ int check_pages(const char* call, const kb_tensor* k_cache, const kb_tensor* v_c
     if (pages == nullptr) return fail(KB_ERR_INVALID_ARG, "%s: null pages", call);
     const int64_t page = k_cache->shape[2], width = pages->max_pages, batch = pages->batch;
     if (page < 1) return fail(KB_ERR_INVALID_ARG, "%s: pages of no key", call);
-    if (batch < 0 || width < 0 || batch > ((int64_t)1 << 20) || page * width > kMaxLen)
+    // (a row of the table is within 2^30 bytes)
+    if (batch < 0 || width < 0 || batch > ((int64_t)1 << 20) || width > ((int64_t)1 << 28) || page * width > kMaxLen)
         return fail(KB_ERR_INVALID_ARG, "%s: batch %d or max_pages %d out of range", call, pages->batch, pages->max_pages);
     if (batch > 1 && (pages->table_stride < width || pages->table_stride > ((int64_t)1 << 40)))
         return fail(KB_ERR_INVALID_ARG, "%s: table_stride %lld out of range", call, (long long)pages->table_stride);

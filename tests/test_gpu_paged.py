@@ -168,6 +168,16 @@ def test_parts(dtype, dim, seqs, heads, kv):
     run(Batch(seqs, 16, heads, kv, dim, dtype, "hnd", one=all(q == 1 for q, _ in seqs)))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("keys", [300, 800])
+def test_many_sequences(dtype, keys):
+    """More than a wave's lanes, some without new tokens; of keys that are split and that are not; also many rows each."""
+    few = [(i % 3, 1 + (i * 37) % keys) for i in range(300)]
+    run(Batch(few, 16, 8, 2, 64, dtype, before=1, after=1))
+    many = [((i * 7) % 40, 40 + (i * 37) % keys) for i in range(70)]
+    run(Batch(many, 16, 8, 2, 64, dtype, before=1, after=1))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_a_wide_table_of_short_sequences(dtype):
     """Rooms for 100,000 keys, of which few are used: work-groups and parts without a key."""

@@ -138,6 +138,7 @@ PAGE_CHANGES = [
     (dict(vc=view(0x500000, C, dtype=F16)), DTYPE),
     (dict(pg=pages(batch=-1)), ARG), (dict(pg=pages(width=-1)), ARG), (dict(pg=pages(batch=(1 << 20) + 1)), ARG),
     (dict(pg=pages(width=1 << 27, stride=1 << 27)), ARG),                  # 2^31 keys
+    (dict(pg=pages(width=(1 << 28) + 1, stride=1 << 29), kc=view(0x300000, (40, 2, 1, 64)), vc=view(0x500000, (40, 2, 1, 64))), ARG),
     (dict(pg=pages(stride=9)), ARG), (dict(pg=pages(stride=-10)), ARG),
     (dict(pg=pages(table=0)), ARG), (dict(pg=pages(lens=0)), ARG),
     (dict(pg=pages(starts=0)), ARG),                                       # 12 tokens, 4 sequences

@@ -18,9 +18,10 @@ def test_a_serving_step_in_a_captured_graph(new):
     batch, h, hk, d, page, width = 3, 8, 2, 64, 16, 120
     gen = torch.Generator(device="cuda").manual_seed(5)
     tokens = batch * new
-    x = torch.empty((tokens, (h + 2 * hk) * d), dtype=torch.float16, device="cuda")
+    # (defined values from the first call on: what it writes stays in the cache)
+    x = torch.randn((tokens, (h + 2 * hk) * d), generator=gen, device="cuda").half()
     q, k, v = (t.unflatten(1, (-1, d)) for t in x.split([h * d, hk * d, hk * d], 1))
-    dx, dy, dk_out = torch.zeros_like(x), torch.empty((tokens, h, d), dtype=torch.float16, device="cuda"), None
+    dx, dy = torch.zeros_like(x), torch.randn((tokens, h, d), generator=gen, device="cuda").half()
     dq, dk, _ = (t.unflatten(1, (-1, d)) for t in dx.split([h * d, hk * d, hk * d], 1))
     w = torch.ones(d, dtype=torch.float32, device="cuda")
     freqs = torch.logspace(0, -4, d // 2, device="cuda")
@@ -29,7 +30,7 @@ def test_a_serving_step_in_a_captured_graph(new):
     starts = None if new == 1 else torch.arange(0, tokens + 1, new, dtype=torch.int32, device="cuda")
     kc, vc = (torch.randn((batch * width, hk, page, d), generator=gen, device="cuda").half() for _ in range(2))
     qo, ko = torch.empty((tokens, h, d), dtype=torch.float16, device="cuda"), torch.empty((tokens, hk, d), dtype=torch.float16, device="cuda")
-    dk_out = torch.empty_like(ko)
+    dk_out = torch.randn((tokens, hk, d), generator=gen, device="cuda").half()
     o, lse = torch.empty_like(qo), torch.empty((tokens, h), device="cuda")
     dwq, dwk = torch.empty_like(w), torch.empty_like(w)
 

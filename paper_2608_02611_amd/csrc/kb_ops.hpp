@@ -234,14 +234,21 @@ struct PagedParams {
     int parts;    // many rows: parts of the keys
 };
 
-// Query rows (query, head of the group) that a sequence has on average up to
-// which a work-group takes 16, or 32, at a time and its waves share the keys.
-constexpr int kFewRows = 32;
 constexpr int kPagedTile = 64;  // keys of a unit of work, 16 a wave
-constexpr int kPagedWhole = 512;  // sequences of no more keys are not split
 
 inline int64_t paged_keys(const PagedParams& p) { return (int64_t)p.width * p.page; }
-inline bool few_rows(const PagedParams& p) { return (int64_t)p.tokens * p.group <= (int64_t)kFewRows * p.batch; }
+// Query rows (queries x heads of the group) of a sequence on average up to which a
+// work-group takes 16, or 32, of them at a time and its waves share the keys; more go
+// in blocks of 128 with the keys in LDS.  32 sequences of up to 4000 keys, 4 heads a
+// key head, dim 128, few / many: bf16 20 rows 53 / 68 us, 32 56 / 65, 48 72 / 72, 64 74 /
+// 80, but 60 prompts of up to 32 tokens 22 / 18 and 200 of them 61 / 36; f32, whose
+// products take eight times as long, 48 rows 171 / 470, 128 421 / 559 (dim 64: 135 / 265).
+inline bool few_rows(const PagedParams& p) {
+    return (int64_t)p.tokens * p.group <= (int64_t)(p.f32 ? 128 : 32) * p.batch;
+}
+// Blocks of 32 rows where there are more than 16, but not of 128 binary32 elements,
+// whose registers do not hold so many (20 rows on the same sequences: 129 us, 172
+// with blocks of 32).
 inline int few_block(const PagedParams& p) {
     return (int64_t)p.tokens * p.group <= (int64_t)16 * p.batch || (p.f32 && p.dim > 64) ? 16 : 32;
 }
@@ -262,9 +269,17 @@ struct PagedHeader {
     int32_t valid, rows, pad;
 };
 inline int paged_dim(const PagedParams& p) { return p.dim <= 64 ? 64 : 128; }
+// Sequences of so few keys are not split, which saves the second kernel (8 key heads,
+// single tokens, whole / split: bf16 1000 keys of 1, 8, 64 sequences 15.0 / 15.8, 16.2 /
+// 18.4, 54 / 56 us, 2000 keys 23 / 15, 25 / 24, 98 / 100; f32 2000 keys of one 42 / 15.8, 700
+// 20.6 / 15.5).
+inline bool paged_whole(const PagedParams& p) { return paged_keys(p) <= (p.f32 ? 512 : 1024); }
+// Work-groups: two a CU (64 sequences of up to 8191 keys, dim 128, bf16: 145 us, 152 with
+// three and 147 with one), four for 16 rows of up to 64 elements (dim 64: 84 us, 89 with
+// two; blocks of 32 rows 39, 33 with two).
 inline int paged_workers(const PagedParams& p) {
     const int64_t most = p.dim <= 64 && few_block(p) == 16 ? 1024 : 512;
-    const int64_t tiles = paged_keys(p) <= kPagedWhole ? 1 : (paged_keys(p) + kPagedTile - 1) / kPagedTile;
+    const int64_t tiles = paged_whole(p) ? 1 : (paged_keys(p) + kPagedTile - 1) / kPagedTile;
     const int64_t pairs = paged_blocks(p, few_block(p)) * p.kv_heads;
     return (int)(pairs >= most || pairs * tiles >= most ? most : pairs * tiles);
 }
@@ -284,7 +299,7 @@ inline int paged_parts(const PagedParams& p) {
 }
 inline int64_t paged_floats(const PagedParams& p) {
     if (few_rows(p))
-        return paged_keys(p) <= kPagedWhole
+        return paged_whole(p)
                    ? 0
                    : (int64_t)paged_headers(p) * 8 + (int64_t)paged_workers(p) * 2 * few_block(p) * (paged_dim(p) + 4);
     const int parts = paged_parts(p);

@@ -715,7 +715,7 @@ int kb_attn_paged(const kb_tensor* q, const kb_tensor* k_cache, const kb_tensor*
     p.lse = lse;
     p.ws = (float*)workspace;
     p.workers = paged_workers(p);
-    p.pairs = paged_keys(p) <= kPagedWhole;
+    p.pairs = paged_whole(p);
     p.headers = paged_headers(p);
     p.by_pair = paged_by_pair(p);
     p.small = paged_small(p);

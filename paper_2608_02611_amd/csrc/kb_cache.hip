@@ -3,8 +3,12 @@
 // lens[b] - end + t, in page table[b][place / page] at place % page.
 //
 // It moves bytes, each read and written once.  A wave has one token: its rows are
-// on their way while it looks for the token's page (a search of the starts, the
-// sequence's length and the table, one after the other).
+// on their way while it looks for the token's page.  Latency is what that is bound by:
+// up to 64 sequences' starts and lengths are read at once, one a lane, and then the
+// table (8 prompts of up to 8191 tokens, 8 heads of 128, f16: 44 us, 4.9 TB/s, where a
+// copy moves 4.8; with a search of the starts, the length and the table one after the
+// other 49.5, which larger batches still have: 100 prompts of up to 1000, 59 us, 4.6
+// TB/s).  64 single tokens, a call's own time, 8 us, of which the kernel has 3.5.
 #include "kb_paged.hpp"
 
 namespace kb {
@@ -84,7 +88,8 @@ template <typename B, int V>
 hipError_t write(const PagedParams& p, hipStream_t stream) {
     const int64_t groups = ((int64_t)p.tokens + kWaves - 1) / kWaves;
     const dim3 grid((unsigned)(groups < 16384 ? groups : 16384));
-    // tokens of a vector a lane need fewer registers, and latency is what bounds them
+    // tokens of a vector a lane: 52 registers instead of 98 (one key head, 8 prompts of up
+    // to 8191 tokens: 10.5 us, 17 with four vectors' registers)
     if (2 * (int64_t)p.kv_heads * (p.dim / V) <= 64) cache_write_kernel<B, V, 1><<<grid, kThreads, 0, stream>>>(p);
     else cache_write_kernel<B, V, 4><<<grid, kThreads, 0, stream>>>(p);
     return hipGetLastError();

@@ -703,7 +703,9 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
 template <int DT, int DP, int NB>
 hipError_t few(const PagedParams& p, hipStream_t stream) {
     const dim3 grid((unsigned)p.workers);
-    if (p.whole && p.page % 16 == 0) paged_few_kernel<DT, DP, NB, true><<<grid, kThreads, 0, stream>>>(p);
+    // (rows of a page that lie apart: the bounds of a descriptor tell them from each other)
+    const bool apart = p.cache[0].sl >= p.dim && p.cache[1].sl >= p.dim;
+    if (p.whole && apart && p.page % 16 == 0) paged_few_kernel<DT, DP, NB, true><<<grid, kThreads, 0, stream>>>(p);
     else paged_few_kernel<DT, DP, NB, false><<<grid, kThreads, 0, stream>>>(p);
     if (!p.pairs) {
         const int64_t most = (p.starts != nullptr ? (int64_t)p.tokens : 1) * p.group;
@@ -759,26 +761,30 @@ struct PagedFiller {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         T* to = tile + wave * L::KB;
         const uint64_t address = (uint64_t)(base + row_offset(c, at.page, at.in_page));
-        const auto from = [&](int row) { return background((const void*)readlane_u64(address, row)); };
-        if (at.present == ~(uint64_t)0) {
+        // (the lanes are asked while all of them are there: the one that knows a row may
+        // have no chunk of its own to send for)
+        if (at.present == ~(uint64_t)0 && p.page % kKeys == 0) {  // all of the tile in one page
+            const auto from = background((const void*)readlane_u64(address, 0));
+            const int row = (int)c.sl * (int)sizeof(T);  // (kKeys of them are within 2^31 bytes)
             if (!in) return;  // (zeros from the beginning)
-            if (p.page % kKeys == 0) {  // all of the tile in one page
-                const auto whole = from(0);
-                const int row = (int)c.sl * (int)sizeof(T);  // (kKeys of them are within 2^31 bytes)
 #pragma unroll
-                for (int k = 0; k < STEPS; ++k)
-                    send<16>(whole, offset, (k * STEP + wave * L::KB_ROWS) * row, to + k * (STEP / L::KB_ROWS * L::KB));
-            } else {
+            for (int k = 0; k < STEPS; ++k)
+                send<16>(from, offset, (k * STEP + wave * L::KB_ROWS) * row, to + k * (STEP / L::KB_ROWS * L::KB));
+        } else if (at.present == ~(uint64_t)0) {
+            uint64_t from[STEPS];
 #pragma unroll
-                for (int k = 0; k < STEPS; ++k)
-                    send<16>(from(k * STEP + wave * L::KB_ROWS), offset, 0, to + k * (STEP / L::KB_ROWS * L::KB));
-            }
+            for (int k = 0; k < STEPS; ++k) from[k] = readlane_u64(address, k * STEP + wave * L::KB_ROWS);
+            if (!in) return;
+#pragma unroll
+            for (int k = 0; k < STEPS; ++k)
+                send<16>(background((const void*)from[k]), offset, 0, to + k * (STEP / L::KB_ROWS * L::KB));
         } else {
 #pragma unroll 1
             for (int k = 0; k < STEPS; ++k) {
                 const int row = k * STEP + wave * L::KB_ROWS;  // the wave's first; if it is not there, none is
+                const uint64_t from = readlane_u64(address, row);
                 if (in && (at.present >> (row + lane / SLOTS) & 1)) {
-                    send<16>(from(row), offset, 0, to);
+                    send<16>(background((const void*)from), offset, 0, to);
                 } else {
                     const u32v4 zero = {0, 0, 0, 0};
                     *(u32v4*)(to + lane * L::VEC) = zero;

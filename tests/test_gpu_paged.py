@@ -122,6 +122,37 @@ def test_write_to_both_halves_of_one_buffer():
 # ---------------------------------------------------------------- attention ---
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("step", [0, 8, 32])
+@pytest.mark.parametrize("seqs", [FEW, MANY])
+def test_rows_that_share_memory(dtype, dim, step, seqs):
+    """Keys and values that are windows of one another, or one row for all (strides less than a row, also 0), heads that
+    are one: the bits of copies of them."""
+    b = Batch(seqs, 16, 4, 2, dim, dtype, "hnd")
+    n = b.k_cache.shape[0]
+    buf = normal((n * 16 * max(step, 1) + dim,), b.q.dtype, 3)
+    k = buf.as_strided((n, 2, 16, dim), (16 * step, 0, step, 1))
+    v = buf.flip(0).as_strided((n, 2, 16, dim), (16 * step, 0, step, 1))
+    b.k_cache, b.v_cache = k.contiguous(), v.contiguous()
+    want = attend(b)
+    b.k_cache, b.v_cache = k, v
+    got = attend(b)
+    u, terms = U[b.q.dtype], 2 * max(x for _, x in seqs) * E
+    # the same sums in other steps, as reordered() and check() have them
+    top = dim ** 0.5 * float(b.q.abs().max() * buf.abs().max())  # no score is larger, nor its magnitudes' sum
+    assert float((got[0].double() - want[0].double()).abs().max()) <= 2 * (2 * u + terms) * float(buf.abs().max())
+    off = 2 * ((dim + 16) * E * top + terms + 4 * E * (1 + float(want[1].abs().max())))
+    assert float((got[1] - want[1]).abs().max()) <= off
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("heads,kv", [(40, 1), (200, 2)])
+def test_single_tokens_of_many_heads(dtype, heads, kv):
+    """More query heads a key head than the blocks of few rows take, without starts."""
+    run(Batch([(1, 90), (1, 1), (1, 700)], 16, heads, kv, 64, dtype, one=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("layout", ["nhd", "hnd"])
 @pytest.mark.parametrize("page", [1, 5, 8, 16, 24, 64, 100])
 @pytest.mark.parametrize("seqs", [FEW, MANY])

@@ -733,8 +733,8 @@ struct TilePages {
     int page, in_page;
     uint64_t present;
 };
-// The table by buffer loads, for the reason that tiles are filled by them; past its
-// end they give 0, which place_in_table's caller does not use.
+// The table by buffer loads, for the reason that tiles are filled by them.  Past its
+// end they give 0; no key is there, and none is taken from that page.
 __device__ __forceinline__ int page_in_table(const PagedParams& p, __amdgpu_buffer_rsrc_t table, int key) {
     return (int)__builtin_amdgcn_raw_buffer_load_b32(table, page_of(p, key) * 4, 0, 0);
 }

@@ -137,8 +137,7 @@ __device__ __forceinline__ float row_sum(float v, int lanes) {
     return v;
 }
 
-// The token's angles, by all lanes of a wave into its own LDS, and from there
-// those of the lane's unit.
+// The token's angles, by all lanes of a wave into its own LDS.
 __device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, int lane, float (*turns)[kMaxPairs]) {
     const int position = p.positions[token];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -146,15 +145,10 @@ __device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, in
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 }
+// Those of the lane's units.
 template <int V, int E>
-__device__ __forceinline__ void token_turns(const QkParams& p, int64_t token, int lane, float (*turns)[kMaxPairs],
-                                            const int (&pair)[E], const bool (&rotates)[E], float (&c)[E][V],
-                                            float (&s)[E][V]) {
-    const int position = p.positions[token];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    for (int i = lane; i < p.rot / 2; i += 64) turn_of(position, p.freqs[i], &turns[0][i], &turns[1][i]);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+__device__ __forceinline__ void unit_turns(const float (*turns)[kMaxPairs], const int (&pair)[E], const bool (&rotates)[E],
+                                           float (&c)[E][V], float (&s)[E][V]) {
 #pragma unroll
     for (int n = 0; n < E; ++n)
 #pragma unroll
@@ -214,7 +208,10 @@ __global__ void __launch_bounds__(kThreads) qk_forward_kernel(QkParams p, int la
         };
         fetch(from);
         float c[E][V], s[E][V];
-        if (p.rot > 0) token_turns<V, E>(p, token, lane, turns[wave], pair, rotates, c, s);
+        if (p.rot > 0) {
+            token_turns(p, token, lane, turns[wave]);
+            unit_turns<V, E>(turns[wave], pair, rotates, c, s);
+        }
         for (int pass = from; pass < to; ++pass) {
             float x[E][2 * V], sum = 0.f;
 #pragma unroll

@@ -130,20 +130,21 @@ struct Step {
     uint32_t k[KC][4], v[4][VW];
     uint32_t seen;  // bit c: key c is there
 
-    // The keys of 16 places, lane c knowing key c's.
+    // The keys of 16 places, lane c knowing key c's.  (WHOLE: load_words.)
+    template <bool WHOLE>
     __device__ __forceinline__ void load(const PagedParams& p, const T* kc, const T* vc, Place w, int lane) {
         const int c = lane & 15, g = lane >> 4;
         const bool have = in_cache(p, w.page);
         seen = (uint32_t)__ballot(have) & 0xFFFFu;
         const T* kr = kc + (have ? row_offset(p.cache[0], w.page, w.at) : 0);
 #pragma unroll
-        for (int n = 0; n < KC; ++n) load_words<DT, 4, false>(kr, (4 * n + g) * KB, p.dim, have, k[n]);
+        for (int n = 0; n < KC; ++n) load_words<DT, 4, WHOLE>(kr, (4 * n + g) * KB, p.dim, have, k[n]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int page = __shfl(w.page, 4 * g + j), at = __shfl(w.at, 4 * g + j);
             const bool in = in_cache(p, page);
             const T* vr = vc + (in ? row_offset(p.cache[1], page, at) : 0);
-            load_words<DT, VW, false>(vr, VB * c, p.dim, in, v[j]);
+            load_words<DT, VW, WHOLE>(vr, VB * c, p.dim, in, v[j]);
         }
     }
     // The same where the 16 keys lie in one page: kr, vr: row 0 of them, of which
@@ -191,6 +192,18 @@ struct Step {
     }
 };
 
+// 16 bits: infinities and NaN as 0.
+template <int DT>
+__device__ __forceinline__ four_t<DT> finite_ones(four_t<DT> v) {
+    typedef uint16_t bits __attribute__((ext_vector_type(4)));
+    constexpr uint16_t kExponent = DT == DT_F16 ? 0x7C00 : 0x7F80;
+    bits u = __builtin_bit_cast(bits, v);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if ((u[k] & kExponent) == kExponent) u[k] = 0;
+    return __builtin_bit_cast(four_t<DT>, u);
+}
+
 // Elements of a row of K or Q as an operand of their product.
 template <int DT>
 __device__ __forceinline__ f32x4 mma_scores(const uint32_t (&a)[4], const uint32_t (&b)[4], f32x4 c) {
@@ -203,16 +216,21 @@ __device__ __forceinline__ f32x4 mma_scores(const uint32_t (&a)[4], const uint32
 // exp(scale (s - m)), F16's 2^kBelow of that so that small ones keep their bits, m a
 // score that follows the maximum when a term would pass 2^kSlack; l: their sum over
 // the lane's keys.
+// Where the sums of term times value end up large (kLarge), the pair is computed once
+// more, CAREFUL: m is the maximum, and terms go into these sums times 2^-shift.  In 16
+// bits an infinite value then counts in the product with a term's first part alone: its
+// second part is 0, or negative where the first one was rounded up, which would make a
+// NaN of the infinity.
 template <int NB>
 struct Rows {
     float m[NB], l[NB];
 };
 
-template <int DT, int DP, int NB>
+template <int DT, int DP, int NB, bool CAREFUL>
 __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>& st,
                                              const uint32_t (&q)[NB][Step<DT, DP>::KC][4],
                                              const Step<DT, DP>& in, float to_log2, const int (&lim)[NB], int key0,
-                                             int every, int lane) {
+                                             int every, int lane, int shift = 0) {
     using T = storage_t<DT>;
     using S = Step<DT, DP>;
     const int g = lane >> 4;
@@ -234,7 +252,8 @@ __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>
     for (int b = 0; b < NB; ++b) {
         float top = __builtin_elementwise_maximum(__builtin_elementwise_maximum(s[b][0], s[b][1]),
                                                   __builtin_elementwise_maximum(s[b][2], s[b][3]));
-        const auto passes = [&] { return st.m[b] == -INFINITY ? top > -INFINITY : (top - st.m[b]) * to_log2 > kSlack<DT>; };
+        constexpr float kMost = CAREFUL ? 0.f : kSlack<DT>;
+        const auto passes = [&] { return st.m[b] == -INFINITY ? top > -INFINITY : (top - st.m[b]) * to_log2 > kMost; };
         if (__any(passes())) {
             // a NaN makes the row's results NaN whatever m is
             top = fmaxf(top, __shfl_xor(top, 16));
@@ -250,8 +269,9 @@ __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>
         const float ref = st.m[b] == -INFINITY ? 0.f : st.m[b];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float t = __builtin_amdgcn_exp2f(fmaf(s[b][r] - ref, to_log2, kBelow<DT>));
+            float t = __builtin_amdgcn_exp2f(fmaf(s[b][r] - ref, to_log2, kBelow<DT>));
             st.l[b] += t;
+            if (CAREFUL && kScaled<DT>) t = ldexpf(t, -shift);
             // 16 bits: the term in two parts, so that what it is rounded by is not lost
             hi[b][r] = (T)t;
             if constexpr (DT != DT_F32) lo[b][r] = (T)(t - (float)hi[b][r]);
@@ -263,7 +283,7 @@ __device__ __forceinline__ void step_forward(f32x4 (&acc)[NB][DP / 16], Rows<NB>
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             acc[b][e] = mma4(a, hi[b], acc[b][e]);
-            if constexpr (DT != DT_F32) acc[b][e] = mma4(a, lo[b], acc[b][e]);
+            if constexpr (DT != DT_F32) acc[b][e] = mma4(CAREFUL ? finite_ones<DT>(a) : a, lo[b], acc[b][e]);
         }
     }
 }
@@ -294,6 +314,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
     constexpr int ROWS = 16 * NB, PITCH = DP + 4;
     __shared__ __align__(16) float sums[kWaves][ROWS][PITCH];
     __shared__ float stat_m[kWaves][ROWS], stat_l[kWaves][ROWS];
+    __shared__ int wave_large[kWaves];
     __shared__ int64_t wave_units[kWaves];
     __shared__ int64_t start_units;
     __shared__ int start_seq;
@@ -456,9 +477,10 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
         const int rows = (int)min((int64_t)ROWS, (int64_t)tok.n * p.group - (int64_t)block * ROWS);
 
         // A product takes every key to every row, with 0 where a row does not see it,
-        // and 0 times NaN is NaN.  So rows of several queries whose sums end up with
-        // such a value are computed once more, query by query, each with its own keys
-        // alone (only >= 0).
+        // and 0 times NaN is NaN.  So where the sums are computed once more, rows of
+        // several queries are so query by query, each with its own keys alone (only >= 0).
+        const bool by_query = p.causal && row_first < row_last;
+        bool careful = false;
         int only = -1;
         for (;;) {
             const int key_end = __builtin_amdgcn_readfirstlane(
@@ -477,9 +499,16 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
             const T* kc = (const T*)p.cache[0].p + h * p.cache[0].sh;
             const T* vc = (const T*)p.cache[1].p + h * p.cache[1].sh;
             const int key0 = tile * kKeys + 16 * wave;
+            const int shift = careful ? large_shift<DT>(klen) : 0;
             // one step is computed while the next one's keys are on their way
             Step<DT, DP> a, b;
-            if constexpr (ONE_PAGE) {
+            if (careful) {
+#pragma unroll 1
+                for (int key = key0; key < key_end; key += kKeys) {
+                    a.template load<ONE_PAGE>(p, kc, vc, place_of(p, table, key + c, key_end), lane);
+                    step_forward<DT, DP, NB, true>(acc, st, q, a, to_log2, lim, key, every, lane, shift);
+                }
+            } else if constexpr (ONE_PAGE) {
                 // the pages of 64 steps, one a lane
                 int pages = 0;
                 const auto load = [&](Step<DT, DP>& to, int n) {
@@ -499,45 +528,36 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
 #pragma unroll 1
                 for (int n = 0, key = key0; key < key_end; n += 2, key += 2 * kKeys) {  // (a step without a key adds nothing)
                     load(b, n + 1);
-                    step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
+                    step_forward<DT, DP, NB, false>(acc, st, q, a, to_log2, lim, key, every, lane);
                     load(a, n + 2);
-                    step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
+                    step_forward<DT, DP, NB, false>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
                 }
             } else {
                 // and the places of the one after that
                 Place w = place_of(p, table, key0 + c, key_end);
                 Place next = place_of(p, table, key0 + kKeys + c, key_end);
-                a.load(p, kc, vc, w, lane);
+                a.template load<false>(p, kc, vc, w, lane);
 #pragma unroll 1
                 for (int key = key0; key < key_end; key += 2 * kKeys) {
                     w = next;
                     next = place_of(p, table, key + 2 * kKeys + c, key_end);
-                    b.load(p, kc, vc, w, lane);
-                    step_forward<DT, DP, NB>(acc, st, q, a, to_log2, lim, key, every, lane);
+                    b.template load<false>(p, kc, vc, w, lane);
+                    step_forward<DT, DP, NB, false>(acc, st, q, a, to_log2, lim, key, every, lane);
                     w = next;
                     next = place_of(p, table, key + 3 * kKeys + c, key_end);
-                    a.load(p, kc, vc, w, lane);
-                    step_forward<DT, DP, NB>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
-                }
-            }
-
-            if (only < 0 && p.causal && row_first < row_last) {
-                float z = 0.f;  // x 0 is 0, or NaN
-#pragma unroll
-                for (int b = 0; b < NB; ++b)
-#pragma unroll
-                    for (int e = 0; e < S::VB; ++e)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) z = fmaf(acc[b][e][r], 0.f, z);
-                if (__syncthreads_or(z != 0.f)) {
-                    only = row_first;
-                    continue;
+                    a.template load<false>(p, kc, vc, w, lane);
+                    step_forward<DT, DP, NB, false>(acc, st, q, b, to_log2, lim, key + kKeys, every, lane);
                 }
             }
 
             // the waves' sums, joined through LDS
+            float largest = 0.f;  // (or NaN)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
+#pragma unroll
+                for (int e = 0; e < S::VB; ++e)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) largest = __builtin_elementwise_maximum(largest, fabsf(acc[b][e][r]));
                 st.l[b] += __shfl_xor(st.l[b], 16);
                 st.l[b] += __shfl_xor(st.l[b], 32);
                 if (g == 0) {
@@ -551,7 +571,15 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
                         *(f32x4*)&sums[wave][b * 16 + c][S::VB * (4 * g + r) + e] =
                             f32x4{acc[b][e][r], acc[b][e + 1][r], acc[b][e + 2][r], acc[b][e + 3][r]};
             }
+            const bool sums_are_large = __any(!(largest <= kLarge));
+            if (lane == 0) wave_large[wave] = sums_are_large;
             __syncthreads();
+            if (!careful && (wave_large[0] | wave_large[1] | wave_large[2] | wave_large[3])) {
+                careful = true;
+                only = by_query ? row_first : -1;
+                __syncthreads();  // every wave has read that
+                continue;
+            }
             const bool begun = tile == 0, ended = tile_end == n_tiles;
             float* part = begun && ended ? nullptr : slot(me, begun ? 1 : 0);
             for (int n = threadIdx.x; n < rows * (DP / 4); n += kThreads) {
@@ -575,12 +603,12 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
                 }
                 if (part != nullptr) {
                     *(f32x4*)(part + r * PITCH + d) = o;
-                    if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, 0.f, 0.f};
+                    if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, (float)shift, 0.f};
                     continue;
                 }
                 const int64_t t = tok.first + i;
                 const bool some = l != 0.f;
-                const float f = 1.f / l;
+                const float f = kScaled<DT> ? ldexpf(1.f / l, shift) : 1.f / l;
                 store_quad<DT>((T*)p.o.p + t * p.o.st + hq * p.o.sh, d, p.dim, some ? o[0] * f : 0.f, some ? o[1] * f : 0.f,
                                some ? o[2] * f : 0.f, some ? o[3] * f : 0.f);
                 if (d == 0 && p.lse != nullptr)
@@ -610,7 +638,7 @@ template <int DT, int DP, int NB, int WAVES>
 __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParams p) {
     using T = storage_t<DT>;
     constexpr int ROWS = 16 * NB, PITCH = DP + 4, E = DP / 64, AHEAD = 8, EACH = kJoinThreads / 64 / WAVES;
-    __shared__ float sums[WAVES][DP], stat_m[WAVES], stat_l[WAVES];
+    __shared__ float sums[WAVES][DP], stat_m[WAVES], stat_l[WAVES], stat_shift[WAVES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WAVES;
     const int r = (int)blockIdx.y * EACH + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WAVES;
     if (p.by_pair) {
@@ -627,29 +655,36 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
     const float* base = p.ws + (int64_t)p.headers * (sizeof(PagedHeader) / sizeof(float)) + r * PITCH;
     const int parts = h.last - me + 1;
     const auto part = [&](int k) { return base + ((int64_t)(me + k) * 2 + (k == 0)) * ROWS * PITCH; };
-    float m = -INFINITY, l = 0.f, o[E];
+    // o is held times 2^-shift, the largest of the parts' shifts (0, but for large sums)
+    float m = -INFINITY, l = 0.f, shift = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     for (int k0 = wave; k0 < parts; k0 += WAVES * AHEAD) {
-        float x[AHEAD][E], xm[AHEAD], xl[AHEAD];
+        float x[AHEAD][E], xm[AHEAD], xl[AHEAD], xs[AHEAD];
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
             const int k = k0 + n * WAVES;
             xm[n] = -INFINITY;
+            xs[n] = 0.f;
             if (k < parts) {
                 const float* at = part(k);
                 xm[n] = at[DP];
                 xl[n] = at[DP + 1];
+                if (kScaled<DT>) xs[n] = at[DP + 2];
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[n][e] = at[lane * E + e];
             }
         }
-        float now = m;
+        float now = m, most = shift;
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n) now = fmaxf(now, xm[n]);
+        for (int n = 0; n < AHEAD; ++n) {
+            now = fmaxf(now, xm[n]);
+            most = fmaxf(most, xs[n]);
+        }
         const float ref = now == -INFINITY ? 0.f : now;
         float f = __builtin_amdgcn_exp2f((m - ref) * to_log2);
         l *= f;
+        if (kScaled<DT>) f = ldexpf(f, (int)(shift - most));
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] *= f;
 #pragma unroll
@@ -657,17 +692,21 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
             if (k0 + n * WAVES >= parts) continue;
             f = __builtin_amdgcn_exp2f((xm[n] - ref) * to_log2);
             l = fmaf(f, xl[n], l);
+            if (kScaled<DT>) f = ldexpf(f, (int)(xs[n] - most));
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = fmaf(f, x[n][e], o[e]);
         }
         m = now;
+        shift = most;
     }
     const uint32_t row = (uint32_t)h.block * ROWS + r;
     const int i = (int)(row / (uint32_t)p.group), hq = h.head * p.group + (int)(row - (uint32_t)i * p.group);
     const int64_t t = tokens_of(p, h.seq).first + i;
     const auto write = [&](int d, float x) {
         const bool some = l != 0.f;
-        if (d < p.dim) ((T*)p.o.p)[t * p.o.st + hq * p.o.sh + d] = (T)(some ? x / l : 0.f);
+        if (kScaled<DT>) x = ldexpf(x / l, (int)shift);
+        else x /= l;
+        if (d < p.dim) ((T*)p.o.p)[t * p.o.st + hq * p.o.sh + d] = (T)(some ? x : 0.f);
         if (d == 0 && p.lse != nullptr)
             p.lse[t * p.heads + hq] = some ? fmaf(m, p.scale, kLn2 * (__builtin_amdgcn_logf(l) - kBelow<DT>)) : -INFINITY;
     };
@@ -680,13 +719,18 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
         if (lane == 0) {
             stat_m[wave] = m;
             stat_l[wave] = l;
+            stat_shift[wave] = shift;
         }
         __syncthreads();
         const int d = threadIdx.x;
         if (d >= p.dim) return;
         m = stat_m[0];
+        shift = stat_shift[0];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, stat_m[w]);
+        for (int w = 1; w < WAVES; ++w) {
+            m = fmaxf(m, stat_m[w]);
+            shift = fmaxf(shift, stat_shift[w]);
+        }
         const float ref = m == -INFINITY ? 0.f : m;
         float x = 0.f;
         l = 0.f;
@@ -694,7 +738,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
         for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f((stat_m[w] - ref) * to_log2);
             l = fmaf(f, stat_l[w], l);
-            x = fmaf(f, sums[w][d], x);
+            x = fmaf(kScaled<DT> ? ldexpf(f, (int)(stat_shift[w] - shift)) : f, sums[w][d], x);
         }
         write(d, x);
     }

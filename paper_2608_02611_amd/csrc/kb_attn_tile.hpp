@@ -20,6 +20,20 @@ template <int DT>
 constexpr float kSlack = DT == DT_F16 ? 6.f : 8.f;
 template <int DT>
 constexpr float kBelow = DT == DT_F16 ? 9.f : 0.f;
+
+// Sums of terms times values: terms of up to 2^kSlack, or many of 1, pass binary32's
+// range with values whose mean does not.  Sums past kLarge are computed once more, with
+// the n keys' terms, relative to their maximum, times 2^-large_shift(n): they come to
+// 1/2 together.  (Of other sums 2^16 can be joined.  F16: 2^30 terms of 2^15 and values
+// of 2^16 stay far inside; there only an infinity or a NaN is past kLarge.)
+constexpr float kLarge = 0x1p110f;
+template <int DT>
+constexpr bool kScaled = DT != DT_F16;
+template <int DT>
+__device__ __forceinline__ int large_shift(int n) {
+    return !kScaled<DT> || n < 2 ? 0 : 33 - __builtin_clz((uint32_t)(n - 1));
+}
+
 struct Softmax {
     float m = -INFINITY, l = 0.f, rounded = 0.f;
     bool low = false;

@@ -939,6 +939,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     const float to_log2 = p.scale * kLog2e;
     f32x16 acc[DP / 32];
     Softmax sm;
+    int shift = 0;
     const auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
@@ -966,21 +967,20 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
             ready = now != ~(uint64_t)0;
             if (ready) break;
             if (wave_any > 0)
-                tile_forward<DT, DP, false, CAREFUL && DT != DT_F32>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+                tile_forward<DT, DP, false, CAREFUL>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0, ~(uint64_t)0, shift);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             if (!ready) next();
             ready = false;
             if (j0 < wave_any)
-                tile_forward<DT, DP, true, CAREFUL, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0, now);
+                tile_forward<DT, DP, true, CAREFUL, true>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0, now, shift);
         }
     };
     pass(std::false_type{});
-    if constexpr (DT == DT_F32) {
-        if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
-    } else if (__syncthreads_or((p.causal && non_finite(acc)) || too_coarse(sm))) {
+    if (__syncthreads_or(too_large(acc) || (DT != DT_F32 && too_coarse(sm)))) {
+        shift = large_shift<DT>(all);
         pass(std::true_type{});
-        if (sm.m > -INFINITY) sm.m = __builtin_amdgcn_fmed3f(fmaf(sm.m, to_log2, -kBelow<DT>), -FLT_MAX, FLT_MAX);
+        if (DT != DT_F32 && sm.m > -INFINITY) sm.m = __builtin_amdgcn_fmed3f(fmaf(sm.m, to_log2, -kBelow<DT>), -FLT_MAX, FLT_MAX);
     }
     if (!live) return;
     const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
@@ -988,12 +988,13 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) paged_many_ker
     if (p.parts > 1) {
         const int64_t dim = (p.dim + 3) / 4 * 4;
         float* to = p.ws + ((t * p.heads + hq) * p.parts + part) * (dim + 4);
-        if (g == 0) *(f32x4*)(to + dim) = f32x4{sm.m, l, rounded, 0.f};
+        if (g == 0) *(f32x4*)(to + dim) = f32x4{sm.m, l, rounded, (float)shift};
         store_part<DP>(to, acc, p.dim, g);
         return;
     }
     const bool some = l != 0.f;  // NaN too: it goes on to o
-    store_column<DT, DP>((T*)p.o.p + t * p.o.st + hq * p.o.sh, acc, 1.f / (DT == DT_F32 ? l : rounded), some, p.dim, g);
+    const float f = DT == DT_F32 ? ldexpf(1.f / l, shift) : 1.f / rounded;
+    store_column<DT, DP>((T*)p.o.p + t * p.o.st + hq * p.o.sh, acc, f, some, p.dim, g);
     if (g == 0 && p.lse != nullptr)
         p.lse[t * p.heads + hq] = some ? fmaf(sm.m, unit_natural<DT>(p.scale), kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
 }
@@ -1012,21 +1013,25 @@ __global__ void __launch_bounds__(kThreads) paged_many_join_kernel(PagedParams p
     if (p.starts != nullptr && (t < p.starts[0] || t >= p.starts[p.batch])) return;  // no sequence's
     const int64_t dim = (p.dim + 3) / 4 * 4, stride = dim + 4;
     const float* in = p.ws + row * p.parts * stride;
-    float m = -INFINITY;
-    for (int s = 0; s < p.parts; ++s) m = fmaxf(m, in[s * stride + dim]);
-    const float shift = m == -INFINITY ? 0.f : m;
+    float m = -INFINITY, most = 0.f;  // (most: the largest of the parts' shifts)
+    for (int s = 0; s < p.parts; ++s) {
+        m = fmaxf(m, in[s * stride + dim]);
+        if (kScaled<DT>) most = fmaxf(most, in[s * stride + dim + 3]);
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f, rounded = 0.f;
     for (int s = 0; s < p.parts; ++s) {
         const f32x4 stat = *(const f32x4*)(in + s * stride + dim), x = *(const f32x4*)(in + s * stride + d);
-        const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * unit_log2<DT>(p.scale));
+        const float w = __builtin_amdgcn_exp2f((stat[0] - ref) * unit_log2<DT>(p.scale));
+        const float scaled = kScaled<DT> ? ldexpf(w, (int)(stat[3] - most)) : w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(scaled, x[e], acc[e]);
         l = fmaf(w, stat[1], l);
-        rounded = fmaf(w, stat[2], rounded);
+        rounded = fmaf(scaled, stat[2], rounded);
     }
     const bool some = l != 0.f;
-    const float f = some ? 1.f / (DT == DT_F32 ? l : rounded) : 0.f;
+    const float f = !some ? 0.f : DT == DT_F32 ? ldexpf(1.f / l, (int)most) : 1.f / rounded;
     store_quad<DT>((T*)p.o.p + t * p.o.st + hq * p.o.sh, d, p.dim, some ? acc[0] * f : 0.f, some ? acc[1] * f : 0.f,
                    some ? acc[2] * f : 0.f, some ? acc[3] * f : 0.f);
     if (d == 0 && p.lse != nullptr)

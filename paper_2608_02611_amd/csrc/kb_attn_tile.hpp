@@ -34,6 +34,16 @@ __device__ __forceinline__ int large_shift(int n) {
     return !kScaled<DT> || n < 2 ? 0 : 33 - __builtin_clz((uint32_t)(n - 1));
 }
 
+template <int N>
+__device__ __forceinline__ bool too_large(const f32x16 (&acc)[N]) {
+    float largest = 0.f;  // (or NaN)
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) largest = __builtin_elementwise_maximum(largest, fabsf(acc[k][r]));
+    return !(largest <= kLarge);
+}
+
 struct Softmax {
     float m = -INFINITY, l = 0.f, rounded = 0.f;
     bool low = false;
@@ -76,12 +86,12 @@ __device__ __forceinline__ float add_terms(frag_t<DT> f, float l) {
 // The keys of one tile for 32 query rows of a wave.  PART: some (row, key)
 // pairs are not seen; the lane's row sees the tile's keys below hi, and with GAPS
 // only those whose bit is set in `present` (the values of the others are zeros).
-// CAREFUL: m is the largest score, as in 32 bits, and mma_seen for rows that are
-// not seen.
+// CAREFUL: m is the largest score, as in 32 bits, terms go into the product (and
+// their rounded sum) times 2^-shift, and mma_seen for rows that are not seen.
 template <int DT, int DP, bool PART, bool CAREFUL, bool GAPS = false>
 __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm, const frag_t<DT> (&qf)[DP / 16],
                                              const storage_t<DT>* kt, const storage_t<DT>* vt, const Reader<DT, DP>& rd,
-                                             float to_log2, int hi, uint64_t present = ~(uint64_t)0) {
+                                             float to_log2, int hi, uint64_t present = ~(uint64_t)0, int shift = 0) {
     constexpr bool SCORE = DT == DT_F32 || CAREFUL;  // m is a score
     const int g = rd.lane >> 5;
     float &m = sm.m, &l = sm.l;
@@ -185,7 +195,10 @@ __device__ __forceinline__ void tile_forward(f32x16 (&acc)[DP / 32], Softmax& sm
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) l += s[t][r] = term(s[t][r]);
+            for (int r = 0; r < 16; ++r) {
+                l += s[t][r] = term(s[t][r]);
+                if (CAREFUL && kScaled<DT>) s[t][r] = ldexpf(s[t][r], -shift);
+            }
             const frag_t<DT> b[2] = {narrow<DT>(s[t], 0), narrow<DT>(s[t], 1)};
             if (DT != DT_F32) sm.rounded = add_terms<DT>(b[1], add_terms<DT>(b[0], sm.rounded));
             mma_rows<DT, DP, PART && CAREFUL>(acc, vt, rd, 32 * t, b, 0, hi);

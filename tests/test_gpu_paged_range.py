@@ -19,6 +19,12 @@ FEW = [
     dict(seqs=[(1, 9000), (1, 3), (5, 2000)], heads=4),
     dict(seqs=[(1, 600 + 13 * i) for i in range(40)], heads=8, kv=8, one=True),
 ]
+MANY = [
+    dict(seqs=[(150, 150), (70, 300)]),
+    dict(seqs=[(200, 200), (1, 1), (33, 90), (1, 700)]),
+    dict(seqs=[(20, 1500), (9, 3000)]),                          # in parts
+    dict(seqs=[(130, 2100), (130, 130)], heads=1, kv=1),
+]
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -62,11 +68,18 @@ def large_values(dtype, dim, page, case, causal, signs):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("page", [16, 5])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 16), (128, 5)])
 @pytest.mark.parametrize("case", FEW)
-@pytest.mark.parametrize("causal,signs", [(True, 1), (True, 2), (False, 1)])
+@pytest.mark.parametrize("causal,signs", [(True, 2), (False, 1)])
 def test_large_values_few_rows(dtype, dim, page, case, causal, signs):
+    large_values(dtype, dim, page, case, causal, signs)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64), (96, 5)])
+@pytest.mark.parametrize("case", MANY)
+@pytest.mark.parametrize("causal,signs", [(True, 2), (False, 1)])
+def test_large_values_many_rows(dtype, dim, page, case, causal, signs):
     large_values(dtype, dim, page, case, causal, signs)
 
 
@@ -92,7 +105,7 @@ def test_a_large_value_after_a_smaller_score(dtype, value, page):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("case", FEW[1:3])
+@pytest.mark.parametrize("case", FEW[1:3] + MANY[:3])
 def test_large_values_leave_other_heads_alone(dtype, case):
     """A key head of ordinary values beside one of large values keeps its bits."""
     b = batch(dtype, 64, 16, **case)
@@ -137,4 +150,12 @@ def infinite(dtype, page, case, causal):
 @pytest.mark.parametrize("case", FEW)
 @pytest.mark.parametrize("causal", [True, False])
 def test_infinite_values_few_rows(dtype, page, case, causal):
+    infinite(dtype, page, case, causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("page", [16, 5])
+@pytest.mark.parametrize("case", MANY)
+@pytest.mark.parametrize("causal", [True, False])
+def test_infinite_values_many_rows(dtype, page, case, causal):
     infinite(dtype, page, case, causal)

@@ -722,7 +722,9 @@ typedef struct kb_attn_opts {
  *   o_i = sum_j exp(s_j - lse_i) v_j.
  * A query that sees no key (or only scores of -infinity), and a query of the
  * padding, has o = 0 and lse = -infinity.  A NaN or infinity reaches just the
- * queries that see it.  q, k, v, o: one dtype, F32, F16 or BF16.  lse: device
+ * queries that see it: an infinity of v as itself, where its term is not 0 (terms
+ * below 2^-90 of the row's largest, F16 2^-34, may be); finite values of v give a
+ * finite o, their mean, whatever their size.  q, k, v, o: one dtype, F32, F16 or BF16.  lse: device
  * float[batch][heads][len_q], never NULL.  With a 16-bit dtype the softmax
  * terms are rounded to it before their product with v and the sum that this is
  * divided by, each by at most 2^-11 (F16) or 2^-8 (BF16) of itself, or, F16,

@@ -79,6 +79,7 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
     const float to_log2 = p.scale * kLog2e;
     f32x16 acc[DP / 32];
     Softmax sm;
+    int shift = 0;
     const auto pass = [&](auto careful) {
         constexpr bool CAREFUL = decltype(careful)::value;
 #pragma unroll
@@ -95,31 +96,32 @@ __global__ void __launch_bounds__(kThreads, DT == DT_F32 ? 1 : 2) attn_forward_k
         for (; j0 + kKeys <= min(block_all, end); j0 += kKeys, buf ^= 1) {
             next();
             if (wave_any > 0)
-                tile_forward<DT, DP, false, CAREFUL && DT != DT_F32>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0);
+                tile_forward<DT, DP, false, CAREFUL>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, 0, ~(uint64_t)0, shift);
         }
         for (; j0 < end; j0 += kKeys, buf ^= 1) {
             next();
-            if (j0 < wave_any) tile_forward<DT, DP, true, CAREFUL>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0);
+            if (j0 < wave_any)
+                tile_forward<DT, DP, true, CAREFUL>(acc, sm, qf, kt[buf], vt[buf], rd, to_log2, lim - j0, ~(uint64_t)0, shift);
         }
     };
     pass(std::false_type{});
-    if constexpr (DT == DT_F32) {
-        if (p.causal && __syncthreads_or(non_finite(acc))) pass(std::true_type{});
-    } else if (__syncthreads_or((p.causal && non_finite(acc)) || too_coarse(sm))) {
+    if (__syncthreads_or(too_large(acc) || (DT != DT_F32 && too_coarse(sm)))) {
+        shift = large_shift<DT>(all);
         pass(std::true_type{});
-        if (sm.m > -INFINITY) sm.m = __builtin_amdgcn_fmed3f(fmaf(sm.m, to_log2, -kBelow<DT>), -FLT_MAX, FLT_MAX);
+        if (DT != DT_F32 && sm.m > -INFINITY) sm.m = __builtin_amdgcn_fmed3f(fmaf(sm.m, to_log2, -kBelow<DT>), -FLT_MAX, FLT_MAX);
     }
     if (!exists) return;
     const float l = sm.l + other_half(sm.l), rounded = sm.rounded + other_half(sm.rounded);
     if (p.parts > 1) {
         const int64_t dim = part_dim(p);
         float* to = p.ws + ((((int64_t)at.b * p.kv_heads + at.h) * p.len_q * p.group + row) * p.parts + part) * (dim + 4);
-        if (g == 0) *(f32x4*)(to + dim) = f32x4{live ? sm.m : -INFINITY, live ? l : 0.f, live ? rounded : 0.f, 0.f};
+        if (g == 0) *(f32x4*)(to + dim) = f32x4{live ? sm.m : -INFINITY, live ? l : 0.f, live ? rounded : 0.f, (float)shift};
         store_part<DP>(to, acc, p.dim, g);
         return;
     }
     const bool some = live && l != 0.f;  // NaN too: it goes on to o
-    store_column<DT, DP>((T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl, acc, 1.f / (DT == DT_F32 ? l : rounded), some, p.dim, g);
+    const float f = DT == DT_F32 ? ldexpf(1.f / l, shift) : 1.f / rounded;
+    store_column<DT, DP>((T*)p.o.p + at.b * p.o.sb + hq * p.o.sh + i * p.o.sl, acc, f, some, p.dim, g);
     if (g == 0)
         p.lse[((int64_t)at.b * p.heads + hq) * p.len_q + i] =
             some ? fmaf(sm.m, unit_natural<DT>(p.scale), kLn2 * __builtin_amdgcn_logf(l)) : -INFINITY;
@@ -137,24 +139,28 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnParams p) {
     if (row >= (int64_t)p.batch * p.heads * p.len_q) return;
     const int64_t stride = part_dim(p) + 4;
     const float* in = p.ws + row * p.parts * stride;
-    float m = -INFINITY;
-    for (int s = 0; s < p.parts; ++s) m = fmaxf(m, in[s * stride + stride - 4]);
-    const float shift = m == -INFINITY ? 0.f : m;
+    float m = -INFINITY, most = 0.f;  // (most: the largest of the parts' shifts)
+    for (int s = 0; s < p.parts; ++s) {
+        m = fmaxf(m, in[s * stride + stride - 4]);
+        if (kScaled<DT>) most = fmaxf(most, in[s * stride + stride - 1]);
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f, rounded = 0.f;
     for (int s = 0; s < p.parts; ++s) {
         const f32x4 stat = *(const f32x4*)(in + s * stride + stride - 4), x = *(const f32x4*)(in + s * stride + d);
-        const float w = __builtin_amdgcn_exp2f((stat[0] - shift) * unit_log2<DT>(p.scale));
+        const float w = __builtin_amdgcn_exp2f((stat[0] - ref) * unit_log2<DT>(p.scale));
+        const float scaled = kScaled<DT> ? ldexpf(w, (int)(stat[3] - most)) : w;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, x[e], acc[e]);
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(scaled, x[e], acc[e]);
         l = fmaf(w, stat[1], l);
-        rounded = fmaf(w, stat[2], rounded);
+        rounded = fmaf(scaled, stat[2], rounded);
     }
     const int64_t per_head = (int64_t)p.len_q * p.group;
     const int pair = (int)(row / per_head), in_head = (int)(row % per_head);
     const int b = pair / p.kv_heads, hq = pair % p.kv_heads * p.group + in_head % p.group, i = in_head / p.group;
     const bool some = l != 0.f;
-    const float f = some ? 1.f / (DT == DT_F32 ? l : rounded) : 0.f;
+    const float f = !some ? 0.f : DT == DT_F32 ? ldexpf(1.f / l, (int)most) : 1.f / rounded;
     store_quad<DT>((T*)p.o.p + b * p.o.sb + hq * p.o.sh + i * p.o.sl, d, p.dim, some ? acc[0] * f : 0.f,
                    some ? acc[1] * f : 0.f, some ? acc[2] * f : 0.f, some ? acc[3] * f : 0.f);
     if (d == 0)

@@ -991,9 +991,26 @@ def _dense(t, dtype, shape, name):
     return t.data_ptr()
 
 
-def _tokens(t):
+def _tokens(t, name):
     """A tensor as [tokens][heads][dim] over its last two axes (a view, never a copy)."""
-    return t if t is None or t.dim() == 3 else t.view(-1, *t.shape[-2:])
+    if t is None or t.dim() == 3:
+        return t
+    if t.dim() < 2:
+        raise ValueError("%s must have the shape [..., heads, dim]" % name)
+    tokens, step = 1, 0
+    if t.numel():
+        for size, stride in zip(t.shape[-3::-1], t.stride()[-3::-1]):
+            if size == 1:
+                continue
+            if tokens == 1:
+                step = stride
+            elif stride != step * tokens:
+                raise ValueError("%s: its axes before the heads lie in no one stride (shape %s, strides %s)"
+                                 % (name, tuple(t.shape), t.stride()))
+            tokens *= size
+    else:
+        tokens = t.shape[:-2].numel()
+    return t.as_strided((tokens, *t.shape[-2:]), (step, *t.stride()[-2:]))
 
 
 def _qk_opts(q, eps, positions, freqs, interleaved):
@@ -1007,8 +1024,9 @@ def _qk_opts(q, eps, positions, freqs, interleaved):
 def kb_qk_norm_forward(q, k, wq, wk, eps=1e-6, positions=None, freqs=None, interleaved=False, q_out=None, k_out=None,
                        stream=None):
     """Root mean square norm of each head row of q [..., heads, dim] and k
-    [..., kv_heads, dim] (views of any strides with a contiguous last dimension),
-    weights wq and wk [dim] (None: 1), then the rotation of the first 2 len(freqs)
+    [..., kv_heads, dim] (views with a contiguous last dimension, whose tokens, the
+    axes before the heads, one stride walks: [batch, len, heads, dim] with the heads
+    outside len has to be called a sequence at a time), weights wq and wk [dim] (None: 1), then the rotation of the first 2 len(freqs)
     elements by positions (int32, of q's leading shape) times freqs (float32,
     radians per position; None: no rotation), as pairs (i, i + len(freqs)) or,
     interleaved, (2i, 2i + 1).  Returns (q_out, k_out), made here where not given."""
@@ -1020,10 +1038,10 @@ def kb_qk_norm_forward(q, k, wq, wk, eps=1e-6, positions=None, freqs=None, inter
             if k_out is None:
                 k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
     _one_device(q, k, wq, wk, positions, freqs, q_out, k_out)
-    pq = pack_view(_tokens(q))
-    _check(lib().kb_qk_norm_forward(pq, pack_view(_tokens(k)), pack_view(wq), pack_view(wk),
-                                    _qk_opts(q, eps, positions, freqs, interleaved), pack_view(_tokens(q_out)),
-                                    pack_view(_tokens(k_out)), _stream_handle(stream)))
+    pq = pack_view(_tokens(q, "q"))
+    _check(lib().kb_qk_norm_forward(pq, pack_view(_tokens(k, "k")), pack_view(wq), pack_view(wk),
+                                    _qk_opts(q, eps, positions, freqs, interleaved), pack_view(_tokens(q_out, "q_out")),
+                                    pack_view(_tokens(k_out, "k_out")), _stream_handle(stream)))
     return q_out, k_out
 
 
@@ -1033,8 +1051,8 @@ def kb_qk_norm_backward_workspace_bytes(dim):
 
 def kb_qk_norm_backward(dq_out, dk_out, q, k, wq, wk, eps=1e-6, positions=None, freqs=None, interleaved=False, dq=None,
                         dk=None, dwq=None, dwk=None, workspace=None, stream=None):
-    """Gradients of kb_qk_norm_forward from those of its outputs: (dq, dk, dwq,
-    dwk), made here where not given; dwq and dwk of the weights' dtype (q's
+    """Gradients of kb_qk_norm_forward from those of its outputs, views as there: (dq,
+    dk, dwq, dwk), made here where not given; dwq and dwk of the weights' dtype (q's
     without a weight)."""
     L = lib()
     if dq is None or dk is None or dwq is None or dwk is None or workspace is None:
@@ -1054,10 +1072,11 @@ def kb_qk_norm_backward(dq_out, dk_out, q, k, wq, wk, eps=1e-6, positions=None, 
                 workspace = _scratch(L.kb_qk_norm_backward_workspace_bytes(q.shape[-1]), q.device)
     _one_device(dq_out, dk_out, q, k, wq, wk, positions, freqs, dq, dk, dwq, dwk, workspace)
     ws, nbytes = _extent(workspace)
-    pq = pack_view(_tokens(q))
-    _check(L.kb_qk_norm_backward(pack_view(_tokens(dq_out)), pack_view(_tokens(dk_out)), pq, pack_view(_tokens(k)),
-                                 pack_view(wq), pack_view(wk), _qk_opts(q, eps, positions, freqs, interleaved),
-                                 pack_view(_tokens(dq)), pack_view(_tokens(dk)), pack_view(dwq), pack_view(dwk), ws, nbytes,
+    pq = pack_view(_tokens(q, "q"))
+    _check(L.kb_qk_norm_backward(pack_view(_tokens(dq_out, "dq_out")), pack_view(_tokens(dk_out, "dk_out")), pq,
+                                 pack_view(_tokens(k, "k")), pack_view(wq), pack_view(wk),
+                                 _qk_opts(q, eps, positions, freqs, interleaved), pack_view(_tokens(dq, "dq")),
+                                 pack_view(_tokens(dk, "dk")), pack_view(dwq), pack_view(dwk), ws, nbytes,
                                  _stream_handle(stream)))
     return dq, dk, dwq, dwk
 

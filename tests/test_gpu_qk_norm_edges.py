@@ -1,4 +1,5 @@
-"""Head norms: the views that the calls take."""
+"""Head norms: cosines and sines of the exact angles, and the views that the calls take."""
+import numpy as np
 import pytest
 import torch
 
@@ -12,6 +13,41 @@ pytestmark = pytest.mark.gpu
 @pytest.fixture(scope="module", autouse=True)
 def built():
     ensure_built()
+
+
+def exact_turns(positions, freqs):
+    """cos and sin of positions x freqs, from two products that binary64 holds exactly: of the position's upper 16 bits and
+    of its lower ones, 16 and 24 bits each, added by the angles' formula (off by a few 2^-53)."""
+    high, low = (positions >> 16).astype(np.float64) * 65536.0, (positions & 0xFFFF).astype(np.float64)
+    a, b = (part[:, None] * freqs.astype(np.float64) for part in (high, low))
+    return np.cos(a) * np.cos(b) - np.sin(a) * np.sin(b), np.sin(a) * np.cos(b) + np.cos(a) * np.sin(b)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_turns_of_far_positions(interleaved):
+    """cos and sin within 2^-23 for angles of up to 2^50, and nothing else: a row of 16 pairs (1, 0), 16 ones and 8 twos has
+    the mean square 1, so that its norm without eps is the row itself, and its pairs become (cos, sin) unrounded."""
+    n, dim = 16, 64
+    rng = np.random.default_rng(1)
+    positions = rng.integers(-2 ** 31, 2 ** 31, 3000)
+    positions[:1500] >>= rng.integers(0, 28, 1500)
+    positions[:8] = [0, 1, -1, 2 ** 31 - 1, -2 ** 31, 2 ** 24 + 1, 1 << 20, 3]
+    x = torch.zeros((3000, 1, dim), device="cuda")
+    first = torch.arange(n, device="cuda") * (2 if interleaved else 1)
+    second = first + (1 if interleaved else n)
+    x[..., first] = 1.0
+    x[..., 2 * n:3 * n], x[..., 3 * n:3 * n + 8] = 1.0, 2.0
+    to = torch.from_numpy(positions.astype(np.int32)).cuda()
+    beside = 0.0
+    for low, high in ((-26, 0), (0, 12), (12, 18.9), (18, 18.99)):
+        freqs = np.exp2(rng.uniform(low, high, n)).astype(np.float32)
+        y, _ = kb.kb_qk_norm_forward(x, x, None, None, 0.0, to, torch.from_numpy(freqs).cuda(), interleaved)
+        c, s = exact_turns(positions, freqs)
+        for got, want in ((y[:, 0, first], c), (y[:, 0, second], s)):
+            assert np.abs(got.double().cpu().numpy() - want).max() <= 2.0 ** -23
+        assert torch.equal(y[..., 2 * n:], x[..., 2 * n:])
+        beside = max(beside, np.abs(np.cos(positions[:, None] * freqs.astype(np.float64)) - c).max())
+    assert beside > 2.0 ** -10  # the rounded product would be seen
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

@@ -67,26 +67,32 @@ def columns(x, heads, kv_heads, dim):
 
 def step(x, new, to, w, freqs, heads, kv_heads, dim):
     """The sublayer's output o [tokens][heads][dim] for the `new` tokens of each sequence (a list), whose keys and values
-    are added to the cache `to`: whole prompts, pieces of them, or one token each."""
+    are added to the cache `to`: whole prompts, pieces of them, or one token each.  A step that raises changes neither
+    the cache's counts nor its lengths."""
     import torch
 
     import paper_2608_02611_amd as kb
+    if len(new) != len(to.counts) or min(new, default=0) < 0:
+        raise ValueError("new tokens %s for %d sequences" % (new, len(to.counts)))
+    counts = [n + m for n, m in zip(to.counts, new)]
     ends, positions = [0], []
-    for b, n in enumerate(new):
-        if to.counts[b] + n > to.table.shape[1] * to.k.shape[2]:
-            raise ValueError("sequence %d has no room for %d keys" % (b, to.counts[b] + n))
-        ends.append(ends[-1] + n)
-        positions += range(to.counts[b], to.counts[b] + n)
-        to.counts[b] += n
+    for b, n in enumerate(counts):
+        if n > to.table.shape[1] * to.k.shape[2]:
+            raise ValueError("sequence %d has no room for %d keys" % (b, n))
+        ends.append(ends[-1] + new[b])
+        positions += range(to.counts[b], n)
 
     def ints(values):
         return torch.tensor(values, dtype=torch.int32, device=x.device)
-    to.lens += ints(new)
+    lens = ints(counts)
     starts = None if all(n == 1 for n in new) else ints(ends)
     q, k, v = columns(x, heads, kv_heads, dim)
     q, k = kb.kb_qk_norm_forward(q, k, w[0], w[1], EPS, ints(positions), freqs)
-    kb.kb_cache_write(k, v, to.k, to.v, to.table, to.lens, starts)
-    return kb.kb_attn_paged(q, to.k, to.v, to.table, to.lens, starts)[0]
+    kb.kb_cache_write(k, v, to.k, to.v, to.table, lens, starts)
+    o, _ = kb.kb_attn_paged(q, to.k, to.v, to.table, lens, starts)
+    to.counts[:] = counts
+    to.lens.copy_(lens)
+    return o
 
 
 def candidates(refs, spreads, seed=0):

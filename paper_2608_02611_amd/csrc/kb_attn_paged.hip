@@ -642,21 +642,15 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WAVES;
     const int r = (int)blockIdx.y * EACH + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WAVES;
     if (p.by_pair) {
-        // A pair's number may be no pair's, and then has no header.  (Where the starts do
-        // not ascend, count_up_to may give any sequence: one that begins later has none either.)
+        // A pair's number may be no pair's, and then has no header.  (Nor has it one where the
+        // starts do not ascend and count_up_to gives a sequence that begins later: unsigned.)
         const int64_t block = blockIdx.x / (uint32_t)p.kv_heads;
         const auto first_block = [&](int b) { return block_before<ROWS>(p, b); };
         const int seq = count_up_to(p.batch, block, lane, first_block) - 1;
-        if (seq < 0 || block < first_block(seq)) return;
-        if ((block - first_block(seq)) * ROWS >= (int64_t)tokens_of(p, seq).n * p.group) return;
+        if (seq < 0 || (uint64_t)((block - first_block(seq)) * ROWS) >= (uint64_t)tokens_of(p, seq).n * p.group) return;
     }
     const PagedHeader h = ((const PagedHeader*)p.ws)[blockIdx.x];
     if (!h.valid || r >= h.rows) return;
-    // (starts that do not ascend: pairs may share a number, and a header has some of each)
-    const Tokens tok = tokens_of(p, h.seq);
-    const uint32_t row = (uint32_t)h.block * ROWS + r;
-    const int i = (int)(row / (uint32_t)p.group), hq = h.head * p.group + (int)(row - (uint32_t)i * p.group);
-    if (i >= tok.n) return;
     const int me = h.first;
     const float to_log2 = p.scale * kLog2e;
     const float* base = p.ws + (int64_t)p.headers * (sizeof(PagedHeader) / sizeof(float)) + r * PITCH;
@@ -706,6 +700,10 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
         m = now;
         shift = most;
     }
+    const uint32_t row = (uint32_t)h.block * ROWS + r;
+    const int i = (int)(row / (uint32_t)p.group), hq = h.head * p.group + (int)(row - (uint32_t)i * p.group);
+    const Tokens tok = tokens_of(p, h.seq);
+    if (i >= tok.n) return;  // (starts that do not ascend: pairs may share a number, and a header has some of each)
     const int64_t t = tok.first + i;
     const auto write = [&](int d, float x) {
         const bool some = l != 0.f;

@@ -830,8 +830,9 @@ int kb_qk_norm_backward(const kb_tensor* dq_out, const kb_tensor* dk_out, const 
  *   starts  device int32[batch + 1], ascending: the tokens starts[b] .. starts[b+1]
  *           of the call are sequence b's new ones, its last.  NULL: token b is
  *           sequence b's, one each.  Tokens before starts[0] and from
- *           starts[batch] on belong to no sequence.  (Where it does not ascend, what
- *           is written for its tokens is undefined; nothing else is.)
+ *           starts[batch] on belong to no sequence.  A value outside [0, tokens]
+ *           counts as the nearer end.  (Where it does not ascend, what is written for
+ *           its tokens is undefined; nothing else is.)
  * batch at most 2^20, max_pages at most 2^28, max_pages page at most 2^30. */
 typedef struct kb_pages {
     const int32_t* table;

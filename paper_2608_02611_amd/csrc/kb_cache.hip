@@ -55,13 +55,13 @@ __global__ void __launch_bounds__(kThreads) cache_write_kernel(PagedParams p) {
             }
             b = __popcll(__ballot(lane < p.batch && last <= token));
             if (b >= p.batch || token < __builtin_amdgcn_readlane(first, b)) continue;  // no sequence's
-            end = __builtin_amdgcn_readlane(last, b);
+            end = min(__builtin_amdgcn_readlane(last, b), p.tokens);
             len = __builtin_amdgcn_readlane(keys, b);
         } else {
             if (p.starts != nullptr) {
                 b = count_up_to(p.batch, token, lane, [&](int i) { return (int64_t)p.starts[i + 1]; });
                 if (b >= p.batch || token < p.starts[b]) continue;
-                end = p.starts[b + 1];
+                end = min(p.starts[b + 1], p.tokens);
             }
             len = paged_len(p, b);
         }

@@ -49,3 +49,21 @@ def test_prompts_beside_single_tokens(dtype, seqs):
     b = Batch(seqs, 16, 8, 2, 64, dtype, "hnd")
     o, lse = kb.kb_attn_paged(b.q, b.k_cache, b.v_cache, *b.pages)
     check(b, 0.125, True, o, lse)
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("first,last", [(-9, 0), (0, 7), (-9, 7)])
+def test_starts_outside_the_tokens(many, first, last):
+    """The first and the last start count as the nearer end of the tokens: the write and the attention have the same bits."""
+    b = Batch([(3, 40), (2, 30)] + [(1, 20)] * (70 if many else 2) + [(4, 25)], 16, 4, 2, 64, "f16")
+    outside = b.starts.clone()
+    outside[0] += first
+    outside[-1] += last
+    k = b.q[:, :2].contiguous()
+    got = []
+    for starts in (b.starts, outside):
+        caches = kb.kb_cache_write(k, k, b.k_cache.clone(), b.v_cache.clone(), b.table, b.lens, starts)
+        got.append([torch.nan_to_num(c, 9.0) for c in caches] +
+                   list(kb.kb_attn_paged(b.q, b.k_cache, b.v_cache, b.table, b.lens, starts)))
+    for a, c in zip(*got):
+        assert torch.equal(a, c)

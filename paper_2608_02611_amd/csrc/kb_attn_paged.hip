@@ -603,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, DP == 64 && NB == 1 && DT != DT_F32 
                 }
                 if (part != nullptr) {
                     *(f32x4*)(part + r * PITCH + d) = o;
-                    if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, (float)shift, 0.f};
+                    if (d == 0) *(f32x4*)(part + r * PITCH + DP) = f32x4{m, l, __int_as_float(shift), 0.f};
                     continue;
                 }
                 const int64_t t = tok.first + i;
@@ -638,7 +638,8 @@ template <int DT, int DP, int NB, int WAVES>
 __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParams p) {
     using T = storage_t<DT>;
     constexpr int ROWS = 16 * NB, PITCH = DP + 4, E = DP / 64, AHEAD = 8, EACH = kJoinThreads / 64 / WAVES;
-    __shared__ float sums[WAVES][DP], stat_m[WAVES], stat_l[WAVES], stat_shift[WAVES];
+    __shared__ float sums[WAVES][DP];
+    __shared__ f32x4 stats[WAVES];  // m, l, shift
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WAVES;
     const int r = (int)blockIdx.y * EACH + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WAVES;
     if (p.by_pair) {
@@ -657,35 +658,39 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
     const int parts = h.last - me + 1;
     const auto part = [&](int k) { return base + ((int64_t)(me + k) * 2 + (k == 0)) * ROWS * PITCH; };
     // o is held times 2^-shift, the largest of the parts' shifts (0, but for large sums)
-    float m = -INFINITY, l = 0.f, shift = 0.f, o[E];
+    float m = -INFINITY, l = 0.f, o[E];
+    int shift = 0;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
     for (int k0 = wave; k0 < parts; k0 += WAVES * AHEAD) {
-        float x[AHEAD][E], xm[AHEAD], xl[AHEAD], xs[AHEAD];
+        float x[AHEAD][E], xm[AHEAD], xl[AHEAD];
+        int xs[AHEAD];
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
             const int k = k0 + n * WAVES;
             xm[n] = -INFINITY;
-            xs[n] = 0.f;
+            xs[n] = 0;
             if (k < parts) {
                 const float* at = part(k);
-                xm[n] = at[DP];
-                xl[n] = at[DP + 1];
-                if (kScaled<DT>) xs[n] = at[DP + 2];
+                const f32x4 stat = *(const f32x4*)(at + DP);
+                xm[n] = stat[0];
+                xl[n] = stat[1];
+                if (kScaled<DT>) xs[n] = __float_as_int(stat[2]);
 #pragma unroll
                 for (int e = 0; e < E; ++e) x[n][e] = at[lane * E + e];
             }
         }
-        float now = m, most = shift;
+        float now = m;
+        int most = shift;
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
             now = fmaxf(now, xm[n]);
-            most = fmaxf(most, xs[n]);
+            most = max(most, xs[n]);
         }
         const float ref = now == -INFINITY ? 0.f : now;
         float f = __builtin_amdgcn_exp2f((m - ref) * to_log2);
         l *= f;
-        if (kScaled<DT>) f = ldexpf(f, (int)(shift - most));
+        if (kScaled<DT>) f = ldexpf(f, shift - most);
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] *= f;
 #pragma unroll
@@ -693,7 +698,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
             if (k0 + n * WAVES >= parts) continue;
             f = __builtin_amdgcn_exp2f((xm[n] - ref) * to_log2);
             l = fmaf(f, xl[n], l);
-            if (kScaled<DT>) f = ldexpf(f, (int)(xs[n] - most));
+            if (kScaled<DT>) f = ldexpf(f, xs[n] - most);
 #pragma unroll
             for (int e = 0; e < E; ++e) o[e] = fmaf(f, x[n][e], o[e]);
         }
@@ -707,7 +712,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
     const int64_t t = tok.first + i;
     const auto write = [&](int d, float x) {
         const bool some = l != 0.f;
-        if (kScaled<DT>) x = ldexpf(x / l, (int)shift);
+        if (kScaled<DT>) x = ldexpf(x / l, shift);
         else x /= l;
         if (d < p.dim) ((T*)p.o.p)[t * p.o.st + hq * p.o.sh + d] = (T)(some ? x : 0.f);
         if (d == 0 && p.lse != nullptr)
@@ -719,29 +724,27 @@ __global__ void __launch_bounds__(kJoinThreads) paged_few_join_kernel(PagedParam
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) sums[wave][lane * E + e] = o[e];
-        if (lane == 0) {
-            stat_m[wave] = m;
-            stat_l[wave] = l;
-            stat_shift[wave] = shift;
-        }
+        if (lane == 0) stats[wave] = f32x4{m, l, __int_as_float(shift), 0.f};
         __syncthreads();
         const int d = threadIdx.x;
         if (d >= p.dim) return;
-        m = stat_m[0];
-        shift = stat_shift[0];
+        f32x4 stat[WAVES];
+        m = -INFINITY;
+        shift = 0;
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) {
-            m = fmaxf(m, stat_m[w]);
-            shift = fmaxf(shift, stat_shift[w]);
+        for (int w = 0; w < WAVES; ++w) {
+            stat[w] = stats[w];
+            m = fmaxf(m, stat[w][0]);
+            shift = max(shift, __float_as_int(stat[w][2]));
         }
         const float ref = m == -INFINITY ? 0.f : m;
         float x = 0.f;
         l = 0.f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const float f = __builtin_amdgcn_exp2f((stat_m[w] - ref) * to_log2);
-            l = fmaf(f, stat_l[w], l);
-            x = fmaf(kScaled<DT> ? ldexpf(f, (int)(stat_shift[w] - shift)) : f, sums[w][d], x);
+            const float f = __builtin_amdgcn_exp2f((stat[w][0] - ref) * to_log2);
+            l = fmaf(f, stat[w][1], l);
+            x = fmaf(kScaled<DT> ? ldexpf(f, __float_as_int(stat[w][2]) - shift) : f, sums[w][d], x);
         }
         write(d, x);
     }

@@ -797,7 +797,8 @@ typedef struct kb_qk_opts {
  *   (a cos - b sin, b cos + a sin).
  * q, k, q_out, k_out: one dtype, F32, F16 or BF16.  wq, wk: [dim], each NULL (1)
  * or of q's dtype or F32, both the same.  q_out may be q, and k_out k.  Heads may
- * be none of q's or k's.
+ * be none of q's or k's.  The squares of a row are summed in binary32, whose range
+ * they must not pass.
  * Errors: KB_ERR_INVALID_ARG (null descriptors or data, a shape, stride, head
  * count, dim, eps, flags or rot_dim out of range), KB_ERR_DTYPE,
  * KB_ERR_ALIGNMENT, KB_ERR_HIP. */
@@ -863,7 +864,10 @@ int kb_cache_write(const kb_tensor* k, const kb_tensor* v, const kb_pages* pages
  * sequence are left as they are.  lse: device float[tokens][heads], may be NULL.
  * One dtype, F32, F16 or BF16.  With a 16-bit dtype and more than 32 query rows
  * (queries x heads / kv_heads) a sequence on average the softmax terms are rounded
- * as kb_attn_forward's; with fewer they keep twice the dtype's digits.  workspace:
+ * as kb_attn_forward's; with fewer they keep twice the dtype's digits.  So a token's
+ * last bits, and its time, depend on what it is batched with: a few tokens on many
+ * keys and whole prompts are best two calls, each with its rows of the table, its
+ * lengths and its starts of the same arrays.  workspace:
  * 16-byte aligned, not less than kb_attn_paged_workspace_bytes (which may be 0:
  * then NULL will do); it needs no initialisation.
  * Errors: as kb_cache_write, and KB_ERR_INVALID_ARG for a scale or flags out of

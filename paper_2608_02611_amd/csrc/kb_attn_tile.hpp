@@ -13,6 +13,10 @@ namespace kb {
 // sums takes as long as a quarter of a tile's products), and next to l, the sum of
 // the terms, there is the sum of the rounded terms, those whose product with v is
 // divided by it: where one term outweighs the others, o is its v to the last bit.
+// (Terms in two parts, as the attention over pages has them for few rows, would take
+// half as many products again: 6 packed prompts of up to 4095 tokens, bf16, 402 us
+// instead of 311, whose error against 64 bits is 2.0e-3; the rounding of o alone makes
+// 1.6e-3.)
 // F16 holds small terms badly (subnormal from 2^-14, nothing under 2^-25), so there
 // the reference is set 2^kBelow under the maximum: terms of up to 2^15, and what the
 // format takes from one is at most 2^-34 of the largest.

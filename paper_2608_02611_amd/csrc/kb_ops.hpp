@@ -243,6 +243,10 @@ inline int64_t paged_keys(const PagedParams& p) { return (int64_t)p.width * p.pa
 // key head, dim 128, few / many: bf16 20 rows 53 / 68 us, 32 56 / 65, 48 72 / 72, 64 74 /
 // 80, but 60 prompts of up to 32 tokens 22 / 18 and 200 of them 61 / 36; f32, whose
 // products take eight times as long, 48 rows 171 / 470, 128 421 / 559 (dim 64: 135 / 265).
+// The whole call goes one way, as the host knows no lengths: a few tokens on many keys
+// beside prompts are then blocks of 128 rows, each with all of its keys behind each other
+// (2048 tokens and one on 131,071 keys 2685 us, 65 and 111 in two calls; and 8 on 8191
+// keys 190, 65 and 53).
 inline bool few_rows(const PagedParams& p) {
     return (int64_t)p.tokens * p.group <= (int64_t)(p.f32 ? 128 : 32) * p.batch;
 }

@@ -159,3 +159,20 @@ def test_infinite_values_few_rows(dtype, page, case, causal):
 @pytest.mark.parametrize("causal", [True, False])
 def test_infinite_values_many_rows(dtype, page, case, causal):
     infinite(dtype, page, case, causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("page", [16, 5, 64])
+@pytest.mark.parametrize("seqs", [[(1, 200), (3, 2500)], [(100, 200), (70, 700)]])
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_values_beside_keys_without_a_page(dtype, page, seqs, causal):
+    b = batch(dtype, 64, page, seqs)
+    enlarge(b, 2)
+    missing = []
+    for s, (_, n) in enumerate(seqs):
+        for i, number in ((0, -1), (1, b.k_cache.shape[0])):
+            b.table[s, i] = number
+            missing += [(s, j) for j in range(i * page, (i + 1) * page)]
+    o, lse = attend(b, causal)
+    assert torch.isfinite(o).all()
+    check(b, b.dim ** -0.5, causal, o, lse, missing)

@@ -16,8 +16,8 @@
 // token each of 64 sequences of up to 8191 keys, pages of 16, bf16: 143 us, 5.1 TB/s;
 // one of 131,071 keys, f16: 100 us, 5.4 TB/s; five each of 32 sequences of up to 4000
 // keys: 52 us, 3.5 TB/s, of which the second kernel has 6 and the beginnings of short
-// pairs most of what is lost; 6 packed prompts of up to 4095 tokens: 286 to 315 us, 0.76
-// to 0.84 PFLOP/s, by the clock that the card holds (7% to 13% more than dense keys:
+// pairs most of what is lost; 6 packed prompts of up to 4095 tokens: 282 to 315 us, 0.76
+// to 0.85 PFLOP/s, by the clock that the card holds (7% to 13% more than dense keys:
 // products under way 42% of the time, as there, and 100 more instructions for a tile's
 // addresses).  8 heads' 200 keys of 64 elements, f32: 9.3 us, four steps behind each
 // other on each wave.
